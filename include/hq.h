@@ -57,7 +57,8 @@ typedef enum {
 typedef enum {
     HQ_F16 = 0, /* IEEE half */
     HQ_F32 = 1, /* IEEE single */
-    HQ_I32 = 2  /* raw int32 accumulators: outputs of the integer stage only */
+    HQ_I32 = 2, /* raw int32 accumulators: outputs of the integer stage only */
+    HQ_BF16 = 3 /* bfloat16: the calls on 8-bit floats and on query and key heads only */
 } hq_dtype;
 
 /* Static, NUL-terminated description of a status code. */
@@ -376,6 +377,110 @@ hq_status hq_int_conv2d_i8(const int8_t *xq, const float *x_scale, const int8_t 
                            const float *w_scale, const void *bias, int nb, int h, int w,
                            int c_in, int c_out, int r, int s, int stride, int pad,
                            void *y, hq_dtype y_dtype, void *stream);
+
+/*
+ * ---- 8-bit floats with block scales -----------------------------------------------
+ *
+ * Linear layers whose operands are E4M3 numbers (4 bits of exponent, 3 of mantissa, largest value 448; "OCP FP8",
+ * torch.float8_e4m3fn), with one fp32 scale for each group of 128 along the contracted axis: for the layers
+ * of a network that do not stand integer codes, and for the products of their gradients.  No Hadamard transform: a
+ * floating code loses no precision to a large neighbour.
+ *
+ * Values x, w, dy, y, dx: HQ_F16, HQ_F32 or HQ_BF16, a row's elements side by side, rows row_stride elements apart
+ * (any number from 0 on; 0 repeats a row).  Their pointers need the alignment of an element only.  Codes are dense, 16-byte aligned, a row's length
+ * rounded up to a multiple of 16 bytes, the end filled with zeros ("pitch" below).
+ *
+ *   amax  = max |x| over the scale's values
+ *   scale = 1 if amax is 0, otherwise max(amax * c, 2^-126), c = 1/448 rounded to fp32
+ *   code  = E4M3(x * (1 / scale)), to nearest, ties to even            (products and quotient rounded to nearest in fp32)
+ *
+ * Values that are not finite: the scale is NaN and the codes of its group are 0, so that every result the group takes part in is NaN.
+ * Zero rows (m = 0) are no error: nothing is computed (dw and db are set to zero).  Rows of codes up to 8 MiB, m up to 8,388,480.
+ */
+/*
+ * Activations: one scale for each row and 128 columns.
+ *   x [m, k] -> xq [m, pitch], x_scale [ceil(k / 128), m]
+ */
+hq_status hq_fp8_quantize_rows(const void *x, hq_dtype x_dtype, int64_t m, int k, int64_t row_stride,
+                               uint8_t *xq, float *x_scale, void *stream);
+/*
+ * Weights: one scale for each block of 128 x 128.
+ *   w [n, k] -> wq [n, pitch of k] (or NULL), wq_t [k, pitch of n], the same codes transposed, which the gradient takes (or NULL),
+ *   w_scale [ceil(n / 128), ceil(k / 128)]
+ */
+hq_status hq_fp8_quantize_blocks(const void *w, hq_dtype w_dtype, int64_t n, int k, int64_t row_stride,
+                                 uint8_t *wq, uint8_t *wq_t, float *w_scale, void *stream);
+/*
+ *   y[i, j] = sum_b x_scale[b, i] w_scale[j / 128, b] (sum over c in group b of xq[i, c] wq[j, c]) + bias[j]
+ *
+ * fp32 sums, rounded once to y_dtype.  bias [n] of y_dtype or NULL; y [m, n], dense.
+ * w_scale_turned: w_scale is [ceil(k / 128), ceil(n / 128)] (codes of a transposed matrix with the scales of the matrix).
+ */
+hq_status hq_fp8_linear(const uint8_t *xq, const float *x_scale, const uint8_t *wq, const float *w_scale,
+                        int w_scale_turned, const void *bias, int64_t m, int n, int k, void *y, hq_dtype y_dtype,
+                        void *stream);
+/*
+ * The whole layer: hq_fp8_quantize_rows and hq_fp8_linear.  workspace: device memory of
+ * hq_act_quant_fp8_linear_workspace(m, k) bytes, 16-byte aligned, written and read by the call.
+ */
+int64_t hq_act_quant_fp8_linear_workspace(int64_t m, int k);
+hq_status hq_act_quant_fp8_linear(const void *x, hq_dtype x_dtype, int64_t row_stride, const uint8_t *wq,
+                                  const float *w_scale, const void *bias, int64_t m, int n, int k, void *workspace,
+                                  void *y, hq_dtype y_dtype, void *stream);
+/*
+ * Its gradients, straight through the roundings of x and w.  dy is quantised twice, with a scale for each row and 128 columns (for
+ * dx) and for each column and 128 rows (for dw); x anew, with a scale for each block of 128 x 128:
+ *
+ *   dx [m, k] = Q(dy) wq          (of `dtype`; wq_t, w_scale as hq_fp8_quantize_blocks writes them)
+ *   dw [n, k] = Q(dy)^T Q(x)      (fp32)
+ *   db [n]    = sum over the rows of dy, not quantised (fp32; or NULL)
+ *
+ * dy, x and dx of `dtype`; dx, dw dense.  workspace: hq_fp8_linear_backward_workspace(m, n, k) bytes, 16-byte aligned.
+ * The order of every sum is fixed: the same inputs give the same bits.
+ */
+int64_t hq_fp8_linear_backward_workspace(int64_t m, int n, int k);
+hq_status hq_fp8_linear_backward(const void *dy, int64_t dy_stride, const void *x, int64_t x_stride, hq_dtype dtype,
+                                 const uint8_t *wq_t, const float *w_scale, int64_t m, int n, int k, void *workspace,
+                                 void *dx, float *dw, float *db, void *stream);
+
+/*
+ * ---- query and key heads: norm and rotation ------------------------------------------
+ *
+ * What follows the query/key/value projection of an attention block, in one pass over q [t, heads, d] and k [t, kv_heads, d]:
+ *
+ *   n = x * weight / sqrt(mean of x^2 over the head + eps)
+ *   y = n with its first `rotary` channels turned in pairs: (a, b) -> (a cos - b sin, b cos + a sin)
+ *
+ * Pair i of a token at position p has cos[p, i], sin[p, i] (both [positions, rotary / 2], fp32) and is channels (i, i + rotary / 2), or
+ * (2i, 2i + 1) where `interleaved` is not 0; the other channels are only normalised.
+ *
+ *   dtype     of q, k and the results: HQ_F16, HQ_F32 or HQ_BF16; sums in fp32, one rounding
+ *   strides   HOST array, in elements, a head's channels side by side: q token, q head, k token, k head, then the results' in that order.
+ *             A result may be its own input (the same memory with the same strides); any other overlap is not allowed.
+ *   q_weight, k_weight  [d] of w_dtype (dtype or HQ_F32), or NULL for ones
+ *   pos       [t] of pos_size bytes (4 or 8) each, or NULL for 0 .. t - 1 (then t <= positions).  A token with a negative position is padding: its
+ *             results are zeros.  One at or beyond `positions` has NaN for results.
+ *   d, rotary even, rotary <= d <= 1024; t * heads below 2^31; eps >= 0
+ *   t = 0 is no error.
+ */
+hq_status hq_qk_norm_rope(const void *q, const void *k, hq_dtype dtype, int64_t t, int heads, int kv_heads, int d,
+                          const int64_t *strides, const void *q_weight, const void *k_weight, hq_dtype w_dtype,
+                          const float *cos, const float *sin, int64_t positions, int rotary, int interleaved,
+                          const void *pos, int pos_size, float eps, void *q_out, void *k_out, void *stream);
+/*
+ * Its gradients.  dq, dk: gradients of the results; q, k: the inputs of the forward pass.
+ *   strides   q token, q head, k token, k head, then those of dq, dk, and those of q_grad, k_grad (12 numbers)
+ *   q_weight_grad, k_weight_grad   [d] fp32, sums over all tokens and heads in a fixed order; or NULL
+ *   workspace hq_qk_norm_rope_backward_workspace(t, heads, kv_heads, d, rotary) bytes, 4-byte aligned
+ * Padding has zeros for gradients and no part in the weights'.  q_grad may be dq or q, k_grad dk or k (the same memory, the same strides).
+ */
+int64_t hq_qk_norm_rope_backward_workspace(int64_t t, int heads, int kv_heads, int d, int rotary);
+hq_status hq_qk_norm_rope_backward(const void *dq, const void *dk, const void *q, const void *k, hq_dtype dtype, int64_t t,
+                                   int heads, int kv_heads, int d, const int64_t *strides, const void *q_weight,
+                                   const void *k_weight, hq_dtype w_dtype, const float *cos, const float *sin,
+                                   int64_t positions, int rotary, int interleaved, const void *pos, int pos_size, float eps,
+                                   void *workspace, void *q_grad, void *k_grad, float *q_weight_grad,
+                                   float *k_weight_grad, void *stream);
 
 #ifdef __cplusplus
 }

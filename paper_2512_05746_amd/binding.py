@@ -20,9 +20,14 @@ SYMBOLS = ("hq_status_string", "hq_quantize_weights", "hq_act_hadamard_quant",
            "hq_quantize_weights_single", "hq_int_linear_single",
            "hq_act_hadamard_quant_width", "hq_int_conv2d_width",
            "hq_int_linear_i8", "hq_int_conv2d_i8", "hq_act_hadamard_quant_i8",
-           "hq_act_quant_int_conv2d", "hq_act_quant_int_linear")
+           "hq_act_quant_int_conv2d", "hq_act_quant_int_linear",
+           "hq_fp8_quantize_rows", "hq_fp8_quantize_blocks", "hq_fp8_linear", "hq_act_quant_fp8_linear",
+           "hq_fp8_linear_backward", "hq_qk_norm_rope", "hq_qk_norm_rope_backward")
+# entry points that return the bytes of a workspace
+WORKSPACE_SYMBOLS = ("hq_act_quant_fp8_linear_workspace", "hq_fp8_linear_backward_workspace",
+                     "hq_qk_norm_rope_backward_workspace")
 # entry points that do not return a status
-INFO_SYMBOLS = ("hq_int_conv2d_kernel_name",)
+INFO_SYMBOLS = ("hq_int_conv2d_kernel_name",) + WORKSPACE_SYMBOLS
 
 
 class HqError(RuntimeError):
@@ -72,12 +77,27 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
     lib.hq_int_conv2d_i8.argtypes = lib.hq_int_conv2d.argtypes
     lib.hq_act_quant_int_conv2d.argtypes = [vp, i32, vp, vp, vp] + [i32] * 11 + [vp, i32, vp, vp, vp]
     lib.hq_act_quant_int_linear.argtypes = [vp, i32, vp, vp, vp, i64, i32, i32, i32, i32, vp, i32, vp, vp, vp]
+    lib.hq_fp8_quantize_rows.argtypes = [vp, i32, i64, i32, i64, vp, vp, vp]
+    lib.hq_fp8_quantize_blocks.argtypes = [vp, i32, i64, i32, i64, vp, vp, vp, vp]
+    lib.hq_fp8_linear.argtypes = [vp] * 4 + [i32, vp, i64, i32, i32, vp, i32, vp]
+    lib.hq_act_quant_fp8_linear.argtypes = [vp, i32, i64, vp, vp, vp, i64, i32, i32, vp, vp, i32, vp]
+    lib.hq_fp8_linear_backward.argtypes = [vp, i64, vp, i64, i32, vp, vp, i64, i32, i32] + [vp] * 5
+    f32 = ctypes.c_float
+    lib.hq_qk_norm_rope.argtypes = [vp, vp, i32, i64, i32, i32, i32, vp, vp, vp, i32, vp, vp, i64, i32, i32, vp, i32,
+                                    f32, vp, vp, vp]
+    lib.hq_qk_norm_rope_backward.argtypes = [vp] * 4 + [i32, i64, i32, i32, i32, vp, vp, vp, i32, vp, vp, i64, i32, i32,
+                                                        vp, i32, f32] + [vp] * 6
+    lib.hq_act_quant_fp8_linear_workspace.argtypes = [i64, i32]
+    lib.hq_fp8_linear_backward_workspace.argtypes = [i64, i32, i32]
+    lib.hq_qk_norm_rope_backward_workspace.argtypes = [i64, i32, i32, i32, i32]
     for name in SYMBOLS[1:]:
         getattr(lib, name).restype = i32
+    for name in WORKSPACE_SYMBOLS:
+        getattr(lib, name).restype = i64
     lib.hq_int_conv2d_kernel_name.argtypes = [i32] * 11
     lib.hq_int_conv2d_kernel_name.restype = ctypes.c_char_p
     from . import _marshal as marshal
-    marshal.bind({name: ctypes.cast(getattr(lib, name), ctypes.c_void_p).value for name in SYMBOLS}, HqError)
+    marshal.bind({name: ctypes.cast(getattr(lib, name), ctypes.c_void_p).value for name in SYMBOLS + WORKSPACE_SYMBOLS}, HqError)
     _lib, _marshal = lib, marshal
     return lib
 
@@ -231,3 +251,61 @@ def hq_int_conv2d_i8(xq: torch.Tensor, x_scale: Optional[torch.Tensor], wq: torc
     stride 1; ksize 3 at stride 2 halves it, rounding up); y_dtype int32 returns the per-tap sums
     [N, Ho, Wo, ksize*ksize, Cout]."""
     return _native().conv2d_i8(xq, x_scale, wq, w_scale, bias, ksize, stride, None, y_dtype, out)
+
+
+# ---- 8-bit floats with block scales ---------------------------------------------------------------
+
+def hq_fp8_quantize_rows(x: torch.Tensor) -> Tuple[torch.Tensor, torch.Tensor]:
+    """x [..., k] fp16/bf16/fp32 -> (xq float8_e4m3fn [..., k up to a multiple of 16], x_scale fp32 [ceil(k / 128), rows]):
+    one scale for each row and 128 columns.  x is contiguous, or a matrix of contiguous rows."""
+    return _native().fp8_quantize_rows(x)
+
+
+def hq_fp8_quantize_blocks(w: torch.Tensor, transposed: bool = False) -> Tuple[torch.Tensor, ...]:
+    """w [n, k] fp16/bf16/fp32 -> (wq float8_e4m3fn [n, k up to a multiple of 16], w_scale fp32 [ceil(n / 128), ceil(k / 128)]):
+    one scale for each block of 128 x 128.  transposed: (wq, wq_t, w_scale), wq_t [k, n up to a multiple of 16] the same
+    codes transposed, for hq_fp8_linear_backward."""
+    return _native().fp8_quantize_blocks(w, transposed)
+
+
+def hq_fp8_linear(xq: torch.Tensor, x_scale: torch.Tensor, wq: torch.Tensor, w_scale: torch.Tensor,
+                  bias: Optional[torch.Tensor] = None, y_dtype: torch.dtype = torch.float16,
+                  out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """xq [..., kp], wq [n, kp] float8_e4m3fn codes as the quantisers write them, with their scales -> y [..., n].  w_scale may be
+    the transposed view of the scales of a matrix whose transposed codes wq holds."""
+    return _native().fp8_linear(xq, x_scale, wq, w_scale, bias, y_dtype, out)
+
+
+def hq_act_quant_fp8_linear(x: torch.Tensor, wq: torch.Tensor, w_scale: torch.Tensor, bias: Optional[torch.Tensor] = None,
+                            y_dtype: torch.dtype = torch.float16, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """The whole layer: x [..., k] fp16/bf16/fp32 -> y [..., n], as hq_fp8_quantize_rows and hq_fp8_linear give it."""
+    return _native().act_quant_fp8_linear(x, wq, w_scale, bias, y_dtype, out)
+
+
+def hq_fp8_linear_backward(dy: torch.Tensor, x: torch.Tensor, wq_t: torch.Tensor, w_scale: torch.Tensor,
+                           bias_grad: bool = False) -> Tuple[torch.Tensor, torch.Tensor, Optional[torch.Tensor]]:
+    """Gradients of hq_act_quant_fp8_linear: dy [..., n], x [..., k] of one type, wq_t and w_scale of
+    hq_fp8_quantize_blocks(w, transposed=True) -> (dx [..., k] of that type, dw fp32 [n, k], db fp32 [n] or None)."""
+    return _native().fp8_linear_backward(dy, x, wq_t, w_scale, bias_grad)
+
+
+# ---- query and key heads: norm and rotation ---------------------------------------------------------
+
+def hq_qk_norm_rope(q: torch.Tensor, k: torch.Tensor, q_weight: Optional[torch.Tensor], k_weight: Optional[torch.Tensor],
+                    cos: torch.Tensor, sin: torch.Tensor, positions: Optional[torch.Tensor] = None, eps: float = 1e-6,
+                    interleaved: bool = False, out: Optional[Tuple[torch.Tensor, torch.Tensor]] = None
+                    ) -> Tuple[torch.Tensor, torch.Tensor]:
+    """q [t, heads, d], k [t, kv_heads, d] fp16/bf16/fp32 with contiguous channels (views of a projection's result, say), weights
+    [d], cos and sin fp32 [positions, rotary / 2], positions int32/int64 [t] (None: 0 .. t - 1; negative: padding) ->
+    both normalised head by head and rotated, contiguous or in `out`, which may be (q, k)."""
+    return _native().qk_norm_rope(q, k, q_weight, k_weight, cos, sin, positions, eps, interleaved, out)
+
+
+def hq_qk_norm_rope_backward(dq: torch.Tensor, dk: torch.Tensor, q: torch.Tensor, k: torch.Tensor,
+                             q_weight: Optional[torch.Tensor], k_weight: Optional[torch.Tensor], cos: torch.Tensor,
+                             sin: torch.Tensor, positions: Optional[torch.Tensor] = None, eps: float = 1e-6,
+                             interleaved: bool = False, out: Optional[Tuple[torch.Tensor, torch.Tensor]] = None
+                             ) -> Tuple[torch.Tensor, torch.Tensor, Optional[torch.Tensor], Optional[torch.Tensor]]:
+    """Gradients of hq_qk_norm_rope: dq, dk of its results, its inputs -> (gradients of q and k, contiguous or in `out`; of the
+    weights, fp32 [d], None for a weight that is None)."""
+    return _native().qk_norm_rope_backward(dq, dk, q, k, q_weight, k_weight, cos, sin, positions, eps, interleaved, out)

@@ -1,0 +1,312 @@
+// Quantisers of 8-bit floats (E4M3: 4 bits of exponent, 3 of mantissa, largest value 448) with a scale for each tile of values:
+// 128 neighbours of a row, 128 neighbours of a column, or a block of 128 x 128.
+//
+//     amax = max |x| over the tile;  s = 1 if amax is 0, else max(amax * c, 2^-126);  code = E4M3(x * (1 / s))
+//
+// c is 1/448 in fp32, and products and quotient are rounded to nearest, so that the codes are a function of the inputs alone; the
+// conversion rounds to nearest, ties to even.  |x (1 / s)| is at most 448 (1 + 2^-22), which rounds to 448.  A tile that holds an infinity or a NaN gets
+// a NaN for its scale and zeros for codes: every product that uses it is NaN.
+//
+// Bound by memory: a value is read once and written as one byte, or as two bytes where codes along rows and along columns are wanted.
+// rows_kernel: 16 lanes own 128 values of a row, 8 each.  tile_kernel: a workgroup of 256 threads owns a tile of 128 x 128; a thread
+// holds 8 rows x 8 columns in registers, so a maximum along a row is one over 16 lanes, along a column one over 16 threads at
+// the same columns (4 lanes of each wave, then LDS), and the codes of a column leave through LDS as whole pieces of 128 bytes.
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include <algorithm>
+
+#include "hq_common.h"
+#include "hq_floats.h"
+#include "hq_fp8.h"
+
+namespace {
+
+constexpr int kGroup = hq::kFp8Group;
+
+__device__ __forceinline__ float scale_of(uint32_t amax_bits) {
+    if (amax_bits >= 0x7F800000u) return __uint_as_float(0x7FC00000u);
+    const float s = fmaxf(__uint_as_float(amax_bits) * (1.0f / 448.0f), 0x1p-126f);
+    return amax_bits == 0 ? 1.0f : s;
+}
+// (0 for a tile that is not finite: its codes are taken from zeros)
+__device__ __forceinline__ float inverse_of(float s) { return s == s ? __fdiv_rn(1.0f, s) : 0.0f; }
+
+__device__ __forceinline__ uint32_t magnitude(float v) { return __float_as_uint(v) & 0x7FFFFFFFu; }
+
+// codes of 4 values in a dword; `inverse` is 0 for a tile that is not finite
+__device__ __forceinline__ uint32_t codes4(const float *v, float inverse) {
+    float t[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) t[i] = inverse == 0.0f ? 0.0f : v[i] * inverse;
+    int w = __builtin_amdgcn_cvt_pk_fp8_f32(t[0], t[1], 0, false);
+    return static_cast<uint32_t>(__builtin_amdgcn_cvt_pk_fp8_f32(t[2], t[3], w, true));
+}
+
+// 8 values of a row from column c on; zeros beyond the row's end
+template <class T>
+__device__ __forceinline__ void load8(const T *row, int c, int columns, float (&v)[8]) {
+    if (c + 8 <= columns) {
+        const typename Vec<T, 8>::type t = load_vec<T, 8>(row + c);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = static_cast<float>(t[i]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = c + i < columns ? static_cast<float>(row[c + i]) : 0.0f;
+    }
+}
+
+struct RowsArgs {
+    const void *x;
+    int64_t m, row_stride;
+    int k, pitch;          // values and bytes of codes a row
+    uint8_t *xq;           // [m, pitch]
+    float *scale;          // [k / 128, m]
+};
+
+template <int DT>
+__global__ __launch_bounds__(256) void rows_kernel(RowsArgs a) {
+    using T = typename Float<DT>::type;
+    const int lane16 = threadIdx.x & 15;
+    const int64_t row = static_cast<int64_t>(blockIdx.x) * 16 + (threadIdx.x >> 4);
+    if (row >= a.m) return;
+    const int groups = (a.k + kGroup - 1) / kGroup;
+    const T *x = static_cast<const T *>(a.x) + row * a.row_stride;
+    for (int b = blockIdx.y; b < groups; b += gridDim.y) {
+        const int c = b * kGroup + lane16 * 8;
+        float v[8];
+        load8(x, c, a.k, v);
+        uint32_t top = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) top = max(top, magnitude(v[i]));
+        const float s = scale_of(max_lanes<16>(top)), inverse = inverse_of(s);
+        if (c < a.pitch) *reinterpret_cast<uint2 *>(a.xq + row * a.pitch + c) = uint2{codes4(v, inverse), codes4(v + 4, inverse)};
+        if (lane16 == 0) a.scale[static_cast<int64_t>(b) * a.m + row] = s;
+    }
+}
+
+struct TileArgs {
+    const void *x;          // [rows, columns]
+    int64_t rows, row_stride;
+    int columns;
+    int pitch;              // bytes a row of q
+    int64_t pitch_t;        // bytes a row of q_t
+    uint8_t *q;             // [rows, pitch], or null
+    uint8_t *q_t;           // [columns, pitch_t], or null
+    float *scale;           // of rows: [columns / 128, rows]; of blocks: [rows / 128, columns / 128]
+    float *scale_t;         // of columns: [rows / 128, columns]
+    float *sums;            // [rows / 128, columns]: sums of a tile's columns; or null
+};
+
+// BLOCKS: one scale for the tile; otherwise codes along the rows in q and along the columns in q_t
+template <int DT, bool BLOCKS>
+__global__ __launch_bounds__(256) void tile_kernel(TileArgs a) {
+    using T = typename Float<DT>::type;
+    __shared__ __attribute__((aligned(16))) uint8_t turned[kGroup * kGroup];
+    __shared__ uint32_t top_of[4][kGroup];
+    __shared__ float sum_of[4][kGroup], inverse_t[kGroup];
+    const int tid = threadIdx.x, lane16 = tid & 15, part = tid >> 4, wave = tid >> 6;
+    const int64_t row0 = static_cast<int64_t>(blockIdx.y) * kGroup;
+    const int column0 = blockIdx.x * kGroup, c = column0 + lane16 * 8;
+    const int blocks_across = (a.columns + kGroup - 1) / kGroup;
+
+    float v[8][8];   // [row][column]
+#pragma unroll
+    for (int r = 0; r < 8; ++r) {
+        const int64_t row = row0 + part * 8 + r;
+        if (row < a.rows) {
+            load8(static_cast<const T *>(a.x) + row * a.row_stride, c, a.columns, v[r]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[r][i] = 0.0f;
+        }
+    }
+
+    // maxima and sums of the columns, over the threads that share them
+    uint32_t top[8];
+    float sum[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        top[i] = 0;
+        sum[i] = 0.0f;
+#pragma unroll
+        for (int r = 0; r < 8; ++r) {
+            top[i] = max(top[i], magnitude(v[r][i]));
+            sum[i] += v[r][i];
+        }
+    }
+    float s_block = 1.0f, inverse_block = 1.0f;
+    if constexpr (BLOCKS) {
+        uint32_t t = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) t = max(t, top[i]);
+        t = max_lanes<64>(t);
+        if ((tid & 63) == 0) top_of[wave][0] = t;
+        __syncthreads();
+        s_block = scale_of(max(max(top_of[0][0], top_of[1][0]), max(top_of[2][0], top_of[3][0])));
+        inverse_block = inverse_of(s_block);
+        if (tid == 0) a.scale[static_cast<int64_t>(blockIdx.y) * blocks_across + blockIdx.x] = s_block;
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            top[i] = max(top[i], static_cast<uint32_t>(__shfl_xor(static_cast<int>(top[i]), 16)));
+            top[i] = max(top[i], static_cast<uint32_t>(__shfl_xor(static_cast<int>(top[i]), 32)));
+            if (a.sums) {
+                sum[i] += __shfl_xor(sum[i], 16);
+                sum[i] += __shfl_xor(sum[i], 32);
+            }
+        }
+        if ((tid & 63) < 16) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                top_of[wave][lane16 * 8 + i] = top[i];
+                sum_of[wave][lane16 * 8 + i] = sum[i];
+            }
+        }
+        __syncthreads();
+        if (tid < kGroup) {
+            const float s = scale_of(max(max(top_of[0][tid], top_of[1][tid]), max(top_of[2][tid], top_of[3][tid])));
+            inverse_t[tid] = inverse_of(s);
+            if (column0 + tid < a.columns) {
+                const int64_t at = static_cast<int64_t>(blockIdx.y) * a.columns + column0 + tid;
+                a.scale_t[at] = s;
+                if (a.sums) a.sums[at] = (sum_of[0][tid] + sum_of[1][tid]) + (sum_of[2][tid] + sum_of[3][tid]);
+            }
+        }
+        __syncthreads();
+    }
+
+    // codes along the rows
+    if (a.q) {
+#pragma unroll
+        for (int r = 0; r < 8; ++r) {
+            const int64_t row = row0 + part * 8 + r;
+            float inverse = inverse_block;
+            if constexpr (!BLOCKS) {
+                uint32_t t = 0;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) t = max(t, magnitude(v[r][i]));
+                const float s = scale_of(max_lanes<16>(t));
+                inverse = inverse_of(s);
+                if (lane16 == 0 && row < a.rows) a.scale[static_cast<int64_t>(blockIdx.x) * a.rows + row] = s;
+            }
+            if (row < a.rows && c < a.pitch)
+                *reinterpret_cast<uint2 *>(a.q + row * a.pitch + c) = uint2{codes4(v[r], inverse), codes4(v[r] + 4, inverse)};
+        }
+    }
+    if (!a.q_t) return;
+
+    // Codes along the columns: a thread's 8 rows of a column are 8 bytes of that column's 128.  The 8-byte pieces of a column are
+    // kept in an order that depends on column / 8, so that 16 lanes write to different banks.
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const int column = lane16 * 8 + i;
+        const float inverse = BLOCKS ? inverse_block : inverse_t[column];
+        float t[8];
+#pragma unroll
+        for (int r = 0; r < 8; ++r) t[r] = v[r][i];
+        *reinterpret_cast<uint2 *>(turned + column * kGroup + ((part ^ lane16) * 8)) = uint2{codes4(t, inverse), codes4(t + 4, inverse)};
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const int column = i * 16 + part;
+        const int64_t at = row0 + lane16 * 8;
+        if (column0 + column < a.columns && at < a.pitch_t)
+            *reinterpret_cast<uint2 *>(a.q_t + static_cast<int64_t>(column0 + column) * a.pitch_t + at) =
+                *reinterpret_cast<const uint2 *>(turned + column * kGroup + ((lane16 ^ (column >> 3)) * 8));
+    }
+}
+
+// out[c] = sum over the rows of part [rows, columns], in the order of the rows within each of 16 threads
+__global__ __launch_bounds__(256) void sum_rows_kernel(const float *part, int64_t rows, int columns, float *out) {
+    __shared__ float s[16][16];
+    const int x = threadIdx.x & 15, y = threadIdx.x >> 4, c = blockIdx.x * 16 + x;
+    float t = 0.0f;
+    if (c < columns)
+        for (int64_t r = y; r < rows; r += 16) t += part[r * columns + c];
+    s[y][x] = t;
+    __syncthreads();
+    if (y == 0 && c < columns) {
+#pragma unroll
+        for (int i = 1; i < 16; ++i) t += s[i][x];
+        out[c] = t;
+    }
+}
+
+template <class F>
+hq_status for_dtype(hq_dtype dt, F f) {
+    switch (dt) {
+        case HQ_F16: return f(std::integral_constant<int, HQ_F16>{});
+        case HQ_BF16: return f(std::integral_constant<int, HQ_BF16>{});
+        case HQ_F32: return f(std::integral_constant<int, HQ_F32>{});
+        default: return HQ_ERR_DTYPE;
+    }
+}
+
+}  // namespace
+
+namespace hq {
+
+hq_status fp8_rows(const void *x, hq_dtype dt, int64_t m, int k, int64_t row_stride, uint8_t *xq, float *scale, hipStream_t st) {
+    const RowsArgs a{x, m, row_stride, k, fp8_pitch(k), xq, scale};
+    const int groups = (k + kGroup - 1) / kGroup;
+    const uint32_t bx = static_cast<uint32_t>((m + 15) / 16);
+    // few rows: a workgroup for each group of 128; many: a workgroup keeps its rows, up to about 16 workgroups a CU
+    const uint32_t want = std::max<uint32_t>(1, static_cast<uint32_t>(compute_units()) * 16 / bx);
+    const dim3 grid(bx, std::min<uint32_t>(groups, want));
+    return for_dtype(dt, [&](auto d) {
+        const LaunchCheck check;
+        rows_kernel<decltype(d)::value><<<grid, 256, 0, st>>>(a);
+        return check.status();
+    });
+}
+
+hq_status fp8_blocks(const void *x, hq_dtype dt, int64_t rows, int columns, int64_t row_stride, uint8_t *q, uint8_t *q_t, float *scale,
+                     hipStream_t st) {
+    const TileArgs a{x, rows, row_stride, columns, fp8_pitch(columns), fp8_pitch64(rows), q, q_t, scale, nullptr, nullptr};
+    const dim3 grid((columns + kGroup - 1) / kGroup, static_cast<uint32_t>((rows + kGroup - 1) / kGroup));
+    return for_dtype(dt, [&](auto d) {
+        const LaunchCheck check;
+        tile_kernel<decltype(d)::value, true><<<grid, 256, 0, st>>>(a);
+        return check.status();
+    });
+}
+
+hq_status fp8_both(const void *x, hq_dtype dt, int64_t rows, int columns, int64_t row_stride, uint8_t *q, float *scale, uint8_t *q_t,
+                   float *scale_t, float *sum_parts, float *sums, hipStream_t st) {
+    const TileArgs a{x,  rows,  row_stride, columns, fp8_pitch(columns), fp8_pitch64(rows), q, q_t, scale, scale_t,
+                     sums ? sum_parts : nullptr};
+    const int64_t row_tiles = (rows + kGroup - 1) / kGroup;
+    const dim3 grid((columns + kGroup - 1) / kGroup, static_cast<uint32_t>(row_tiles));
+    return for_dtype(dt, [&](auto d) {
+        const LaunchCheck check;
+        tile_kernel<decltype(d)::value, false><<<grid, 256, 0, st>>>(a);
+        if (sums) sum_rows_kernel<<<(columns + 15) / 16, 256, 0, st>>>(sum_parts, row_tiles, columns, sums);
+        return check.status();
+    });
+}
+
+}  // namespace hq
+
+extern "C" hq_status hq_fp8_quantize_rows(const void *x, hq_dtype x_dtype, int64_t m, int k, int64_t row_stride, uint8_t *xq,
+                                          float *x_scale, void *stream) {
+    if (m > 0 && (!x || !xq || !x_scale)) return HQ_ERR_NULL;
+    if (!hq::is_float(x_dtype)) return HQ_ERR_DTYPE;
+    if (m < 0 || k <= 0 || row_stride < 0) return HQ_ERR_SHAPE;
+    if (!hq::aligned_to(x, hq::size_of(x_dtype)) || !hq::aligned16(xq) || !hq::aligned_to(x_scale, 4)) return HQ_ERR_ALIGN;
+    if (!hq::fp8_fits(m, k)) return HQ_ERR_UNSUPPORTED;
+    if (m == 0) return HQ_OK;
+    return hq::fp8_rows(x, x_dtype, m, k, row_stride, xq, x_scale, static_cast<hipStream_t>(stream));
+}
+
+extern "C" hq_status hq_fp8_quantize_blocks(const void *w, hq_dtype w_dtype, int64_t n, int k, int64_t row_stride, uint8_t *wq,
+                                            uint8_t *wq_t, float *w_scale, void *stream) {
+    if (!w || (!wq && !wq_t) || !w_scale) return HQ_ERR_NULL;
+    if (!hq::is_float(w_dtype)) return HQ_ERR_DTYPE;
+    if (n <= 0 || k <= 0 || row_stride < 0) return HQ_ERR_SHAPE;
+    if (!hq::aligned_to(w, hq::size_of(w_dtype)) || !hq::aligned16(wq) || !hq::aligned16(wq_t) || !hq::aligned_to(w_scale, 4))
+        return HQ_ERR_ALIGN;
+    if (!hq::fp8_fits(n, k)) return HQ_ERR_UNSUPPORTED;
+    return hq::fp8_blocks(w, w_dtype, n, k, row_stride, wq, wq_t, w_scale, static_cast<hipStream_t>(stream));
+}

@@ -31,7 +31,10 @@ namespace {
     X(hq_status_string) X(hq_quantize_weights) X(hq_act_hadamard_quant) X(hq_int_linear) X(hq_int_conv2d)            \
     X(hq_act_hadamard_quant_static) X(hq_int_linear_static) X(hq_int_conv2d_static) X(hq_quantize_weights_single)    \
     X(hq_int_linear_single) X(hq_act_hadamard_quant_width) X(hq_int_conv2d_width) X(hq_int_linear_i8)                \
-    X(hq_int_conv2d_i8) X(hq_act_hadamard_quant_i8) X(hq_act_quant_int_conv2d) X(hq_act_quant_int_linear)
+    X(hq_int_conv2d_i8) X(hq_act_hadamard_quant_i8) X(hq_act_quant_int_conv2d) X(hq_act_quant_int_linear) \
+    X(hq_fp8_quantize_rows) X(hq_fp8_quantize_blocks) X(hq_fp8_linear) X(hq_act_quant_fp8_linear)                    \
+    X(hq_act_quant_fp8_linear_workspace) X(hq_fp8_linear_backward) X(hq_fp8_linear_backward_workspace)               \
+    X(hq_qk_norm_rope) X(hq_qk_norm_rope_backward) X(hq_qk_norm_rope_backward_workspace)
 
 struct Library {
 #define X(name) decltype(&::name) name;
@@ -214,6 +217,20 @@ PyObject *wrap(const at::Tensor &a, const at::Tensor &b) {
     PyObject *p = pa && pb ? PyTuple_Pack(2, pa, pb) : nullptr;
     Py_XDECREF(pa);
     Py_XDECREF(pb);
+    return p;
+}
+
+PyObject *wrap(std::initializer_list<at::Tensor> ts) {   // None for one that is not defined
+    PyObject *p = PyTuple_New(static_cast<Py_ssize_t>(ts.size()));
+    Py_ssize_t i = 0;
+    for (const at::Tensor &t : ts) {
+        PyObject *o = p ? t.defined() ? THPVariable_Wrap(t) : Py_NewRef(Py_None) : nullptr;
+        if (!o) {
+            Py_XDECREF(p);
+            return nullptr;
+        }
+        PyTuple_SET_ITEM(p, i++, o);
+    }
     return p;
 }
 
@@ -523,6 +540,275 @@ PyObject *conv2d_width(Args a) {
     return wrap(y);
 }
 
+// ---- 8-bit floats with block scales ----------------------------------------------------------------------------
+constexpr at::ScalarType kE4m3 = at::kFloat8_e4m3fn;
+int64_t pitch_of(int64_t values) { return (values + 15) / 16 * 16; }
+int64_t groups_of(int64_t values) { return (values + 127) / 128; }
+
+hq_dtype float_type(at::ScalarType dt, const char *name) {
+    switch (dt) {
+        case at::kHalf: return HQ_F16;
+        case at::kFloat: return HQ_F32;
+        case at::kBFloat16: return HQ_BF16;
+        default: refuse(std::string(name) + " must be torch.float16, torch.bfloat16 or torch.float32");
+    }
+}
+
+bool truth(PyObject *o) {
+    const int v = PyObject_IsTrue(o);
+    if (v < 0) throw PythonError();
+    return v != 0;
+}
+
+// A matrix of contiguous rows: a contiguous tensor, its leading axes taken together, or a matrix whose rows are apart.
+struct Rows {
+    const at::Tensor &t;
+    hq_dtype type;
+    int64_t m, k, stride;
+};
+Rows rows_of(Args &a, const char *name) {
+    const at::Tensor &t = a.tensor(name);
+    if (!t.is_cuda()) refuse(std::string(name) + " must be a device tensor");
+    if (t.dim() < 1) refuse(std::string(name) + " must have a channel axis");
+    const int64_t k = t.size(-1);
+    if (k < 1) refuse(std::string(name) + " has no channels");
+    const hq_dtype type = float_type(t.scalar_type(), name);
+    expect_32bit({k});
+    if (t.is_contiguous()) return {t, type, t.numel() / k, k, k};
+    if (t.dim() != 2 || (t.stride(1) != 1 && k > 1) || t.stride(0) < 0)
+        refuse(std::string(name) + " must be contiguous, or a matrix of contiguous rows");
+    return {t, type, t.size(0), k, t.stride(0)};
+}
+
+const at::Tensor &fp8_codes(Args &a, const char *name) {
+    const at::Tensor &t = a.device(name);
+    if (t.scalar_type() != kE4m3) refuse(std::string(name) + " must hold torch.float8_e4m3fn codes");
+    if (t.dim() < 1 || t.size(-1) < 1 || t.size(-1) % 16) refuse(std::string(name) + " must have rows of a multiple of 16 codes");
+    return t;
+}
+
+// scales [rows, columns], or the transposed view of such a matrix that is contiguous: then *turned
+const float *block_scales(Args &a, const char *name, int64_t rows, int64_t columns, int *turned) {
+    const at::Tensor &t = a.tensor(name);
+    const bool plain = t.is_contiguous();
+    if (!t.is_cuda() || t.scalar_type() != at::kFloat || t.dim() != 2 || t.size(0) != rows || t.size(1) != columns ||
+        (!plain && !(t.stride(0) == 1 && t.stride(1) == rows)))
+        refuse(std::string(name) + " must be a device tensor of Float, [" + std::to_string(rows) + ", " + std::to_string(columns) +
+               "], contiguous or the transposed view of a contiguous one");
+    *turned = plain ? 0 : 1;
+    return static_cast<const float *>(t.const_data_ptr());
+}
+
+PyObject *fp8_quantize_rows(Args a) {
+    const Rows x = rows_of(a, "x");
+    const at::Tensor xq = empty(with_last(x.t, pitch_of(x.k)), kE4m3, x.t);
+    const at::Tensor xs = empty({groups_of(x.k), x.m}, at::kFloat, x.t);
+    check("hq_fp8_quantize_rows", call(lib.hq_fp8_quantize_rows, x.t.const_data_ptr(), x.type, x.m, narrow(x.k), x.stride,
+                                       static_cast<uint8_t *>(xq.data_ptr()), static_cast<float *>(xs.data_ptr()), stream()));
+    return wrap(xq, xs);
+}
+
+PyObject *fp8_quantize_blocks(Args a) {
+    const Rows w = rows_of(a, "w");
+    const bool transposed = truth(a.next());
+    expect_dims(w.t, 2, "w must be [n, k]");
+    if (w.m < 1) refuse("w has no rows");
+    const at::Tensor wq = empty({w.m, pitch_of(w.k)}, kE4m3, w.t);
+    const at::Tensor ws = empty({groups_of(w.m), groups_of(w.k)}, at::kFloat, w.t);
+    at::Tensor wt;
+    if (transposed) wt = empty({w.k, pitch_of(w.m)}, kE4m3, w.t);
+    check("hq_fp8_quantize_blocks", call(lib.hq_fp8_quantize_blocks, w.t.const_data_ptr(), w.type, w.m, narrow(w.k), w.stride,
+                                         static_cast<uint8_t *>(wq.data_ptr()),
+                                         transposed ? static_cast<uint8_t *>(wt.data_ptr()) : nullptr,
+                                         static_cast<float *>(ws.data_ptr()), stream()));
+    return transposed ? wrap({wq, wt, ws}) : wrap(wq, ws);
+}
+
+PyObject *fp8_linear(Args a) {
+    const at::Tensor &xq = fp8_codes(a, "xq");
+    const int64_t kp = xq.size(-1), m = xq.numel() / kp;
+    expect_32bit({kp});
+    const at::Tensor &sx = a.device("x_scale");
+    if (sx.scalar_type() != at::kFloat || sx.numel() != groups_of(kp) * m || sx.dim() < 1 || sx.size(0) != groups_of(kp))
+        refuse("x_scale must be a contiguous device tensor of Float, [" + std::to_string(groups_of(kp)) + ", " + std::to_string(m) + "]");
+    const at::Tensor &wq = fp8_codes(a, "wq");
+    if (wq.dim() != 2 || wq.size(1) != kp) refuse("wq does not match xq in k");
+    const int64_t n = wq.size(0);
+    expect_32bit({n});
+    int turned = 0;
+    const float *sw = block_scales(a, "w_scale", groups_of(n), groups_of(kp), &turned);
+    PyObject *bias = a.next();
+    const at::ScalarType ydt = a.dtype();
+    const hq_dtype dt = float_type(ydt, "y_dtype");
+    const void *b = Args{&bias, 1}.vec(n, ydt, "bias");
+    const at::Tensor y = result(a.next(), with_last(xq, n), ydt, xq);
+    check("hq_fp8_linear", call(lib.hq_fp8_linear, u8(xq), f32(sx.const_data_ptr()), u8(wq), sw, turned, b, m, narrow(n), narrow(kp),
+                                y.data_ptr(), dt, stream()));
+    return wrap(y);
+}
+
+PyObject *act_quant_fp8_linear(Args a) {
+    const Rows x = rows_of(a, "x");
+    const at::Tensor &wq = fp8_codes(a, "wq");
+    if (wq.dim() != 2 || wq.size(1) != pitch_of(x.k)) refuse("wq does not match x in k");
+    const int64_t n = wq.size(0);
+    expect_32bit({n});
+    int turned = 0;
+    const float *sw = block_scales(a, "w_scale", groups_of(n), groups_of(x.k), &turned);
+    if (turned) refuse("w_scale must be contiguous");
+    PyObject *bias = a.next();
+    const at::ScalarType ydt = a.dtype();
+    const hq_dtype dt = float_type(ydt, "y_dtype");
+    const void *b = Args{&bias, 1}.vec(n, ydt, "bias");
+    const at::Tensor y = result(a.next(), with_last(x.t, n), ydt, x.t);
+    const at::Tensor space = empty({lib.hq_act_quant_fp8_linear_workspace(x.m, narrow(x.k))}, at::kByte, x.t);
+    check("hq_act_quant_fp8_linear", call(lib.hq_act_quant_fp8_linear, x.t.const_data_ptr(), x.type, x.stride, u8(wq), sw, b, x.m, narrow(n),
+                                          narrow(x.k), space.data_ptr(), y.data_ptr(), dt, stream()));
+    return wrap(y);
+}
+
+PyObject *fp8_linear_backward(Args a) {
+    const Rows dy = rows_of(a, "dy"), x = rows_of(a, "x");
+    if (x.type != dy.type) refuse("dy and x must have one type");
+    if (x.m != dy.m) refuse("dy does not match x in rows");
+    const at::Tensor &wt = fp8_codes(a, "wq_t");
+    if (wt.dim() != 2 || wt.size(0) != x.k || wt.size(1) != pitch_of(dy.k)) refuse("wq_t does not match x and dy");
+    int turned = 0;
+    const float *sw = block_scales(a, "w_scale", groups_of(dy.k), groups_of(x.k), &turned);
+    if (turned) refuse("w_scale must be contiguous");
+    const bool bias = truth(a.next());
+    const at::Tensor dx = empty(with_last(x.t, x.k), x.t.scalar_type(), x.t);
+    const at::Tensor dw = empty({dy.k, x.k}, at::kFloat, x.t);
+    at::Tensor db;
+    if (bias) db = empty({dy.k}, at::kFloat, x.t);
+    const at::Tensor space = empty({lib.hq_fp8_linear_backward_workspace(x.m, narrow(dy.k), narrow(x.k))}, at::kByte, x.t);
+    check("hq_fp8_linear_backward",
+          call(lib.hq_fp8_linear_backward, dy.t.const_data_ptr(), dy.stride, x.t.const_data_ptr(), x.stride, x.type, u8(wt), sw, x.m,
+               narrow(dy.k), narrow(x.k), space.data_ptr(), dx.data_ptr(), static_cast<float *>(dw.data_ptr()),
+               bias ? static_cast<float *>(db.data_ptr()) : nullptr, stream()));
+    return wrap({dx, dw, db});
+}
+
+// ---- query and key heads ---------------------------------------------------------------------------------------------
+// [t, heads, d] with contiguous channels
+const at::Tensor &heads_of(PyObject *o, const char *name, const at::Tensor *like) {
+    if (!THPVariable_Check(o)) {
+        PyErr_Format(PyExc_TypeError, "%s must be a tensor", name);
+        throw PythonError();
+    }
+    const at::Tensor &t = THPVariable_Unpack(o);
+    if (!t.is_cuda() || t.dim() != 3 || (t.stride(2) != 1 && t.size(2) > 1))
+        refuse(std::string(name) + " must be a device tensor [tokens, heads, channels] with contiguous channels");
+    if (like && (t.scalar_type() != like->scalar_type() || t.sizes() != like->sizes()))
+        refuse(std::string(name) + " has another type or shape than what it belongs to");
+    return t;
+}
+// memory that is written through strides: no element twice
+void expect_distinct(const at::Tensor &t, const char *name) {
+    const int64_t n0 = t.size(0), n1 = t.size(1), d = t.size(2), s0 = t.stride(0), s1 = t.stride(1);
+    const bool heads_inside = (n1 < 2 || s1 >= d) && (n0 < 2 || s0 >= (n1 - 1) * s1 + d);
+    const bool tokens_inside = (n0 < 2 || s0 >= d) && (n1 < 2 || s1 >= (n0 - 1) * s0 + d);
+    if (!heads_inside && !tokens_inside) refuse(std::string(name) + " must not overlap itself");
+}
+
+struct Qk {
+    const at::Tensor &q, &k;
+    hq_dtype type, weight_type;
+    const void *q_weight, *k_weight;
+    const float *cos, *sin;
+    int64_t positions;
+    int rotary;
+    const void *pos;
+    int pos_size;
+    float eps;
+    int interleaved;
+    int64_t t() const { return q.size(0); }
+    int d() const { return narrow(q.size(2)); }
+    int heads() const { return narrow(q.size(1)); }
+    int kv_heads() const { return narrow(k.size(1)); }
+};
+Qk qk_of(Args &a) {
+    const at::Tensor &q = heads_of(a.next(), "q", nullptr), &k = heads_of(a.next(), "k", nullptr);
+    const hq_dtype type = float_type(q.scalar_type(), "q");
+    if (k.scalar_type() != q.scalar_type() || k.size(0) != q.size(0) || k.size(2) != q.size(2)) refuse("k does not match q");
+    expect_32bit({q.size(1), k.size(1), q.size(2)});
+    PyObject *w[2] = {a.next(), a.next()};
+    at::ScalarType wdt = q.scalar_type();
+    for (PyObject *o : w)
+        if (THPVariable_Check(o) && THPVariable_Unpack(o).scalar_type() == at::kFloat) wdt = at::kFloat;
+    const void *qw = Args{&w[0], 1}.vec(q.size(2), wdt, "q_weight"), *kw = Args{&w[1], 1}.vec(q.size(2), wdt, "k_weight");
+    const at::Tensor &cos = a.device("cos"), &sin = a.device("sin");
+    if (cos.scalar_type() != at::kFloat || sin.scalar_type() != at::kFloat || cos.dim() != 2 || cos.sizes() != sin.sizes())
+        refuse("cos and sin must be Float, [positions, rotary / 2]");
+    expect_32bit({cos.size(1) * 2});
+    const void *pos = nullptr;
+    int pos_size = 0;
+    if (a.none()) {
+        a.next();
+    } else {
+        const at::Tensor &p = a.device("positions");
+        if ((p.scalar_type() != at::kInt && p.scalar_type() != at::kLong) || p.numel() != q.size(0))
+            refuse("positions must hold one torch.int32 or torch.int64 for each token");
+        pos = p.const_data_ptr();
+        pos_size = p.scalar_type() == at::kLong ? 8 : 4;
+    }
+    const double eps = PyFloat_AsDouble(a.next());
+    if (eps == -1.0 && PyErr_Occurred()) throw PythonError();
+    const bool interleaved = truth(a.next());
+    return {q, k, type, float_type(wdt, "q_weight"), qw, kw, f32(cos.const_data_ptr()), f32(sin.const_data_ptr()), cos.size(0),
+            narrow(cos.size(1) * 2), pos, pos_size, static_cast<float>(eps), interleaved ? 1 : 0};
+}
+
+// the results: new, or the caller's
+struct QkOut {
+    at::Tensor q, k;
+    QkOut(PyObject *out, const Qk &in) {
+        if (out == Py_None) {
+            q = empty(in.q.sizes(), in.q.scalar_type(), in.q);
+            k = empty(in.k.sizes(), in.k.scalar_type(), in.k);
+            return;
+        }
+        const Pair pair(out);
+        q = heads_of(pair.a, "out[0]", &in.q);
+        k = heads_of(pair.b, "out[1]", &in.k);
+        expect_distinct(q, "out[0]");
+        expect_distinct(k, "out[1]");
+    }
+};
+
+PyObject *qk_norm_rope(Args a) {
+    const Qk in = qk_of(a);
+    const QkOut out(a.next(), in);
+    const int64_t strides[8] = {in.q.stride(0), in.q.stride(1), in.k.stride(0), in.k.stride(1),
+                                out.q.stride(0), out.q.stride(1), out.k.stride(0), out.k.stride(1)};
+    check("hq_qk_norm_rope", call(lib.hq_qk_norm_rope, in.q.const_data_ptr(), in.k.const_data_ptr(), in.type, in.t(), in.heads(),
+                                  in.kv_heads(), in.d(), static_cast<const int64_t *>(strides), in.q_weight, in.k_weight, in.weight_type,
+                                  in.cos, in.sin, in.positions, in.rotary, in.interleaved, in.pos, in.pos_size, in.eps,
+                                  out.q.data_ptr(), out.k.data_ptr(), stream()));
+    return wrap(out.q, out.k);
+}
+
+PyObject *qk_norm_rope_backward(Args a) {
+    PyObject *dq_o = a.next(), *dk_o = a.next();
+    const Qk in = qk_of(a);
+    const at::Tensor &dq = heads_of(dq_o, "dq", &in.q), &dk = heads_of(dk_o, "dk", &in.k);
+    const QkOut out(a.next(), in);
+    at::Tensor qw, kw;
+    if (in.q_weight) qw = empty({in.d()}, at::kFloat, in.q);
+    if (in.k_weight) kw = empty({in.d()}, at::kFloat, in.q);
+    const at::Tensor space = empty({lib.hq_qk_norm_rope_backward_workspace(in.t(), in.heads(), in.kv_heads(), in.d(), in.rotary)},
+                                   at::kByte, in.q);
+    const int64_t strides[12] = {in.q.stride(0), in.q.stride(1), in.k.stride(0), in.k.stride(1), dq.stride(0), dq.stride(1),
+                                 dk.stride(0), dk.stride(1), out.q.stride(0), out.q.stride(1), out.k.stride(0), out.k.stride(1)};
+    check("hq_qk_norm_rope_backward",
+          call(lib.hq_qk_norm_rope_backward, dq.const_data_ptr(), dk.const_data_ptr(), in.q.const_data_ptr(), in.k.const_data_ptr(),
+               in.type, in.t(), in.heads(), in.kv_heads(), in.d(), static_cast<const int64_t *>(strides), in.q_weight, in.k_weight,
+               in.weight_type, in.cos, in.sin, in.positions, in.rotary, in.interleaved, in.pos, in.pos_size, in.eps, space.data_ptr(),
+               out.q.data_ptr(), out.k.data_ptr(), qw.defined() ? static_cast<float *>(qw.data_ptr()) : nullptr,
+               kw.defined() ? static_cast<float *>(kw.data_ptr()) : nullptr, stream()));
+    return wrap({out.q, out.k, qw, kw});
+}
+
 // ---- module -----------------------------------------------------------------------------------------------------
 template <PyObject *(*F)(Args)>
 PyObject *entry(PyObject *, PyObject *const *args, Py_ssize_t n) {
@@ -569,6 +855,8 @@ PyMethodDef methods[] = {
     HQ_METHOD(conv2d), HQ_METHOD(conv2d_static), HQ_METHOD(conv2d_i8),
     HQ_METHOD(act_quant_conv2d), HQ_METHOD(act_quant_linear), HQ_METHOD(quantize_weights_single), HQ_METHOD(linear_single),
     HQ_METHOD(act_hadamard_quant_width), HQ_METHOD(conv2d_width),
+    HQ_METHOD(fp8_quantize_rows), HQ_METHOD(fp8_quantize_blocks), HQ_METHOD(fp8_linear), HQ_METHOD(act_quant_fp8_linear),
+    HQ_METHOD(fp8_linear_backward), HQ_METHOD(qk_norm_rope), HQ_METHOD(qk_norm_rope_backward),
     {"bind", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(bind)), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 

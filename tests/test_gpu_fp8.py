@@ -1,0 +1,362 @@
+"""Layers of 8-bit floats with block scales against their definitions in 64 bits (NumPy).
+
+Tolerances.  Codes and scales are compared exactly: they are fixed by fp32 operations that NumPy rounds in the same way.  A product of
+given codes differs from the 64-bit one by the sums alone.  With `a` = sum |terms| of an output: in fp32 128 products are added, and
+K / 128 of those sums, each addition off by at most 2^-23 of a partial sum that is at most a, so (128 + K / 128 + 4) 2^-23 a bounds it
+whatever the order; rounding to the output's type adds half a unit of its last place.  Results of 16 bits may be taken with the matrix
+instruction of 8-bit floats, which cuts the products of each eight below 2^-13 of the eight's largest: 8 x 2^-13 of that largest one, 2^-10 a
+at most, more.  Products of small whole numbers lie within those 13 bits, so their sums have to be exact."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2512_05746_amd as hq
+
+pytestmark = pytest.mark.gpu
+
+DTYPES = {"f16": torch.float16, "bf16": torch.bfloat16, "f32": torch.float32}
+ULP = {"f16": 2.0 ** -11, "bf16": 2.0 ** -8, "f32": 2.0 ** -24}      # half a unit of the last place, relative
+TINY = {"f16": 2.0 ** -25, "bf16": 0.0, "f32": 0.0}                  # half of the smallest subnormal
+
+
+def up(a, b):
+    return -(-a // b)
+
+
+def values(shape, dtype, seed, scale=1.0):
+    """Normal values, some channels larger by 20, as a tensor of the type; and what it holds, as float32."""
+    rng = np.random.default_rng(seed)
+    x = rng.standard_normal(shape) * scale
+    x[..., rng.permutation(shape[-1])[:max(1, shape[-1] // 50)]] *= 20
+    t = torch.from_numpy(x.astype(np.float32)).to(DTYPES[dtype])
+    return t.cuda(), t.float().numpy()
+
+
+# ---- the definition -------------------------------------------------------------------------------------------
+
+def e4m3(v):
+    """fp32 -> the nearest E4M3 number, ties to even."""
+    v = v.astype(np.float64)
+    step = 2.0 ** (np.maximum(np.floor(np.log2(np.maximum(np.abs(v), 2.0 ** -20))), -6) - 3)
+    return np.rint(v / step) * step
+
+
+def quantised(x, rows):
+    """float32 x [r, c] -> (code values [r, c], scales [ceil(r / rows), ceil(c / 128)]), tiles of rows x 128."""
+    r, c = x.shape
+    rb, cb = up(r, rows), up(c, 128)
+    t = np.zeros((rb * rows, cb * 128), np.float32)
+    t[:r, :c] = x
+    t = t.reshape(rb, rows, cb, 128)
+    with np.errstate(invalid="ignore"):
+        top = np.abs(t).max(axis=(1, 3))
+        s = np.where(top == 0, np.float32(1), np.maximum(top * (np.float32(1) / np.float32(448)), np.float32(2.0 ** -126)))
+        s = np.where(np.isfinite(top), s, np.float32(np.nan)).astype(np.float32)
+        inverse = np.where(np.isnan(s), np.float32(0), np.float32(1) / s)[:, None, :, None]
+        q = e4m3(np.where(inverse == 0, np.float32(0), t) * inverse)
+    return q.reshape(rb * rows, cb * 128)[:r, :c], s
+
+
+def spread(s, rows, r, c):
+    return np.repeat(np.repeat(s.astype(np.float64), rows, 0), 128, 1)[:r, :c]
+
+
+def held(codes):
+    return codes.cpu().float().numpy().astype(np.float64)
+
+
+def product_bound(x, w, steps, dtype):
+    return (np.abs(x) @ np.abs(w).T) * ((128 + steps + 4) * 2.0 ** -23 + (0 if dtype == "f32" else 2.0 ** -10))
+
+
+def close(got, want, bound, dtype):
+    got = got.detach().cpu().double().numpy().reshape(want.shape)
+    off = np.abs(got - want)
+    room = bound + ULP[dtype] * (np.abs(want) + bound) + TINY[dtype]
+    worst = np.unravel_index(np.argmax(off - room), off.shape) if off.size else None
+    assert (off <= room).all(), "%s: %g off, %g allowed" % (worst, off[worst], room[worst])
+
+
+# ---- quantisers -----------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("m,k", [(1, 1), (1, 128), (3, 127), (17, 129), (16, 8), (33, 200), (5, 1001), (130, 384), (2049, 960)])
+def test_rows(m, k, dtype):
+    x, xf = values((m, k), dtype, m * 1000 + k)
+    xq, s = hq.hq_fp8_quantize_rows(x)
+    q, sr = quantised(xf, 1)
+    assert xq.shape == (m, up(k, 16) * 16) and s.shape == (up(k, 128), m)
+    assert np.array_equal(s.cpu().numpy(), sr.T)
+    got = held(xq)
+    assert np.array_equal(got[:, :k], q) and not got[:, k:].any()
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("n,k", [(1, 1), (1, 16), (127, 129), (128, 128), (129, 40), (264, 520), (960, 1001)])
+def test_blocks(n, k, dtype):
+    w, wf = values((n, k), dtype, n * 1000 + k, 0.02)
+    wq, wt, s = hq.hq_fp8_quantize_blocks(w, transposed=True)
+    q, sr = quantised(wf, 128)
+    assert np.array_equal(s.cpu().numpy(), sr)
+    assert wq.shape == (n, up(k, 16) * 16) and wt.shape == (k, up(n, 16) * 16)
+    assert np.array_equal(held(wq)[:, :k], q) and not held(wq)[:, k:].any()
+    assert np.array_equal(held(wt)[:, :n], q.T) and not held(wt)[:, n:].any()
+    alone, s1 = hq.hq_fp8_quantize_blocks(w)
+    assert torch.equal(alone.view(torch.uint8), wq.view(torch.uint8)) and torch.equal(s1, s)
+
+
+def test_special_values():
+    """Zero groups, the smallest and the largest numbers, ties, infinities and NaN."""
+    x = np.zeros((12, 256), np.float32)
+    x[1, 3] = 1e-45
+    x[2, 5], x[2, 6] = 3.4028235e38, -3.4028235e38
+    x[3, :128] = np.arange(128) * 2.0 ** -130
+    x[4, 0], x[4, 1:33] = 448.0, np.arange(32) + 0.5          # every second one a tie between two numbers of this size
+    x[5, 0], x[5, 1:65] = 448.0, np.arange(64) * 2.0 ** -11   # subnormal codes and their ties
+    x[6, 200] = np.inf
+    x[7, 10] = -np.inf
+    x[8, 127], x[8, 128] = np.nan, 2.0
+    x[9] = -1.0
+    x[10, 255] = 1e-37
+    x[11, 0] = np.float32(2.0 ** -117)
+    t = torch.from_numpy(x).cuda()
+    xq, s = hq.hq_fp8_quantize_rows(t)
+    q, sr = quantised(x, 1)
+    assert np.array_equal(s.cpu().numpy(), sr.T, equal_nan=True)
+    assert np.array_equal(held(xq), q)
+    assert np.isnan(sr[6, 1]) and not np.isnan(sr[6, 0]) and np.isnan(sr[8, 0]) and not np.isnan(sr[8, 1])
+    w = torch.ones((3, 256), device="cuda")
+    wq, ws = hq.hq_fp8_quantize_blocks(w)
+    y = hq.hq_fp8_linear(xq, s, wq, ws, y_dtype=torch.float32)
+    bad = torch.isnan(y).all(1).cpu().numpy()
+    assert bad.tolist() == [i in (6, 7, 8) for i in range(12)] and not torch.isnan(y[~torch.from_numpy(bad).cuda()]).any()
+
+
+def test_rows_apart_and_repeated():
+    """Rows with a stride, at addresses that are only aligned to an element, and a row that is repeated."""
+    whole, wf = values((40, 333), "f16", 5)
+    part = whole[:, 7:208]
+    xq, s = hq.hq_fp8_quantize_rows(part)
+    q, sr = quantised(wf[:, 7:208], 1)
+    assert np.array_equal(held(xq)[:, :201], q) and np.array_equal(s.cpu().numpy(), sr.T)
+    row = whole[:1, 3:300].expand(21, 297)
+    xq, s = hq.hq_fp8_quantize_rows(row)
+    q, sr = quantised(np.repeat(wf[:1, 3:300], 21, 0), 1)
+    assert np.array_equal(held(xq)[:, :297], q) and np.array_equal(s.cpu().numpy(), sr.T)
+    wq, ws = hq.hq_fp8_quantize_blocks(whole[1::2, 1:300])
+    q, sr = quantised(wf[1::2, 1:300], 128)
+    assert np.array_equal(held(wq)[:, :299], q) and np.array_equal(ws.cpu().numpy(), sr)
+
+
+# ---- the product ----------------------------------------------------------------------------------------------
+
+SHAPES = [(1, 1, 1), (1, 16, 16), (2, 128, 3), (1, 960, 384), (7, 129, 130), (15, 64, 17), (16, 1000, 129), (17, 384, 640), (31, 144, 257),
+          (33, 1001, 77), (64, 128, 64), (65, 2000, 65), (100, 576, 1728), (127, 272, 128), (129, 48, 300), (255, 1040, 520),
+          (257, 200, 264), (300, 130, 1000), (520, 4000, 200), (1025, 640, 776), (2048, 128, 2049)]
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("m,k,n", SHAPES)
+def test_product(m, k, n, dtype):
+    x, _ = values((m, k), "f32", m + k)
+    w, _ = values((n, k), "f32", n + k, 0.02)
+    b, bf = values((n,), dtype, n)
+    xq, sx = hq.hq_fp8_quantize_rows(x)
+    wq, sw = hq.hq_fp8_quantize_blocks(w)
+    xd = held(xq)[:, :k] * spread(sx.cpu().numpy().T, 1, m, k)
+    wd = held(wq)[:, :k] * spread(sw.cpu().numpy(), 128, n, k)
+    y = hq.hq_fp8_linear(xq, sx, wq, sw, b, y_dtype=DTYPES[dtype])
+    bias = bf.astype(np.float64)
+    bound = product_bound(xd, wd, up(k, 128), dtype) + 2.0 ** -23 * np.abs(bias)
+    close(y, xd @ wd.T + bias, bound, dtype)
+    # without a bias, into a buffer, from leading axes; the bits do not depend on the way
+    out = torch.full((m, n), 7.0, dtype=DTYPES[dtype], device="cuda")
+    again = hq.hq_fp8_linear(xq, sx, wq, sw, None, y_dtype=DTYPES[dtype], out=out)
+    assert again.data_ptr() == out.data_ptr()
+    close(out, xd @ wd.T, bound, dtype)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("m,k,n", SHAPES)
+def test_products_of_whole_numbers(m, k, n, dtype):
+    """Sums of small whole numbers times powers of two for scales, with zeros in most places where fp16 would overflow: exact."""
+    rng = np.random.default_rng(m + k + n)
+    x = (rng.integers(-7, 8, (m, k)) * (rng.random((m, k)) < 0.2)).astype(np.float32)
+    w = rng.integers(-3, 4, (n, k)).astype(np.float32)
+    code = lambda v: torch.nn.functional.pad(torch.from_numpy(v), (0, -k % 16)).to(torch.float8_e4m3fn).cuda()
+    sx, sw = (2.0 ** rng.integers(-3, 1, s) for s in ((up(k, 128), m), (up(n, 128), up(k, 128))))
+    y = hq.hq_fp8_linear(code(x), torch.from_numpy(sx.astype(np.float32)).cuda(), code(w), torch.from_numpy(sw.astype(np.float32)).cuda(),
+                         y_dtype=DTYPES[dtype])
+    want = (x * spread(sx.T, 1, m, k)) @ (w * spread(sw, 128, n, k)).T
+    assert torch.equal(y.cpu(), torch.from_numpy(want).to(torch.float32).to(DTYPES[dtype]))
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("m,k,n", SHAPES)
+def test_layer(m, k, n, dtype):
+    """The whole layer is the two calls."""
+    x, xf = values((m, k), dtype, 3 * m + k)
+    w, _ = values((n, k), "f32", n + k, 0.02)
+    wq, sw = hq.hq_fp8_quantize_blocks(w)
+    y = hq.hq_act_quant_fp8_linear(x, wq, sw, y_dtype=torch.float32)
+    q, s = quantised(xf, 1)
+    xd, wd = q * spread(s, 1, m, k), held(wq)[:, :k] * spread(sw.cpu().numpy(), 128, n, k)
+    close(y, xd @ wd.T, product_bound(xd, wd, up(k, 128), "f32"), "f32")
+
+
+def test_nothing_is_written_beyond_the_result():
+    for m, n in ((5, 3), (19, 129), (200, 333), (300, 264)):
+        x, _ = values((m, 200), "f16", m)
+        w, _ = values((n, 200), "f16", n)
+        wq, sw = hq.hq_fp8_quantize_blocks(w)
+        guard = torch.full((m * n + 1024,), 5.0, dtype=torch.float16, device="cuda")
+        hq.hq_act_quant_fp8_linear(x, wq, sw, y_dtype=torch.float16, out=guard[512:512 + m * n].view(m, n))
+        assert (guard[:512] == 5).all() and (guard[512 + m * n:] == 5).all()
+
+
+def test_leading_axes_and_empty():
+    x, _ = values((3, 4, 5, 200), "bf16", 1)
+    w, _ = values((40, 200), "bf16", 2)
+    wq, sw = hq.hq_fp8_quantize_blocks(w)
+    y = hq.hq_act_quant_fp8_linear(x, wq, sw, y_dtype=torch.bfloat16)
+    assert y.shape == (3, 4, 5, 40)
+    assert torch.equal(y.view(60, 40), hq.hq_act_quant_fp8_linear(x.view(60, 200), wq, sw, y_dtype=torch.bfloat16))
+    none = hq.hq_act_quant_fp8_linear(x[:0], wq, sw, y_dtype=torch.bfloat16)
+    assert none.shape == (0, 4, 5, 40)
+    xq, s = hq.hq_fp8_quantize_rows(x[:0])
+    assert xq.shape == (0, 4, 5, 208) and s.shape == (2, 0)
+    assert hq.hq_fp8_linear(xq, s, wq, sw).shape == (0, 4, 5, 40)
+    wt = hq.hq_fp8_quantize_blocks(w, transposed=True)[1]
+    dx, dw, db = hq.hq_fp8_linear_backward(none, x[:0], wt, sw, bias_grad=True)
+    assert dx.shape == (0, 4, 5, 200) and dw.shape == (40, 200) and not dw.any() and db.shape == (40,) and not db.any()
+
+
+# ---- gradients ------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("m,k,n", [(1, 1, 1), (1, 960, 384), (5, 129, 130), (128, 128, 128), (129, 200, 72), (300, 520, 264), (1000, 64, 777),
+                                   (2049, 384, 129)])
+def test_gradients(m, k, n, dtype):
+    """Against the formula: dx = Q(dy) W, dW = Q(dy)^T Q(x), db = sum dy, each Q along the axis that is summed over."""
+    x, xf = values((m, k), dtype, m + k)
+    dy, dyf = values((m, n), dtype, m + n, 1e-2)
+    w, _ = values((n, k), "f32", n + k, 0.02)
+    wq, wt, sw = hq.hq_fp8_quantize_blocks(w, transposed=True)
+    dx, dw, db = hq.hq_fp8_linear_backward(dy, x, wt, sw, bias_grad=True)
+    assert dx.dtype == DTYPES[dtype] and dw.dtype == torch.float32
+    wd = held(wq)[:, :k] * spread(sw.cpu().numpy(), 128, n, k)
+    q, s = quantised(dyf, 1)
+    dyd = q * spread(s, 1, m, n)
+    close(dx, dyd @ wd, product_bound(dyd, wd.T, up(n, 128), dtype), dtype)
+    q, s = quantised(np.ascontiguousarray(dyf.T), 1)
+    dyt = q * spread(s, 1, n, m)
+    q, s = quantised(np.ascontiguousarray(xf.T), 128)
+    xt = q * spread(s, 128, k, m)
+    close(dw, dyt @ xt.T, product_bound(dyt, xt, up(m, 128), "f32"), "f32")
+    close(db, dyf.astype(np.float64).sum(0), np.abs(dyf).sum(0) * (up(m, 128) + 128) * 2.0 ** -23, "f32")
+    only = hq.hq_fp8_linear_backward(dy, x, wt, sw)
+    assert only[2] is None and torch.equal(only[0], dx) and torch.equal(only[1], dw)   # the same bits again
+
+
+def test_gradients_by_differences():
+    """On values that E4M3 holds exactly the layer is linear, so differences along any direction are its gradient."""
+    rng = np.random.default_rng(11)
+    m, k, n = 37, 200, 70
+    grid = lambda shape: rng.integers(-7, 8, shape).astype(np.float32) * 64   # with 448 in every tile: scale 1, codes exact
+    x, w, dy = grid((m, k)), grid((n, k)), grid((m, n))
+    for t in (x, w, dy):
+        t[:, 0::128], t[0] = 448, 448
+    t = lambda v: torch.from_numpy(v).cuda()
+    wq, wt, sw = hq.hq_fp8_quantize_blocks(t(w), transposed=True)
+    dx, dw, _ = hq.hq_fp8_linear_backward(t(dy), t(x), wt, sw)
+    layer = lambda xx, ww: hq.hq_act_quant_fp8_linear(t(xx), *hq.hq_fp8_quantize_blocks(t(ww)), y_dtype=torch.float32).cpu().double().numpy()
+    base = (layer(x, w) * dy).sum()
+    for _ in range(20):
+        i, j, c = int(rng.integers(m)), int(rng.integers(n)), int(rng.integers(1, 100))
+        step = np.zeros_like(x)
+        step[i, c] = -x[i, c] if x[i, c] else 64
+        assert ((layer(x + step, w) * dy).sum() - base) == float(dx[i, c]) * step[i, c]
+        step = np.zeros_like(w)
+        step[j, c] = -w[j, c] if w[j, c] else 64
+        assert ((layer(x, w + step) * dy).sum() - base) == float(dw[j, c]) * step[j, c]
+
+
+def test_gradients_of_views():
+    """dy and x as columns of wider matrices, and dy a repeated row (the gradient of a sum over the rows)."""
+    wide, _ = values((150, 400), "bf16", 3)
+    x, dy = wide[:, 5:205], wide[:, 210:300]
+    w, _ = values((90, 200), "bf16", 4)
+    _, wt, sw = hq.hq_fp8_quantize_blocks(w, transposed=True)
+    got = hq.hq_fp8_linear_backward(dy, x, wt, sw, bias_grad=True)
+    want = hq.hq_fp8_linear_backward(dy.contiguous(), x.contiguous(), wt, sw, bias_grad=True)
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    row = wide[:1, 210:300].expand(150, 90)
+    got = hq.hq_fp8_linear_backward(row, x, wt, sw, bias_grad=True)
+    want = hq.hq_fp8_linear_backward(row.contiguous(), x.contiguous(), wt, sw, bias_grad=True)
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+def test_another_stream_and_a_graph():
+    x, _ = values((300, 520), "f16", 1)
+    w, _ = values((264, 520), "f16", 2)
+    dy, _ = values((300, 264), "f16", 3)
+    wq, wt, sw = hq.hq_fp8_quantize_blocks(w, transposed=True)
+    step = lambda: (hq.hq_act_quant_fp8_linear(x, wq, sw),) + hq.hq_fp8_linear_backward(dy, x, wt, sw, bias_grad=True)
+    want = [t.clone() for t in step()]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        got = step()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            held_out = step()
+    torch.cuda.current_stream().wait_stream(side)
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    for _ in range(3):
+        for t in held_out:
+            t.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(held_out, want))
+        x.mul_(0.5)
+        want = [t.clone() for t in step()]
+
+
+# ---- refusals -------------------------------------------------------------------------------------------------
+
+def test_refusals():
+    x, _ = values((8, 200), "f16", 1)
+    w, _ = values((24, 200), "f16", 2)
+    wq, wt, sw = hq.hq_fp8_quantize_blocks(w, transposed=True)
+    xq, sx = hq.hq_fp8_quantize_rows(x)
+    dy = torch.zeros((8, 24), dtype=torch.float16, device="cuda")
+    bad = [
+        lambda: hq.hq_fp8_quantize_rows(x.cpu()),
+        lambda: hq.hq_fp8_quantize_rows(x.double()),
+        lambda: hq.hq_fp8_quantize_rows(x.t()),
+        lambda: hq.hq_fp8_quantize_rows(x[:, ::2]),
+        lambda: hq.hq_fp8_quantize_rows(x[:, :0]),
+        lambda: hq.hq_fp8_quantize_blocks(x.view(2, 4, 200)),
+        lambda: hq.hq_fp8_quantize_blocks(x[:0]),
+        lambda: hq.hq_fp8_linear(xq.view(torch.uint8), sx, wq, sw),
+        lambda: hq.hq_fp8_linear(xq[:, :16].contiguous(), sx, wq, sw),
+        lambda: hq.hq_fp8_linear(xq, sx[:1], wq, sw),
+        lambda: hq.hq_fp8_linear(xq, sx.half(), wq, sw),
+        lambda: hq.hq_fp8_linear(xq, sx, wq, sw.t()),
+        lambda: hq.hq_fp8_linear(xq, sx, wq, sw, torch.zeros(24, device="cuda")),          # a bias of another type
+        lambda: hq.hq_fp8_linear(xq, sx, wq, sw, y_dtype=torch.int32),
+        lambda: hq.hq_fp8_linear(xq, sx, wq, sw, out=torch.empty((8, 23), dtype=torch.float16, device="cuda")),
+        lambda: hq.hq_act_quant_fp8_linear(x[:, :100], wq, sw),
+        lambda: hq.hq_act_quant_fp8_linear(x, wq, sw[:, :1]),
+        lambda: hq.hq_fp8_linear_backward(dy, x.float(), wt, sw),
+        lambda: hq.hq_fp8_linear_backward(dy[:7], x, wt, sw),
+        lambda: hq.hq_fp8_linear_backward(dy, x, wq, sw),
+    ]
+    for i, call in enumerate(bad):
+        with pytest.raises(ValueError):
+            call()
+            pytest.fail("case %d was not refused" % i)
+    unaligned = torch.zeros(24 * 208 + 1, dtype=torch.uint8, device="cuda")[1:].view(24, 208).view(torch.float8_e4m3fn)
+    with pytest.raises(hq.HqError) as e:
+        hq.hq_fp8_linear(xq, sx, unaligned, sw)
+    assert e.value.code == 5
