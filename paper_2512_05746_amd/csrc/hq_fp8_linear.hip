@@ -58,140 +58,243 @@ template <> struct Operand<true> {
         }
     }
 };
-__device__ __forceinline__ f32x4 multiply(const Operand<false> &a, const Operand<false> &b) { return mfma_fp8(a.v, b.v); }
-__device__ __forceinline__ f32x4 multiply(const Operand<true> &a, const Operand<true> &b) {
-    f32x4 p{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) p = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.v[i], b.v[i], p, 0, 0, 0);
-    return p;
-}
 
 // A tile of BM tokens x BN channels; WM x WN waves.  Codes of one step, [row][8 pieces of 16 bytes], go from memory straight into LDS;
 // the pieces of a row are kept in an order that depends on the row, so that the 8 lanes of an LDS access read different banks.
+// Two buffers.  The loads are written out: of the compiler's own it cannot tell which buffer they fill, and would let every read of LDS wait for
+// all of them.  They have no register for a result; a wave waits for its own before the barrier that hands the buffer over.
+__device__ __forceinline__ v4i words_of(const void *p, uint32_t bytes) {   // of a buffer's descriptor
+    const uint64_t at = reinterpret_cast<uint64_t>(p);
+    return v4i{static_cast<int>(at), static_cast<int>(at >> 32), static_cast<int>(bytes), 0x00027000};
+}
+// lane i's 16 (4) bytes to lds + 16 i (4 i); zeros from beyond the buffer
+__device__ __forceinline__ void load16_to_lds(const v4i &buffer, uint32_t offset, uint32_t lds) {
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(offset), "s"(buffer), "s"(lds) : "memory", "m0");
+}
+__device__ __forceinline__ void load4_to_lds(const v4i &buffer, uint32_t offset, uint32_t lds) {
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dword %0, %1, 0 offen lds" ::"v"(offset), "s"(buffer), "s"(lds) : "memory", "m0");
+}
+
 template <int OUT, int BM, int BN, int WM, int WN>
-__global__ __launch_bounds__(WM *WN * 64) void product_kernel(ProductArgs a) {
+struct Product {
     using Out = typename Float<OUT>::type;
-    constexpr int NW = WM * WN, TM = BM / WM, TN = BN / WN, MT = TM / 16, NT = TN / 16;
-    constexpr int NG = NT < 4 ? NT : 4, SHIFT = NG == 4 ? 4 : NG == 2 ? 3 : 2;   // a lane's neighbouring channels: 4 NG
-    extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
-    constexpr int kTile = (BM + BN) * kStep;
+    static constexpr bool kFp32 = OUT == HQ_F32;
+    static constexpr int NW = WM * WN, TM = BM / WM, TN = BN / WN, MT = TM / 16, NT = TN / 16;
+    static constexpr int NG = NT < 4 ? NT : 4, SHIFT = NG == 4 ? 4 : NG == 2 ? 3 : 2;   // a lane's neighbouring channels: 4 NG
+    static constexpr int kCodes = (BM + BN) * kStep, LX = BM / 8 / NW, LW = BN / 8 / NW;
+    // after the codes: the tokens' scales, then those of the blocks of channels, 64 copies of each
+    static constexpr int SX = (BM + 63) / 64, SW = (BN + kStep - 1) / kStep, kTile = kCodes + (SX + SW) * 256;
+    static_assert(LX >= 1 && LW >= 1 && (NW * 8) % 32 == 0, "whole loads; the order of pieces is the same in all loads of a wave");
 
-    const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, quarter = lane >> 4;
-    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), wm = wave % WM, wn = wave / WM;
-    const int64_t m0 = static_cast<int64_t>(blockIdx.x) * BM;
-    const int n0 = blockIdx.y * BN;
+    __device__ static __forceinline__ int key_x(int row) { return row & 7; }
+    __device__ static __forceinline__ int key_w(int row) { return (row & 3) | ((row >> SHIFT & 1) << 2); }
 
-    const int64_t rows_x = a.m - m0 < BM ? a.m - m0 : BM, rows_w = a.n - n0 < BN ? a.n - n0 : BN;
-    const __amdgpu_buffer_rsrc_t xb = buffer_of(a.x + m0 * a.pitch, static_cast<uint32_t>(rows_x) * a.pitch);
-    const __amdgpu_buffer_rsrc_t wb = buffer_of(a.w + static_cast<int64_t>(n0) * a.pitch, static_cast<uint32_t>(rows_w) * a.pitch);
-
-    const auto key_x = [](int row) { return row & 7; };
-    const auto key_w = [](int row) { return (row & 3) | ((row >> SHIFT & 1) << 2); };
-
-    // a wave's load brings 8 rows: lane = (row, piece)
-    const int l_row = lane >> 3, l_piece = lane & 7;
-    const auto load = [&](int step, int buffer) {
-        const uint32_t at = static_cast<uint32_t>(step) * kStep;
-#pragma unroll
-        for (int i = wave; i < (BM + BN) / 8; i += NW) {
-            const bool is_x = i < BM / 8;
-            const int row = (is_x ? i : i - BM / 8) * 8 + l_row;
-            const int piece = l_piece ^ (is_x ? key_x(row) : key_w(row));
-            const uint32_t off = at + piece * 16 < static_cast<uint32_t>(a.pitch) ? static_cast<uint32_t>(row) * a.pitch + piece * 16 : 0x80000000u;
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(is_x ? xb : wb, (__attribute__((address_space(3))) void *)(lds + buffer * kTile + i * 1024), 16,
-                                                     off, at, 0, 0);
-        }
-    };
-
+    const ProductArgs &a;
+    int lane, l16, quarter, wave, wm, wn, n0;
+    int64_t m0;
+    v4i xb, wb;
+    uint32_t off_x, off_w, piece_x, piece_w, at = 0;   // of the lane's next loads
+    uint32_t sx_bytes;
+    uint32_t x_at[2], w_at[2], s_at;   // of the lane's two pieces of its first rows, and of its first scale, in a buffer
     f32x4 acc[NT][MT];
-#pragma unroll
-    for (int i = 0; i < NT; ++i)
-#pragma unroll
-        for (int j = 0; j < MT; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
 
-    // (channels that a wave's tile has beyond the last block are not stored)
-    const int block_w = (n0 + wn * TN) / kStep, last_w = (a.n - 1) / kStep;
-    const float *sw = a.sw + static_cast<int64_t>(block_w < last_w ? block_w : last_w) * a.sw_block;
-    int64_t token[MT];
+    __device__ __forceinline__ Product(const ProductArgs &args, uint32_t tile_m, uint32_t tile_n) : a(args) {
+        const int tid = threadIdx.x;
+        lane = tid & 63, l16 = lane & 15, quarter = lane >> 4;
+        wave = __builtin_amdgcn_readfirstlane(tid >> 6), wm = wave % WM, wn = wave / WM;
+        m0 = static_cast<int64_t>(tile_m) * BM, n0 = static_cast<int>(tile_n) * BN;
+        const int rows_x = a.m - m0 < BM ? static_cast<int>(a.m - m0) : BM, rows_w = a.n - n0 < BN ? a.n - n0 : BN;
+        xb = words_of(a.x + m0 * a.pitch, static_cast<uint32_t>(rows_x) * a.pitch);
+        wb = words_of(a.w + static_cast<int64_t>(n0) * a.pitch, static_cast<uint32_t>(rows_w) * a.pitch);
+        // a wave's load brings 8 rows: lane = (row, piece)
+        const int row = wave * 8 + (lane >> 3);
+        piece_x = ((lane & 7) ^ key_x(row)) * 16, piece_w = ((lane & 7) ^ key_w(row)) * 16;
+        off_x = static_cast<uint32_t>(row) * a.pitch + piece_x, off_w = static_cast<uint32_t>(row) * a.pitch + piece_w;
+        sx_bytes = static_cast<uint32_t>(rows_x) * 4;
+        const uint32_t lx = wm * TM + l16, lw = wn * TN + (l16 >> 2) * (4 * NG) + (l16 & 3);
 #pragma unroll
-    for (int j = 0; j < MT; ++j) {
-        const int64_t t = m0 + wm * TM + j * 16 + l16;
-        token[j] = t < a.m ? t : a.m - 1;
+        for (int h = 0; h < 2; ++h) {
+            x_at[h] = lx * kStep + ((quarter * 2 + h) ^ key_x(lx)) * 16;
+            w_at[h] = (BM + lw) * kStep + ((quarter * 2 + h) ^ key_w(lw)) * 16;
+        }
+        s_at = kCodes + lx * 4;
+        // (the compiler would otherwise keep an address for every read: it cannot tell that the offsets add without a carry)
+        asm("" : "+v"(x_at[0]), "+v"(x_at[1]), "+v"(w_at[0]), "+v"(w_at[1]), "+v"(s_at));
+#pragma unroll
+        for (int i = 0; i < NT; ++i)
+#pragma unroll
+            for (int j = 0; j < MT; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
-    load(0, 0);
-    for (int step = 0; step < a.steps; ++step) {
-        __syncthreads();
-        if (step + 1 < a.steps) load(step + 1, (step + 1) & 1);
-        const uint8_t *tx = lds + (step & 1) * kTile, *tw = tx + BM * kStep;
-        const float s_w = sw[static_cast<int64_t>(step) * a.sw_step];
+
+    // Requests the codes and scales of the next step for the buffer at `lds`.
+    __device__ __forceinline__ void request(uint32_t lds, int step) {
+        // (the last step may end inside: pieces beyond the rows' end come from beyond the buffer, as zeros)
+        const uint32_t ox = at + piece_x < static_cast<uint32_t>(a.pitch) ? off_x : 0x80000000u;
+        const uint32_t ow = at + piece_w < static_cast<uint32_t>(a.pitch) ? off_w : 0x80000000u;
+#pragma unroll
+        for (int i = 0; i < LX; ++i) load16_to_lds(xb, ox + static_cast<uint32_t>(i * NW * 8) * a.pitch, lds + (i * NW + wave) * 1024);
+#pragma unroll
+        for (int i = 0; i < LW; ++i) load16_to_lds(wb, ow + static_cast<uint32_t>(i * NW * 8) * a.pitch, lds + (BM / 8 + i * NW + wave) * 1024);
+        off_x += kStep, off_w += kStep, at += kStep;
+#pragma unroll
+        for (int i = wave; i < SX + SW; i += NW) {
+            const bool tokens = i < SX;
+            // (channels of a tile beyond the last block are not stored)
+            const int block = n0 / kStep + i - SX, last = (a.n - 1) / kStep;
+            const float *from = tokens ? a.sx + static_cast<int64_t>(step) * a.m + m0
+                                       : a.sw + static_cast<int64_t>(block < last ? block : last) * a.sw_block + static_cast<int64_t>(step) * a.sw_step;
+            load4_to_lds(words_of(from, tokens ? sx_bytes : 4), tokens ? (i * 64 + lane) * 4 : 0, lds + kCodes + i * 256);
+        }
+    }
+    // The wave's loads have landed, and so have the others'; all have read the buffer that is filled next.
+    __device__ __forceinline__ static void hand_over() {
+        wait_vmem<0>();
+        lds_barrier();
+    }
+
+    __device__ __forceinline__ static void fetch(Operand<kFp32> &o, const uint8_t *lo, const uint8_t *hi) {
+        o.set(*reinterpret_cast<const v4i *>(lo), *reinterpret_cast<const v4i *>(hi));
+    }
+    __device__ __forceinline__ void fetch_w(Operand<kFp32> &o, const uint8_t *lds, int i) const {
+        const int skip = ((i / NG) * (16 * NG) + (i % NG) * 4) * kStep;
+        fetch(o, lds + w_at[0] + skip, lds + w_at[1] + skip);
+    }
+
+    // One step from LDS.  The products of a row of tiles are folded into the sums beside the products of the next row.
+    __device__ __forceinline__ void step(const uint8_t *lds) {
+        Operand<kFp32> x[MT], w[2];
         float s[MT];
-        Operand<OUT == HQ_F32> b[MT];
+        const float s_w = *reinterpret_cast<const float *>(lds + kCodes + (SX + wn * TN / kStep) * 256);
 #pragma unroll
         for (int j = 0; j < MT; ++j) {
-            s[j] = a.sx[static_cast<int64_t>(step) * a.m + token[j]] * s_w;
-            const int row = wm * TM + j * 16 + l16;
-            const v4i lo = *reinterpret_cast<const v4i *>(tx + row * kStep + ((quarter * 2) ^ key_x(row)) * 16);
-            const v4i hi = *reinterpret_cast<const v4i *>(tx + row * kStep + ((quarter * 2 + 1) ^ key_x(row)) * 16);
-            b[j].set(lo, hi);
+            fetch(x[j], lds + x_at[0] + j * 16 * kStep, lds + x_at[1] + j * 16 * kStep);
+            s[j] = *reinterpret_cast<const float *>(lds + s_at + j * 64) * s_w;
         }
+        fetch_w(w[0], lds, 0);
+        f32x4 p[MT];
 #pragma unroll
-        for (int i = 0; i < NT; ++i) {
-            const int row = wn * TN + (i / NG) * (16 * NG) + (l16 >> 2) * (4 * NG) + (i % NG) * 4 + (l16 & 3);
-            const v4i lo = *reinterpret_cast<const v4i *>(tw + row * kStep + ((quarter * 2) ^ key_w(row)) * 16);
-            const v4i hi = *reinterpret_cast<const v4i *>(tw + row * kStep + ((quarter * 2 + 1) ^ key_w(row)) * 16);
-            Operand<OUT == HQ_F32> w;
-            w.set(lo, hi);
+        for (int i = 0; i <= NT; ++i) {
+            if (i + 1 < NT) fetch_w(w[(i + 1) & 1], lds, i + 1);
+            if constexpr (!kFp32) {
+#pragma unroll
+                for (int j = 0; j < MT; ++j) {
+                    if (i > 0) fold(i - 1, j, p[j], s[j]);
+                    if (i < NT) p[j] = mfma_fp8(w[i & 1].v, x[j].v);
+                }
+                // four multiply-adds of the row before, a product, in this order
+                if (i + 1 < NT) __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+#pragma unroll
+                for (int j = 0; j < MT; ++j) {
+                    if (i > 0) __builtin_amdgcn_sched_group_barrier(0x2, 4, 0);
+                    if (i < NT) __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            } else {
+                f32x4 q[MT];
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+#pragma unroll
+                    for (int j = 0; j < MT; ++j) {
+                        if (i < NT)
+                            q[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[i & 1].v[k], x[j].v[k], k ? q[j] : f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+                        if (i > 0 && k == 0) fold(i - 1, j, p[j], s[j]);
+                    }
+#pragma unroll
+                for (int j = 0; j < MT; ++j) p[j] = q[j];
+            }
+        }
+    }
+    __device__ __forceinline__ void fold(int i, int j, const f32x4 &p, float s) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[i][j][e] = fmaf(p[e], s, acc[i][j][e]);
+    }
+
+    // Results: a lane has 4 NG neighbouring channels of a token.
+    __device__ __forceinline__ void store() const {
+        constexpr int CH = 4 * NG;
+#pragma unroll
+        for (int g = 0; g < NT / NG; ++g) {
+            const int c = n0 + wn * TN + g * 16 * NG + quarter * CH;
+            const bool whole = c + CH <= a.n;
+            float bias[CH];
+#pragma unroll
+            for (int e = 0; e < CH; ++e) bias[e] = 0.0f;
+            if (a.bias) {
+                const Out *b = static_cast<const Out *>(a.bias);
+#pragma unroll
+                for (int e = 0; e < CH; ++e) bias[e] = static_cast<float>(b[c + e < a.n ? c + e : a.n - 1]);
+            }
 #pragma unroll
             for (int j = 0; j < MT; ++j) {
-                const f32x4 p = multiply(w, b[j]);
+                const int64_t t = m0 + wm * TM + j * 16 + l16;
+                if (t >= a.m) continue;
+                Out *y = static_cast<Out *>(a.y) + t * a.n + c;
+                typename Vec<Out, CH>::type v;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) acc[i][j][e] = fmaf(p[e], s[j], acc[i][j][e]);
+                for (int e = 0; e < CH; ++e) v[e] = round_to<Out>(acc[g * NG + e / 4][j][e % 4] + bias[e]);
+                if (whole) {
+                    store_vec<Out, CH>(y, v);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < CH; ++e)
+                        if (c + e < a.n) y[e] = v[e];
+                }
             }
         }
     }
+};
 
-    // results: a lane has 4 NG neighbouring channels of a token
-    constexpr int CH = 4 * NG;
-#pragma unroll
-    for (int g = 0; g < NT / NG; ++g) {
-        const int c = n0 + wn * TN + g * 16 * NG + quarter * CH;
-        if (c >= a.n) continue;
-        float bias[CH];
-#pragma unroll
-        for (int e = 0; e < CH; ++e)
-            bias[e] = a.bias && c + e < a.n ? static_cast<float>(static_cast<const Out *>(a.bias)[c + e]) : 0.0f;
-#pragma unroll
-        for (int j = 0; j < MT; ++j) {
-            const int64_t t = m0 + wm * TM + j * 16 + l16;
-            if (t >= a.m) continue;
-            Out *y = static_cast<Out *>(a.y) + t * a.n + c;
-            typename Vec<Out, CH>::type v;
-#pragma unroll
-            for (int e = 0; e < CH; ++e) v[e] = round_to<Out>(acc[g * NG + e / 4][j][e % 4] + bias[e]);
-            if (c + CH <= a.n) {
-                store_vec<Out, CH>(y, v);
-            } else {
-#pragma unroll
-                for (int e = 0; e < CH; ++e)
-                    if (c + e < a.n) y[e] = v[e];
-            }
-        }
+// Neighbouring workgroups share tiles' codes in the L2 of their XCD: workgroup b runs on XCD b % 8, each XCD takes a contiguous run of tiles,
+// and those go through bands of 4 tiles of tokens.
+struct Tiles {
+    uint32_t m, n;   // counts
+};
+__device__ __forceinline__ Tiles tile_of(uint32_t b, Tiles count) {
+    const uint32_t all = count.m * count.n, xcd = b & 7, q = all >> 3, r = all & 7;
+    const uint32_t t = xcd * q + (xcd < r ? xcd : r) + (b >> 3);
+    const uint32_t band = t / (4 * count.n), in = t - band * 4 * count.n, left = count.m - band * 4, high = left < 4 ? left : 4;
+    return {band * 4 + in % high, in / high};
+}
+
+template <int OUT, int BM, int BN, int WM, int WN>
+__global__ __launch_bounds__(WM *WN * 64) void product_kernel(ProductArgs a, Tiles count) {
+    using P = Product<OUT, BM, BN, WM, WN>;
+    extern __shared__ __attribute__((aligned(1024))) uint8_t lds[];
+    const uint32_t lds_at = lds_address(lds);
+    const Tiles tile = tile_of(blockIdx.x, count);
+    P p(a, tile.m, tile.n);
+    uint32_t now = 0;   // the buffer that is read
+    p.request(lds_at, 0);
+    for (int i = 0; i < a.steps; ++i) {
+        P::hand_over();
+        if (i + 1 < a.steps) p.request(lds_at + (P::kTile - now), i + 1);
+        p.step(lds + now);
+        now = P::kTile - now;
     }
+    p.store();
 }
 
 __global__ __launch_bounds__(256) void zero_kernel(float *p, int64_t n) {
     for (int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; i < n; i += static_cast<int64_t>(gridDim.x) * 256) p[i] = 0.0f;
 }
 
+template <int OUT, int BM, int BN, int WM, int WN>
+hq_status launch_tiles(const ProductArgs &a, hipStream_t st) {
+    const Tiles count{static_cast<uint32_t>((a.m + BM - 1) / BM), static_cast<uint32_t>((a.n + BN - 1) / BN)};
+    static std::atomic<uint64_t> allowed;
+    if (const hq_status s = allow_lds(reinterpret_cast<const void *>(product_kernel<OUT, BM, BN, WM, WN>), allowed)) return s;
+    const hq::LaunchCheck check;
+    product_kernel<OUT, BM, BN, WM, WN><<<count.m * count.n, WM * WN * 64, 2 * Product<OUT, BM, BN, WM, WN>::kTile, st>>>(a, count);
+    return check.status();
+}
+
 template <int OUT>
 hq_status launch(const ProductArgs &a, hipStream_t st) {
-    constexpr int BM = 128, BN = 128;
-    const dim3 grid(static_cast<uint32_t>((a.m + BM - 1) / BM), (a.n + BN - 1) / BN);
-    static std::atomic<uint64_t> allowed;
-    if (const hq_status s = allow_lds(reinterpret_cast<const void *>(product_kernel<OUT, BM, BN, 2, 2>), allowed)) return s;
-    const hq::LaunchCheck check;
-    product_kernel<OUT, BM, BN, 2, 2><<<grid, 256, 2 * (BM + BN) * kStep, st>>>(a);
-    return check.status();
+    const int64_t large = ((a.m + 255) / 256) * ((a.n + 255) / 256);
+    if constexpr (OUT != HQ_F32) {
+        if (large >= 200) return launch_tiles<OUT, 256, 256, 4, 2>(a, st);
+    }
+    return launch_tiles<OUT, 128, 128, 2, 2>(a, st);
 }
 
 hq_status product(const uint8_t *xq, const float *x_scale, const uint8_t *wq, const float *w_scale, bool scale_turned, const void *bias,
@@ -209,7 +312,7 @@ hq_status product(const uint8_t *xq, const float *x_scale, const uint8_t *wq, co
 
 // Rows of codes whose tiles are addressed with 31-bit offsets, and tile counts that fit a grid.
 bool product_fits(int64_t m, int64_t n, int64_t k) {
-    return k <= (int64_t{1} << 31) / 256 - 16 && n <= int64_t{65535} * 64 && m <= int64_t{0x7FFFFFFF} * 16;
+    return k <= (int64_t{1} << 31) / 256 - 16 && ((m + 15) / 16) * ((n + 15) / 16) <= 0x7FFFFFFF;
 }
 
 int64_t up256(int64_t v) { return (v + 255) & ~int64_t{255}; }
