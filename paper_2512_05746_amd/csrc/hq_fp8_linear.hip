@@ -12,6 +12,7 @@
 #include <stdint.h>
 
 #include <algorithm>
+#include <cstdlib>
 
 #include "hq_buffer.h"
 #include "hq_common.h"
@@ -60,7 +61,9 @@ template <> struct Operand<true> {
 };
 
 // A tile of BM tokens x BN channels; WM x WN waves.  Codes of one step, [row][8 pieces of 16 bytes], go from memory straight into LDS;
-// the pieces of a row are kept in an order that depends on the row, so that the 8 lanes of an LDS access read different banks.
+// the pieces of a row are kept in an order that depends on the row, so that the 16 lanes of an LDS access read different banks (16 rows, two to a
+// line of the 64 banks: 8 cycles a read of 16 bytes a lane without it, 4 with it).  Rows of weights are kept so that a lane's channels in NG tiles of results are
+// neighbours.
 // Two buffers.  The loads are written out: of the compiler's own it cannot tell which buffer they fill, and would let every read of LDS wait for
 // all of them.  They have no register for a result; a wave waits for its own before the barrier that hands the buffer over.
 __device__ __forceinline__ v4i words_of(const void *p, uint32_t bytes) {   // of a buffer's descriptor
@@ -75,25 +78,30 @@ __device__ __forceinline__ void load4_to_lds(const v4i &buffer, uint32_t offset,
     asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dword %0, %1, 0 offen lds" ::"v"(offset), "s"(buffer), "s"(lds) : "memory", "m0");
 }
 
-template <int OUT, int BM, int BN, int WM, int WN>
+template <int OUT, int BM, int BN, int WM, int WN, int STAGES>
 struct Product {
     using Out = typename Float<OUT>::type;
     static constexpr bool kFp32 = OUT == HQ_F32;
     static constexpr int NW = WM * WN, TM = BM / WM, TN = BN / WN, MT = TM / 16, NT = TN / 16;
-    static constexpr int NG = NT < 4 ? NT : 4, SHIFT = NG == 4 ? 4 : NG == 2 ? 3 : 2;   // a lane's neighbouring channels: 4 NG
+    static constexpr int NG = NT < 4 ? NT : 4;   // a lane's neighbouring channels: 4 NG
     static constexpr int kCodes = (BM + BN) * kStep, LX = BM / 8 / NW, LW = BN / 8 / NW;
     // after the codes: the tokens' scales, then those of the blocks of channels, 64 copies of each
     static constexpr int SX = (BM + 63) / 64, SW = (BN + kStep - 1) / kStep, kTile = kCodes + (SX + SW) * 256;
-    static_assert(LX >= 1 && LW >= 1 && (NW * 8) % 32 == 0, "whole loads; the order of pieces is the same in all loads of a wave");
+    static constexpr int LS = (SX + SW + NW - 1) / NW, kLoads = LX + LW + LS;   // of a wave and step
+    static_assert(LX >= 1 && LW >= 1 && (NW * 8) % 16 == 0, "whole loads; the order of pieces is the same in all loads of a wave");
 
-    __device__ static __forceinline__ int key_x(int row) { return row & 7; }
-    __device__ static __forceinline__ int key_w(int row) { return (row & 3) | ((row >> SHIFT & 1) << 2); }
+    __device__ static __forceinline__ int key(int row) { return row >> 1 & 7; }
+    // the channel that a row of LDS holds
+    __host__ __device__ static constexpr int channel(int row) {
+        return row / (16 * NG) * (16 * NG) + (row >> 2 & 3) * (4 * NG) + row / 16 % NG * 4 + (row & 3);
+    }
 
     const ProductArgs &a;
     int lane, l16, quarter, wave, wm, wn, n0;
     int64_t m0;
     v4i xb, wb;
-    uint32_t off_x, off_w, piece_x, piece_w, at = 0;   // of the lane's next loads
+    uint32_t off_x, off_w, piece, at = 0;   // of the lane's next loads
+    uint32_t ox, ow;                        // (beyond the buffer for a piece beyond the rows' end)
     uint32_t sx_bytes;
     uint32_t x_at[2], w_at[2], s_at;   // of the lane's two pieces of its first rows, and of its first scale, in a buffer
     f32x4 acc[NT][MT];
@@ -108,14 +116,14 @@ struct Product {
         wb = words_of(a.w + static_cast<int64_t>(n0) * a.pitch, static_cast<uint32_t>(rows_w) * a.pitch);
         // a wave's load brings 8 rows: lane = (row, piece)
         const int row = wave * 8 + (lane >> 3);
-        piece_x = ((lane & 7) ^ key_x(row)) * 16, piece_w = ((lane & 7) ^ key_w(row)) * 16;
-        off_x = static_cast<uint32_t>(row) * a.pitch + piece_x, off_w = static_cast<uint32_t>(row) * a.pitch + piece_w;
+        piece = ((lane & 7) ^ key(row)) * 16;
+        off_x = static_cast<uint32_t>(row) * a.pitch + piece, off_w = static_cast<uint32_t>(channel(row)) * a.pitch + piece;
         sx_bytes = static_cast<uint32_t>(rows_x) * 4;
-        const uint32_t lx = wm * TM + l16, lw = wn * TN + (l16 >> 2) * (4 * NG) + (l16 & 3);
+        const uint32_t lx = wm * TM + l16, lw = BM + wn * TN + l16;
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            x_at[h] = lx * kStep + ((quarter * 2 + h) ^ key_x(lx)) * 16;
-            w_at[h] = (BM + lw) * kStep + ((quarter * 2 + h) ^ key_w(lw)) * 16;
+            x_at[h] = lx * kStep + ((quarter * 2 + h) ^ key(lx)) * 16;
+            w_at[h] = lw * kStep + ((quarter * 2 + h) ^ key(lw)) * 16;
         }
         s_at = kCodes + lx * 4;
         // (the compiler would otherwise keep an address for every read: it cannot tell that the offsets add without a carry)
@@ -126,18 +134,21 @@ struct Product {
             for (int j = 0; j < MT; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
 
-    // Requests the codes and scales of the next step for the buffer at `lds`.
-    __device__ __forceinline__ void request(uint32_t lds, int step) {
-        // (the last step may end inside: pieces beyond the rows' end come from beyond the buffer, as zeros)
-        const uint32_t ox = at + piece_x < static_cast<uint32_t>(a.pitch) ? off_x : 0x80000000u;
-        const uint32_t ow = at + piece_w < static_cast<uint32_t>(a.pitch) ? off_w : 0x80000000u;
-#pragma unroll
-        for (int i = 0; i < LX; ++i) load16_to_lds(xb, ox + static_cast<uint32_t>(i * NW * 8) * a.pitch, lds + (i * NW + wave) * 1024);
-#pragma unroll
-        for (int i = 0; i < LW; ++i) load16_to_lds(wb, ow + static_cast<uint32_t>(i * NW * 8) * a.pitch, lds + (BM / 8 + i * NW + wave) * 1024);
+    // Requests the codes and scales of the next step for the buffer at `lds`, in kLoads parts.
+    __device__ __forceinline__ void begin_request() {
+        const bool inside = at + piece < static_cast<uint32_t>(a.pitch);   // (the last step may end inside)
+        ox = inside ? off_x : 0x80000000u, ow = inside ? off_w : 0x80000000u;
         off_x += kStep, off_w += kStep, at += kStep;
-#pragma unroll
-        for (int i = wave; i < SX + SW; i += NW) {
+    }
+    __device__ __forceinline__ void request_part(int part, uint32_t lds, int step) const {
+        if (part < LX) {
+            load16_to_lds(xb, ox + static_cast<uint32_t>(part * NW * 8) * a.pitch, lds + (part * NW + wave) * 1024);
+        } else if (part < LX + LW) {
+            const int l = part - LX;
+            load16_to_lds(wb, ow + static_cast<uint32_t>(channel(l * NW * 8)) * a.pitch, lds + (BM / 8 + l * NW + wave) * 1024);
+        } else {
+            // (waves without a piece of their own repeat the last one: all count the same loads)
+            const int l = part - LX - LW, i = l * NW + wave < SX + SW ? l * NW + wave : SX + SW - 1;
             const bool tokens = i < SX;
             // (channels of a tile beyond the last block are not stored)
             const int block = n0 / kStep + i - SX, last = (a.n - 1) / kStep;
@@ -146,9 +157,16 @@ struct Product {
             load4_to_lds(words_of(from, tokens ? sx_bytes : 4), tokens ? (i * 64 + lane) * 4 : 0, lds + kCodes + i * 256);
         }
     }
-    // The wave's loads have landed, and so have the others'; all have read the buffer that is filled next.
-    __device__ __forceinline__ static void hand_over() {
-        wait_vmem<0>();
+    __device__ __forceinline__ void request(uint32_t lds, int step) {
+        begin_request();
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) request_part(i, lds, step);
+    }
+    // The wave's loads for this step have landed (those for the AHEAD steps after it may be under way), and so have the others'; all
+    // have read the buffer that is filled next.
+    template <int AHEAD> __device__ __forceinline__ static void hand_over() {
+        static_assert(AHEAD * kLoads < 64, "the counter of loads has 6 bits");
+        wait_vmem<AHEAD * kLoads>();
         lds_barrier();
     }
 
@@ -156,12 +174,14 @@ struct Product {
         o.set(*reinterpret_cast<const v4i *>(lo), *reinterpret_cast<const v4i *>(hi));
     }
     __device__ __forceinline__ void fetch_w(Operand<kFp32> &o, const uint8_t *lds, int i) const {
-        const int skip = ((i / NG) * (16 * NG) + (i % NG) * 4) * kStep;
+        const int skip = i * 16 * kStep;
         fetch(o, lds + w_at[0] + skip, lds + w_at[1] + skip);
     }
 
-    // One step from LDS.  The products of a row of tiles are folded into the sums beside the products of the next row.
-    __device__ __forceinline__ void step(const uint8_t *lds) {
+    // One step from LDS.  The products of a row of tiles are folded into the sums beside the products of the next row; the loads of step `ahead`
+    // (if REQUEST) are dealt over the rows, since a wave that issues them all at once waits for the path to memory.
+    template <bool REQUEST> __device__ __forceinline__ void step(const uint8_t *lds, uint32_t fill = 0, int ahead = 0) {
+        if constexpr (REQUEST) begin_request();
         Operand<kFp32> x[MT], w[2];
         float s[MT];
         const float s_w = *reinterpret_cast<const float *>(lds + kCodes + (SX + wn * TN / kStep) * 256);
@@ -175,6 +195,10 @@ struct Product {
 #pragma unroll
         for (int i = 0; i <= NT; ++i) {
             if (i + 1 < NT) fetch_w(w[(i + 1) & 1], lds, i + 1);
+            if constexpr (REQUEST) {
+#pragma unroll
+                for (int part = i * kLoads / NT; part < (i + 1) * kLoads / NT && i < NT; ++part) request_part(part, fill, ahead);
+            }
             if constexpr (!kFp32) {
 #pragma unroll
                 for (int j = 0; j < MT; ++j) {
@@ -256,20 +280,31 @@ __device__ __forceinline__ Tiles tile_of(uint32_t b, Tiles count) {
     return {band * 4 + in % high, in / high};
 }
 
-template <int OUT, int BM, int BN, int WM, int WN>
+template <int OUT, int BM, int BN, int WM, int WN, int STAGES>
 __global__ __launch_bounds__(WM *WN * 64) void product_kernel(ProductArgs a, Tiles count) {
-    using P = Product<OUT, BM, BN, WM, WN>;
+    using P = Product<OUT, BM, BN, WM, WN, STAGES>;
     extern __shared__ __attribute__((aligned(1024))) uint8_t lds[];
     const uint32_t lds_at = lds_address(lds);
     const Tiles tile = tile_of(blockIdx.x, count);
     P p(a, tile.m, tile.n);
-    uint32_t now = 0;   // the buffer that is read
-    p.request(lds_at, 0);
-    for (int i = 0; i < a.steps; ++i) {
-        P::hand_over();
-        if (i + 1 < a.steps) p.request(lds_at + (P::kTile - now), i + 1);
-        p.step(lds + now);
-        now = P::kTile - now;
+#pragma unroll
+    for (int i = 0; i < STAGES - 1; ++i)
+        if (i < a.steps) p.request(lds_at + i * P::kTile, i);
+    uint32_t now = 0, next = (STAGES - 1) * P::kTile;   // the buffers that are read and filled
+    const auto turn = [&] {
+        next = now;
+        now = now + P::kTile < STAGES * P::kTile ? now + P::kTile : 0;
+    };
+    int i = 0;
+    for (; i + STAGES - 1 < a.steps; ++i) {
+        P::template hand_over<STAGES - 2>();
+        p.template step<true>(lds + now, lds_at + next, i + STAGES - 1);
+        turn();
+    }
+    for (; i < a.steps; ++i) {
+        P::template hand_over<0>();
+        p.template step<false>(lds + now);
+        turn();
     }
     p.store();
 }
@@ -278,23 +313,40 @@ __global__ __launch_bounds__(256) void zero_kernel(float *p, int64_t n) {
     for (int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; i < n; i += static_cast<int64_t>(gridDim.x) * 256) p[i] = 0.0f;
 }
 
-template <int OUT, int BM, int BN, int WM, int WN>
+template <int OUT, int BM, int BN, int WM, int WN, int STAGES>
 hq_status launch_tiles(const ProductArgs &a, hipStream_t st) {
     const Tiles count{static_cast<uint32_t>((a.m + BM - 1) / BM), static_cast<uint32_t>((a.n + BN - 1) / BN)};
+    constexpr auto kernel = product_kernel<OUT, BM, BN, WM, WN, STAGES>;
     static std::atomic<uint64_t> allowed;
-    if (const hq_status s = allow_lds(reinterpret_cast<const void *>(product_kernel<OUT, BM, BN, WM, WN>), allowed)) return s;
+    if (const hq_status s = allow_lds(reinterpret_cast<const void *>(kernel), allowed)) return s;
     const hq::LaunchCheck check;
-    product_kernel<OUT, BM, BN, WM, WN><<<count.m * count.n, WM * WN * 64, 2 * Product<OUT, BM, BN, WM, WN>::kTile, st>>>(a, count);
+    kernel<<<count.m * count.n, WM * WN * 64, STAGES * Product<OUT, BM, BN, WM, WN, STAGES>::kTile, st>>>(a, count);
     return check.status();
 }
 
 template <int OUT>
 hq_status launch(const ProductArgs &a, hipStream_t st) {
+    static const int force = getenv("HQ_TILE") ? atoi(getenv("HQ_TILE")) : -1;
+    switch (force) {
+        case 0: if constexpr (OUT != HQ_F32) return launch_tiles<OUT, 256, 256, 4, 2, 2>(a, st); else return launch_tiles<OUT, 256, 128, 4, 2, 2>(a, st);
+        case 1: return launch_tiles<OUT, 128, 128, 2, 2, 2>(a, st);
+        case 2: return launch_tiles<OUT, 128, 128, 2, 2, 4>(a, st);
+        case 3: return launch_tiles<OUT, 64, 128, 2, 2, 3>(a, st);
+        case 4: return launch_tiles<OUT, 64, 128, 2, 2, 6>(a, st);
+        case 5: return launch_tiles<OUT, 64, 64, 2, 2, 4>(a, st);
+        case 6: return launch_tiles<OUT, 256, 128, 4, 2, 2>(a, st);
+        case 7: return launch_tiles<OUT, 256, 128, 4, 2, 3>(a, st);
+        case 8: return launch_tiles<OUT, 128, 128, 2, 4, 4>(a, st);
+        case 9: return launch_tiles<OUT, 128, 128, 2, 4, 2>(a, st);
+        case 10: return launch_tiles<OUT, 128, 256, 2, 2, 2>(a, st);
+        case 11: return launch_tiles<OUT, 64, 64, 2, 2, 8>(a, st);
+        case 12: return launch_tiles<OUT, 128, 256, 2, 4, 3>(a, st);
+    }
     const int64_t large = ((a.m + 255) / 256) * ((a.n + 255) / 256);
     if constexpr (OUT != HQ_F32) {
-        if (large >= 200) return launch_tiles<OUT, 256, 256, 4, 2>(a, st);
+        if (large >= 200) return launch_tiles<OUT, 256, 256, 4, 2, 2>(a, st);
     }
-    return launch_tiles<OUT, 128, 128, 2, 2>(a, st);
+    return launch_tiles<OUT, 128, 128, 2, 2, 2>(a, st);
 }
 
 hq_status product(const uint8_t *xq, const float *x_scale, const uint8_t *wq, const float *w_scale, bool scale_turned, const void *bias,
