@@ -31,4 +31,24 @@ hq_status fp8_blocks(const void *x, hq_dtype dt, int64_t rows, int columns, int6
 hq_status fp8_both(const void *x, hq_dtype dt, int64_t rows, int columns, int64_t row_stride, uint8_t *q, float *scale, uint8_t *q_t,
                    float *scale_t, float *sum_parts, float *sums, hipStream_t st);
 
+// A product's arguments.
+struct Fp8Product {
+    const uint8_t *x, *w;        // codes [m, pitch], [n, pitch]
+    const float *sx, *sw;        // [steps, m]; sw[block of channels * sw_block + step * sw_step]
+    const void *bias;            // [n] of the output type, or null
+    void *y;                     // [m, n]
+    int64_t m;
+    int n, pitch, steps;
+    int sw_block, sw_step;
+};
+
+// The product with K split over the waves of a workgroup (hq_fp8_split.hip): of codes, or of rows that it quantises itself.
+struct Fp8Cut {
+    int mt, nt;   // tiles of 16 tokens, of 16 channels, of a workgroup
+    float us;     // estimated
+};
+// the best cut; in: the type of rows that are quantised, or null for codes
+Fp8Cut fp8_split_cut(int64_t m, int64_t n, int64_t steps, const hq_dtype *in, hq_dtype out);
+hq_status fp8_split(const Fp8Product &p, Fp8Cut cut, const void *x, hq_dtype x_dtype, int64_t row_stride, int k, hq_dtype out, hipStream_t st);
+
 }  // namespace hq

@@ -12,70 +12,38 @@
 #include <stdint.h>
 
 #include <algorithm>
-#include <cstdlib>
 
 #include "hq_buffer.h"
 #include "hq_common.h"
 #include "hq_floats.h"
 #include "hq_fp8.h"
-#include "hq_fp6.h"
+#include "hq_fp8_product.h"
 
 namespace {
 
-constexpr int kStep = hq::kFp8Group;   // bytes of a row in one step, and values that share a scale
-
-typedef float f32x4 __attribute__((ext_vector_type(4)));
-
-struct ProductArgs {
-    const uint8_t *x, *w;        // codes [m, pitch], [n, pitch]
-    const float *sx, *sw;        // [steps, m]; sw[block of channels * sw_block + step * sw_step]
-    const void *bias;            // [n] of the output type, or null
-    void *y;                     // [m, n]
-    int64_t m;
-    int n, pitch, steps;
-    int sw_block, sw_step;
-};
-
-__device__ __forceinline__ f32x4 mfma_fp8(const v8i &a, const v8i &b) {
-    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0, 0, 0, 0);
-}
-
-// A lane's 32 codes of a step as an operand of the 8-bit instruction, or of four bf16 ones (E4M3 numbers are bf16 numbers).
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-template <bool FP32> struct Operand {
-    v8i v;
-    __device__ __forceinline__ void set(const v4i &lo, const v4i &hi) { v = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7); }
-};
-template <> struct Operand<true> {
-    bf16x8 v[4];
-    __device__ __forceinline__ void set(const v4i &lo, const v4i &hi) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const uint32_t w = static_cast<uint32_t>(i < 4 ? lo[i] : hi[i - 4]);
-            const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, false), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, true);
-            const int at = (i & 1) * 4;
-            v[i / 2][at] = a[0], v[i / 2][at + 1] = a[1], v[i / 2][at + 2] = b[0], v[i / 2][at + 3] = b[1];
-        }
-    }
-};
-
 // A tile of BM tokens x BN channels; WM x WN waves.  Codes of one step, [row][8 pieces of 16 bytes], go from memory straight into LDS;
-// the pieces of a row are kept in an order that depends on the row, so that the 16 lanes of an LDS access read different banks (16 rows, two to a
-// line of the 64 banks: 8 cycles a read of 16 bytes a lane without it, 4 with it).  Rows of weights are kept so that a lane's channels in NG tiles of results are
-// neighbours.
-// Two buffers.  The loads are written out: of the compiler's own it cannot tell which buffer they fill, and would let every read of LDS wait for
-// all of them.  They have no register for a result; a wave waits for its own before the barrier that hands the buffer over.
+// the pieces of a row are kept in an order that depends on the row, so that lanes that are served together read different banks.  Rows of weights
+// are kept so that a lane's channels in NG tiles of results are neighbours.
+//
+// A wave takes the products of a step in a fixed order, each with the fold of the one four before it (the multiply-adds issue while
+// the matrix pipe is busy): rows of its tiles, the last two rows together, column by column.  Each operand is read from LDS two rows ahead, and
+// the tokens' operands of the next step as soon as the last product with their predecessor has been issued, so that no step begins
+// with a wait.  The one barrier of a step stands before the last two rows: there all waves have read the buffer of this step, which is then
+// filled again, and the buffer of the next one has landed.  The loads of a step are dealt over the products, since a wave that issues them all at once
+// waits for the path to memory.
+//
+// The loads are written out: of the compiler's own it cannot tell which buffer they fill, and would let every read of LDS wait for
+// all of them.  They have no register for a result.
 __device__ __forceinline__ v4i words_of(const void *p, uint32_t bytes) {   // of a buffer's descriptor
     const uint64_t at = reinterpret_cast<uint64_t>(p);
     return v4i{static_cast<int>(at), static_cast<int>(at >> 32), static_cast<int>(bytes), 0x00027000};
 }
 // lane i's 16 (4) bytes to lds + 16 i (4 i); zeros from beyond the buffer
 __device__ __forceinline__ void load16_to_lds(const v4i &buffer, uint32_t offset, uint32_t lds) {
-    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(offset), "s"(buffer), "s"(lds) : "memory", "m0");
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(offset), "s"(buffer), "s"(lds) : "memory");
 }
 __device__ __forceinline__ void load4_to_lds(const v4i &buffer, uint32_t offset, uint32_t lds) {
-    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dword %0, %1, 0 offen lds" ::"v"(offset), "s"(buffer), "s"(lds) : "memory", "m0");
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dword %0, %1, 0 offen lds" ::"v"(offset), "s"(buffer), "s"(lds) : "memory");
 }
 
 template <int OUT, int BM, int BN, int WM, int WN, int STAGES>
@@ -96,15 +64,23 @@ struct Product {
         return row / (16 * NG) * (16 * NG) + (row >> 2 & 3) * (4 * NG) + row / 16 % NG * 4 + (row & 3);
     }
 
+    static constexpr int T = MT * NT, kBody = (NT - 2) * MT, RING = 4;   // products of a step, those before the last two rows
+    static_assert(T >= RING && MT % 2 == 0 && (NT == 2 || NT % 4 == 0), "the order of the products");
+    __host__ __device__ static constexpr int row_of(int t) { return t < kBody ? t / MT : NT - 2 + ((t - kBody) & 1); }
+    __host__ __device__ static constexpr int column_of(int t) { return t < kBody ? t % MT : (t - kBody) / 2; }
+
     const ProductArgs &a;
     int lane, l16, quarter, wave, wm, wn, n0;
     int64_t m0;
     v4i xb, wb;
-    uint32_t off_x, off_w, piece, at = 0;   // of the lane's next loads
-    uint32_t ox, ow;                        // (beyond the buffer for a piece beyond the rows' end)
-    uint32_t sx_bytes;
-    uint32_t x_at[2], w_at[2], s_at;   // of the lane's two pieces of its first rows, and of its first scale, in a buffer
-    f32x4 acc[NT][MT];
+    uint32_t off_x, off_w, piece;            // of the lane's next loads
+    uint32_t ox, ow;                         // (beyond the buffer for a piece beyond the rows' end)
+    uint32_t fill, sx_bytes;
+    int requested = 0;                       // steps
+    uint32_t x_at[2], w_at[2], s_at;         // of the lane's two pieces of its first rows, and of its first scale, in a buffer
+    v8i x[MT], w[4];
+    f32x4 acc[NT][MT], p[RING];
+    float s[MT], s_old[2], s_new[MT], s_w;   // scales of this step, of the columns whose products of the step before are not folded yet, of the next step
 
     __device__ __forceinline__ Product(const ProductArgs &args, uint32_t tile_m, uint32_t tile_n) : a(args) {
         const int tid = threadIdx.x;
@@ -132,105 +108,150 @@ struct Product {
         for (int i = 0; i < NT; ++i)
 #pragma unroll
             for (int j = 0; j < MT; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int i = 0; i < RING; ++i) p[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+        s_old[0] = s_old[1] = 0.0f;
     }
 
-    // Requests the codes and scales of the next step for the buffer at `lds`, in kLoads parts.
-    __device__ __forceinline__ void begin_request() {
-        const bool inside = at + piece < static_cast<uint32_t>(a.pitch);   // (the last step may end inside)
+    // Requests the codes and scales of the next step for the buffer at `lds`, in kLoads parts.  Beyond the last step: zeros from beyond the
+    // buffers, so that all steps count the same loads.
+    __device__ __forceinline__ void begin_request(uint32_t lds) {
+        fill = lds;
+        const bool inside = requested * kStep + static_cast<int>(piece) < a.pitch;   // (the last step may end inside)
         ox = inside ? off_x : 0x80000000u, ow = inside ? off_w : 0x80000000u;
-        off_x += kStep, off_w += kStep, at += kStep;
+        off_x += kStep, off_w += kStep, ++requested;
     }
-    __device__ __forceinline__ void request_part(int part, uint32_t lds, int step) const {
+    __device__ __forceinline__ void request_part(int part) const {
         if (part < LX) {
-            load16_to_lds(xb, ox + static_cast<uint32_t>(part * NW * 8) * a.pitch, lds + (part * NW + wave) * 1024);
+            load16_to_lds(xb, ox + static_cast<uint32_t>(part * NW * 8) * a.pitch, fill + (part * NW + wave) * 1024);
         } else if (part < LX + LW) {
             const int l = part - LX;
-            load16_to_lds(wb, ow + static_cast<uint32_t>(channel(l * NW * 8)) * a.pitch, lds + (BM / 8 + l * NW + wave) * 1024);
+            load16_to_lds(wb, ow + static_cast<uint32_t>(channel(l * NW * 8)) * a.pitch, fill + (BM / 8 + l * NW + wave) * 1024);
         } else {
-            // (waves without a piece of their own repeat the last one: all count the same loads)
-            const int l = part - LX - LW, i = l * NW + wave < SX + SW ? l * NW + wave : SX + SW - 1;
+            // (waves without a piece of their own repeat the last one)
+            const int l = part - LX - LW, i = l * NW + wave < SX + SW ? l * NW + wave : SX + SW - 1, step = requested - 1;
             const bool tokens = i < SX;
             // (channels of a tile beyond the last block are not stored)
             const int block = n0 / kStep + i - SX, last = (a.n - 1) / kStep;
             const float *from = tokens ? a.sx + static_cast<int64_t>(step) * a.m + m0
                                        : a.sw + static_cast<int64_t>(block < last ? block : last) * a.sw_block + static_cast<int64_t>(step) * a.sw_step;
-            load4_to_lds(words_of(from, tokens ? sx_bytes : 4), tokens ? (i * 64 + lane) * 4 : 0, lds + kCodes + i * 256);
+            load4_to_lds(words_of(from, step >= a.steps ? 0 : tokens ? sx_bytes : 4), tokens ? (i * 64 + lane) * 4 : 0, fill + kCodes + i * 256);
         }
     }
-    __device__ __forceinline__ void request(uint32_t lds, int step) {
-        begin_request();
+    __device__ __forceinline__ void request(uint32_t lds) {
+        begin_request(lds);
 #pragma unroll
-        for (int i = 0; i < kLoads; ++i) request_part(i, lds, step);
+        for (int i = 0; i < kLoads; ++i) request_part(i);
     }
-    // The wave's loads for this step have landed (those for the AHEAD steps after it may be under way), and so have the others'; all
-    // have read the buffer that is filled next.
-    template <int AHEAD> __device__ __forceinline__ static void hand_over() {
-        static_assert(AHEAD * kLoads < 64, "the counter of loads has 6 bits");
-        wait_vmem<AHEAD * kLoads>();
+    // All but the wave's last LATER loads have landed, and so have the others'; all have read what is filled next.
+    template <int LATER> __device__ __forceinline__ static void hand_over() {
+        wait_vmem<LATER>();
         lds_barrier();
     }
 
-    __device__ __forceinline__ static void fetch(Operand<kFp32> &o, const uint8_t *lo, const uint8_t *hi) {
-        o.set(*reinterpret_cast<const v4i *>(lo), *reinterpret_cast<const v4i *>(hi));
+    __device__ __forceinline__ static v8i fetch(const uint8_t *lo, const uint8_t *hi) {
+        return __builtin_shufflevector(*reinterpret_cast<const v4i *>(lo), *reinterpret_cast<const v4i *>(hi), 0, 1, 2, 3, 4, 5, 6, 7);
     }
-    __device__ __forceinline__ void fetch_w(Operand<kFp32> &o, const uint8_t *lds, int i) const {
-        const int skip = i * 16 * kStep;
-        fetch(o, lds + w_at[0] + skip, lds + w_at[1] + skip);
+    __device__ __forceinline__ void fetch_x(const uint8_t *lds, int j) { x[j] = fetch(lds + x_at[0] + j * 16 * kStep, lds + x_at[1] + j * 16 * kStep); }
+    __device__ __forceinline__ void fetch_w(const uint8_t *lds, int i) { w[i & 3] = fetch(lds + w_at[0] + i * 16 * kStep, lds + w_at[1] + i * 16 * kStep); }
+    __device__ __forceinline__ void fetch_scales(const uint8_t *lds) {
+        s_w = *reinterpret_cast<const float *>(lds + kCodes + (SX + wn * TN / kStep) * 256);
+#pragma unroll
+        for (int j = 0; j < MT; ++j) s_new[j] = *reinterpret_cast<const float *>(lds + s_at + j * 64);
+    }
+    __device__ __forceinline__ void take_scales() {
+        s_old[0] = s[MT - 2], s_old[1] = s[MT - 1];
+#pragma unroll
+        for (int j = 0; j < MT; ++j) s[j] = s_new[j] * s_w;
+    }
+    // what the first step begins with
+    __device__ __forceinline__ void begin(const uint8_t *lds) {
+#pragma unroll
+        for (int j = 0; j < MT; ++j) s[j] = 0.0f, fetch_x(lds, j);
+        fetch_w(lds, 0);
+        fetch_w(lds, 1);
+        fetch_scales(lds);
+        take_scales();
     }
 
-    // One step from LDS.  The products of a row of tiles are folded into the sums beside the products of the next row; the loads of step `ahead`
-    // (if REQUEST) are dealt over the rows, since a wave that issues them all at once waits for the path to memory.
-    template <bool REQUEST> __device__ __forceinline__ void step(const uint8_t *lds, uint32_t fill = 0, int ahead = 0) {
-        if constexpr (REQUEST) begin_request();
-        Operand<kFp32> x[MT], w[2];
-        float s[MT];
-        const float s_w = *reinterpret_cast<const float *>(lds + kCodes + (SX + wn * TN / kStep) * 256);
+    // adds the product that went into p[t % RING]; t < 0: of the step before
+    __device__ __forceinline__ void fold(int t) {
+        const int u = t < 0 ? t + T : t, i = row_of(u), j = column_of(u);
+        const float scale = t < 0 ? s_old[j - (MT - 2)] : s[j];
 #pragma unroll
-        for (int j = 0; j < MT; ++j) {
-            fetch(x[j], lds + x_at[0] + j * 16 * kStep, lds + x_at[1] + j * 16 * kStep);
-            s[j] = *reinterpret_cast<const float *>(lds + s_at + j * 64) * s_w;
+        for (int e = 0; e < 4; ++e) acc[i][j][e] = fmaf(p[u % RING][e], scale, acc[i][j][e]);
+    }
+    __device__ __forceinline__ void finish() {   // (s_old holds the last step's)
+#pragma unroll
+        for (int t = -RING; t < 0; ++t) fold(t);
+    }
+
+    // reads that go with product t (of NT >= 4 rows)
+    __device__ __forceinline__ void before(int t, const uint8_t *now, const uint8_t *next) {
+        if (t < kBody && t % MT == 0) fetch_w(now, t / MT + 2);
+        if constexpr (NT > 2) {
+            if (t == kBody) fetch_w(next, 0);
+            if (t == kBody + 2) fetch_w(next, 1);
         }
-        fetch_w(w[0], lds, 0);
-        f32x4 p[MT];
+        if (t == T - 2) fetch_scales(next);
+    }
+    __device__ __forceinline__ void after(int t, const uint8_t *next) {
+        if (t >= kBody && (t - kBody) % 2 == 1) fetch_x(next, column_of(t));
+        if (NT == 2 && t >= T - 2) fetch_w(next, t - (T - 2));
+    }
+    // loads that go with product t: a request begins after the barrier and goes on in the next step
+    static constexpr int OVER = T < 16 ? T : 16, kFirst = (2 * MT < OVER ? 2 * MT : OVER) * kLoads / OVER;   // parts of a request before the next step
+    __device__ __forceinline__ void deal(int t) const {
+        const int slot = t >= kBody ? t - kBody : t + 2 * MT;
+        if (slot < OVER) {
 #pragma unroll
-        for (int i = 0; i <= NT; ++i) {
-            if (i + 1 < NT) fetch_w(w[(i + 1) & 1], lds, i + 1);
-            if constexpr (REQUEST) {
-#pragma unroll
-                for (int part = i * kLoads / NT; part < (i + 1) * kLoads / NT && i < NT; ++part) request_part(part, fill, ahead);
-            }
-            if constexpr (!kFp32) {
-#pragma unroll
-                for (int j = 0; j < MT; ++j) {
-                    if (i > 0) fold(i - 1, j, p[j], s[j]);
-                    if (i < NT) p[j] = mfma_fp8(w[i & 1].v, x[j].v);
-                }
-                // four multiply-adds of the row before, a product, in this order
-                if (i + 1 < NT) __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
-#pragma unroll
-                for (int j = 0; j < MT; ++j) {
-                    if (i > 0) __builtin_amdgcn_sched_group_barrier(0x2, 4, 0);
-                    if (i < NT) __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
-                }
-                __builtin_amdgcn_sched_barrier(0);
-            } else {
-                f32x4 q[MT];
-#pragma unroll
-                for (int k = 0; k < 4; ++k)
-#pragma unroll
-                    for (int j = 0; j < MT; ++j) {
-                        if (i < NT)
-                            q[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[i & 1].v[k], x[j].v[k], k ? q[j] : f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
-                        if (i > 0 && k == 0) fold(i - 1, j, p[j], s[j]);
-                    }
-#pragma unroll
-                for (int j = 0; j < MT; ++j) p[j] = q[j];
-            }
+            for (int part = slot * kLoads / OVER; part < (slot + 1) * kLoads / OVER; ++part) request_part(part);
         }
     }
-    __device__ __forceinline__ void fold(int i, int j, const f32x4 &p, float s) {
+
+    // One step from the buffer `now`, which is filled for a later step from its barrier on; `next` holds the step after it.
+    template <int LATER> __device__ __forceinline__ void step(const uint8_t *now, const uint8_t *next, uint32_t now_at) {
+        Halves xh[kFp32 ? MT : 1], wh[2];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) acc[i][j][e] = fmaf(p[e], s, acc[i][j][e]);
+        for (int t = 0; t < T; ++t) {
+            if (t == kBody) {
+                hand_over<LATER>();
+                begin_request(now_at);
+            }
+            before(t, now, next);
+            deal(t);
+            const int i = row_of(t), j = column_of(t);
+            if constexpr (!kFp32) {
+                fold(t - RING);
+                p[t % RING] = mfma_fp8(w[i & 3], x[j]);
+                __builtin_amdgcn_sched_barrier(0);
+                after(t, next);
+            } else {
+                // (converted once: the tokens' operands at the start of the step, those of the weights with their rows)
+                if (t == 0) {
+#pragma unroll
+                    for (int c = 0; c < MT; ++c) xh[c] = halves_of(x[c]);
+                }
+                if (t < kBody ? t % MT == 0 : t == kBody) wh[0] = halves_of(w[i & 3]);
+                if (t == kBody) wh[1] = halves_of(w[(NT - 1) & 3]);
+                if (t % 2 == 1) {   // two products side by side: the four instructions of one wait for each other
+                    const bool body = t < kBody;
+                    fold(t - 1 - RING);
+                    fold(t - RING);
+                    f32x4 a0{0.f, 0.f, 0.f, 0.f}, a1{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        a0 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wh[0].v[k], xh[column_of(t - 1)].v[k], a0, 0, 0, 0);
+                        a1 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wh[body ? 0 : 1].v[k], xh[j].v[k], a1, 0, 0, 0);
+                    }
+                    p[(t - 1) % RING] = a0, p[t % RING] = a1;
+                    __builtin_amdgcn_sched_barrier(0);
+                    after(t - 1, next);
+                    after(t, next);
+                }
+            }
+        }
+        take_scales();
     }
 
     // Results: a lane has 4 NG neighbouring channels of a token.
@@ -288,24 +309,20 @@ __global__ __launch_bounds__(WM *WN * 64) void product_kernel(ProductArgs a, Til
     const Tiles tile = tile_of(blockIdx.x, count);
     P p(a, tile.m, tile.n);
 #pragma unroll
-    for (int i = 0; i < STAGES - 1; ++i)
-        if (i < a.steps) p.request(lds_at + i * P::kTile, i);
-    uint32_t now = 0, next = (STAGES - 1) * P::kTile;   // the buffers that are read and filled
-    const auto turn = [&] {
-        next = now;
-        now = now + P::kTile < STAGES * P::kTile ? now + P::kTile : 0;
-    };
-    int i = 0;
-    for (; i + STAGES - 1 < a.steps; ++i) {
-        P::template hand_over<STAGES - 2>();
-        p.template step<true>(lds + now, lds_at + next, i + STAGES - 1);
-        turn();
+    for (int i = 0; i < STAGES - 1; ++i) p.request(lds_at + i * P::kTile);
+    p.begin_request(lds_at + (STAGES - 1) * P::kTile);
+#pragma unroll
+    for (int i = 0; i < P::kFirst; ++i) p.request_part(i);
+    P::template hand_over<(STAGES - 2) * P::kLoads + P::kFirst>();
+    p.begin(lds);
+    uint32_t now = 0;
+    for (int i = 0; i < a.steps; ++i) {
+        const uint32_t next = now + P::kTile < STAGES * P::kTile ? now + P::kTile : 0;
+        p.template step<(STAGES - 2) * P::kLoads>(lds + now, lds + next, lds_at + now);
+        now = next;
     }
-    for (; i < a.steps; ++i) {
-        P::template hand_over<0>();
-        p.template step<false>(lds + now);
-        turn();
-    }
+    p.finish();
+    wait_vmem<0>();   // (nothing may land in LDS that the workgroup no longer owns)
     p.store();
 }
 
@@ -324,41 +341,59 @@ hq_status launch_tiles(const ProductArgs &a, hipStream_t st) {
     return check.status();
 }
 
-template <int OUT>
-hq_status launch(const ProductArgs &a, hipStream_t st) {
-    static const int force = getenv("HQ_TILE") ? atoi(getenv("HQ_TILE")) : -1;
-    switch (force) {
-        case 0: if constexpr (OUT != HQ_F32) return launch_tiles<OUT, 256, 256, 4, 2, 2>(a, st); else return launch_tiles<OUT, 256, 128, 4, 2, 2>(a, st);
-        case 1: return launch_tiles<OUT, 128, 128, 2, 2, 2>(a, st);
-        case 2: return launch_tiles<OUT, 128, 128, 2, 2, 4>(a, st);
-        case 3: return launch_tiles<OUT, 64, 128, 2, 2, 3>(a, st);
-        case 4: return launch_tiles<OUT, 64, 128, 2, 2, 6>(a, st);
-        case 5: return launch_tiles<OUT, 64, 64, 2, 2, 4>(a, st);
-        case 6: return launch_tiles<OUT, 256, 128, 4, 2, 2>(a, st);
-        case 7: return launch_tiles<OUT, 256, 128, 4, 2, 3>(a, st);
-        case 8: return launch_tiles<OUT, 128, 128, 2, 4, 4>(a, st);
-        case 9: return launch_tiles<OUT, 128, 128, 2, 4, 2>(a, st);
-        case 10: return launch_tiles<OUT, 128, 256, 2, 2, 2>(a, st);
-        case 11: return launch_tiles<OUT, 64, 64, 2, 2, 8>(a, st);
-        case 12: return launch_tiles<OUT, 128, 256, 2, 4, 3>(a, st);
+// The tiles of the product, 16-bit results first, then 32-bit ones.  A step of a lone workgroup takes `round` us, a CU's share of a
+// step `each` us a tile when it has several; measured with 8192 x 4096 -> 8192 and 4096 x 8192 -> 4096 (shares), 2048 x 3840 -> 960 and 1024 x 1024 -> 1024
+// (rounds).  128 x 128 tiles were never the fastest.
+enum Tile { kTile256, kTile128, kTile64x128, kTile64 };
+struct TileCost {
+    Tile tile;
+    int bm, bn;
+    float begin[2], round[2], each[2];
+};
+constexpr TileCost kTiles[] = {{kTile256, 256, 256, {3.5f, 1e30f}, {1.4f, 1e30f}, {1.6f, 1e30f}},
+                               {kTile128, 256, 128, {3.0f, 3.0f}, {0.9f, 1.6f}, {1.18f, 1.95f}},
+                               {kTile64x128, 64, 128, {2.5f, 2.5f}, {0.44f, 0.8f}, {0.38f, 0.6f}},
+                               {kTile64, 64, 64, {2.3f, 2.3f}, {0.37f, 0.62f}, {0.24f, 0.38f}}};
+struct TileChoice {
+    Tile tile;
+    float us;
+};
+TileChoice choose_tile(int64_t m, int64_t n, int64_t steps, hq_dtype out) {
+    TileChoice best{kTile64, 1e30f};
+    for (const TileCost &c : kTiles) {
+        const int o = out == HQ_F32;
+        const int64_t tiles = ((m + c.bm - 1) / c.bm) * ((n + c.bn - 1) / c.bn), cu = hq::compute_units();
+        const float us = c.begin[o] + steps * std::max(c.round[o], ((tiles + cu - 1) / cu) * c.each[o]);
+        if (us < best.us) best = {c.tile, us};
     }
-    const int64_t large = ((a.m + 255) / 256) * ((a.n + 255) / 256);
-    if constexpr (OUT != HQ_F32) {
-        if (large >= 200) return launch_tiles<OUT, 256, 256, 4, 2, 2>(a, st);
-    }
-    return launch_tiles<OUT, 128, 128, 2, 2, 2>(a, st);
+    return best;
 }
 
-hq_status product(const uint8_t *xq, const float *x_scale, const uint8_t *wq, const float *w_scale, bool scale_turned, const void *bias,
-                  int64_t m, int n, int k, void *y, hq_dtype dt, hipStream_t st) {
-    const int steps = static_cast<int>(hq::fp8_groups(k));
-    const int blocks = static_cast<int>(hq::fp8_groups(n));
-    const ProductArgs a{xq, wq, x_scale, w_scale, bias, y, m, n, hq::fp8_pitch(k), steps, scale_turned ? 1 : steps, scale_turned ? blocks : 1};
+template <int OUT>
+hq_status launch(const ProductArgs &a, Tile tile, hipStream_t st) {
+    switch (tile) {
+        case kTile256:
+            if constexpr (OUT != HQ_F32) return launch_tiles<OUT, 256, 256, 4, 2, 2>(a, st);   // (sums in fp32 products need more registers)
+        case kTile128: return launch_tiles<OUT, 256, 128, 4, 2, 3>(a, st);
+        case kTile64x128: return launch_tiles<OUT, 64, 128, 2, 2, 3>(a, st);
+        default: return launch_tiles<OUT, 64, 64, 2, 2, 4>(a, st);
+    }
+}
+
+ProductArgs product_args(const uint8_t *xq, const float *x_scale, const uint8_t *wq, const float *w_scale, bool scale_turned, const void *bias,
+                         int64_t m, int n, int k, void *y) {
+    const int steps = static_cast<int>(hq::fp8_groups(k)), blocks = static_cast<int>(hq::fp8_groups(n));
+    return {xq, wq, x_scale, w_scale, bias, y, m, n, hq::fp8_pitch(k), steps, scale_turned ? 1 : steps, scale_turned ? blocks : 1};
+}
+
+hq_status product(const ProductArgs &a, hq_dtype dt, hipStream_t st) {
+    const hq::Fp8Cut cut = hq::fp8_split_cut(a.m, a.n, a.steps, nullptr, dt);
+    const TileChoice tile = choose_tile(a.m, a.n, a.steps, dt);
+    if (cut.us < tile.us) return hq::fp8_split(a, cut, nullptr, dt, 0, 0, dt, st);
     switch (dt) {
-        case HQ_F16: return launch<HQ_F16>(a, st);
-        case HQ_BF16: return launch<HQ_BF16>(a, st);
-        case HQ_F32: return launch<HQ_F32>(a, st);
-        default: return HQ_ERR_DTYPE;
+        case HQ_F16: return launch<HQ_F16>(a, tile.tile, st);
+        case HQ_BF16: return launch<HQ_BF16>(a, tile.tile, st);
+        default: return launch<HQ_F32>(a, tile.tile, st);
     }
 }
 
@@ -403,7 +438,7 @@ extern "C" hq_status hq_fp8_linear(const uint8_t *xq, const float *x_scale, cons
         return HQ_ERR_ALIGN;
     if (!product_fits(m, n, k)) return HQ_ERR_UNSUPPORTED;
     if (m == 0) return HQ_OK;
-    return product(xq, x_scale, wq, w_scale, w_scale_turned != 0, bias, m, n, k, y, y_dtype, static_cast<hipStream_t>(stream));
+    return product(product_args(xq, x_scale, wq, w_scale, w_scale_turned != 0, bias, m, n, k, y), y_dtype, static_cast<hipStream_t>(stream));
 }
 
 extern "C" int64_t hq_act_quant_fp8_linear_workspace(int64_t m, int k) {
@@ -426,8 +461,15 @@ extern "C" hq_status hq_act_quant_fp8_linear(const void *x, hq_dtype x_dtype, in
     hipStream_t st = static_cast<hipStream_t>(stream);
     uint8_t *xq = static_cast<uint8_t *>(workspace);
     float *sx = reinterpret_cast<float *>(xq + up256(m * hq::fp8_pitch64(k)));
+    // one launch that quantises rows as it multiplies, or two
+    ProductArgs p = product_args(nullptr, nullptr, wq, w_scale, false, bias, m, n, k, y);
+    const hq::Fp8Cut fused = hq::fp8_split_cut(m, n, p.steps, &x_dtype, y_dtype), split = hq::fp8_split_cut(m, n, p.steps, nullptr, y_dtype);
+    const float rows = 2.2f + static_cast<float>(m) * k * (hq::size_of(x_dtype) + 1) / 4.5e6f;
+    if (fused.us < rows + std::min(split.us, choose_tile(m, n, p.steps, y_dtype).us))
+        return hq::fp8_split(p, fused, x, x_dtype, row_stride, k, y_dtype, st);
     if (const hq_status s = hq::fp8_rows(x, x_dtype, m, k, row_stride, xq, sx, st)) return s;
-    return product(xq, sx, wq, w_scale, false, bias, m, n, k, y, y_dtype, st);
+    p.x = xq, p.sx = sx;
+    return product(p, y_dtype, st);
 }
 
 extern "C" int64_t hq_fp8_linear_backward_workspace(int64_t m, int n, int k) {
@@ -461,8 +503,8 @@ extern "C" hq_status hq_fp8_linear_backward(const void *dy, int64_t dy_stride, c
         return s;
     if (const hq_status s = hq::fp8_blocks(x, dtype, m, k, x_stride, nullptr, base + at.xq_t, f32(at.x_scale), st)) return s;
     // dx [m, k] = dy [m, n] W [n, k]: the weights' codes with rows of n, their scales as those of W
-    if (const hq_status s = product(base + at.dyq, f32(at.dy_scale), wq_t, w_scale, true, nullptr, m, k, n, dx, dtype, st)) return s;
+    if (const hq_status s = product(product_args(base + at.dyq, f32(at.dy_scale), wq_t, w_scale, true, nullptr, m, k, n, dx), dtype, st)) return s;
     // dW [n, k] = dy^T [n, m] x [m, k]
-    return product(base + at.dyq_t, f32(at.dy_scale_t), base + at.xq_t, f32(at.x_scale), true, nullptr, n, k, static_cast<int>(m), dw,
+    return product(product_args(base + at.dyq_t, f32(at.dy_scale_t), base + at.xq_t, f32(at.x_scale), true, nullptr, n, k, static_cast<int>(m), dw),
                    HQ_F32, st);
 }

@@ -1,0 +1,40 @@
+// Product of E4M3 codes: arguments and matrix instructions, shared by its kernels.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "hq_buffer.h"
+#include "hq_floats.h"
+#include "hq_fp6.h"
+#include "hq_fp8.h"
+
+namespace {
+
+constexpr int kStep = hq::kFp8Group;   // bytes of a row in one step, and values that share a scale
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+
+using ProductArgs = hq::Fp8Product;
+
+__device__ __forceinline__ f32x4 mfma_fp8(const v8i &a, const v8i &b) {
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0, 0, 0, 0);
+}
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+struct Halves {   // a lane's 32 codes of a step as operands of four bf16 instructions (E4M3 numbers are bf16 numbers)
+    bf16x8 v[4];
+};
+__device__ __forceinline__ Halves halves_of(const v8i &codes) {
+    Halves h;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const uint32_t w = static_cast<uint32_t>(codes[i]);
+        const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, false), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, true);
+        const int at = (i & 1) * 4;
+        h.v[i / 2][at] = a[0], h.v[i / 2][at + 1] = a[1], h.v[i / 2][at + 2] = b[0], h.v[i / 2][at + 3] = b[1];
+    }
+    return h;
+}
+
+}  // namespace

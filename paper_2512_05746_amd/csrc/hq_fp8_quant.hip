@@ -19,42 +19,9 @@
 #include "hq_common.h"
 #include "hq_floats.h"
 #include "hq_fp8.h"
+#include "hq_fp8_codes.h"
 
 namespace {
-
-constexpr int kGroup = hq::kFp8Group;
-
-__device__ __forceinline__ float scale_of(uint32_t amax_bits) {
-    if (amax_bits >= 0x7F800000u) return __uint_as_float(0x7FC00000u);
-    const float s = fmaxf(__uint_as_float(amax_bits) * (1.0f / 448.0f), 0x1p-126f);
-    return amax_bits == 0 ? 1.0f : s;
-}
-// (0 for a tile that is not finite: its codes are taken from zeros)
-__device__ __forceinline__ float inverse_of(float s) { return s == s ? __fdiv_rn(1.0f, s) : 0.0f; }
-
-__device__ __forceinline__ uint32_t magnitude(float v) { return __float_as_uint(v) & 0x7FFFFFFFu; }
-
-// codes of 4 values in a dword; `inverse` is 0 for a tile that is not finite
-__device__ __forceinline__ uint32_t codes4(const float *v, float inverse) {
-    float t[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) t[i] = inverse == 0.0f ? 0.0f : v[i] * inverse;
-    int w = __builtin_amdgcn_cvt_pk_fp8_f32(t[0], t[1], 0, false);
-    return static_cast<uint32_t>(__builtin_amdgcn_cvt_pk_fp8_f32(t[2], t[3], w, true));
-}
-
-// 8 values of a row from column c on; zeros beyond the row's end
-template <class T>
-__device__ __forceinline__ void load8(const T *row, int c, int columns, float (&v)[8]) {
-    if (c + 8 <= columns) {
-        const typename Vec<T, 8>::type t = load_vec<T, 8>(row + c);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = static_cast<float>(t[i]);
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = c + i < columns ? static_cast<float>(row[c + i]) : 0.0f;
-    }
-}
 
 struct RowsArgs {
     const void *x;
@@ -74,12 +41,14 @@ __global__ __launch_bounds__(256) void rows_kernel(RowsArgs a) {
     const T *x = static_cast<const T *>(a.x) + row * a.row_stride;
     for (int b = blockIdx.y; b < groups; b += gridDim.y) {
         const int c = b * kGroup + lane16 * 8;
+        Raw8<T> raw;
+        if (c + 8 <= a.k) raw.load(x + c);
+        else raw.load_some(x + c, a.k - c);
+        Top<T> top;
+        top.add(raw);
         float v[8];
-        load8(x, c, a.k, v);
-        uint32_t top = 0;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) top = max(top, magnitude(v[i]));
-        const float s = scale_of(max_lanes<16>(top)), inverse = inverse_of(s);
+        raw.floats(v);
+        const float s = scale_of(max_lanes<16>(top.bits())), inverse = inverse_of(s);
         if (c < a.pitch) *reinterpret_cast<uint2 *>(a.xq + row * a.pitch + c) = uint2{codes4(v, inverse), codes4(v + 4, inverse)};
         if (lane16 == 0) a.scale[static_cast<int64_t>(b) * a.m + row] = s;
     }
@@ -115,7 +84,11 @@ __global__ __launch_bounds__(256) void tile_kernel(TileArgs a) {
     for (int r = 0; r < 8; ++r) {
         const int64_t row = row0 + part * 8 + r;
         if (row < a.rows) {
-            load8(static_cast<const T *>(a.x) + row * a.row_stride, c, a.columns, v[r]);
+            const T *from = static_cast<const T *>(a.x) + row * a.row_stride + c;
+            Raw8<T> raw;
+            if (c + 8 <= a.columns) raw.load(from);
+            else raw.load_some(from, a.columns - c);
+            raw.floats(v[r]);
         } else {
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[r][i] = 0.0f;
