@@ -420,10 +420,10 @@ hq_status hq_fp8_linear(const uint8_t *xq, const float *x_scale, const uint8_t *
                         int w_scale_turned, const void *bias, int64_t m, int n, int k, void *y, hq_dtype y_dtype,
                         void *stream);
 /*
- * The whole layer: hq_fp8_quantize_rows and hq_fp8_linear.  workspace: device memory of
- * hq_act_quant_fp8_linear_workspace(m, k) bytes, 16-byte aligned, written and read by the call.
+ * The whole layer, with the results of hq_fp8_quantize_rows and hq_fp8_linear; small ones are one launch.  workspace: device memory of
+ * hq_act_quant_fp8_linear_workspace(..) bytes, 16-byte aligned, written and read by the call; NULL where that is 0.
  */
-int64_t hq_act_quant_fp8_linear_workspace(int64_t m, int k);
+int64_t hq_act_quant_fp8_linear_workspace(hq_dtype x_dtype, int64_t m, int n, int k, hq_dtype y_dtype);
 hq_status hq_act_quant_fp8_linear(const void *x, hq_dtype x_dtype, int64_t row_stride, const uint8_t *wq,
                                   const float *w_scale, const void *bias, int64_t m, int n, int k, void *workspace,
                                   void *y, hq_dtype y_dtype, void *stream);

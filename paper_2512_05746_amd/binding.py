@@ -87,7 +87,7 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
                                     f32, vp, vp, vp]
     lib.hq_qk_norm_rope_backward.argtypes = [vp] * 4 + [i32, i64, i32, i32, i32, vp, vp, vp, i32, vp, vp, i64, i32, i32,
                                                         vp, i32, f32] + [vp] * 6
-    lib.hq_act_quant_fp8_linear_workspace.argtypes = [i64, i32]
+    lib.hq_act_quant_fp8_linear_workspace.argtypes = [i32, i64, i32, i32, i32]
     lib.hq_fp8_linear_backward_workspace.argtypes = [i64, i32, i32]
     lib.hq_qk_norm_rope_backward_workspace.argtypes = [i64, i32, i32, i32, i32]
     for name in SYMBOLS[1:]:

@@ -441,15 +441,29 @@ extern "C" hq_status hq_fp8_linear(const uint8_t *xq, const float *x_scale, cons
     return product(product_args(xq, x_scale, wq, w_scale, w_scale_turned != 0, bias, m, n, k, y), y_dtype, static_cast<hipStream_t>(stream));
 }
 
-extern "C" int64_t hq_act_quant_fp8_linear_workspace(int64_t m, int k) {
-    if (m <= 0 || k <= 0) return 0;
+namespace {
+// Whether a layer is one launch that quantises its rows as it multiplies (and with which cut), or two.
+struct LayerChoice {
+    bool one_launch;
+    hq::Fp8Cut cut;
+};
+LayerChoice choose_layer(hq_dtype x_dtype, int64_t m, int n, int k, hq_dtype y_dtype) {
+    const int64_t steps = hq::fp8_groups(k);
+    const hq::Fp8Cut fused = hq::fp8_split_cut(m, n, steps, &x_dtype, y_dtype), split = hq::fp8_split_cut(m, n, steps, nullptr, y_dtype);
+    const float rows = 2.2f + static_cast<float>(m) * k * (hq::size_of(x_dtype) + 1) / 4.5e6f;
+    return {fused.us < rows + std::min(split.us, choose_tile(m, n, steps, y_dtype).us), fused};
+}
+}  // namespace
+
+extern "C" int64_t hq_act_quant_fp8_linear_workspace(hq_dtype x_dtype, int64_t m, int n, int k, hq_dtype y_dtype) {
+    if (m <= 0 || n <= 0 || k <= 0 || choose_layer(x_dtype, m, n, k, y_dtype).one_launch) return 0;
     return up256(m * hq::fp8_pitch64(k)) + up256(4 * hq::fp8_groups(k) * m);
 }
 
 extern "C" hq_status hq_act_quant_fp8_linear(const void *x, hq_dtype x_dtype, int64_t row_stride, const uint8_t *wq, const float *w_scale,
                                              const void *bias, int64_t m, int n, int k, void *workspace, void *y, hq_dtype y_dtype,
                                              void *stream) {
-    if (!wq || !w_scale || (m > 0 && (!x || !y || !workspace))) return HQ_ERR_NULL;
+    if (!wq || !w_scale || (m > 0 && (!x || !y))) return HQ_ERR_NULL;
     if (!hq::is_float(x_dtype) || !hq::is_float(y_dtype)) return HQ_ERR_DTYPE;
     if (m < 0 || n <= 0 || k <= 0 || row_stride < 0) return HQ_ERR_SHAPE;
     const int size = hq::size_of(y_dtype);
@@ -459,14 +473,12 @@ extern "C" hq_status hq_act_quant_fp8_linear(const void *x, hq_dtype x_dtype, in
     if (!product_fits(m, n, k) || !hq::fp8_fits(m, k)) return HQ_ERR_UNSUPPORTED;
     if (m == 0) return HQ_OK;
     hipStream_t st = static_cast<hipStream_t>(stream);
+    ProductArgs p = product_args(nullptr, nullptr, wq, w_scale, false, bias, m, n, k, y);
+    const LayerChoice choice = choose_layer(x_dtype, m, n, k, y_dtype);
+    if (choice.one_launch) return hq::fp8_split(p, choice.cut, x, x_dtype, row_stride, k, y_dtype, st);
+    if (!workspace) return HQ_ERR_NULL;
     uint8_t *xq = static_cast<uint8_t *>(workspace);
     float *sx = reinterpret_cast<float *>(xq + up256(m * hq::fp8_pitch64(k)));
-    // one launch that quantises rows as it multiplies, or two
-    ProductArgs p = product_args(nullptr, nullptr, wq, w_scale, false, bias, m, n, k, y);
-    const hq::Fp8Cut fused = hq::fp8_split_cut(m, n, p.steps, &x_dtype, y_dtype), split = hq::fp8_split_cut(m, n, p.steps, nullptr, y_dtype);
-    const float rows = 2.2f + static_cast<float>(m) * k * (hq::size_of(x_dtype) + 1) / 4.5e6f;
-    if (fused.us < rows + std::min(split.us, choose_tile(m, n, p.steps, y_dtype).us))
-        return hq::fp8_split(p, fused, x, x_dtype, row_stride, k, y_dtype, st);
     if (const hq_status s = hq::fp8_rows(x, x_dtype, m, k, row_stride, xq, sx, st)) return s;
     p.x = xq, p.sx = sx;
     return product(p, y_dtype, st);

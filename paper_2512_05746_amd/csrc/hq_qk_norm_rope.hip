@@ -152,6 +152,7 @@ __global__ __launch_bounds__(256) void heads_kernel(QkArgs a) {
         const bool mine = base + slot < h.items;
         const uint32_t item = mine ? base + slot : h.items - 1;
         const uint32_t token = hq::div_magic31(item, h.heads, h.magic, h.shift), head = item - token * h.heads;
+        const Turn t = turn_of(a, token);   // (first: the tables' addresses wait for it)
         const T *x = static_cast<const T *>(h.x) + static_cast<int64_t>(token) * h.x_token + static_cast<int64_t>(head) * h.x_head;
         float u[C], v[C], gu[C], gv[C], c[C], s[C];
         load_floats<T, C>(x + at.first, u);
@@ -161,7 +162,6 @@ __global__ __launch_bounds__(256) void heads_kernel(QkArgs a) {
             load_floats<T, C>(dy + at.first, gu);
             load_floats<T, C>(dy + at.second, gv);
         }
-        const Turn t = turn_of(a, token);
         if (at.rotated) {
             load_floats<float, C>(t.cos + p, c);
             load_floats<float, C>(t.sin + p, s);
@@ -327,23 +327,43 @@ __global__ __launch_bounds__(256) void wave_kernel(QkArgs a) {
     }
 }
 
-// dw of queries (workgroups in x of the first half) and keys: the workgroups' parts, 16 threads to a channel
-__global__ __launch_bounds__(256) void weight_sums_kernel(QkArgs a) {
-    __shared__ float s[16][16];
+// dw of queries (workgroups of the first half) and keys: the workgroups' parts, of which there are up to 1024.  8 channels a workgroup, 128 threads
+// to a channel with 8 loads under way each: one round of them, where the parts come from other XCDs' caches (1024 parts of 128 channels:
+// 22 us with 16 threads and one load after the other, 13 with 32 and 4 loads).
+__global__ __launch_bounds__(1024) void weight_sums_kernel(QkArgs a) {
+    __shared__ float s[128][8];
     const uint32_t half = gridDim.x >> 1;
     const bool keys = blockIdx.x >= half;
     const Heads &h = a.part[keys];
-    const int x = threadIdx.x & 15, y = threadIdx.x >> 4, c = (blockIdx.x - (keys ? half : 0)) * 16 + x;
-    const float *sums = a.sums + (keys ? static_cast<int64_t>(a.part[0].blocks) * a.d : 0);
-    float t = 0.0f;
+    const int x = threadIdx.x & 7, y = threadIdx.x >> 3, c = (blockIdx.x - (keys ? half : 0)) * 8 + x;
+    const float *sums = a.sums + (keys ? static_cast<int64_t>(a.part[0].blocks) * a.d : 0) + c;
+    float sum = 0.0f;
     if (c < a.d)
-        for (uint32_t r = y; r < h.blocks; r += 16) t += sums[static_cast<int64_t>(r) * a.d + c];
-    s[y][x] = t;
+        for (uint32_t r = y; r < h.blocks; r += 1024) {
+            float t[8];
+#pragma unroll
+            for (uint32_t i = 0; i < 8; ++i) {
+                const uint32_t row = r + 128 * i;
+                const float v = sums[static_cast<int64_t>(row < h.blocks ? row : r) * a.d];
+                t[i] = row < h.blocks ? v : 0.0f;
+            }
+            sum += ((t[0] + t[1]) + (t[2] + t[3])) + ((t[4] + t[5]) + (t[6] + t[7]));
+        }
+    s[y][x] = sum;
+    __syncthreads();
+    if (y < 16) {
+        sum = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sum += s[y + 16 * i][x];
+    }
+    __syncthreads();
+    if (y < 16) s[y][x] = sum;
     __syncthreads();
     if (y == 0 && c < a.d && h.dw) {
+        sum = 0.0f;
 #pragma unroll
-        for (int i = 1; i < 16; ++i) t += s[i][x];
-        h.dw[c] = t;
+        for (int i = 0; i < 16; ++i) sum += s[i][x];
+        h.dw[c] = sum;
     }
 }
 
@@ -390,7 +410,7 @@ void launch(const QkArgs &a, Cut cut, hipStream_t st) {
         else if (cut.c == 4) with_c(std::integral_constant<int, 4>{});
         else wave_kernel<DT, BACK><<<blocks, 256, 0, st>>>(a);
     }
-    if (BACK) weight_sums_kernel<<<2 * ((a.d + 15) / 16), 256, 0, st>>>(a);
+    if (BACK) weight_sums_kernel<<<2 * ((a.d + 7) / 8), 1024, 0, st>>>(a);
 }
 
 template <bool BACK>

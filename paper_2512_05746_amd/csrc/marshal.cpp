@@ -661,9 +661,11 @@ PyObject *act_quant_fp8_linear(Args a) {
     const hq_dtype dt = float_type(ydt, "y_dtype");
     const void *b = Args{&bias, 1}.vec(n, ydt, "bias");
     const at::Tensor y = result(a.next(), with_last(x.t, n), ydt, x.t);
-    const at::Tensor space = empty({lib.hq_act_quant_fp8_linear_workspace(x.m, narrow(x.k))}, at::kByte, x.t);
+    at::Tensor space;
+    const int64_t bytes = lib.hq_act_quant_fp8_linear_workspace(x.type, x.m, narrow(n), narrow(x.k), dt);
+    if (bytes) space = empty({bytes}, at::kByte, x.t);
     check("hq_act_quant_fp8_linear", call(lib.hq_act_quant_fp8_linear, x.t.const_data_ptr(), x.type, x.stride, u8(wq), sw, b, x.m, narrow(n),
-                                          narrow(x.k), space.data_ptr(), y.data_ptr(), dt, stream()));
+                                          narrow(x.k), bytes ? space.data_ptr() : nullptr, y.data_ptr(), dt, stream()));
     return wrap(y);
 }
 
