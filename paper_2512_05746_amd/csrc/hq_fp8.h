@@ -27,9 +27,14 @@ inline bool fp8_fits(int64_t rows, int64_t columns) {
 hq_status fp8_rows(const void *x, hq_dtype dt, int64_t m, int k, int64_t row_stride, uint8_t *xq, float *scale, hipStream_t st);
 hq_status fp8_blocks(const void *x, hq_dtype dt, int64_t rows, int columns, int64_t row_stride, uint8_t *q, uint8_t *q_t, float *scale,
                      hipStream_t st);
-// codes along the rows and along the columns in one pass; sums (of the columns) may be null; sum_parts [rows / 128, columns]
-hq_status fp8_both(const void *x, hq_dtype dt, int64_t rows, int columns, int64_t row_stride, uint8_t *q, float *scale, uint8_t *q_t,
-                   float *scale_t, float *sum_parts, float *sums, hipStream_t st);
+// What a backward pass quantises: dy [m, n] along its rows and along its columns, x [m, k] in blocks, transposed; the sums of 128 rows of dy.
+struct Fp8Gradient {
+    uint8_t *dyq, *dyq_t, *xq_t;              // [m, pitch of n], [n, pitch of m], [k, pitch of m]
+    float *dy_scale, *dy_scale_t, *x_scale;   // [n / 128, m], [m / 128, n], [m / 128, k / 128]
+    float *sums;                              // [m / 128, n], or null
+};
+hq_status fp8_gradient(const void *dy, int64_t dy_stride, const void *x, int64_t x_stride, hq_dtype dt, int64_t m, int n, int k, const Fp8Gradient &out,
+                       hipStream_t st);
 
 // A product's arguments.
 struct Fp8Product {
@@ -50,5 +55,15 @@ struct Fp8Cut {
 // the best cut; in: the type of rows that are quantised, or null for codes
 Fp8Cut fp8_split_cut(int64_t m, int64_t n, int64_t steps, const hq_dtype *in, hq_dtype out);
 hq_status fp8_split(const Fp8Product &p, Fp8Cut cut, const void *x, hq_dtype x_dtype, int64_t row_stride, int k, hq_dtype out, hipStream_t st);
+
+// Two products in one launch, `a` with results of type out, `b` of fp32, and the sums over the rows of a matrix, both of a backward pass.
+struct Fp8Sums {
+    const float *parts;   // [rows, columns]; or null
+    int64_t rows;
+    int columns;
+    float *out;           // [columns]
+};
+Fp8Cut fp8_split_pair_cut(const Fp8Product &a, const Fp8Product &b, hq_dtype out);
+hq_status fp8_split_pair(const Fp8Product &a, const Fp8Product &b, const Fp8Sums &sums, Fp8Cut cut, hq_dtype out, hipStream_t st);
 
 }  // namespace hq

@@ -12,6 +12,7 @@
 #include <stdint.h>
 
 #include <algorithm>
+#include <cmath>
 
 #include "hq_buffer.h"
 #include "hq_common.h"
@@ -302,11 +303,10 @@ __device__ __forceinline__ Tiles tile_of(uint32_t b, Tiles count) {
 }
 
 template <int OUT, int BM, int BN, int WM, int WN, int STAGES>
-__global__ __launch_bounds__(WM *WN * 64) void product_kernel(ProductArgs a, Tiles count) {
+__device__ __forceinline__ void product_tile(const ProductArgs &a, Tiles count, uint32_t block, uint8_t *lds) {
     using P = Product<OUT, BM, BN, WM, WN, STAGES>;
-    extern __shared__ __attribute__((aligned(1024))) uint8_t lds[];
     const uint32_t lds_at = lds_address(lds);
-    const Tiles tile = tile_of(blockIdx.x, count);
+    const Tiles tile = tile_of(block, count);
     P p(a, tile.m, tile.n);
 #pragma unroll
     for (int i = 0; i < STAGES - 1; ++i) p.request(lds_at + i * P::kTile);
@@ -326,18 +326,55 @@ __global__ __launch_bounds__(WM *WN * 64) void product_kernel(ProductArgs a, Til
     p.store();
 }
 
+template <int OUT, int BM, int BN, int WM, int WN, int STAGES>
+__global__ __launch_bounds__(WM *WN * 64) void product_kernel(ProductArgs a, Tiles count) {
+    extern __shared__ __attribute__((aligned(1024))) uint8_t lds[];
+    product_tile<OUT, BM, BN, WM, WN, STAGES>(a, count, blockIdx.x, lds);
+}
+
+// Two products, `b` with fp32 results, and sums: workgroups of b first, then of a, then of the sums.
+template <int OUT, int BM, int BN, int WM, int WN, int STAGES>
+__global__ __launch_bounds__(WM *WN * 64) void product_pair_kernel(ProductArgs a, Tiles a_count, ProductArgs b, Tiles b_count, hq::Fp8Sums sums) {
+    extern __shared__ __attribute__((aligned(1024))) uint8_t lds[];
+    const uint32_t na = a_count.m * a_count.n, nb = b_count.m * b_count.n;
+    if (blockIdx.x < nb) product_tile<HQ_F32, BM, BN, WM, WN, STAGES>(b, b_count, blockIdx.x, lds);
+    else if (blockIdx.x < nb + na) product_tile<OUT, BM, BN, WM, WN, STAGES>(a, a_count, blockIdx.x - nb, lds);
+    else sum_rows(sums, blockIdx.x - nb - na, threadIdx.x, reinterpret_cast<float *>(lds));
+}
+__global__ __launch_bounds__(256) void sum_rows_kernel(hq::Fp8Sums sums) {
+    __shared__ float lds[256];
+    sum_rows(sums, blockIdx.x, threadIdx.x, lds);
+}
+
 __global__ __launch_bounds__(256) void zero_kernel(float *p, int64_t n) {
     for (int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; i < n; i += static_cast<int64_t>(gridDim.x) * 256) p[i] = 0.0f;
 }
 
+template <int BM, int BN>
+Tiles tiles_of(const ProductArgs &a) {
+    return {static_cast<uint32_t>((a.m + BM - 1) / BM), static_cast<uint32_t>((a.n + BN - 1) / BN)};
+}
+
 template <int OUT, int BM, int BN, int WM, int WN, int STAGES>
 hq_status launch_tiles(const ProductArgs &a, hipStream_t st) {
-    const Tiles count{static_cast<uint32_t>((a.m + BM - 1) / BM), static_cast<uint32_t>((a.n + BN - 1) / BN)};
+    const Tiles count = tiles_of<BM, BN>(a);
     constexpr auto kernel = product_kernel<OUT, BM, BN, WM, WN, STAGES>;
     static std::atomic<uint64_t> allowed;
     if (const hq_status s = allow_lds(reinterpret_cast<const void *>(kernel), allowed)) return s;
     const hq::LaunchCheck check;
     kernel<<<count.m * count.n, WM * WN * 64, STAGES * Product<OUT, BM, BN, WM, WN, STAGES>::kTile, st>>>(a, count);
+    return check.status();
+}
+
+template <int OUT, int BM, int BN, int WM, int WN, int STAGES>
+hq_status launch_pair(const ProductArgs &a, const ProductArgs &b, const hq::Fp8Sums &sums, hipStream_t st) {
+    const Tiles ca = tiles_of<BM, BN>(a), cb = tiles_of<BM, BN>(b);
+    constexpr auto kernel = product_pair_kernel<OUT, BM, BN, WM, WN, STAGES>;
+    static std::atomic<uint64_t> allowed;
+    if (const hq_status s = allow_lds(reinterpret_cast<const void *>(kernel), allowed)) return s;
+    constexpr int bytes = STAGES * std::max(Product<OUT, BM, BN, WM, WN, STAGES>::kTile, Product<HQ_F32, BM, BN, WM, WN, STAGES>::kTile);
+    const hq::LaunchCheck check;
+    kernel<<<ca.m * ca.n + cb.m * cb.n + sum_blocks(sums), WM * WN * 64, bytes, st>>>(a, ca, b, cb, sums);
     return check.status();
 }
 
@@ -358,12 +395,28 @@ struct TileChoice {
     Tile tile;
     float us;
 };
+// tiles a CU, in shares of a CU
+float tiles_per_cu(const TileCost &c, int64_t m, int64_t n) {
+    return static_cast<float>(((m + c.bm - 1) / c.bm) * ((n + c.bn - 1) / c.bn)) / hq::compute_units();
+}
 TileChoice choose_tile(int64_t m, int64_t n, int64_t steps, hq_dtype out) {
     TileChoice best{kTile64, 1e30f};
     for (const TileCost &c : kTiles) {
         const int o = out == HQ_F32;
-        const int64_t tiles = ((m + c.bm - 1) / c.bm) * ((n + c.bn - 1) / c.bn), cu = hq::compute_units();
-        const float us = c.begin[o] + steps * std::max(c.round[o], ((tiles + cu - 1) / cu) * c.each[o]);
+        const float us = c.begin[o] + steps * std::max(c.round[o], ceilf(tiles_per_cu(c, m, n)) * c.each[o]);
+        if (us < best.us) best = {c.tile, us};
+    }
+    return best;
+}
+TileChoice choose_pair(const ProductArgs &a, const ProductArgs &b, hq_dtype out) {
+    TileChoice best{kTile64, 1e30f};
+    for (const TileCost &c : kTiles) {
+        if (c.tile == kTile256) continue;
+        const int o = out == HQ_F32;
+        const float share = a.steps * tiles_per_cu(c, a.m, a.n) * c.each[o] + b.steps * tiles_per_cu(c, b.m, b.n) * c.each[1];
+        // (the last round is only partly filled: half of the longer tile)
+        const float longest = std::max(a.steps * c.each[o], b.steps * c.each[1]);
+        const float us = c.begin[1] + std::max(std::max(a.steps * c.round[o], b.steps * c.round[1]), share + 0.5f * longest);
         if (us < best.us) best = {c.tile, us};
     }
     return best;
@@ -380,21 +433,64 @@ hq_status launch(const ProductArgs &a, Tile tile, hipStream_t st) {
     }
 }
 
+template <int OUT>
+hq_status launch_pair(const ProductArgs &a, const ProductArgs &b, const hq::Fp8Sums &sums, Tile tile, hipStream_t st) {
+    switch (tile) {
+        case kTile128: return launch_pair<OUT, 256, 128, 4, 2, 3>(a, b, sums, st);
+        case kTile64x128: return launch_pair<OUT, 64, 128, 2, 2, 3>(a, b, sums, st);
+        default: return launch_pair<OUT, 64, 64, 2, 2, 4>(a, b, sums, st);
+    }
+}
+
 ProductArgs product_args(const uint8_t *xq, const float *x_scale, const uint8_t *wq, const float *w_scale, bool scale_turned, const void *bias,
                          int64_t m, int n, int k, void *y) {
     const int steps = static_cast<int>(hq::fp8_groups(k)), blocks = static_cast<int>(hq::fp8_groups(n));
     return {xq, wq, x_scale, w_scale, bias, y, m, n, hq::fp8_pitch(k), steps, scale_turned ? 1 : steps, scale_turned ? blocks : 1};
 }
 
+// What a product takes: a cut of K, or tiles.
+struct ProductChoice {
+    bool split;
+    hq::Fp8Cut cut;
+    TileChoice tile;
+    float us() const { return split ? cut.us : tile.us; }
+};
+ProductChoice choose(int64_t m, int64_t n, int64_t steps, hq_dtype out) {
+    const hq::Fp8Cut cut = hq::fp8_split_cut(m, n, steps, nullptr, out);
+    const TileChoice tile = choose_tile(m, n, steps, out);
+    return {cut.us < tile.us, cut, tile};
+}
+
 hq_status product(const ProductArgs &a, hq_dtype dt, hipStream_t st) {
-    const hq::Fp8Cut cut = hq::fp8_split_cut(a.m, a.n, a.steps, nullptr, dt);
-    const TileChoice tile = choose_tile(a.m, a.n, a.steps, dt);
-    if (cut.us < tile.us) return hq::fp8_split(a, cut, nullptr, dt, 0, 0, dt, st);
+    const ProductChoice c = choose(a.m, a.n, a.steps, dt);
+    if (c.split) return hq::fp8_split(a, c.cut, nullptr, dt, 0, 0, dt, st);
     switch (dt) {
-        case HQ_F16: return launch<HQ_F16>(a, tile.tile, st);
-        case HQ_BF16: return launch<HQ_BF16>(a, tile.tile, st);
-        default: return launch<HQ_F32>(a, tile.tile, st);
+        case HQ_F16: return launch<HQ_F16>(a, c.tile.tile, st);
+        case HQ_BF16: return launch<HQ_BF16>(a, c.tile.tile, st);
+        default: return launch<HQ_F32>(a, c.tile.tile, st);
     }
+}
+
+// a with results of type dt, b with fp32 ones, and sums: in one launch, or one for each
+hq_status product_pair(const ProductArgs &a, const ProductArgs &b, const hq::Fp8Sums &sums, hq_dtype dt, hipStream_t st) {
+    const hq::Fp8Cut cut = hq::fp8_split_pair_cut(a, b, dt);
+    const TileChoice tile = choose_pair(a, b, dt);
+    const float alone = choose(a.m, a.n, a.steps, dt).us() + choose(b.m, b.n, b.steps, HQ_F32).us() + (sums.parts ? 2.0f : 0.0f);
+    if (cut.us < tile.us && cut.us < alone) return hq::fp8_split_pair(a, b, sums, cut, dt, st);
+    if (tile.us < alone) {
+        switch (dt) {
+            case HQ_F16: return launch_pair<HQ_F16>(a, b, sums, tile.tile, st);
+            case HQ_BF16: return launch_pair<HQ_BF16>(a, b, sums, tile.tile, st);
+            default: return launch_pair<HQ_F32>(a, b, sums, tile.tile, st);
+        }
+    }
+    if (sums.parts) {
+        const hq::LaunchCheck check;
+        sum_rows_kernel<<<sum_blocks(sums), 256, 0, st>>>(sums);
+        if (const hq_status s = check.status()) return s;
+    }
+    if (const hq_status s = product(a, dt, st)) return s;
+    return product(b, HQ_F32, st);
 }
 
 // Rows of codes whose tiles are addressed with 31-bit offsets, and tile counts that fit a grid.
@@ -449,9 +545,9 @@ struct LayerChoice {
 };
 LayerChoice choose_layer(hq_dtype x_dtype, int64_t m, int n, int k, hq_dtype y_dtype) {
     const int64_t steps = hq::fp8_groups(k);
-    const hq::Fp8Cut fused = hq::fp8_split_cut(m, n, steps, &x_dtype, y_dtype), split = hq::fp8_split_cut(m, n, steps, nullptr, y_dtype);
-    const float rows = 2.2f + static_cast<float>(m) * k * (hq::size_of(x_dtype) + 1) / 4.5e6f;
-    return {fused.us < rows + std::min(split.us, choose_tile(m, n, steps, y_dtype).us), fused};
+    const hq::Fp8Cut fused = hq::fp8_split_cut(m, n, steps, &x_dtype, y_dtype);
+    const float rows = 2.2f + static_cast<float>(m) * k * (hq::size_of(x_dtype) + 1) / 4.5e6f;   // us of quantising them by themselves
+    return {fused.us < rows + choose(m, n, steps, y_dtype).us(), fused};
 }
 }  // namespace
 
@@ -499,7 +595,9 @@ extern "C" hq_status hq_fp8_linear_backward(const void *dy, int64_t dy_stride, c
     if (!hq::aligned_to(dy, size) || !hq::aligned_to(x, size) || !hq::aligned_to(dx, size) || !hq::aligned16(wq_t) ||
         !hq::aligned_to(w_scale, 4) || !hq::aligned16(workspace) || !hq::aligned_to(dw, 4) || !hq::aligned_to(db, 4))
         return HQ_ERR_ALIGN;
-    if (!product_fits(m, k, n) || !product_fits(n, k, m) || !hq::fp8_fits(m, n) || !hq::fp8_fits(m, k)) return HQ_ERR_UNSUPPORTED;
+    if (!product_fits(m, k, n) || !product_fits(n, k, m) || !hq::fp8_fits(m, n) || !hq::fp8_fits(m, k) ||
+        hq::fp8_groups(m) * (hq::fp8_groups(n) + hq::fp8_groups(k)) > 0x7FFFFFFF)
+        return HQ_ERR_UNSUPPORTED;
     hipStream_t st = static_cast<hipStream_t>(stream);
     if (m == 0) {
         const hq::LaunchCheck check;
@@ -510,13 +608,12 @@ extern "C" hq_status hq_fp8_linear_backward(const void *dy, int64_t dy_stride, c
     uint8_t *base = static_cast<uint8_t *>(workspace);
     const BackwardSpace at(m, n, k);
     const auto f32 = [&](int64_t offset) { return reinterpret_cast<float *>(base + offset); };
-    if (const hq_status s = hq::fp8_both(dy, dtype, m, n, dy_stride, base + at.dyq, f32(at.dy_scale), base + at.dyq_t, f32(at.dy_scale_t),
-                                         f32(at.sums), db, st))
-        return s;
-    if (const hq_status s = hq::fp8_blocks(x, dtype, m, k, x_stride, nullptr, base + at.xq_t, f32(at.x_scale), st)) return s;
+    const hq::Fp8Gradient q{base + at.dyq, base + at.dyq_t, base + at.xq_t, f32(at.dy_scale), f32(at.dy_scale_t), f32(at.x_scale),
+                            db ? f32(at.sums) : nullptr};
+    if (const hq_status s = hq::fp8_gradient(dy, dy_stride, x, x_stride, dtype, m, n, k, q, st)) return s;
     // dx [m, k] = dy [m, n] W [n, k]: the weights' codes with rows of n, their scales as those of W
-    if (const hq_status s = product(product_args(base + at.dyq, f32(at.dy_scale), wq_t, w_scale, true, nullptr, m, k, n, dx), dtype, st)) return s;
+    const ProductArgs for_x = product_args(q.dyq, q.dy_scale, wq_t, w_scale, true, nullptr, m, k, n, dx);
     // dW [n, k] = dy^T [n, m] x [m, k]
-    return product(product_args(base + at.dyq_t, f32(at.dy_scale_t), base + at.xq_t, f32(at.x_scale), true, nullptr, n, k, static_cast<int>(m), dw),
-                   HQ_F32, st);
+    const ProductArgs for_w = product_args(q.dyq_t, q.dy_scale_t, q.xq_t, q.x_scale, true, nullptr, n, k, static_cast<int>(m), dw);
+    return product_pair(for_x, for_w, {q.sums, hq::fp8_groups(m), n, db}, dtype, st);
 }

@@ -37,4 +37,20 @@ __device__ __forceinline__ Halves halves_of(const v8i &codes) {
     return h;
 }
 
+// 16 columns of sums over the rows, by 256 threads: 16 to a column, each in the order of its rows; lds: 256 floats
+__device__ __forceinline__ void sum_rows(const hq::Fp8Sums &s, uint32_t block, int tid, float *lds) {
+    const int x = tid & 15, y = tid >> 4, c = block * 16 + x;
+    float t = 0.0f;
+    if (tid < 256 && c < s.columns)
+        for (int64_t r = y; r < s.rows; r += 16) t += s.parts[r * s.columns + c];
+    if (tid < 256) lds[y * 16 + x] = t;
+    __syncthreads();
+    if (tid < 16 && c < s.columns) {
+#pragma unroll
+        for (int i = 1; i < 16; ++i) t += lds[i * 16 + x];
+        s.out[c] = t;
+    }
+}
+inline uint32_t sum_blocks(const hq::Fp8Sums &s) { return s.parts ? static_cast<uint32_t>((s.columns + 15) / 16) : 0; }
+
 }  // namespace

@@ -8,7 +8,7 @@
 // a NaN for its scale and zeros for codes: every product that uses it is NaN.
 //
 // Bound by memory: a value is read once and written as one byte, or as two bytes where codes along rows and along columns are wanted.
-// rows_kernel: 16 lanes own 128 values of a row, 8 each.  tile_kernel: a workgroup of 256 threads owns a tile of 128 x 128; a thread
+// rows_kernel: 16 lanes own 128 values of a row, 8 each.  tile: a workgroup of 256 threads owns a tile of 128 x 128; a thread
 // holds 8 rows x 8 columns in registers, so a maximum along a row is one over 16 lanes, along a column one over 16 threads at
 // the same columns (4 lanes of each wave, then LDS), and the codes of a column leave through LDS as whole pieces of 128 bytes.
 #include <hip/hip_runtime.h>
@@ -67,16 +67,23 @@ struct TileArgs {
     float *sums;            // [rows / 128, columns]: sums of a tile's columns; or null
 };
 
-// BLOCKS: one scale for the tile; otherwise codes along the rows in q and along the columns in q_t
+struct TileSpace {
+    __attribute__((aligned(16))) uint8_t turned[kGroup * kGroup];
+    uint32_t top_of[4][kGroup];
+    float sum_of[4][kGroup], inverse_t[kGroup];
+};
+
+// Tile (bx, by).  BLOCKS: one scale for the tile; otherwise codes along the rows in q and along the columns in q_t
 template <int DT, bool BLOCKS>
-__global__ __launch_bounds__(256) void tile_kernel(TileArgs a) {
+__device__ __forceinline__ void tile(const TileArgs &a, TileSpace &lds, uint32_t bx, uint32_t by) {
     using T = typename Float<DT>::type;
-    __shared__ __attribute__((aligned(16))) uint8_t turned[kGroup * kGroup];
-    __shared__ uint32_t top_of[4][kGroup];
-    __shared__ float sum_of[4][kGroup], inverse_t[kGroup];
+    auto &turned = lds.turned;
+    auto &top_of = lds.top_of;
+    auto &sum_of = lds.sum_of;
+    auto &inverse_t = lds.inverse_t;
     const int tid = threadIdx.x, lane16 = tid & 15, part = tid >> 4, wave = tid >> 6;
-    const int64_t row0 = static_cast<int64_t>(blockIdx.y) * kGroup;
-    const int column0 = blockIdx.x * kGroup, c = column0 + lane16 * 8;
+    const int64_t row0 = static_cast<int64_t>(by) * kGroup;
+    const int column0 = bx * kGroup, c = column0 + lane16 * 8;
     const int blocks_across = (a.columns + kGroup - 1) / kGroup;
 
     float v[8][8];   // [row][column]
@@ -118,7 +125,7 @@ __global__ __launch_bounds__(256) void tile_kernel(TileArgs a) {
         __syncthreads();
         s_block = scale_of(max(max(top_of[0][0], top_of[1][0]), max(top_of[2][0], top_of[3][0])));
         inverse_block = inverse_of(s_block);
-        if (tid == 0) a.scale[static_cast<int64_t>(blockIdx.y) * blocks_across + blockIdx.x] = s_block;
+        if (tid == 0) a.scale[static_cast<int64_t>(by) * blocks_across + bx] = s_block;
     } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
@@ -141,7 +148,7 @@ __global__ __launch_bounds__(256) void tile_kernel(TileArgs a) {
             const float s = scale_of(max(max(top_of[0][tid], top_of[1][tid]), max(top_of[2][tid], top_of[3][tid])));
             inverse_t[tid] = inverse_of(s);
             if (column0 + tid < a.columns) {
-                const int64_t at = static_cast<int64_t>(blockIdx.y) * a.columns + column0 + tid;
+                const int64_t at = static_cast<int64_t>(by) * a.columns + column0 + tid;
                 a.scale_t[at] = s;
                 if (a.sums) a.sums[at] = (sum_of[0][tid] + sum_of[1][tid]) + (sum_of[2][tid] + sum_of[3][tid]);
             }
@@ -161,7 +168,7 @@ __global__ __launch_bounds__(256) void tile_kernel(TileArgs a) {
                 for (int i = 0; i < 8; ++i) t = max(t, magnitude(v[r][i]));
                 const float s = scale_of(max_lanes<16>(t));
                 inverse = inverse_of(s);
-                if (lane16 == 0 && row < a.rows) a.scale[static_cast<int64_t>(blockIdx.x) * a.rows + row] = s;
+                if (lane16 == 0 && row < a.rows) a.scale[static_cast<int64_t>(bx) * a.rows + row] = s;
             }
             if (row < a.rows && c < a.pitch)
                 *reinterpret_cast<uint2 *>(a.q + row * a.pitch + c) = uint2{codes4(v[r], inverse), codes4(v[r] + 4, inverse)};
@@ -191,20 +198,19 @@ __global__ __launch_bounds__(256) void tile_kernel(TileArgs a) {
     }
 }
 
-// out[c] = sum over the rows of part [rows, columns], in the order of the rows within each of 16 threads
-__global__ __launch_bounds__(256) void sum_rows_kernel(const float *part, int64_t rows, int columns, float *out) {
-    __shared__ float s[16][16];
-    const int x = threadIdx.x & 15, y = threadIdx.x >> 4, c = blockIdx.x * 16 + x;
-    float t = 0.0f;
-    if (c < columns)
-        for (int64_t r = y; r < rows; r += 16) t += part[r * columns + c];
-    s[y][x] = t;
-    __syncthreads();
-    if (y == 0 && c < columns) {
-#pragma unroll
-        for (int i = 1; i < 16; ++i) t += s[i][x];
-        out[c] = t;
-    }
+template <int DT>
+__global__ __launch_bounds__(256) void blocks_kernel(TileArgs a) {
+    __shared__ TileSpace lds;
+    tile<DT, true>(a, lds, blockIdx.x, blockIdx.y);
+}
+
+// A gradient, both ways, and the activations, in blocks: what a backward pass quantises, in one launch.  across: tiles in a row of each;
+// the first `first` workgroups are the gradient's.
+template <int DT>
+__global__ __launch_bounds__(256) void gradient_kernel(TileArgs dy, TileArgs x, uint32_t dy_across, uint32_t x_across, uint32_t first) {
+    __shared__ TileSpace lds;
+    if (blockIdx.x < first) tile<DT, false>(dy, lds, blockIdx.x % dy_across, blockIdx.x / dy_across);
+    else tile<DT, true>(x, lds, (blockIdx.x - first) % x_across, (blockIdx.x - first) / x_across);
 }
 
 template <class F>
@@ -241,21 +247,20 @@ hq_status fp8_blocks(const void *x, hq_dtype dt, int64_t rows, int columns, int6
     const dim3 grid((columns + kGroup - 1) / kGroup, static_cast<uint32_t>((rows + kGroup - 1) / kGroup));
     return for_dtype(dt, [&](auto d) {
         const LaunchCheck check;
-        tile_kernel<decltype(d)::value, true><<<grid, 256, 0, st>>>(a);
+        blocks_kernel<decltype(d)::value><<<grid, 256, 0, st>>>(a);
         return check.status();
     });
 }
 
-hq_status fp8_both(const void *x, hq_dtype dt, int64_t rows, int columns, int64_t row_stride, uint8_t *q, float *scale, uint8_t *q_t,
-                   float *scale_t, float *sum_parts, float *sums, hipStream_t st) {
-    const TileArgs a{x,  rows,  row_stride, columns, fp8_pitch(columns), fp8_pitch64(rows), q, q_t, scale, scale_t,
-                     sums ? sum_parts : nullptr};
-    const int64_t row_tiles = (rows + kGroup - 1) / kGroup;
-    const dim3 grid((columns + kGroup - 1) / kGroup, static_cast<uint32_t>(row_tiles));
+hq_status fp8_gradient(const void *dy, int64_t dy_stride, const void *x, int64_t x_stride, hq_dtype dt, int64_t m, int n, int k, const Fp8Gradient &out,
+                       hipStream_t st) {
+    const TileArgs g{dy, m, dy_stride, n, fp8_pitch(n), fp8_pitch64(m), out.dyq, out.dyq_t, out.dy_scale, out.dy_scale_t, out.sums};
+    const TileArgs b{x, m, x_stride, k, fp8_pitch(k), fp8_pitch64(m), nullptr, out.xq_t, out.x_scale, nullptr, nullptr};
+    const int64_t down = fp8_groups(m), dy_across = fp8_groups(n), x_across = fp8_groups(k);
     return for_dtype(dt, [&](auto d) {
         const LaunchCheck check;
-        tile_kernel<decltype(d)::value, false><<<grid, 256, 0, st>>>(a);
-        if (sums) sum_rows_kernel<<<(columns + 15) / 16, 256, 0, st>>>(sum_parts, row_tiles, columns, sums);
+        gradient_kernel<decltype(d)::value><<<static_cast<uint32_t>(down * (dy_across + x_across)), 256, 0, st>>>(
+            g, b, static_cast<uint32_t>(dy_across), static_cast<uint32_t>(x_across), static_cast<uint32_t>(down * dy_across));
         return check.status();
     });
 }

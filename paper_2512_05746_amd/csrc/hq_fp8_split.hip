@@ -29,16 +29,16 @@ struct SplitArgs {
     int k;
 };
 
+// tile (bx, by) of channels and tokens; part: [NW][16 MT][16 NT + 4]
 template <int IN, int OUT, int MT, int NT>
-__global__ __launch_bounds__(NW * 64) void split_kernel(SplitArgs a) {
+__device__ __forceinline__ void split(const SplitArgs &a, uint32_t bx, uint32_t by, float *part) {
     using Out = typename Float<OUT>::type;
     constexpr bool kFp32 = OUT == HQ_F32;
     constexpr int TM = MT * 16, TN = NT * 16, PITCH = TN + 4;   // floats of a token's row in LDS
-    extern __shared__ __attribute__((aligned(16))) float part[];   // [NW][TM][PITCH]
     const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, quarter = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int64_t m0 = static_cast<int64_t>(blockIdx.y) * TM;
-    const int n0 = blockIdx.x * TN;
+    const int64_t m0 = static_cast<int64_t>(by) * TM;
+    const int n0 = bx * TN;
     const int rows_x = a.p.m - m0 < TM ? static_cast<int>(a.p.m - m0) : TM, rows_w = a.p.n - n0 < TN ? a.p.n - n0 : TN;
     const uint32_t pitch = a.p.pitch;
     const __amdgpu_buffer_rsrc_t wb = buffer_of(a.p.w + static_cast<int64_t>(n0) * pitch, static_cast<uint32_t>(rows_w) * pitch);
@@ -164,14 +164,59 @@ __global__ __launch_bounds__(NW * 64) void split_kernel(SplitArgs a) {
 }
 
 template <int IN, int OUT, int MT, int NT>
+__global__ __launch_bounds__(NW * 64) void split_kernel(SplitArgs a) {
+    extern __shared__ __attribute__((aligned(16))) float part[];
+    split<IN, OUT, MT, NT>(a, blockIdx.x, blockIdx.y, part);
+}
+
+// Two products of codes, `b` with fp32 results, and sums: workgroups of b first, then of a, then of the sums.
+template <int OUT, int MT, int NT>
+__global__ __launch_bounds__(NW * 64) void pair_kernel(SplitArgs a, SplitArgs b, hq::Fp8Sums sums, uint32_t a_across, uint32_t b_across, uint32_t a_groups,
+                                                       uint32_t b_groups) {
+    extern __shared__ __attribute__((aligned(16))) float part[];
+    if (blockIdx.x < b_groups) {
+        split<kCodes, HQ_F32, MT, NT>(b, blockIdx.x % b_across, blockIdx.x / b_across, part);
+    } else if (blockIdx.x < b_groups + a_groups) {
+        const uint32_t i = blockIdx.x - b_groups;
+        split<kCodes, OUT, MT, NT>(a, i % a_across, i / a_across, part);
+    } else {
+        sum_rows(sums, blockIdx.x - b_groups - a_groups, threadIdx.x, part);
+    }
+}
+
+constexpr int lds_bytes(int mt, int nt) { return NW * mt * 16 * (nt * 16 + 4) * 4; }
+
+template <int IN, int OUT, int MT, int NT>
 hq_status launch(const SplitArgs &a, hipStream_t st) {
     constexpr auto kernel = split_kernel<IN, OUT, MT, NT>;
     static std::atomic<uint64_t> allowed;
     if (const hq_status s = allow_lds(reinterpret_cast<const void *>(kernel), allowed)) return s;
     const dim3 grid((a.p.n + NT * 16 - 1) / (NT * 16), static_cast<uint32_t>((a.p.m + MT * 16 - 1) / (MT * 16)));
     const hq::LaunchCheck check;
-    kernel<<<grid, NW * 64, NW * MT * 16 * (NT * 16 + 4) * 4, st>>>(a);
+    kernel<<<grid, NW * 64, lds_bytes(MT, NT), st>>>(a);
     return check.status();
+}
+
+template <int OUT, int MT, int NT>
+hq_status launch_pair(const SplitArgs &a, const SplitArgs &b, const hq::Fp8Sums &sums, hipStream_t st) {
+    constexpr auto kernel = pair_kernel<OUT, MT, NT>;
+    static std::atomic<uint64_t> allowed;
+    if (const hq_status s = allow_lds(reinterpret_cast<const void *>(kernel), allowed)) return s;
+    const auto across = [](const SplitArgs &x) { return static_cast<uint32_t>((x.p.n + NT * 16 - 1) / (NT * 16)); };
+    const auto groups = [&](const SplitArgs &x) { return across(x) * static_cast<uint32_t>((x.p.m + MT * 16 - 1) / (MT * 16)); };
+    const uint32_t ga = groups(a), gb = groups(b);
+    const hq::LaunchCheck check;
+    kernel<<<ga + gb + sum_blocks(sums), NW * 64, lds_bytes(MT, NT), st>>>(a, b, sums, across(a), across(b), ga, gb);
+    return check.status();
+}
+template <int OUT>
+hq_status pair_with_cut(const SplitArgs &a, const SplitArgs &b, const hq::Fp8Sums &sums, hq::Fp8Cut cut, hipStream_t st) {
+    if (cut.mt == 2) return launch_pair<OUT, 2, 2>(a, b, sums, st);
+    switch (cut.nt) {
+        case 1: return launch_pair<OUT, 1, 1>(a, b, sums, st);
+        case 2: return launch_pair<OUT, 1, 2>(a, b, sums, st);
+        default: return launch_pair<OUT, 1, 4>(a, b, sums, st);
+    }
 }
 
 template <int IN, int OUT>
@@ -192,29 +237,56 @@ hq_status with_out(const SplitArgs &a, hq::Fp8Cut cut, hq_dtype out, hipStream_t
 
 namespace hq {
 
+namespace {
+// One round of a wave takes `round` us (latency), a workgroup's share of one step `each` us of a CU that has several; measured with 1 x 960 -> 3840,
+// 16 x 4096 -> 4096, 64 x 960 -> 3840 (rounds), 2048 x 3840 -> 960 and 960 x 4096 -> 256 (shares), us without the launch.  Activations of
+// 32 bits are twice the loads, and quantising costs each workgroup.
+struct Cost {
+    int mt, nt;
+    float round[3], each[3];   // codes; 16-bit, 32-bit activations
+
+    int64_t groups(int64_t m, int64_t n) const { return ((m + 16 * mt - 1) / (16 * mt)) * ((n + 16 * nt - 1) / (16 * nt)); }
+    float shares(int64_t m, int64_t n, int64_t steps, int kind, hq_dtype out) const {   // us, of all workgroups, of all CUs
+        return static_cast<float>(groups(m, n)) * steps * each[kind] * (out == HQ_F32 && !kind ? 1.2f : 1.0f);
+    }
+    float rounds(int64_t steps, int kind) const { return round[kind] * ((steps + NW - 1) / NW); }
+};
+constexpr Cost costs[] = {{1, 1, {1.0f, 1.5f, 2.0f}, {0.113f, 0.165f, 0.33f}},
+                          {1, 2, {1.4f, 1.6f, 2.3f}, {0.17f, 0.224f, 0.51f}},
+                          {1, 4, {2.6f, 2.6f, 3.0f}, {0.30f, 0.365f, 0.65f}},
+                          {2, 2, {1.9f, 3.0f, 3.5f}, {0.245f, 0.373f, 1.1f}}};
+constexpr float kBegin = 2.2f;
+}  // namespace
+
 Fp8Cut fp8_split_cut(int64_t m, int64_t n, int64_t steps, const hq_dtype *in, hq_dtype out) {
-    // One round of a wave takes `round` us (latency), a workgroup's share of one step `each` us of a CU that has several; measured with 1 x 960 -> 3840,
-    // 16 x 4096 -> 4096, 64 x 960 -> 3840 (rounds), 2048 x 3840 -> 960 and 960 x 4096 -> 256 (shares), us without the launch.  Activations of
-    // 32 bits are twice the loads, and quantising costs each workgroup.
-    struct Cost {
-        int mt, nt;
-        float round[3], each[3];   // codes; 16-bit, 32-bit activations
-    };
-    static constexpr Cost costs[] = {{1, 1, {1.0f, 1.5f, 2.0f}, {0.113f, 0.165f, 0.33f}},
-                                     {1, 2, {1.4f, 1.6f, 2.3f}, {0.17f, 0.224f, 0.51f}},
-                                     {1, 4, {2.6f, 2.6f, 3.0f}, {0.30f, 0.365f, 0.65f}},
-                                     {2, 2, {1.9f, 3.0f, 3.5f}, {0.245f, 0.373f, 1.1f}}};
     const int kind = !in ? 0 : *in == HQ_F32 ? 2 : 1;
-    const float slower = out == HQ_F32 && !in ? 1.2f : 1.0f;
     Fp8Cut best{0, 0, 1e30f};
     for (const Cost &c : costs) {
-        const int64_t groups = ((m + 16 * c.mt - 1) / (16 * c.mt)) * ((n + 16 * c.nt - 1) / (16 * c.nt));
         if ((m + 16 * c.mt - 1) / (16 * c.mt) > 65535) continue;   // (the grid's limit in y)
-        const float shares = std::max(1.0f, static_cast<float>(groups) / compute_units());
-        const float us = 2.2f + std::max(c.round[kind] * ((steps + NW - 1) / NW), shares * steps * c.each[kind] * slower);
+        // (fewer workgroups than CUs: each has a CU of its own)
+        const float share = std::max(c.shares(m, n, steps, kind, out) / compute_units(), c.shares(1, 1, steps, kind, out));
+        const float us = kBegin + std::max(c.rounds(steps, kind), share);
         if (us < best.us) best = {c.mt, c.nt, us};
     }
     return best;
+}
+
+Fp8Cut fp8_split_pair_cut(const Fp8Product &a, const Fp8Product &b, hq_dtype out) {
+    Fp8Cut best{0, 0, 1e30f};
+    for (const Cost &c : costs) {
+        if (c.groups(a.m, a.n) + c.groups(b.m, b.n) > 0x3FFFFFFF) continue;
+        const float share = std::max((c.shares(a.m, a.n, a.steps, 0, out) + c.shares(b.m, b.n, b.steps, 0, HQ_F32)) / compute_units(),
+                                     c.shares(1, 1, std::max(a.steps, b.steps), 0, HQ_F32));
+        const float us = kBegin + std::max(c.rounds(std::max(a.steps, b.steps), 0), share);
+        if (us < best.us) best = {c.mt, c.nt, us};
+    }
+    return best;
+}
+
+hq_status fp8_split_pair(const Fp8Product &a, const Fp8Product &b, const Fp8Sums &sums, Fp8Cut cut, hq_dtype out, hipStream_t st) {
+    const SplitArgs x{a, nullptr, 0, 0}, y{b, nullptr, 0, 0};
+    return out == HQ_F16 ? pair_with_cut<HQ_F16>(x, y, sums, cut, st) : out == HQ_BF16 ? pair_with_cut<HQ_BF16>(x, y, sums, cut, st)
+                                                                                      : pair_with_cut<HQ_F32>(x, y, sums, cut, st);
 }
 
 hq_status fp8_split(const Fp8Product &p, Fp8Cut cut, const void *x, hq_dtype x_dtype, int64_t row_stride, int k, hq_dtype out, hipStream_t st) {
