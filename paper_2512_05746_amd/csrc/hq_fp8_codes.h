@@ -46,32 +46,45 @@ template <class T> struct Raw8 {
     }
 };
 
-// The largest magnitude of values by their bits: of floats of 16 bits two at a time.
+// The largest magnitudes of values by their bits, of each of 8 columns: floats of 16 bits two at a time.
 typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
-template <class T> struct Top;
-template <> struct Top<float> {
-    uint32_t t = 0;
-    __device__ __forceinline__ void add(const Raw8<float> &r) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) t = max(t, magnitude(r.v[i]));
-    }
-    __device__ __forceinline__ uint32_t bits() const { return t; }
-};
-template <class T> struct Top16 {
-    u16x2 t = {0, 0};
+typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+template <class T> struct Tops {
+    static constexpr int kWords = 4;   // of two
+    u16x2 t[4] = {};
     __device__ __forceinline__ void add(const Raw8<T> &r) {
-        typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
         const u32x4 w = __builtin_bit_cast(u32x4, r.v) & 0x7FFF7FFFu;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) t = __builtin_elementwise_max(t, __builtin_bit_cast(u16x2, static_cast<uint32_t>(w[i])));
+        for (int i = 0; i < 4; ++i) t[i] = __builtin_elementwise_max(t[i], __builtin_bit_cast(u16x2, static_cast<uint32_t>(w[i])));
+    }
+    // with the values of the lane that `from` names
+    template <class F> __device__ __forceinline__ void join(F from) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            t[i] = __builtin_elementwise_max(t[i], __builtin_bit_cast(u16x2, from(__builtin_bit_cast(int, t[i]))));
     }
     // as the bits of a float
-    __device__ __forceinline__ uint32_t bits() const {
-        const unsigned short m = t[0] > t[1] ? t[0] : t[1];
-        return __float_as_uint(static_cast<float>(__builtin_bit_cast(T, m)));
+    __device__ __forceinline__ static uint32_t wide(unsigned short bits) { return __float_as_uint(static_cast<float>(__builtin_bit_cast(T, bits))); }
+    __device__ __forceinline__ uint32_t column(int i) const { return wide(t[i / 2][i & 1]); }
+    __device__ __forceinline__ uint32_t all() const {
+        const u16x2 m = __builtin_elementwise_max(__builtin_elementwise_max(t[0], t[1]), __builtin_elementwise_max(t[2], t[3]));
+        return wide(m[0] > m[1] ? m[0] : m[1]);
     }
 };
-template <> struct Top<_Float16> : Top16<_Float16> {};
-template <> struct Top<__bf16> : Top16<__bf16> {};
+template <> struct Tops<float> {
+    uint32_t t[8] = {};
+    __device__ __forceinline__ void add(const Raw8<float> &r) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) t[i] = max(t[i], magnitude(r.v[i]));
+    }
+    template <class F> __device__ __forceinline__ void join(F from) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) t[i] = max(t[i], static_cast<uint32_t>(from(static_cast<int>(t[i]))));
+    }
+    __device__ __forceinline__ uint32_t column(int i) const { return t[i]; }
+    __device__ __forceinline__ uint32_t all() const {
+        return max(max(max(t[0], t[1]), max(t[2], t[3])), max(max(t[4], t[5]), max(t[6], t[7])));
+    }
+};
 
 }  // namespace

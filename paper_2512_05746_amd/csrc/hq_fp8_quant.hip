@@ -44,11 +44,11 @@ __global__ __launch_bounds__(256) void rows_kernel(RowsArgs a) {
         Raw8<T> raw;
         if (c + 8 <= a.k) raw.load(x + c);
         else raw.load_some(x + c, a.k - c);
-        Top<T> top;
+        Tops<T> top;
         top.add(raw);
         float v[8];
         raw.floats(v);
-        const float s = scale_of(max_lanes<16>(top.bits())), inverse = inverse_of(s);
+        const float s = scale_of(max_lanes<16>(top.all())), inverse = inverse_of(s);
         if (c < a.pitch) *reinterpret_cast<uint2 *>(a.xq + row * a.pitch + c) = uint2{codes4(v, inverse), codes4(v + 4, inverse)};
         if (lane16 == 0) a.scale[static_cast<int64_t>(b) * a.m + row] = s;
     }
@@ -73,65 +73,69 @@ struct TileSpace {
     float sum_of[4][kGroup], inverse_t[kGroup];
 };
 
-// Tile (bx, by).  BLOCKS: one scale for the tile; otherwise codes along the rows in q and along the columns in q_t
-template <int DT, bool BLOCKS>
-__device__ __forceinline__ void tile(const TileArgs &a, TileSpace &lds, uint32_t bx, uint32_t by) {
+// the value of lane N of each row of 16 lanes
+template <int N>
+__device__ __forceinline__ float of_lane(float v) {
+    return __int_as_float(dpp<0x150 + N>(__float_as_int(v)));
+}
+
+// Tile (bx, by).  BLOCKS: one scale for the tile; otherwise codes along the rows in q and along the columns in q_t.  WHOLE: it lies inside.
+template <int DT, bool BLOCKS, bool WHOLE>
+__device__ __forceinline__ void tile_body(const TileArgs &a, TileSpace &lds, uint32_t bx, uint32_t by) {
     using T = typename Float<DT>::type;
-    auto &turned = lds.turned;
-    auto &top_of = lds.top_of;
-    auto &sum_of = lds.sum_of;
-    auto &inverse_t = lds.inverse_t;
     const int tid = threadIdx.x, lane16 = tid & 15, part = tid >> 4, wave = tid >> 6;
-    const int64_t row0 = static_cast<int64_t>(by) * kGroup;
+    const int64_t row0 = static_cast<int64_t>(by) * kGroup, my_row = row0 + part * 8;
     const int column0 = bx * kGroup, c = column0 + lane16 * 8;
     const int blocks_across = (a.columns + kGroup - 1) / kGroup;
 
-    float v[8][8];   // [row][column]
+    Raw8<T> raw[8];   // of 8 rows
+    Tops<T> tops;     // of the columns
+    {
+        const T *from = static_cast<const T *>(a.x) + my_row * a.row_stride + c;
 #pragma unroll
-    for (int r = 0; r < 8; ++r) {
-        const int64_t row = row0 + part * 8 + r;
-        if (row < a.rows) {
-            const T *from = static_cast<const T *>(a.x) + row * a.row_stride + c;
-            Raw8<T> raw;
-            if (c + 8 <= a.columns) raw.load(from);
-            else raw.load_some(from, a.columns - c);
-            raw.floats(v[r]);
-        } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[r][i] = 0.0f;
+        for (int r = 0; r < 8; ++r, from += a.row_stride) {
+            if (WHOLE || (my_row + r < a.rows && c + 8 <= a.columns)) raw[r].load(from);
+            else if (my_row + r < a.rows && c < a.columns) raw[r].load_some(from, a.columns - c);
+            else raw[r].zero();
         }
     }
-
-    // maxima and sums of the columns, over the threads that share them
-    uint32_t top[8];
-    float sum[8];
+    float inverse[8];   // of the rows
+    if constexpr (BLOCKS) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        top[i] = 0;
-        sum[i] = 0.0f;
+        for (int r = 0; r < 8; ++r) tops.add(raw[r]);
+        const uint32_t t = max_lanes<64>(tops.all());
+        if ((tid & 63) == 0) lds.top_of[wave][0] = t;
+        __syncthreads();
+        const float s = scale_of(max(max(lds.top_of[0][0], lds.top_of[1][0]), max(lds.top_of[2][0], lds.top_of[3][0])));
+        const float inv = inverse_of(s);
+#pragma unroll
+        for (int r = 0; r < 8; ++r) inverse[r] = inv;
+        if (tid == 0) a.scale[static_cast<int64_t>(by) * blocks_across + bx] = s;
+    } else {
+        // Rows: lane r of 16 gets the maximum of row r, takes its scale, and hands the inverse to the others.
+        uint32_t mine = 0;
 #pragma unroll
         for (int r = 0; r < 8; ++r) {
-            top[i] = max(top[i], magnitude(v[r][i]));
-            sum[i] += v[r][i];
+            Tops<T> row;
+            row.add(raw[r]);
+            const uint32_t t = max_lanes<16>(row.all());
+            mine = lane16 == r ? t : mine;
+            tops.add(raw[r]);
         }
-    }
-    float s_block = 1.0f, inverse_block = 1.0f;
-    if constexpr (BLOCKS) {
-        uint32_t t = 0;
+        const float s_row = scale_of(mine), inv = inverse_of(s_row);
+        inverse[0] = of_lane<0>(inv), inverse[1] = of_lane<1>(inv), inverse[2] = of_lane<2>(inv), inverse[3] = of_lane<3>(inv);
+        inverse[4] = of_lane<4>(inv), inverse[5] = of_lane<5>(inv), inverse[6] = of_lane<6>(inv), inverse[7] = of_lane<7>(inv);
+        if (lane16 < 8 && (WHOLE || my_row + lane16 < a.rows)) a.scale[static_cast<int64_t>(bx) * a.rows + my_row + lane16] = s_row;
+        // columns: over the 4 lanes of a wave that share them, then over the waves
+        tops.join([](int v) { return __shfl_xor(v, 16); });
+        tops.join([](int v) { return __shfl_xor(v, 32); });
+        float sum[8];
+        if (a.sums) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) t = max(t, top[i]);
-        t = max_lanes<64>(t);
-        if ((tid & 63) == 0) top_of[wave][0] = t;
-        __syncthreads();
-        s_block = scale_of(max(max(top_of[0][0], top_of[1][0]), max(top_of[2][0], top_of[3][0])));
-        inverse_block = inverse_of(s_block);
-        if (tid == 0) a.scale[static_cast<int64_t>(by) * blocks_across + bx] = s_block;
-    } else {
+            for (int i = 0; i < 8; ++i) {
+                sum[i] = 0.0f;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            top[i] = max(top[i], static_cast<uint32_t>(__shfl_xor(static_cast<int>(top[i]), 16)));
-            top[i] = max(top[i], static_cast<uint32_t>(__shfl_xor(static_cast<int>(top[i]), 32)));
-            if (a.sums) {
+                for (int r = 0; r < 8; ++r) sum[i] += static_cast<float>(raw[r].v[i]);
                 sum[i] += __shfl_xor(sum[i], 16);
                 sum[i] += __shfl_xor(sum[i], 32);
             }
@@ -139,18 +143,18 @@ __device__ __forceinline__ void tile(const TileArgs &a, TileSpace &lds, uint32_t
         if ((tid & 63) < 16) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                top_of[wave][lane16 * 8 + i] = top[i];
-                sum_of[wave][lane16 * 8 + i] = sum[i];
+                lds.top_of[wave][lane16 * 8 + i] = tops.column(i);
+                if (a.sums) lds.sum_of[wave][lane16 * 8 + i] = sum[i];
             }
         }
         __syncthreads();
         if (tid < kGroup) {
-            const float s = scale_of(max(max(top_of[0][tid], top_of[1][tid]), max(top_of[2][tid], top_of[3][tid])));
-            inverse_t[tid] = inverse_of(s);
-            if (column0 + tid < a.columns) {
+            const float s = scale_of(max(max(lds.top_of[0][tid], lds.top_of[1][tid]), max(lds.top_of[2][tid], lds.top_of[3][tid])));
+            lds.inverse_t[tid] = inverse_of(s);
+            if (WHOLE || column0 + tid < a.columns) {
                 const int64_t at = static_cast<int64_t>(by) * a.columns + column0 + tid;
                 a.scale_t[at] = s;
-                if (a.sums) a.sums[at] = (sum_of[0][tid] + sum_of[1][tid]) + (sum_of[2][tid] + sum_of[3][tid]);
+                if (a.sums) a.sums[at] = (lds.sum_of[0][tid] + lds.sum_of[1][tid]) + (lds.sum_of[2][tid] + lds.sum_of[3][tid]);
             }
         }
         __syncthreads();
@@ -158,20 +162,13 @@ __device__ __forceinline__ void tile(const TileArgs &a, TileSpace &lds, uint32_t
 
     // codes along the rows
     if (a.q) {
+        uint8_t *to = a.q + my_row * a.pitch + c;
 #pragma unroll
-        for (int r = 0; r < 8; ++r) {
-            const int64_t row = row0 + part * 8 + r;
-            float inverse = inverse_block;
-            if constexpr (!BLOCKS) {
-                uint32_t t = 0;
-#pragma unroll
-                for (int i = 0; i < 8; ++i) t = max(t, magnitude(v[r][i]));
-                const float s = scale_of(max_lanes<16>(t));
-                inverse = inverse_of(s);
-                if (lane16 == 0 && row < a.rows) a.scale[static_cast<int64_t>(bx) * a.rows + row] = s;
-            }
-            if (row < a.rows && c < a.pitch)
-                *reinterpret_cast<uint2 *>(a.q + row * a.pitch + c) = uint2{codes4(v[r], inverse), codes4(v[r] + 4, inverse)};
+        for (int r = 0; r < 8; ++r, to += a.pitch) {
+            float v[8];
+            raw[r].floats(v);
+            if (WHOLE || (my_row + r < a.rows && c < a.pitch))
+                *reinterpret_cast<uint2 *>(to) = uint2{codes4(v, inverse[r]), codes4(v + 4, inverse[r])};
         }
     }
     if (!a.q_t) return;
@@ -181,21 +178,27 @@ __device__ __forceinline__ void tile(const TileArgs &a, TileSpace &lds, uint32_t
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         const int column = lane16 * 8 + i;
-        const float inverse = BLOCKS ? inverse_block : inverse_t[column];
+        const float inv = BLOCKS ? inverse[0] : lds.inverse_t[column];
         float t[8];
 #pragma unroll
-        for (int r = 0; r < 8; ++r) t[r] = v[r][i];
-        *reinterpret_cast<uint2 *>(turned + column * kGroup + ((part ^ lane16) * 8)) = uint2{codes4(t, inverse), codes4(t + 4, inverse)};
+        for (int r = 0; r < 8; ++r) t[r] = static_cast<float>(raw[r].v[i]);
+        *reinterpret_cast<uint2 *>(lds.turned + column * kGroup + ((part ^ lane16) * 8)) = uint2{codes4(t, inv), codes4(t + 4, inv)};
     }
     __syncthreads();
+    uint8_t *to = a.q_t + static_cast<int64_t>(column0 + part) * a.pitch_t + row0 + lane16 * 8;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
+    for (int i = 0; i < 8; ++i, to += 16 * a.pitch_t) {
         const int column = i * 16 + part;
-        const int64_t at = row0 + lane16 * 8;
-        if (column0 + column < a.columns && at < a.pitch_t)
-            *reinterpret_cast<uint2 *>(a.q_t + static_cast<int64_t>(column0 + column) * a.pitch_t + at) =
-                *reinterpret_cast<const uint2 *>(turned + column * kGroup + ((lane16 ^ (column >> 3)) * 8));
+        if (WHOLE || (column0 + column < a.columns && row0 + lane16 * 8 < a.pitch_t))
+            *reinterpret_cast<uint2 *>(to) = *reinterpret_cast<const uint2 *>(lds.turned + column * kGroup + ((lane16 ^ (column >> 3)) * 8));
     }
+}
+template <int DT, bool BLOCKS>
+__device__ __forceinline__ void tile(const TileArgs &a, TileSpace &lds, uint32_t bx, uint32_t by) {
+    if ((by + 1) * static_cast<int64_t>(kGroup) <= a.rows && static_cast<int64_t>(bx + 1) * kGroup <= a.columns)
+        tile_body<DT, BLOCKS, true>(a, lds, bx, by);
+    else
+        tile_body<DT, BLOCKS, false>(a, lds, bx, by);
 }
 
 template <int DT>

@@ -91,10 +91,10 @@ __device__ __forceinline__ void split(const SplitArgs &a, uint32_t bx, uint32_t 
             }
 #pragma unroll
             for (int j = 0; j < MT; ++j) {
-                Top<T> tops;
+                Tops<T> tops;
 #pragma unroll
                 for (int q = 0; q < 4; ++q) tops.add(raw[j][q]);
-                uint32_t top = tops.bits();
+                uint32_t top = tops.all();
                 top = max(top, static_cast<uint32_t>(__shfl_xor(static_cast<int>(top), 16)));
                 top = max(top, static_cast<uint32_t>(__shfl_xor(static_cast<int>(top), 32)));
                 s[j] = scale_of(top);
