@@ -444,6 +444,13 @@ hq_status hq_fp8_linear_backward(const void *dy, int64_t dy_stride, const void *
                                  void *dx, float *dw, float *db, void *stream);
 
 /*
+ * Diagnostics, host logic only: the kernel a layer takes (x_dtype HQ_I32: hq_fp8_linear, on codes), and the one that multiplies for both gradients
+ * ("two launches": one each).  "split" and "one launch": the waves of a workgroup split k.
+ */
+const char *hq_fp8_linear_kernel_name(hq_dtype x_dtype, int64_t m, int n, int k, hq_dtype y_dtype);
+const char *hq_fp8_linear_backward_kernel_name(hq_dtype dtype, int64_t m, int n, int k, int bias_grad);
+
+/*
  * ---- query and key heads: norm and rotation ------------------------------------------
  *
  * What follows the query/key/value projection of an attention block, in one pass over q [t, heads, d] and k [t, kv_heads, d]:

@@ -27,7 +27,7 @@ SYMBOLS = ("hq_status_string", "hq_quantize_weights", "hq_act_hadamard_quant",
 WORKSPACE_SYMBOLS = ("hq_act_quant_fp8_linear_workspace", "hq_fp8_linear_backward_workspace",
                      "hq_qk_norm_rope_backward_workspace")
 # entry points that do not return a status
-INFO_SYMBOLS = ("hq_int_conv2d_kernel_name",) + WORKSPACE_SYMBOLS
+INFO_SYMBOLS = ("hq_int_conv2d_kernel_name", "hq_fp8_linear_kernel_name", "hq_fp8_linear_backward_kernel_name") + WORKSPACE_SYMBOLS
 
 
 class HqError(RuntimeError):
@@ -94,6 +94,9 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
         getattr(lib, name).restype = i32
     for name in WORKSPACE_SYMBOLS:
         getattr(lib, name).restype = i64
+    lib.hq_fp8_linear_kernel_name.argtypes = [i32, i64, i32, i32, i32]
+    lib.hq_fp8_linear_backward_kernel_name.argtypes = [i32, i64, i32, i32, i32]
+    lib.hq_fp8_linear_kernel_name.restype = lib.hq_fp8_linear_backward_kernel_name.restype = ctypes.c_char_p
     lib.hq_int_conv2d_kernel_name.argtypes = [i32] * 11
     lib.hq_int_conv2d_kernel_name.restype = ctypes.c_char_p
     from . import _marshal as marshal
@@ -280,6 +283,20 @@ def hq_act_quant_fp8_linear(x: torch.Tensor, wq: torch.Tensor, w_scale: torch.Te
                             y_dtype: torch.dtype = torch.float16, out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """The whole layer: x [..., k] fp16/bf16/fp32 -> y [..., n], as hq_fp8_quantize_rows and hq_fp8_linear give it."""
     return _native().act_quant_fp8_linear(x, wq, w_scale, bias, y_dtype, out)
+
+
+_FLOATS = {torch.float16: 0, torch.float32: 1, torch.bfloat16: 3}
+
+
+def hq_fp8_linear_kernel_name(m: int, n: int, k: int, y_dtype: torch.dtype = torch.float16,
+                              x_dtype: Optional[torch.dtype] = None) -> str:
+    """Name of the kernel that hq_fp8_linear takes for these sizes, or hq_act_quant_fp8_linear for x_dtype (host logic only)."""
+    return load_library().hq_fp8_linear_kernel_name(2 if x_dtype is None else _FLOATS[x_dtype], m, n, k, _FLOATS[y_dtype]).decode()
+
+
+def hq_fp8_linear_backward_kernel_name(m: int, n: int, k: int, dtype: torch.dtype = torch.float16, bias_grad: bool = False) -> str:
+    """Name of the kernel that multiplies in hq_fp8_linear_backward (host logic only)."""
+    return load_library().hq_fp8_linear_backward_kernel_name(_FLOATS[dtype], m, n, k, 1 if bias_grad else 0).decode()
 
 
 def hq_fp8_linear_backward(dy: torch.Tensor, x: torch.Tensor, wq_t: torch.Tensor, w_scale: torch.Tensor,

@@ -380,17 +380,18 @@ hq_status launch_pair(const ProductArgs &a, const ProductArgs &b, const hq::Fp8S
 
 // The tiles of the product, 16-bit results first, then 32-bit ones.  A step of a lone workgroup takes `round` us, a CU's share of a
 // step `each` us a tile when it has several; measured with 8192 x 4096 -> 8192 and 4096 x 8192 -> 4096 (shares), 2048 x 3840 -> 960 and 1024 x 1024 -> 1024
-// (rounds).  128 x 128 tiles were never the fastest.
+// (rounds); begin: launch, first
+// loads and results.  128 x 128 tiles were never the fastest.
 enum Tile { kTile256, kTile128, kTile64x128, kTile64 };
 struct TileCost {
     Tile tile;
     int bm, bn;
     float begin[2], round[2], each[2];
 };
-constexpr TileCost kTiles[] = {{kTile256, 256, 256, {3.5f, 1e30f}, {1.4f, 1e30f}, {1.6f, 1e30f}},
-                               {kTile128, 256, 128, {3.0f, 3.0f}, {0.9f, 1.6f}, {1.18f, 1.95f}},
-                               {kTile64x128, 64, 128, {2.5f, 2.5f}, {0.44f, 0.8f}, {0.38f, 0.6f}},
-                               {kTile64, 64, 64, {2.3f, 2.3f}, {0.37f, 0.62f}, {0.24f, 0.38f}}};
+constexpr TileCost kTiles[] = {{kTile256, 256, 256, {4.3f, 1e30f}, {1.4f, 1e30f}, {1.6f, 1e30f}},
+                               {kTile128, 256, 128, {4.0f, 4.0f}, {0.9f, 1.6f}, {1.18f, 1.95f}},
+                               {kTile64x128, 64, 128, {3.3f, 3.3f}, {0.44f, 0.8f}, {0.38f, 0.6f}},
+                               {kTile64, 64, 64, {3.2f, 3.2f}, {0.37f, 0.62f}, {0.24f, 0.38f}}};
 struct TileChoice {
     Tile tile;
     float us;
@@ -471,17 +472,28 @@ hq_status product(const ProductArgs &a, hq_dtype dt, hipStream_t st) {
     }
 }
 
-// a with results of type dt, b with fp32 ones, and sums: in one launch, or one for each
-hq_status product_pair(const ProductArgs &a, const ProductArgs &b, const hq::Fp8Sums &sums, hq_dtype dt, hipStream_t st) {
+// What two products take: one launch, with a cut of K or with tiles, or one launch each.
+struct PairChoice {
+    enum { kSplit, kTiles, kAlone } how;
+    hq::Fp8Cut cut;
+    Tile tile;
+};
+PairChoice choose_pair_launch(const ProductArgs &a, const ProductArgs &b, bool sums, hq_dtype dt) {
     const hq::Fp8Cut cut = hq::fp8_split_pair_cut(a, b, dt);
     const TileChoice tile = choose_pair(a, b, dt);
-    const float alone = choose(a.m, a.n, a.steps, dt).us() + choose(b.m, b.n, b.steps, HQ_F32).us() + (sums.parts ? 2.0f : 0.0f);
-    if (cut.us < tile.us && cut.us < alone) return hq::fp8_split_pair(a, b, sums, cut, dt, st);
-    if (tile.us < alone) {
+    const float alone = choose(a.m, a.n, a.steps, dt).us() + choose(b.m, b.n, b.steps, HQ_F32).us() + (sums ? 2.0f : 0.0f);
+    return {cut.us < tile.us && cut.us < alone ? PairChoice::kSplit : tile.us < alone ? PairChoice::kTiles : PairChoice::kAlone, cut, tile.tile};
+}
+
+// a with results of type dt, b with fp32 ones, and sums
+hq_status product_pair(const ProductArgs &a, const ProductArgs &b, const hq::Fp8Sums &sums, hq_dtype dt, hipStream_t st) {
+    const PairChoice c = choose_pair_launch(a, b, sums.parts != nullptr, dt);
+    if (c.how == PairChoice::kSplit) return hq::fp8_split_pair(a, b, sums, c.cut, dt, st);
+    if (c.how == PairChoice::kTiles) {
         switch (dt) {
-            case HQ_F16: return launch_pair<HQ_F16>(a, b, sums, tile.tile, st);
-            case HQ_BF16: return launch_pair<HQ_BF16>(a, b, sums, tile.tile, st);
-            default: return launch_pair<HQ_F32>(a, b, sums, tile.tile, st);
+            case HQ_F16: return launch_pair<HQ_F16>(a, b, sums, c.tile, st);
+            case HQ_BF16: return launch_pair<HQ_BF16>(a, b, sums, c.tile, st);
+            default: return launch_pair<HQ_F32>(a, b, sums, c.tile, st);
         }
     }
     if (sums.parts) {
@@ -546,7 +558,9 @@ struct LayerChoice {
 LayerChoice choose_layer(hq_dtype x_dtype, int64_t m, int n, int k, hq_dtype y_dtype) {
     const int64_t steps = hq::fp8_groups(k);
     const hq::Fp8Cut fused = hq::fp8_split_cut(m, n, steps, &x_dtype, y_dtype);
-    const float rows = 2.2f + static_cast<float>(m) * k * (hq::size_of(x_dtype) + 1) / 4.5e6f;   // us of quantising them by themselves
+    // us of quantising them by themselves: 2.2 on the card, and a launch more on the host (333 x 1001 -> 777 7.2 against 8.4 us of one launch in a graph,
+    // called one by one 11.3 against 8.1)
+    const float rows = 4.0f + static_cast<float>(m) * k * (hq::size_of(x_dtype) + 1) / 4.5e6f;
     return {fused.us < rows + choose(m, n, steps, y_dtype).us(), fused};
 }
 }  // namespace
@@ -580,6 +594,32 @@ extern "C" hq_status hq_act_quant_fp8_linear(const void *x, hq_dtype x_dtype, in
     return product(p, y_dtype, st);
 }
 
+namespace {
+const char *name_of(const hq::Fp8Cut &c, bool one_launch) {
+    static const char *const names[2][3] = {{"split (16 x 16)", "split (16 x 32)", "split (32 x 32)"},
+                                            {"one launch (16 x 16)", "one launch (16 x 32)", "one launch (16 x 64)"}};
+    return names[one_launch][c.mt == 2 || c.nt == 4 ? 2 : c.nt - 1];
+}
+const char *name_of(Tile t) {
+    switch (t) {
+        case kTile256: return "tile (256 x 256)";
+        case kTile128: return "tile (256 x 128)";
+        case kTile64x128: return "tile (64 x 128)";
+        default: return "tile (64 x 64)";
+    }
+}
+}  // namespace
+
+extern "C" const char *hq_fp8_linear_kernel_name(hq_dtype x_dtype, int64_t m, int n, int k, hq_dtype y_dtype) {
+    if (m <= 0 || n <= 0 || k <= 0 || !hq::is_float(y_dtype) || !product_fits(m, n, k)) return "none";
+    if (hq::is_float(x_dtype)) {
+        const LayerChoice l = choose_layer(x_dtype, m, n, k, y_dtype);
+        if (l.one_launch) return name_of(l.cut, true);
+    }
+    const ProductChoice c = choose(m, n, hq::fp8_groups(k), y_dtype);
+    return c.split ? name_of(c.cut, false) : name_of(c.tile.tile);
+}
+
 extern "C" int64_t hq_fp8_linear_backward_workspace(int64_t m, int n, int k) {
     if (m <= 0 || n <= 0 || k <= 0) return 0;
     return BackwardSpace(m, n, k).total;
@@ -601,7 +641,7 @@ extern "C" hq_status hq_fp8_linear_backward(const void *dy, int64_t dy_stride, c
     hipStream_t st = static_cast<hipStream_t>(stream);
     if (m == 0) {
         const hq::LaunchCheck check;
-        zero_kernel<<<std::min<uint32_t>(1024, (static_cast<int64_t>(n) * k + 255) / 256), 256, 0, st>>>(dw, static_cast<int64_t>(n) * k);
+        zero_kernel<<<static_cast<uint32_t>(std::min<int64_t>(1024, (static_cast<int64_t>(n) * k + 255) / 256)), 256, 0, st>>>(dw, static_cast<int64_t>(n) * k);
         if (db) zero_kernel<<<std::min<uint32_t>(1024, (n + 255) / 256), 256, 0, st>>>(db, n);
         return check.status();
     }
@@ -616,4 +656,12 @@ extern "C" hq_status hq_fp8_linear_backward(const void *dy, int64_t dy_stride, c
     // dW [n, k] = dy^T [n, m] x [m, k]
     const ProductArgs for_w = product_args(q.dyq_t, q.dy_scale_t, q.xq_t, q.x_scale, true, nullptr, n, k, static_cast<int>(m), dw);
     return product_pair(for_x, for_w, {q.sums, hq::fp8_groups(m), n, db}, dtype, st);
+}
+
+extern "C" const char *hq_fp8_linear_backward_kernel_name(hq_dtype dtype, int64_t m, int n, int k, int bias_grad) {
+    if (m <= 0 || n <= 0 || k <= 0 || !hq::is_float(dtype) || !product_fits(m, k, n) || !product_fits(n, k, m)) return "none";
+    const ProductArgs x = product_args(nullptr, nullptr, nullptr, nullptr, true, nullptr, m, k, n, nullptr);
+    const ProductArgs w = product_args(nullptr, nullptr, nullptr, nullptr, true, nullptr, n, k, static_cast<int>(m), nullptr);
+    const PairChoice c = choose_pair_launch(x, w, bias_grad != 0, dtype);
+    return c.how == PairChoice::kSplit ? name_of(c.cut, false) : c.how == PairChoice::kTiles ? name_of(c.tile) : "two launches";
 }

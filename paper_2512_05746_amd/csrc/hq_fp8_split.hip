@@ -11,6 +11,7 @@
 #include <stdint.h>
 
 #include <algorithm>
+#include <cmath>
 
 #include "hq_common.h"
 #include "hq_fp8.h"
@@ -211,22 +212,17 @@ hq_status launch_pair(const SplitArgs &a, const SplitArgs &b, const hq::Fp8Sums 
 }
 template <int OUT>
 hq_status pair_with_cut(const SplitArgs &a, const SplitArgs &b, const hq::Fp8Sums &sums, hq::Fp8Cut cut, hipStream_t st) {
-    if (cut.mt == 2) return launch_pair<OUT, 2, 2>(a, b, sums, st);
-    switch (cut.nt) {
-        case 1: return launch_pair<OUT, 1, 1>(a, b, sums, st);
-        case 2: return launch_pair<OUT, 1, 2>(a, b, sums, st);
-        default: return launch_pair<OUT, 1, 4>(a, b, sums, st);
-    }
+    if (cut.mt == 1 && cut.nt == 1) return launch_pair<OUT, 1, 1>(a, b, sums, st);
+    if (cut.mt == 1 && cut.nt == 2) return launch_pair<OUT, 1, 2>(a, b, sums, st);
+    return launch_pair<OUT, 2, 2>(a, b, sums, st);
 }
 
 template <int IN, int OUT>
 hq_status with_cut(const SplitArgs &a, hq::Fp8Cut cut, hipStream_t st) {
-    if (cut.mt == 2) return launch<IN, OUT, 2, 2>(a, st);
-    switch (cut.nt) {
-        case 1: return launch<IN, OUT, 1, 1>(a, st);
-        case 2: return launch<IN, OUT, 1, 2>(a, st);
-        default: return launch<IN, OUT, 1, 4>(a, st);
-    }
+    if (cut.mt == 1 && cut.nt == 1) return launch<IN, OUT, 1, 1>(a, st);
+    if (cut.mt == 1 && cut.nt == 2) return launch<IN, OUT, 1, 2>(a, st);
+    if constexpr (IN == kCodes) return launch<IN, OUT, 2, 2>(a, st);
+    else return launch<IN, OUT, 1, 4>(a, st);
 }
 template <int IN>
 hq_status with_out(const SplitArgs &a, hq::Fp8Cut cut, hq_dtype out, hipStream_t st) {
@@ -240,7 +236,8 @@ namespace hq {
 namespace {
 // One round of a wave takes `round` us (latency), a workgroup's share of one step `each` us of a CU that has several; measured with 1 x 960 -> 3840,
 // 16 x 4096 -> 4096, 64 x 960 -> 3840 (rounds), 2048 x 3840 -> 960 and 960 x 4096 -> 256 (shares), us without the launch.  Activations of
-// 32 bits are twice the loads, and quantising costs each workgroup.
+// 32 bits are twice the loads, and quantising costs each workgroup: there a workgroup takes more channels (16 x 64) where on codes it takes more of
+// both (32 x 32; 16 x 64 is slower by 0 .. 20 % there, 32 x 32 by 10 .. 20 % here).
 struct Cost {
     int mt, nt;
     float round[3], each[3];   // codes; 16-bit, 32-bit activations
@@ -251,20 +248,23 @@ struct Cost {
     }
     float rounds(int64_t steps, int kind) const { return round[kind] * ((steps + NW - 1) / NW); }
 };
+constexpr float kNot = 1e30f;
 constexpr Cost costs[] = {{1, 1, {1.0f, 1.5f, 2.0f}, {0.113f, 0.165f, 0.33f}},
                           {1, 2, {1.4f, 1.6f, 2.3f}, {0.17f, 0.224f, 0.51f}},
-                          {1, 4, {2.6f, 2.6f, 3.0f}, {0.30f, 0.365f, 0.65f}},
-                          {2, 2, {1.9f, 3.0f, 3.5f}, {0.245f, 0.373f, 1.1f}}};
+                          {1, 4, {kNot, 2.6f, 3.0f}, {0.30f, 0.365f, 0.65f}},
+                          {2, 2, {1.9f, kNot, kNot}, {0.245f, 0.373f, 1.1f}}};
 constexpr float kBegin = 2.2f;
 }  // namespace
 
 Fp8Cut fp8_split_cut(int64_t m, int64_t n, int64_t steps, const hq_dtype *in, hq_dtype out) {
     const int kind = !in ? 0 : *in == HQ_F32 ? 2 : 1;
-    Fp8Cut best{0, 0, 1e30f};
+    Fp8Cut best{1, 1, 1e30f};
     for (const Cost &c : costs) {
         if ((m + 16 * c.mt - 1) / (16 * c.mt) > 65535) continue;   // (the grid's limit in y)
-        // (fewer workgroups than CUs: each has a CU of its own)
-        const float share = std::max(c.shares(m, n, steps, kind, out) / compute_units(), c.shares(1, 1, steps, kind, out));
+        // Fewer workgroups than CUs: each has a CU of its own.  Those that quantise keep a CU's vector units busy, so that a second one on it waits (333 x
+        // 1024 -> 768 5.7 us, -> 777 8.6); those on codes wait for loads.
+        float share = std::max(c.shares(m, n, steps, kind, out) / compute_units(), c.shares(1, 1, steps, kind, out));
+        if (in) share = ceilf(static_cast<float>(c.groups(m, n)) / compute_units()) * c.shares(1, 1, steps, kind, out);
         const float us = kBegin + std::max(c.rounds(steps, kind), share);
         if (us < best.us) best = {c.mt, c.nt, us};
     }
@@ -272,7 +272,7 @@ Fp8Cut fp8_split_cut(int64_t m, int64_t n, int64_t steps, const hq_dtype *in, hq
 }
 
 Fp8Cut fp8_split_pair_cut(const Fp8Product &a, const Fp8Product &b, hq_dtype out) {
-    Fp8Cut best{0, 0, 1e30f};
+    Fp8Cut best{1, 1, 1e30f};
     for (const Cost &c : costs) {
         if (c.groups(a.m, a.n) + c.groups(b.m, b.n) > 0x3FFFFFFF) continue;
         const float share = std::max((c.shares(a.m, a.n, a.steps, 0, out) + c.shares(b.m, b.n, b.steps, 0, HQ_F32)) / compute_units(),

@@ -204,6 +204,60 @@ def test_layer(m, k, n, dtype):
     close(y, xd @ wd.T, product_bound(xd, wd, up(k, 128), "f32"), "f32")
 
 
+KERNELS = [   # m, k, n, type, kernel on codes
+    (1, 500, 40, "f16", "split (16 x 16)"), (300, 500, 700, "bf16", "split (16 x 32)"), (33, 1000, 4100, "f16", "split (32 x 32)"),
+    (300, 100, 4100, "bf16", "tile (64 x 64)"), (1025, 500, 1030, "f16", "tile (64 x 128)"), (4096, 576, 1728, "f16", "tile (256 x 128)"),
+    (2049, 500, 4100, "bf16", "tile (256 x 256)"), (1, 500, 40, "f32", "split (16 x 16)"), (33, 500, 4100, "f32", "split (16 x 32)"),
+    (2049, 500, 130, "f32", "split (32 x 32)"), (300, 100, 4100, "f32", "tile (64 x 64)"), (1025, 100, 4100, "f32", "tile (64 x 128)"),
+    (4096, 576, 1728, "f32", "tile (256 x 128)")]
+
+
+@pytest.mark.parametrize("m,k,n,dtype,kernel", KERNELS)
+def test_every_kernel_of_the_product(m, k, n, dtype, kernel):
+    assert hq.hq_fp8_linear_kernel_name(m, n, k, DTYPES[dtype]) == kernel
+    test_product(m, k, n, dtype)
+    test_products_of_whole_numbers(m, k, n, dtype)
+
+
+@pytest.mark.parametrize("m,k,n,dtype,kernel", [
+    (1, 100, 40, "f16", "one launch (16 x 16)"), (1, 1000, 4100, "bf16", "one launch (16 x 32)"), (1025, 1000, 130, "f16", "one launch (16 x 64)"),
+    (1, 100, 40, "f32", "one launch (16 x 16)"), (1, 500, 4100, "f32", "one launch (16 x 32)"), (4100, 100, 130, "f32", "one launch (16 x 64)"),
+    (130, 4100, 1030, "f16", "split (16 x 32)"), (2049, 500, 4100, "bf16", "tile (256 x 256)")])
+def test_every_kernel_of_the_layer(m, k, n, dtype, kernel):
+    assert hq.hq_fp8_linear_kernel_name(m, n, k, DTYPES[dtype], DTYPES[dtype]) == kernel
+    x, xf = values((m, k), dtype, 3 * m + k)
+    w, _ = values((n, k), "f32", n + k, 0.02)
+    b, bf = values((n,), dtype, n)
+    wq, sw = hq.hq_fp8_quantize_blocks(w)
+    y = hq.hq_act_quant_fp8_linear(x, wq, sw, b, y_dtype=DTYPES[dtype])
+    q, s = quantised(xf, 1)
+    xd, wd = q * spread(s, 1, m, k), held(wq)[:, :k] * spread(sw.cpu().numpy(), 128, n, k)
+    bias = bf.astype(np.float64)
+    close(y, xd @ wd.T + bias, product_bound(xd, wd, up(k, 128), dtype) + 2.0 ** -23 * np.abs(bias), dtype)
+
+
+@pytest.mark.parametrize("m,k,n", [(3, 200, 24), (300, 520, 264), (1025, 500, 1030)])
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_values_that_are_not_finite(m, k, n, dtype):
+    """A row with an infinity or a NaN has NaN for results, and no other row; gradients: what such a group takes part in."""
+    x, _ = values((m, k), dtype, 1)
+    dy, _ = values((m, n), dtype, 2)
+    w, _ = values((n, k), dtype, 3, 0.02)
+    wq, wt, sw = hq.hq_fp8_quantize_blocks(w, transposed=True)
+    clean = hq.hq_act_quant_fp8_linear(x, wq, sw, y_dtype=DTYPES[dtype])
+    x[0, 5], x[m - 1, k - 1] = float("inf"), float("nan")
+    y = hq.hq_act_quant_fp8_linear(x, wq, sw, y_dtype=DTYPES[dtype])
+    assert torch.isnan(y[[0, m - 1]]).all() and torch.equal(y[1:m - 1], clean[1:m - 1])
+    dy[1, 7] = float("-inf")
+    dx, dw, db = hq.hq_fp8_linear_backward(dy, x, wt, sw, bias_grad=True)
+    bad = torch.isnan(dx).all(1)
+    assert bad[1] and bad.sum() == 1 and torch.isfinite(dx[~bad]).all()
+    with_bad = torch.zeros((n, k), dtype=torch.bool, device="cuda")   # row 7 of dy^T, the blocks of x of both columns
+    with_bad[7], with_bad[:, :128], with_bad[:, (k - 1) // 128 * 128:] = True, True, True
+    assert torch.equal(torch.isnan(dw), with_bad) and torch.isfinite(dw[~with_bad]).all()
+    assert torch.isinf(db[7]) and torch.isfinite(db).sum() == n - 1
+
+
 def test_nothing_is_written_beyond_the_result():
     for m, n in ((5, 3), (19, 129), (200, 333), (300, 264)):
         x, _ = values((m, 200), "f16", m)
@@ -256,6 +310,17 @@ def test_gradients(m, k, n, dtype):
     close(db, dyf.astype(np.float64).sum(0), np.abs(dyf).sum(0) * (up(m, 128) + 128) * 2.0 ** -23, "f32")
     only = hq.hq_fp8_linear_backward(dy, x, wt, sw)
     assert only[2] is None and torch.equal(only[0], dx) and torch.equal(only[1], dw)   # the same bits again
+
+
+@pytest.mark.parametrize("m,k,n,dtype,kernel", [
+    (1, 100, 40, "f16", "split (16 x 16)"), (1, 2100, 300, "bf16", "split (16 x 32)"), (1, 2100, 700, "f16", "split (32 x 32)"),
+    (130, 2100, 300, "f16", "tile (64 x 64)"), (700, 1000, 1030, "bf16", "tile (64 x 128)"), (4100, 2100, 4100, "f16", "tile (256 x 128)"),
+    (4100, 4100, 40, "bf16", "two launches"), (1, 100, 40, "f32", "split (16 x 16)"), (1, 2100, 300, "f32", "split (16 x 32)"),
+    (1025, 500, 300, "f32", "split (32 x 32)"), (520, 2100, 130, "f32", "tile (64 x 64)"), (520, 2100, 700, "f32", "tile (64 x 128)"),
+    (4100, 2100, 4100, "f32", "tile (256 x 128)"), (4100, 4100, 40, "f32", "two launches")])
+def test_every_kernel_of_the_gradients(m, k, n, dtype, kernel):
+    assert hq.hq_fp8_linear_backward_kernel_name(m, n, k, DTYPES[dtype], bias_grad=True) == kernel
+    test_gradients(m, k, n, dtype)
 
 
 def test_gradients_by_differences():
