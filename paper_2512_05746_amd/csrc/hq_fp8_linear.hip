@@ -52,7 +52,8 @@ struct Product {
     using Out = typename Float<OUT>::type;
     static constexpr bool kFp32 = OUT == HQ_F32;
     static constexpr int NW = WM * WN, TM = BM / WM, TN = BN / WN, MT = TM / 16, NT = TN / 16;
-    static constexpr int NG = NT < 4 ? NT : 4;   // a lane's neighbouring channels: 4 NG
+    // A lane's neighbouring channels, 4 NG, are the 16 bytes of a store: the 4 lanes of a token then write 64 bytes in a row.
+    static constexpr int NG = kFp32 ? 1 : 2;
     static constexpr int kCodes = (BM + BN) * kStep, LX = BM / 8 / NW, LW = BN / 8 / NW;
     // after the codes: the tokens' scales, then those of the blocks of channels, 64 copies of each
     static constexpr int SX = (BM + 63) / 64, SW = (BN + kStep - 1) / kStep, kTile = kCodes + (SX + SW) * 256;
@@ -397,24 +398,26 @@ struct TileChoice {
     float us;
 };
 // tiles a CU, in shares of a CU
-float tiles_per_cu(const TileCost &c, int64_t m, int64_t n) {
-    return static_cast<float>(((m + c.bm - 1) / c.bm) * ((n + c.bn - 1) / c.bn)) / hq::compute_units();
+float tiles_per_cu(const TileCost &c, int64_t m, int64_t n, float cu) {
+    return static_cast<float>(((m + c.bm - 1) / c.bm) * ((n + c.bn - 1) / c.bn)) / cu;
 }
 TileChoice choose_tile(int64_t m, int64_t n, int64_t steps, hq_dtype out) {
+    const float cu = static_cast<float>(hq::compute_units());
     TileChoice best{kTile64, 1e30f};
     for (const TileCost &c : kTiles) {
         const int o = out == HQ_F32;
-        const float us = c.begin[o] + steps * std::max(c.round[o], ceilf(tiles_per_cu(c, m, n)) * c.each[o]);
+        const float us = c.begin[o] + steps * std::max(c.round[o], ceilf(tiles_per_cu(c, m, n, cu)) * c.each[o]);
         if (us < best.us) best = {c.tile, us};
     }
     return best;
 }
 TileChoice choose_pair(const ProductArgs &a, const ProductArgs &b, hq_dtype out) {
+    const float cu = static_cast<float>(hq::compute_units());
     TileChoice best{kTile64, 1e30f};
     for (const TileCost &c : kTiles) {
         if (c.tile == kTile256) continue;
         const int o = out == HQ_F32;
-        const float share = a.steps * tiles_per_cu(c, a.m, a.n) * c.each[o] + b.steps * tiles_per_cu(c, b.m, b.n) * c.each[1];
+        const float share = a.steps * tiles_per_cu(c, a.m, a.n, cu) * c.each[o] + b.steps * tiles_per_cu(c, b.m, b.n, cu) * c.each[1];
         // (the last round is only partly filled: half of the longer tile)
         const float longest = std::max(a.steps * c.each[o], b.steps * c.each[1]);
         const float us = c.begin[1] + std::max(std::max(a.steps * c.round[o], b.steps * c.round[1]), share + 0.5f * longest);

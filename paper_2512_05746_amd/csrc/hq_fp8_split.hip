@@ -258,13 +258,14 @@ constexpr float kBegin = 2.2f;
 
 Fp8Cut fp8_split_cut(int64_t m, int64_t n, int64_t steps, const hq_dtype *in, hq_dtype out) {
     const int kind = !in ? 0 : *in == HQ_F32 ? 2 : 1;
+    const float cu = static_cast<float>(compute_units());
     Fp8Cut best{1, 1, 1e30f};
     for (const Cost &c : costs) {
         if ((m + 16 * c.mt - 1) / (16 * c.mt) > 65535) continue;   // (the grid's limit in y)
         // Fewer workgroups than CUs: each has a CU of its own.  Those that quantise keep a CU's vector units busy, so that a second one on it waits (333 x
         // 1024 -> 768 5.7 us, -> 777 8.6); those on codes wait for loads.
-        float share = std::max(c.shares(m, n, steps, kind, out) / compute_units(), c.shares(1, 1, steps, kind, out));
-        if (in) share = ceilf(static_cast<float>(c.groups(m, n)) / compute_units()) * c.shares(1, 1, steps, kind, out);
+        float share = std::max(c.shares(m, n, steps, kind, out) / cu, c.shares(1, 1, steps, kind, out));
+        if (in) share = ceilf(static_cast<float>(c.groups(m, n)) / cu) * c.shares(1, 1, steps, kind, out);
         const float us = kBegin + std::max(c.rounds(steps, kind), share);
         if (us < best.us) best = {c.mt, c.nt, us};
     }
@@ -272,10 +273,11 @@ Fp8Cut fp8_split_cut(int64_t m, int64_t n, int64_t steps, const hq_dtype *in, hq
 }
 
 Fp8Cut fp8_split_pair_cut(const Fp8Product &a, const Fp8Product &b, hq_dtype out) {
+    const float cu = static_cast<float>(compute_units());
     Fp8Cut best{1, 1, 1e30f};
     for (const Cost &c : costs) {
         if (c.groups(a.m, a.n) + c.groups(b.m, b.n) > 0x3FFFFFFF) continue;
-        const float share = std::max((c.shares(a.m, a.n, a.steps, 0, out) + c.shares(b.m, b.n, b.steps, 0, HQ_F32)) / compute_units(),
+        const float share = std::max((c.shares(a.m, a.n, a.steps, 0, out) + c.shares(b.m, b.n, b.steps, 0, HQ_F32)) / cu,
                                      c.shares(1, 1, std::max(a.steps, b.steps), 0, HQ_F32));
         const float us = kBegin + std::max(c.rounds(std::max(a.steps, b.steps), 0), share);
         if (us < best.us) best = {c.mt, c.nt, us};
