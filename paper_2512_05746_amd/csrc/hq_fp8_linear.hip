@@ -433,7 +433,7 @@ hq_status launch(const ProductArgs &a, Tile tile, hipStream_t st) {
             if constexpr (OUT != HQ_F32) return launch_tiles<OUT, 256, 256, 4, 2, 2>(a, st);   // (sums in fp32 products need more registers)
         case kTile128: return launch_tiles<OUT, 256, 128, 4, 2, 3>(a, st);
         case kTile64x128: return launch_tiles<OUT, 64, 128, 2, 2, 3>(a, st);
-        default: return launch_tiles<OUT, 64, 64, 2, 2, 4>(a, st);
+        default: return launch_tiles<OUT, 64, 64, 2, 2, 3>(a, st);
     }
 }
 
@@ -442,7 +442,7 @@ hq_status launch_pair(const ProductArgs &a, const ProductArgs &b, const hq::Fp8S
     switch (tile) {
         case kTile128: return launch_pair<OUT, 256, 128, 4, 2, 3>(a, b, sums, st);
         case kTile64x128: return launch_pair<OUT, 64, 128, 2, 2, 3>(a, b, sums, st);
-        default: return launch_pair<OUT, 64, 64, 2, 2, 4>(a, b, sums, st);
+        default: return launch_pair<OUT, 64, 64, 2, 2, 3>(a, b, sums, st);
     }
 }
 
