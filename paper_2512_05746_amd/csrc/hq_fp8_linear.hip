@@ -379,20 +379,22 @@ hq_status launch_pair(const ProductArgs &a, const ProductArgs &b, const hq::Fp8S
     return check.status();
 }
 
-// The tiles of the product, 16-bit results first, then 32-bit ones.  A step of a lone workgroup takes `round` us, a CU's share of a
-// step `each` us a tile when it has several; measured with 8192 x 4096 -> 8192 and 4096 x 8192 -> 4096 (shares), 2048 x 3840 -> 960 and 1024 x 1024 -> 1024
-// (rounds); begin: launch, first
-// loads and results.  128 x 128 tiles were never the fastest.
+// The tiles of the product, for 16-bit results first, then for 32-bit ones.  A step of a lone workgroup takes `round` us, a CU's share of a
+// step `each` us a tile when it has several; measured with 8192 x 4096 -> 8192 and 4096 x 8192 -> 4096 (shares), 2048 x 3840 -> 960 and 1024 x 1024
+// -> 1024 (rounds); begin: launch, first loads and results.  Tiles of 128 x 128, two workgroups a CU, are not among them: 335 us for 8192 x 4096 -> 8192 where
+// 256 x 128 takes 302 and 256 x 256 257; with fp32 results 246 us for 4096 x 8192 -> 4096 where 256 x 128 takes 239 (the card's power is the limit
+// there, and larger tiles move less through LDS).
 enum Tile { kTile256, kTile128, kTile64x128, kTile64 };
 struct TileCost {
     Tile tile;
     int bm, bn;
-    float begin[2], round[2], each[2];
+    float begin, round[2], each[2];
 };
-constexpr TileCost kTiles[] = {{kTile256, 256, 256, {4.3f, 1e30f}, {1.4f, 1e30f}, {1.6f, 1e30f}},
-                               {kTile128, 256, 128, {4.0f, 4.0f}, {0.9f, 1.6f}, {1.18f, 1.95f}},
-                               {kTile64x128, 64, 128, {3.3f, 3.3f}, {0.44f, 0.8f}, {0.38f, 0.6f}},
-                               {kTile64, 64, 64, {3.2f, 3.2f}, {0.37f, 0.62f}, {0.24f, 0.38f}}};
+constexpr float kNot = 1e30f;
+constexpr TileCost kTiles[] = {{kTile256, 256, 256, 4.3f, {1.4f, kNot}, {1.6f, kNot}},
+                               {kTile128, 256, 128, 4.0f, {0.9f, 1.6f}, {1.18f, 1.87f}},
+                               {kTile64x128, 64, 128, 3.3f, {0.44f, 0.8f}, {0.38f, 0.6f}},
+                               {kTile64, 64, 64, 3.2f, {0.37f, 0.62f}, {0.24f, 0.38f}}};
 struct TileChoice {
     Tile tile;
     float us;
@@ -406,7 +408,7 @@ TileChoice choose_tile(int64_t m, int64_t n, int64_t steps, hq_dtype out) {
     TileChoice best{kTile64, 1e30f};
     for (const TileCost &c : kTiles) {
         const int o = out == HQ_F32;
-        const float us = c.begin[o] + steps * std::max(c.round[o], ceilf(tiles_per_cu(c, m, n, cu)) * c.each[o]);
+        const float us = c.begin + steps * std::max(c.round[o], ceilf(tiles_per_cu(c, m, n, cu)) * c.each[o]);
         if (us < best.us) best = {c.tile, us};
     }
     return best;
@@ -420,7 +422,7 @@ TileChoice choose_pair(const ProductArgs &a, const ProductArgs &b, hq_dtype out)
         const float share = a.steps * tiles_per_cu(c, a.m, a.n, cu) * c.each[o] + b.steps * tiles_per_cu(c, b.m, b.n, cu) * c.each[1];
         // (the last round is only partly filled: half of the longer tile)
         const float longest = std::max(a.steps * c.each[o], b.steps * c.each[1]);
-        const float us = c.begin[1] + std::max(std::max(a.steps * c.round[o], b.steps * c.round[1]), share + 0.5f * longest);
+        const float us = c.begin + std::max(std::max(a.steps * c.round[o], b.steps * c.round[1]), share + 0.5f * longest);
         if (us < best.us) best = {c.tile, us};
     }
     return best;
@@ -430,7 +432,8 @@ template <int OUT>
 hq_status launch(const ProductArgs &a, Tile tile, hipStream_t st) {
     switch (tile) {
         case kTile256:
-            if constexpr (OUT != HQ_F32) return launch_tiles<OUT, 256, 256, 4, 2, 2>(a, st);   // (sums in fp32 products need more registers)
+            if constexpr (OUT != HQ_F32) return launch_tiles<OUT, 256, 256, 4, 2, 2>(a, st);   // (not with fp32 results: too many registers)
+            [[fallthrough]];
         case kTile128: return launch_tiles<OUT, 256, 128, 4, 2, 3>(a, st);
         case kTile64x128: return launch_tiles<OUT, 64, 128, 2, 2, 3>(a, st);
         default: return launch_tiles<OUT, 64, 64, 2, 2, 3>(a, st);
