@@ -14,6 +14,9 @@
 // Bound by memory (two passes over q and k, three backwards).  A head is owned by G neighbouring lanes, a lane owns C channel pairs: it loads C channels of
 // each half of the head (or 2 C neighbours, where these are the pairs), so that both channels of a pair meet in one lane and only
 // the sum of squares crosses lanes (permutes inside a row of 16).  Heads that no such cut fits take a wave each.
+// 65536 tokens of 32 + 8 heads of 128 in bf16: 252 us (5.3 TB/s, a large copy 5.15); backwards, 32768 tokens: 191 us and 4.5 for the weights' sums
+// (5.2 TB/s).  Few tokens are bound by latency: launch, the position, the tables' row that it names, results (1 token 2.5 us, 1021 tokens of
+// 32 heads of 72 in fp16 5.7).
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
