@@ -478,10 +478,10 @@ hq_status hq_qk_norm_rope(const void *q, const void *k, hq_dtype dtype, int64_t 
  * Its gradients.  dq, dk: gradients of the results; q, k: the inputs of the forward pass.
  *   strides   q token, q head, k token, k head, then those of dq, dk, and those of q_grad, k_grad (12 numbers)
  *   q_weight_grad, k_weight_grad   [d] fp32, sums over all tokens and heads in a fixed order; or NULL
- *   workspace hq_qk_norm_rope_backward_workspace(t, heads, kv_heads, d, rotary) bytes, 4-byte aligned
+ *   workspace hq_qk_norm_rope_backward_workspace(..) bytes, 4-byte aligned
  * Padding has zeros for gradients and no part in the weights'.  q_grad may be dq or q, k_grad dk or k (the same memory, the same strides).
  */
-int64_t hq_qk_norm_rope_backward_workspace(int64_t t, int heads, int kv_heads, int d, int rotary);
+int64_t hq_qk_norm_rope_backward_workspace(hq_dtype dtype, int64_t t, int heads, int kv_heads, int d, int rotary);
 hq_status hq_qk_norm_rope_backward(const void *dq, const void *dk, const void *q, const void *k, hq_dtype dtype, int64_t t,
                                    int heads, int kv_heads, int d, const int64_t *strides, const void *q_weight,
                                    const void *k_weight, hq_dtype w_dtype, const float *cos, const float *sin,

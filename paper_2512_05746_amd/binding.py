@@ -89,7 +89,7 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
                                                         vp, i32, f32] + [vp] * 6
     lib.hq_act_quant_fp8_linear_workspace.argtypes = [i32, i64, i32, i32, i32]
     lib.hq_fp8_linear_backward_workspace.argtypes = [i64, i32, i32]
-    lib.hq_qk_norm_rope_backward_workspace.argtypes = [i64, i32, i32, i32, i32]
+    lib.hq_qk_norm_rope_backward_workspace.argtypes = [i32, i64, i32, i32, i32, i32]
     for name in SYMBOLS[1:]:
         getattr(lib, name).restype = i32
     for name in WORKSPACE_SYMBOLS:

@@ -370,15 +370,20 @@ __global__ __launch_bounds__(1024) void weight_sums_kernel(QkArgs a) {
     }
 }
 
-// Lanes to a head and pairs to a lane; lanes 0: a wave for a head.
+// Pairs to a lane and lanes to a head, a power of two (g = 0: a wave for a head).  Eight pairs are two loads of 16 bytes for floats of 16 bits.  For
+// 32 bits four are, and forwards that is faster: 36918 tokens of 36 heads of 96 258 -> 216 us, 30000 of 128 219 -> 217; backwards where eight
+// would leave lanes without a pair (heads of 96 358 -> 315 us, of 80 208 -> 198), else eight are (heads of 128 332 us, with four 339).
+// (Lanes that are no power of two, 60 of 64 busy instead of 40 .. 48: 3 to 6 % less for many tokens of 80 or 96 channels, up to 10 % more
+// for a thousand, since their sums take five exchanges through LDS.)
 struct Cut {
     int c, g;
 };
-Cut cut_of(int d, int rotary) {
+Cut cut_of(int d, int rotary, hq_dtype dt, bool back) {
+    const bool full = d % 16 == 0 && ((d >> 4) & ((d >> 4) - 1)) == 0;
     for (const int c : {8, 4}) {
         if ((rotary >> 1) % c || (d >> 1) % c) continue;
         const int lanes = (d >> 1) / c;
-        if (lanes > 32) continue;
+        if (lanes > 32 || (c == 8 && dt == HQ_F32 && d <= 256 && !(back && full))) continue;
         int g = 2;
         while (g < lanes) g *= 2;
         return {c, g};
@@ -461,7 +466,7 @@ extern "C" hq_status hq_qk_norm_rope(const void *q, const void *k, hq_dtype dtyp
     for (const void *p : {q_weight, k_weight})
         if (!hq::aligned_to(p, hq::size_of(w_dtype))) return HQ_ERR_ALIGN;
     if (!hq::aligned_to(cos, 4) || !hq::aligned_to(sin, 4) || !hq::aligned_to(pos, pos_size == 8 ? 8 : 4)) return HQ_ERR_ALIGN;
-    const Cut cut = cut_of(d, rotary);
+    const Cut cut = cut_of(d, rotary, dtype, false);
     const int slots = cut.g ? 256 / cut.g : 4;
     QkArgs a{};
     a.part[0] = Heads{q, nullptr, q_weight, q_out, nullptr, strides[0], strides[1], 0, 0, strides[4], strides[5]};
@@ -473,9 +478,9 @@ extern "C" hq_status hq_qk_norm_rope(const void *q, const void *k, hq_dtype dtyp
     return run<false>(a, dtype, cut, static_cast<hipStream_t>(stream));
 }
 
-extern "C" int64_t hq_qk_norm_rope_backward_workspace(int64_t t, int heads, int kv_heads, int d, int rotary) {
-    if (check_sizes(t, heads, kv_heads, d, rotary, 1, &t, 4, 0.0f) != HQ_OK) return 0;
-    const Cut cut = cut_of(d, rotary);
+extern "C" int64_t hq_qk_norm_rope_backward_workspace(hq_dtype dtype, int64_t t, int heads, int kv_heads, int d, int rotary) {
+    if (!hq::is_float(dtype) || check_sizes(t, heads, kv_heads, d, rotary, 1, &t, 4, 0.0f) != HQ_OK) return 0;
+    const Cut cut = cut_of(d, rotary, dtype, true);
     const int slots = cut.g ? 256 / cut.g : 4;
     const int64_t blocks = int64_t{blocks_for(static_cast<uint32_t>(t * heads), slots, true)} +
                            blocks_for(static_cast<uint32_t>(t * kv_heads), slots, true);
@@ -499,7 +504,7 @@ extern "C" hq_status hq_qk_norm_rope_backward(const void *dq, const void *dk, co
     if (!hq::aligned_to(cos, 4) || !hq::aligned_to(sin, 4) || !hq::aligned_to(pos, pos_size == 8 ? 8 : 4) ||
         !hq::aligned_to(workspace, 4) || !hq::aligned_to(q_weight_grad, 4) || !hq::aligned_to(k_weight_grad, 4))
         return HQ_ERR_ALIGN;
-    const Cut cut = cut_of(d, rotary);
+    const Cut cut = cut_of(d, rotary, dtype, true);
     const int slots = cut.g ? 256 / cut.g : 4;
     QkArgs a{};
     a.part[0] = Heads{q, dq, q_weight, q_grad, q_weight_grad, strides[0], strides[1], strides[4], strides[5], strides[8], strides[9]};

@@ -798,7 +798,7 @@ PyObject *qk_norm_rope_backward(Args a) {
     at::Tensor qw, kw;
     if (in.q_weight) qw = empty({in.d()}, at::kFloat, in.q);
     if (in.k_weight) kw = empty({in.d()}, at::kFloat, in.q);
-    const at::Tensor space = empty({lib.hq_qk_norm_rope_backward_workspace(in.t(), in.heads(), in.kv_heads(), in.d(), in.rotary)},
+    const at::Tensor space = empty({lib.hq_qk_norm_rope_backward_workspace(in.type, in.t(), in.heads(), in.kv_heads(), in.d(), in.rotary)},
                                    at::kByte, in.q);
     const int64_t strides[12] = {in.q.stride(0), in.q.stride(1), in.k.stride(0), in.k.stride(1), dq.stride(0), dq.stride(1),
                                  dk.stride(0), dk.stride(1), out.q.stride(0), out.q.stride(1), out.k.stride(0), out.k.stride(1)};

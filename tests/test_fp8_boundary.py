@@ -90,8 +90,8 @@ def test_heads_arguments(lib):
         assert f(q=P + 1) == ALIGN and f(ko=P + 1) == ALIGN and f(qw=P + 1) == ALIGN and f(cos=P + 2) == ALIGN and f(pos=P + 4) == ALIGN
     assert heads(t=0, q=None, k=None, qo=None, ko=None) == OK
     assert back(space=P + 2) == ALIGN and back(dqw=P + 2) == ALIGN
-    assert lib.hq_qk_norm_rope_backward_workspace(8, 4, 2, 63, 62) == 0
-    assert lib.hq_qk_norm_rope_backward_workspace(8, 4, 2, 64, 64) >= 2 * 64 * 4
+    assert lib.hq_qk_norm_rope_backward_workspace(F16, 8, 4, 2, 63, 62) == 0
+    assert lib.hq_qk_norm_rope_backward_workspace(F16, 8, 4, 2, 64, 64) >= 2 * 64 * 4
 
 
 def test_calls_on_integer_codes_do_not_take_bfloat16(lib):
