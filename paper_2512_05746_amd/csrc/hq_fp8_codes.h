@@ -50,7 +50,6 @@ template <class T> struct Raw8 {
 typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
 typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
 template <class T> struct Tops {
-    static constexpr int kWords = 4;   // of two
     u16x2 t[4] = {};
     __device__ __forceinline__ void add(const Raw8<T> &r) {
         const u32x4 w = __builtin_bit_cast(u32x4, r.v) & 0x7FFF7FFFu;

@@ -37,7 +37,7 @@ namespace {
 // all of them.  They have no register for a result.
 //
 // What bounds it: 8192 x 4096 -> 8192 with 256 x 256 tiles 239 us (2.3 PFLOP/s; a library product of the same codes with one scale for the tensor
-// 229 .. 231): the matrix pipe is busy in 65 % of the cycles and the clock is at 1.73 of 2.4 GHz, so it is power; at few workgroups LDS (192 KB
+// 229 .. 231): the matrix pipe is busy in 62 % of the cycles and the clock is at 1.73 of 2.4 GHz, so it is power; at few workgroups LDS (192 KB
 // of reads and 64 KB of loads a step, 128 bytes a cycle, against 2048 cycles of the matrix pipe).  fp32 results: 4096 x 8192 -> 4096 239 us (1.15
 // PFLOP/s; bf16 products of a library 1.42).  Small K (4096 x 576 -> 1728 12.2 us, 8.2 with K = 128): launch, first loads and results (14 MB)
 // of one round of workgroups.
