@@ -13,7 +13,8 @@
 //
 // Bound by memory (two passes over q and k, three backwards).  A head is owned by G neighbouring lanes, a lane owns C channel pairs: it loads C channels of
 // each half of the head (or 2 C neighbours, where these are the pairs), so that both channels of a pair meet in one lane and only
-// the sum of squares crosses lanes (permutes inside a row of 16).  Heads that no such cut fits take a wave each.
+// the sum of squares crosses lanes (permutes inside a row of 16).  Heads that no such cut fits (more than 64 lanes of the pairs that divide
+// both their rotated and their other channels) take a wave each, whose lanes have pairs 64 apart.
 // 65536 tokens of 32 + 8 heads of 128 in bf16: 252 us (5.3 TB/s, a large copy 5.15); backwards, 32768 tokens: 191 us and 4.5 for the weights' sums
 // (5.2 TB/s).  Few tokens are bound by latency: launch, the position, the tables' row that it names, results (1 token 2.5 us, 1021 tokens of
 // 32 heads of 72 in fp16 5.7).
@@ -236,7 +237,8 @@ __global__ __launch_bounds__(256) void heads_kernel(QkArgs a) {
     }
 }
 
-// Any even number of channels up to 1024: a wave for each head, a lane's pairs 64 apart.
+// Any even number of channels up to 1024: a wave for each head, a lane's pairs 64 apart (4096 tokens of 16 heads of 514 in bf16 118 us, of 1024 271, where the
+// kernel above takes 62).
 constexpr int kMostPairs = 8;   // of a lane
 template <int DT, bool BACK>
 __global__ __launch_bounds__(256) void wave_kernel(QkArgs a) {
@@ -370,7 +372,9 @@ __global__ __launch_bounds__(1024) void weight_sums_kernel(QkArgs a) {
     }
 }
 
-// Pairs to a lane and lanes to a head, a power of two (g = 0: a wave for a head).  Eight pairs are two loads of 16 bytes for floats of 16 bits.  For
+// Pairs to a lane and lanes to a head, a power of two (g = 0: a wave for a head).  As many pairs as divide both parts of the head, for a lane's channels have to
+// be neighbours: 20000 tokens of 32 heads of 72 in bf16 with 36 of them turned, two pairs, 87 us (137 with gradients), with 18, one pair, 124 (207),
+// where a wave for each head takes 368 and 364 (702, 691).  Eight pairs are two loads of 16 bytes for floats of 16 bits.  For
 // 32 bits four are, and forwards that is faster: 36918 tokens of 36 heads of 96 258 -> 216 us, 30000 of 128 219 -> 217; backwards where eight
 // would leave lanes without a pair (heads of 96 358 -> 315 us, of 80 208 -> 198), else eight are (heads of 128 332 us, with four 339).
 // (Lanes that are no power of two, 60 of 64 busy instead of 40 .. 48: 3 to 6 % less for many tokens of 80 or 96 channels, up to 10 % more
@@ -380,15 +384,15 @@ struct Cut {
 };
 Cut cut_of(int d, int rotary, hq_dtype dt, bool back) {
     const bool full = d % 16 == 0 && ((d >> 4) & ((d >> 4) - 1)) == 0;
-    for (const int c : {8, 4}) {
+    for (const int c : {8, 4, 2, 1}) {
         if ((rotary >> 1) % c || (d >> 1) % c) continue;
         const int lanes = (d >> 1) / c;
-        if (lanes > 32 || (c == 8 && dt == HQ_F32 && d <= 256 && !(back && full))) continue;
+        if (lanes > 64 || (c == 8 && dt == HQ_F32 && d <= 256 && !(back && full))) continue;
         int g = 2;
         while (g < lanes) g *= 2;
         return {c, g};
     }
-    return {1, 0};
+    return {0, 0};
 }
 
 // Forwards 24 workgroups a CU (65536 tokens of 40 heads of 128 in 16 bits: 252 us, 290 with a workgroup for every 32 heads, 259 with 8 a CU);
@@ -412,11 +416,14 @@ void launch(const QkArgs &a, Cut cut, hipStream_t st) {
                 case 4: return go(c, std::integral_constant<int, 4>{});
                 case 8: return go(c, std::integral_constant<int, 8>{});
                 case 16: return go(c, std::integral_constant<int, 16>{});
-                default: return go(c, std::integral_constant<int, 32>{});
+                case 32: return go(c, std::integral_constant<int, 32>{});
+                default: return go(c, std::integral_constant<int, 64>{});
             }
         };
         if (cut.c == 8) with_c(std::integral_constant<int, 8>{});
         else if (cut.c == 4) with_c(std::integral_constant<int, 4>{});
+        else if (cut.c == 2) with_c(std::integral_constant<int, 2>{});
+        else if (cut.c == 1) with_c(std::integral_constant<int, 1>{});
         else wave_kernel<DT, BACK><<<blocks, 256, 0, st>>>(a);
     }
     if (BACK) weight_sums_kernel<<<2 * ((a.d + 7) / 8), 1024, 0, st>>>(a);

@@ -134,6 +134,11 @@ CASES = [
     dict(t=7, heads=3, kv_heads=1, d=130, rotary=66, pos="random"), dict(t=700, heads=32, kv_heads=8, d=128, rotary=128, pos="random"),
     dict(t=4, heads=4, kv_heads=1, d=64, rotary=64, pos="padding"), dict(t=1500, heads=3, kv_heads=1, d=40, rotary=20, pos="padded"),
 ]
+# every number of pairs to a lane with every number of lanes to a head, and heads beyond them
+CUTS = [dict(t=37, heads=3, kv_heads=1, d=2 * c * (g - g // 4), rotary=2 * c * max(1, g // 2 - 1), pos="padded")
+        for c in (1, 2, 4, 8) for g in (2, 4, 8, 16, 32, 64)]
+CUTS += [dict(t=13, heads=2, kv_heads=1, d=d, rotary=r, pos="padded") for d, r in
+         ((4, 4), (72, 36), (72, 18), (128, 66), (130, 66), (256, 68), (260, 260), (512, 24), (516, 12), (1008, 16), (1024, 8))]
 
 
 @pytest.mark.parametrize("interleaved", [False, True])
@@ -145,6 +150,15 @@ def test_forward_and_gradients(case, dtype, interleaved):
     got = c.backward()
     c.check_backward(got)
     assert all(torch.equal(a, b) for a, b in zip(got, c.backward()))   # a fixed order: the same bits again
+
+
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("case", CUTS, ids=lambda c: "d%(d)d_r%(rotary)d" % c)
+def test_cuts_of_a_head(case, dtype, interleaved):
+    c = Case(dtype=dtype, interleaved=interleaved, **case)
+    c.check_forward(c.forward())
+    c.check_backward(c.backward())
 
 
 @pytest.mark.parametrize("weights", ["f32", "none"])
