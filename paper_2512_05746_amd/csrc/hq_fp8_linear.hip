@@ -33,26 +33,13 @@ namespace {
 // filled again, and the buffer of the next one has landed.  The loads of a step are dealt over the products, since a wave that issues them all at once
 // waits for the path to memory.
 //
-// The loads are written out: of the compiler's own it cannot tell which buffer they fill, and would let every read of LDS wait for
-// all of them.  They have no register for a result.
+// (The loads have to be those of hq_fp8_product.h, which the compiler does not wait for.)
 //
 // What bounds it: 8192 x 4096 -> 8192 with 256 x 256 tiles 239 us (2.3 PFLOP/s; a library product of the same codes with one scale for the tensor
 // 229 .. 231): the matrix pipe is busy in 62 % of the cycles and the clock is at 1.73 of 2.4 GHz, so it is power; at few workgroups LDS (192 KB
 // of reads and 64 KB of loads a step, 128 bytes a cycle, against 2048 cycles of the matrix pipe).  fp32 results: 4096 x 8192 -> 4096 239 us (1.15
 // PFLOP/s; bf16 products of a library 1.42).  Small K (4096 x 576 -> 1728 12.2 us, 8.2 with K = 128): launch, first loads and results (14 MB)
 // of one round of workgroups.
-__device__ __forceinline__ v4i words_of(const void *p, uint32_t bytes) {   // of a buffer's descriptor
-    const uint64_t at = reinterpret_cast<uint64_t>(p);
-    return v4i{static_cast<int>(at), static_cast<int>(at >> 32), static_cast<int>(bytes), 0x00027000};
-}
-// lane i's 16 (4) bytes to lds + 16 i (4 i); zeros from beyond the buffer
-__device__ __forceinline__ void load16_to_lds(const v4i &buffer, uint32_t offset, uint32_t lds) {
-    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(offset), "s"(buffer), "s"(lds) : "memory");
-}
-__device__ __forceinline__ void load4_to_lds(const v4i &buffer, uint32_t offset, uint32_t lds) {
-    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dword %0, %1, 0 offen lds" ::"v"(offset), "s"(buffer), "s"(lds) : "memory");
-}
-
 template <int OUT, int BM, int BN, int WM, int WN, int STAGES>
 struct Product {
     using Out = typename Float<OUT>::type;
@@ -386,21 +373,22 @@ hq_status launch_pair(const ProductArgs &a, const ProductArgs &b, const hq::Fp8S
 }
 
 // The tiles of the product, for 16-bit results first, then for 32-bit ones.  A step of a lone workgroup takes `round` us, a CU's share of a
-// step `each` us a tile when it has several; measured with 8192 x 4096 -> 8192 and 4096 x 8192 -> 4096 (shares), 2048 x 3840 -> 960 and 1024 x 1024
-// -> 1024 (rounds); begin: launch, first loads and results.  Tiles of 128 x 128, two workgroups a CU, are not among them: 335 us for 8192 x 4096 -> 8192 where
+// step `each` us a tile when it has several; measured with 8192 x 4096 -> 8192 and 4096 x 8192 -> 4096 (shares), 2048 x 3840 -> 960, 1024 x 1024
+// -> 1024 and 256 x 4096 -> 4096 (rounds); begin: launch, first loads and results (300 x 100 -> 4100, 1025 x 500 -> 1030), again: those of a CU's further
+// tiles (2048 x 512 -> 2048, 4096 x 256 -> 1024).  Tiles of 128 x 128, two workgroups a CU, are not among them: 335 us for 8192 x 4096 -> 8192 where
 // 256 x 128 takes 302 and 256 x 256 257; with fp32 results 246 us for 4096 x 8192 -> 4096 where 256 x 128 takes 239 (the card's power is the limit
 // there, and larger tiles move less through LDS).
 enum Tile { kTile256, kTile128, kTile64x128, kTile64 };
 struct TileCost {
     Tile tile;
     int bm, bn;
-    float begin, round[2], each[2];
+    float begin, again, round[2], each[2];
 };
 constexpr float kNot = 1e30f;
-constexpr TileCost kTiles[] = {{kTile256, 256, 256, 4.3f, {1.4f, kNot}, {1.6f, kNot}},
-                               {kTile128, 256, 128, 4.0f, {0.9f, 1.6f}, {1.18f, 1.87f}},
-                               {kTile64x128, 64, 128, 3.3f, {0.44f, 0.8f}, {0.38f, 0.6f}},
-                               {kTile64, 64, 64, 3.2f, {0.37f, 0.62f}, {0.24f, 0.38f}}};
+constexpr TileCost kTiles[] = {{kTile256, 256, 256, 7.0f, 0.0f, {1.4f, kNot}, {1.6f, kNot}},
+                               {kTile128, 256, 128, 5.1f, 0.0f, {0.9f, 1.6f}, {1.18f, 1.87f}},
+                               {kTile64x128, 64, 128, 3.3f, 0.5f, {0.44f, 0.8f}, {0.38f, 0.6f}},
+                               {kTile64, 64, 64, 2.6f, 0.5f, {0.33f, 0.49f}, {0.24f, 0.38f}}};
 struct TileChoice {
     Tile tile;
     float us;
@@ -414,7 +402,7 @@ TileChoice choose_tile(int64_t m, int64_t n, int64_t steps, hq_dtype out) {
     TileChoice best{kTile64, 1e30f};
     for (const TileCost &c : kTiles) {
         const int o = out == HQ_F32;
-        const float us = c.begin + steps * std::max(c.round[o], ceilf(tiles_per_cu(c, m, n, cu)) * c.each[o]);
+        const float tiles = ceilf(tiles_per_cu(c, m, n, cu)), us = c.begin + (tiles - 1.0f) * c.again + steps * std::max(c.round[o], tiles * c.each[o]);
         if (us < best.us) best = {c.tile, us};
     }
     return best;
@@ -570,9 +558,9 @@ struct LayerChoice {
 LayerChoice choose_layer(hq_dtype x_dtype, int64_t m, int n, int k, hq_dtype y_dtype) {
     const int64_t steps = hq::fp8_groups(k);
     const hq::Fp8Cut fused = hq::fp8_split_cut(m, n, steps, &x_dtype, y_dtype);
-    // us of quantising them by themselves: 2.2 on the card, and a launch more on the host (333 x 1001 -> 777 7.2 against 8.4 us of one launch in a graph,
-    // called one by one 11.3 against 8.1)
-    const float rows = 4.0f + static_cast<float>(m) * k * (hq::size_of(x_dtype) + 1) / 4.5e6f;
+    // us of quantising them by themselves: 2.2 on the card, and a launch more on the host, which counts where calls follow one another (16 x 4096 -> 4096: 6.8
+    // against 8.4 us of one launch in a graph, called one by one 9.6 against 9.1)
+    const float rows = 3.2f + static_cast<float>(m) * k * (hq::size_of(x_dtype) + 1) / 4.5e6f;
     return {fused.us < rows + choose(m, n, steps, y_dtype).us(), fused};
 }
 }  // namespace
@@ -608,9 +596,9 @@ extern "C" hq_status hq_act_quant_fp8_linear(const void *x, hq_dtype x_dtype, in
 
 namespace {
 const char *name_of(const hq::Fp8Cut &c, bool one_launch) {
-    static const char *const names[2][3] = {{"split (16 x 16)", "split (16 x 32)", "split (32 x 32)"},
-                                            {"one launch (16 x 16)", "one launch (16 x 32)", "one launch (16 x 64)"}};
-    return names[one_launch][c.mt == 2 || c.nt == 4 ? 2 : c.nt - 1];
+    static const char *const names[2][4] = {{"split (16 x 16)", "split (16 x 32)", "split (32 x 32)", "split (64 x 64)"},
+                                            {"one launch (16 x 16)", "one launch (16 x 32)", "one launch (16 x 64)", nullptr}};
+    return names[one_launch][c.mt == 4 ? 3 : c.mt == 2 || c.nt == 4 ? 2 : c.nt - 1];
 }
 const char *name_of(Tile t) {
     switch (t) {

@@ -20,6 +20,20 @@ __device__ __forceinline__ f32x4 mfma_fp8(const v8i &a, const v8i &b) {
     return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0, 0, 0, 0);
 }
 
+// Loads from memory straight into LDS.  They are written out: of the compiler's own it cannot tell which bytes they fill, and would let
+// every read of LDS wait for all of them.  They have no register for a result.
+__device__ __forceinline__ v4i words_of(const void *p, uint32_t bytes) {   // of a buffer's descriptor
+    const uint64_t at = reinterpret_cast<uint64_t>(p);
+    return v4i{static_cast<int>(at), static_cast<int>(at >> 32), static_cast<int>(bytes), 0x00027000};
+}
+// lane i's 16 (4) bytes to lds + 16 i (4 i); zeros from beyond the buffer
+__device__ __forceinline__ void load16_to_lds(const v4i &buffer, uint32_t offset, uint32_t lds) {
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(offset), "s"(buffer), "s"(lds) : "memory");
+}
+__device__ __forceinline__ void load4_to_lds(const v4i &buffer, uint32_t offset, uint32_t lds) {
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dword %0, %1, 0 offen lds" ::"v"(offset), "s"(buffer), "s"(lds) : "memory");
+}
+
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 struct Halves {   // a lane's 32 codes of a step as operands of four bf16 instructions (E4M3 numbers are bf16 numbers)

@@ -205,11 +205,12 @@ def test_layer(m, k, n, dtype):
 
 
 KERNELS = [   # m, k, n, type, kernel on codes
-    (1, 500, 40, "f16", "split (16 x 16)"), (300, 500, 700, "bf16", "split (16 x 32)"), (33, 1000, 4100, "f16", "split (32 x 32)"),
-    (300, 100, 4100, "bf16", "tile (64 x 64)"), (1025, 500, 1030, "f16", "tile (64 x 128)"), (4096, 576, 1728, "f16", "tile (256 x 128)"),
-    (2049, 500, 4100, "bf16", "tile (256 x 256)"), (1, 500, 40, "f32", "split (16 x 16)"), (33, 500, 4100, "f32", "split (16 x 32)"),
+    (1, 500, 40, "f16", "split (16 x 16)"), (300, 500, 700, "bf16", "split (16 x 32)"), (33, 1000, 4100, "f16", "split (16 x 32)"),
+    (300, 100, 4100, "bf16", "tile (64 x 64)"), (1025, 500, 1030, "f16", "tile (64 x 64)"), (4096, 576, 1728, "f16", "tile (256 x 128)"),
+    (2049, 500, 4100, "bf16", "tile (64 x 128)"), (1, 500, 40, "f32", "split (16 x 16)"), (33, 500, 4100, "f32", "split (16 x 32)"),
     (2049, 500, 130, "f32", "split (32 x 32)"), (300, 100, 4100, "f32", "tile (64 x 64)"), (1025, 100, 4100, "f32", "tile (64 x 128)"),
-    (4096, 576, 1728, "f32", "tile (256 x 128)")]
+    (4096, 576, 1728, "f32", "tile (256 x 128)"), (2049, 900, 4100, "bf16", "tile (256 x 256)"), (300, 500, 1030, "f16", "split (32 x 32)"),
+    (500, 2100, 2010, "f16", "split (64 x 64)"), (500, 2100, 2010, "f32", "split (64 x 64)"), (1025, 100, 4100, "f16", "tile (64 x 128)")]
 
 
 @pytest.mark.parametrize("m,k,n,dtype,kernel", KERNELS)
@@ -222,7 +223,8 @@ def test_every_kernel_of_the_product(m, k, n, dtype, kernel):
 @pytest.mark.parametrize("m,k,n,dtype,kernel", [
     (1, 100, 40, "f16", "one launch (16 x 16)"), (1, 1000, 4100, "bf16", "one launch (16 x 32)"), (1025, 1000, 130, "f16", "one launch (16 x 64)"),
     (1, 100, 40, "f32", "one launch (16 x 16)"), (1, 500, 4100, "f32", "one launch (16 x 32)"), (4100, 100, 130, "f32", "one launch (16 x 64)"),
-    (130, 4100, 1030, "f16", "split (16 x 32)"), (2049, 500, 4100, "bf16", "tile (256 x 256)")])
+    (130, 4100, 1030, "f16", "split (16 x 32)"), (2049, 500, 4100, "bf16", "tile (64 x 128)"),
+    (2049, 900, 4100, "bf16", "tile (256 x 256)")])
 def test_every_kernel_of_the_layer(m, k, n, dtype, kernel):
     assert hq.hq_fp8_linear_kernel_name(m, n, k, DTYPES[dtype], DTYPES[dtype]) == kernel
     x, xf = values((m, k), dtype, 3 * m + k)
@@ -313,11 +315,13 @@ def test_gradients(m, k, n, dtype):
 
 
 @pytest.mark.parametrize("m,k,n,dtype,kernel", [
-    (1, 100, 40, "f16", "split (16 x 16)"), (1, 2100, 300, "bf16", "split (16 x 32)"), (1, 2100, 700, "f16", "split (32 x 32)"),
-    (130, 2100, 300, "f16", "tile (64 x 64)"), (700, 1000, 1030, "bf16", "tile (64 x 128)"), (4100, 2100, 4100, "f16", "tile (256 x 128)"),
+    (1, 100, 40, "f16", "split (16 x 16)"), (1, 2100, 300, "bf16", "tile (64 x 64)"), (1, 2100, 700, "f16", "tile (64 x 64)"),
+    (130, 2100, 300, "f16", "tile (64 x 64)"), (700, 1000, 1030, "bf16", "tile (64 x 64)"), (4100, 2100, 4100, "f16", "tile (256 x 128)"),
     (4100, 4100, 40, "bf16", "two launches"), (1, 100, 40, "f32", "split (16 x 16)"), (1, 2100, 300, "f32", "split (16 x 32)"),
-    (1025, 500, 300, "f32", "split (32 x 32)"), (520, 2100, 130, "f32", "tile (64 x 64)"), (520, 2100, 700, "f32", "tile (64 x 128)"),
-    (4100, 2100, 4100, "f32", "tile (256 x 128)"), (4100, 4100, 40, "f32", "two launches")])
+    (1025, 500, 300, "f32", "split (32 x 32)"), (520, 2100, 130, "f32", "tile (64 x 64)"), (520, 2100, 700, "f32", "tile (64 x 64)"),
+    (4100, 2100, 4100, "f32", "tile (256 x 128)"), (4100, 4100, 40, "f32", "two launches"),
+    (300, 300, 300, "bf16", "split (16 x 32)"), (300, 500, 700, "f16", "split (32 x 32)"), (700, 2100, 1030, "bf16", "tile (64 x 128)"),
+    (1025, 2100, 1030, "f32", "tile (64 x 128)")])
 def test_every_kernel_of_the_gradients(m, k, n, dtype, kernel):
     assert hq.hq_fp8_linear_backward_kernel_name(m, n, k, DTYPES[dtype], bias_grad=True) == kernel
     test_gradients(m, k, n, dtype)
