@@ -596,9 +596,8 @@ extern "C" hq_status hq_act_quant_fp8_linear(const void *x, hq_dtype x_dtype, in
 
 namespace {
 const char *name_of(const hq::Fp8Cut &c, bool one_launch) {
-    static const char *const names[2][4] = {{"split (16 x 16)", "split (16 x 32)", "split (32 x 32)", "split (64 x 64)"},
-                                            {"one launch (16 x 16)", "one launch (16 x 32)", "one launch (16 x 64)", nullptr}};
-    return names[one_launch][c.mt == 4 ? 3 : c.mt == 2 || c.nt == 4 ? 2 : c.nt - 1];
+    if (one_launch) return c.nt == 1 ? "one launch (16 x 16)" : c.nt == 2 ? "one launch (16 x 32)" : c.nt == 4 ? "one launch (16 x 64)" : "one launch (16 x 128)";
+    return c.mt == 4 ? "split (64 x 64)" : c.mt == 2 ? "split (32 x 32)" : c.nt == 2 ? "split (16 x 32)" : "split (16 x 16)";
 }
 const char *name_of(Tile t) {
     switch (t) {

@@ -303,7 +303,8 @@ hq_status with_cut(const SplitArgs &a, hq::Fp8Cut cut, hipStream_t st) {
         if (cut.mt == 2) return launch<IN, OUT, 2, 2>(a, st);
         return launch<IN, OUT, 4, 4>(a, st);
     } else {
-        return launch<IN, OUT, 1, 4>(a, st);
+        if (cut.nt == 4) return launch<IN, OUT, 1, 4>(a, st);
+        return launch<IN, OUT, 1, 8>(a, st);
     }
 }
 template <int IN>
@@ -320,7 +321,8 @@ namespace {
 // with 1 and 16 x 960 -> 3840, 16 and 64 x 4096 -> 4096 (rounds), 512 x 4096 -> 512 and 2048, 512 x 1024 -> 2048, 2048 x 2048 -> 2048 and
 // 2048 x 512 -> 2048 (shares), us in a graph; fp32: what a workgroup takes longer with fp32 results.  On codes a cut of 64 x 64 is for products that give
 // every CU one of them (512 x 4096 -> 2048 10.3 us, 32 x 32 13.9, 64 x 64 tiles 13.0); between those 32 x 64 is no faster than the better of its neighbours by
-// more than 6 %.  Activations that are quantised: there a workgroup takes more channels (16 x 64: 333 x 1024 -> 768 4.5 us, 16 x 32 5.2).
+// more than 6 %.  Activations that are quantised: there a workgroup takes more channels (16 x 64:
+// 333 x 1024 -> 768 4.6 us, 16 x 32 5.4, 16 x 128 5.2; 16 x 128 where these are more than the CUs: 512 x 1024 -> 1024 5.5, 16 x 64 6.1, 32-bit 6.4 and 8.4).
 struct Cost {
     int mt, nt;
     float begin, fp32, fixed[3], round[3], each[3];   // codes; 16-bit, 32-bit activations
@@ -336,6 +338,7 @@ constexpr float kNot = 1e30f;
 constexpr Cost costs[] = {{1, 1, 2.0f, 1.03f, {0.09f, 0.15f, 0.3f}, {0.57f, 1.6f, 1.9f}, {0.042f, 0.135f, 0.17f}},
                           {1, 2, 2.1f, 1.08f, {0.15f, 0.15f, 0.3f}, {0.62f, 1.5f, 1.85f}, {0.06f, 0.165f, 0.22f}},
                           {1, 4, 2.3f, 1.0f, {kNot, 0.25f, 0.2f}, {kNot, 1.9f, 2.6f}, {kNot, 0.2f, 0.37f}},
+                          {1, 8, 2.6f, 1.0f, {kNot, 1.1f, 1.1f}, {kNot, 1.7f, 2.4f}, {kNot, 0.21f, 0.33f}},
                           {2, 2, 2.1f, 1.05f, {0.35f, kNot, kNot}, {0.88f, kNot, kNot}, {0.085f, kNot, kNot}},
                           {4, 4, 2.2f, 1.3f, {1.6f, kNot, kNot}, {1.2f, kNot, kNot}, {0.205f, kNot, kNot}}};
 }  // namespace
@@ -347,13 +350,13 @@ Fp8Cut fp8_split_cut(int64_t m, int64_t n, int64_t steps, const hq_dtype *in, hq
     for (const Cost &c : costs) {
         if ((m + 16 * c.mt - 1) / (16 * c.mt) > 65535) continue;   // (the grid's limit in y)
         // Fewer workgroups than CUs: each has a CU of its own.  Those that quantise keep a CU's vector units busy, so that a second one on it waits (333 x
-        // 1024 -> 768, 252 of them, 4.5 us, 512 x 1024 -> 1024, 512, 5.9); those on codes wait for loads.  64 x 64 fill a CU's LDS: no more than one for each
-        // CU (2048 x 3840 -> 960, 480 of them, 24 us, 64 x 128 tiles 16).
+        // 1024 -> 768, 252 of them, 4.5 us, 512 x 1024 -> 1024, 512, 6.1); those on codes wait for loads.  64 x 64 and 16 x 128 fill a CU's LDS: no
+        // more than one for each CU (2048 x 3840 -> 960, 480 of 64 x 64, 24 us, 64 x 128 tiles 16; 1024 x 1024 -> 1024, 512 of 16 x 128, 9.9, two launches 7.7).
         const float groups = static_cast<float>(c.groups(m, n)) / cu;
         float share = kind ? ceilf(groups) : std::max(groups, 1.0f);
         // (32 x 32 in eight waves: LDS for two on a CU, and a last round that is partly filled takes as long; 1429 x 2543 -> 393, 585 of them, 12.5 us)
         if (c.mt == 2 && groups > 2.0f && 3 * std::min<int64_t>(NW, steps) * wave_bytes(2, 2) > kLdsPerCu) share = 2.0f * ceilf(groups / 2.0f);
-        if (c.mt == 4 && groups > 1.0f) continue;
+        if (groups > 1.0f && 2 * NW * wave_bytes(c.mt, c.nt) > kLdsPerCu) continue;
         const float us = c.begin + std::max(c.rounds(steps, kind), share * c.workgroup(steps, kind, out));
         if (us < best.us) best = {c.mt, c.nt, us};
     }

@@ -224,7 +224,8 @@ def test_every_kernel_of_the_product(m, k, n, dtype, kernel):
     (1, 100, 40, "f16", "one launch (16 x 16)"), (1, 1000, 4100, "bf16", "one launch (16 x 32)"), (1025, 1000, 130, "f16", "one launch (16 x 64)"),
     (1, 100, 40, "f32", "one launch (16 x 16)"), (1, 500, 4100, "f32", "one launch (16 x 32)"), (4100, 100, 130, "f32", "one launch (16 x 64)"),
     (130, 4100, 1030, "f16", "split (16 x 32)"), (2049, 500, 4100, "bf16", "tile (64 x 128)"),
-    (2049, 900, 4100, "bf16", "tile (256 x 256)")])
+    (2049, 900, 4100, "bf16", "tile (256 x 256)"), (333, 1001, 777, "f16", "one launch (16 x 128)"),
+    (333, 1001, 777, "f32", "one launch (16 x 128)")])
 def test_every_kernel_of_the_layer(m, k, n, dtype, kernel):
     assert hq.hq_fp8_linear_kernel_name(m, n, k, DTYPES[dtype], DTYPES[dtype]) == kernel
     x, xf = values((m, k), dtype, 3 * m + k)
