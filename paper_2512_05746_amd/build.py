@@ -22,7 +22,7 @@ SOURCES = ["hq_hadamard_quant.hip", "hq_int_gemm.hip", "hq_int_gemm_128x128.hip"
            "hq_single_weights.hip", "hq_width_quant.hip", "hq_fp8_quant.hip", "hq_fp8_linear.hip", "hq_fp8_split.hip", "hq_qk_norm_rope.hip"]
 HEADERS = ["hq_common.h", "hq_int_gemm_kernel.h", "hq_hadamard_mfma.h", "hq_conv3x3_res_kernel.h",
            "hq_resident_kernel.h", "hq_fp6.h", "hq_buffer.h", "hq_floats.h", "hq_fp8.h",
-           "hq_fp8_codes.h", "hq_fp8_product.h"]
+           "hq_fp8_codes.h", "hq_fp8_product.h", "hq_qk_cut.h"]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",

@@ -26,6 +26,7 @@
 #include "hq_common.h"
 #include "hq_floats.h"
 #include "hq_fp8.h"
+#include "hq_qk_cut.h"
 
 namespace {
 
@@ -96,19 +97,6 @@ __device__ __forceinline__ void load_weights(const QkArgs &a, const void *w, int
     }
 }
 
-// The channels of a lane that owns C pairs from pair p on: C from `first`, C from `second`.  Interleaved: 2 C neighbours, and pair i is
-// their (2i, 2i + 1).  Channels that are not rotated are dealt in the same way.
-struct Place {
-    int first, second;
-    bool rotated;
-};
-template <int C>
-__device__ __forceinline__ Place place_of(const QkArgs &a, int p) {
-    const int r = a.rotary >> 1;
-    if (a.interleaved) return {2 * p, 2 * p + C, p < r};
-    return p < r ? Place{p, p + r, true} : Place{r + p, r + p + (a.d >> 1) - r, false};
-}
-
 // (u, v) <- pairs turned by the angles; with -sin the other way round
 template <int C>
 __device__ __forceinline__ void rotate(bool interleaved, const float *c, const float *s, float sign, float *u, float *v) {
@@ -139,9 +127,11 @@ __global__ __launch_bounds__(256) void heads_kernel(QkArgs a) {
     const bool keys = blockIdx.x >= a.part[0].blocks;
     const Heads &h = a.part[keys];
     const uint32_t block = keys ? blockIdx.x - a.part[0].blocks : blockIdx.x;
-    const int in = threadIdx.x % G, slot = threadIdx.x / G, p = in * C;
-    const bool live = p < a.d >> 1;
-    const Place at = place_of<C>(a, live ? p : 0);
+    const int in = threadIdx.x % G, slot = threadIdx.x / G;
+    const hq::QkLane lane = hq::qk_lane_of(a.d, a.rotary, a.interleaved, C, in);
+    const bool live = lane.live;
+    const int p = lane.p;
+    const hq::QkPlace at = lane.at;
     float w1[C], w2[C];
     load_weights<T, C>(a, h.w, at.first, w1);
     load_weights<T, C>(a, h.w, at.second, w2);
@@ -228,9 +218,10 @@ __global__ __launch_bounds__(256) void heads_kernel(QkArgs a) {
             float sum = 0.0f;
             for (int i = 0; i < SLOTS; ++i) sum += part[i * 2 * C * G + e];
             const bool other = e >= C * G;
-            const int lane = (other ? e - C * G : e) / C, k = e % C;
-            if (lane * C < a.d >> 1) {
-                const Place q = place_of<C>(a, lane * C);
+            const hq::QkLane l = hq::qk_lane_of(a.d, a.rotary, a.interleaved, C, (other ? e - C * G : e) / C);
+            const hq::QkPlace q = l.at;
+            const int k = e % C;
+            if (l.live) {
                 a.sums[static_cast<int64_t>(blockIdx.x) * a.d + (other ? q.second : q.first) + k] = sum;
             }
         }
@@ -263,7 +254,7 @@ __global__ __launch_bounds__(256) void wave_kernel(QkArgs a) {
             u[i] = v[i] = 0.0f;
             const int p = lane + 64 * i;
             if (p < pairs) {
-                const Place at = place_of<1>(a, p);
+                const hq::QkPlace at = hq::qk_place_of(a.d, a.rotary, a.interleaved, 1, p);
                 u[i] = static_cast<float>(x[at.first]);
                 v[i] = static_cast<float>(x[at.second]);
             }
@@ -279,7 +270,7 @@ __global__ __launch_bounds__(256) void wave_kernel(QkArgs a) {
             v[i] *= rstd;
             const int p = lane + 64 * i;
             if (BACK && p < pairs) {
-                const Place at = place_of<1>(a, p);
+                const hq::QkPlace at = hq::qk_place_of(a.d, a.rotary, a.interleaved, 1, p);
                 float gx = static_cast<float>(dy[at.first]), gy = static_cast<float>(dy[at.second]), w1, w2;
                 if (at.rotated) rotate<1>(false, t.cos + p, t.sin + p, -1.0f, &gx, &gy);
                 load_weights<T, 1>(a, h.w, at.first, &w1);
@@ -298,7 +289,7 @@ __global__ __launch_bounds__(256) void wave_kernel(QkArgs a) {
         for (int i = 0; i < kMostPairs; ++i) {
             const int p = lane + 64 * i;
             if (p >= pairs) continue;
-            const Place at = place_of<1>(a, p);
+            const hq::QkPlace at = hq::qk_place_of(a.d, a.rotary, a.interleaved, 1, p);
             float y1, y2;
             if constexpr (BACK) {
                 y1 = rstd * (gu[i] - u[i] * dot);
@@ -321,7 +312,7 @@ __global__ __launch_bounds__(256) void wave_kernel(QkArgs a) {
         for (int i = 0; i < kMostPairs; ++i) {
             const int p = lane + 64 * i;
             if (p < pairs) {
-                const Place at = place_of<1>(a, p);
+                const hq::QkPlace at = hq::qk_place_of(a.d, a.rotary, a.interleaved, 1, p);
                 part[wave][at.first] = dw1[i];
                 part[wave][at.second] = dw2[i];
             }
@@ -372,29 +363,6 @@ __global__ __launch_bounds__(1024) void weight_sums_kernel(QkArgs a) {
     }
 }
 
-// Pairs to a lane and lanes to a head, a power of two (g = 0: a wave for a head).  As many pairs as divide both parts of the head, for a lane's channels have to
-// be neighbours: 20000 tokens of 32 heads of 72 in bf16 with 36 of them turned, two pairs, 87 us (137 with gradients), with 18, one pair, 124 (207),
-// where a wave for each head takes 368 and 364 (702, 691).  Eight pairs are two loads of 16 bytes for floats of 16 bits.  For
-// 32 bits four are, and forwards that is faster: 36918 tokens of 36 heads of 96 258 -> 216 us, 30000 of 128 219 -> 217; backwards where eight
-// would leave lanes without a pair (heads of 96 358 -> 315 us, of 80 208 -> 198), else eight are (heads of 128 332 us, with four 339).
-// (Lanes that are no power of two, 60 of 64 busy instead of 40 .. 48: 3 to 6 % less for many tokens of 80 or 96 channels, up to 10 % more
-// for a thousand, since their sums take five exchanges through LDS.)
-struct Cut {
-    int c, g;
-};
-Cut cut_of(int d, int rotary, hq_dtype dt, bool back) {
-    const bool full = d % 16 == 0 && ((d >> 4) & ((d >> 4) - 1)) == 0;
-    for (const int c : {8, 4, 2, 1}) {
-        if ((rotary >> 1) % c || (d >> 1) % c) continue;
-        const int lanes = (d >> 1) / c;
-        if (lanes > 64 || (c == 8 && dt == HQ_F32 && d <= 256 && !(back && full))) continue;
-        int g = 2;
-        while (g < lanes) g *= 2;
-        return {c, g};
-    }
-    return {0, 0};
-}
-
 // Forwards 24 workgroups a CU (65536 tokens of 40 heads of 128 in 16 bits: 252 us, 290 with a workgroup for every 32 heads, 259 with 8 a CU);
 // backwards, where a workgroup keeps sums, 4 (2 to 8 within 1 %).
 uint32_t blocks_for(uint32_t items, int slots, bool back) {
@@ -403,7 +371,7 @@ uint32_t blocks_for(uint32_t items, int slots, bool back) {
 }
 
 template <int DT, bool BACK>
-void launch(const QkArgs &a, Cut cut, hipStream_t st) {
+void launch(const QkArgs &a, hq::QkCut cut, hipStream_t st) {
     const uint32_t blocks = a.part[0].blocks + a.part[1].blocks;
     if (blocks) {
         const auto go = [&](auto c, auto g) {
@@ -430,7 +398,7 @@ void launch(const QkArgs &a, Cut cut, hipStream_t st) {
 }
 
 template <bool BACK>
-hq_status run(const QkArgs &a, hq_dtype dt, Cut cut, hipStream_t st) {
+hq_status run(const QkArgs &a, hq_dtype dt, hq::QkCut cut, hipStream_t st) {
     const hq::LaunchCheck check;
     switch (dt) {
         case HQ_F16: launch<HQ_F16, BACK>(a, cut, st); break;
@@ -473,7 +441,7 @@ extern "C" hq_status hq_qk_norm_rope(const void *q, const void *k, hq_dtype dtyp
     for (const void *p : {q_weight, k_weight})
         if (!hq::aligned_to(p, hq::size_of(w_dtype))) return HQ_ERR_ALIGN;
     if (!hq::aligned_to(cos, 4) || !hq::aligned_to(sin, 4) || !hq::aligned_to(pos, pos_size == 8 ? 8 : 4)) return HQ_ERR_ALIGN;
-    const Cut cut = cut_of(d, rotary, dtype, false);
+    const hq::QkCut cut = hq::qk_cut_of(d, rotary, dtype, false);
     const int slots = cut.g ? 256 / cut.g : 4;
     QkArgs a{};
     a.part[0] = Heads{q, nullptr, q_weight, q_out, nullptr, strides[0], strides[1], 0, 0, strides[4], strides[5]};
@@ -487,7 +455,7 @@ extern "C" hq_status hq_qk_norm_rope(const void *q, const void *k, hq_dtype dtyp
 
 extern "C" int64_t hq_qk_norm_rope_backward_workspace(hq_dtype dtype, int64_t t, int heads, int kv_heads, int d, int rotary) {
     if (!hq::is_float(dtype) || check_sizes(t, heads, kv_heads, d, rotary, 1, &t, 4, 0.0f) != HQ_OK) return 0;
-    const Cut cut = cut_of(d, rotary, dtype, true);
+    const hq::QkCut cut = hq::qk_cut_of(d, rotary, dtype, true);
     const int slots = cut.g ? 256 / cut.g : 4;
     const int64_t blocks = int64_t{blocks_for(static_cast<uint32_t>(t * heads), slots, true)} +
                            blocks_for(static_cast<uint32_t>(t * kv_heads), slots, true);
@@ -511,7 +479,7 @@ extern "C" hq_status hq_qk_norm_rope_backward(const void *dq, const void *dk, co
     if (!hq::aligned_to(cos, 4) || !hq::aligned_to(sin, 4) || !hq::aligned_to(pos, pos_size == 8 ? 8 : 4) ||
         !hq::aligned_to(workspace, 4) || !hq::aligned_to(q_weight_grad, 4) || !hq::aligned_to(k_weight_grad, 4))
         return HQ_ERR_ALIGN;
-    const Cut cut = cut_of(d, rotary, dtype, true);
+    const hq::QkCut cut = hq::qk_cut_of(d, rotary, dtype, true);
     const int slots = cut.g ? 256 / cut.g : 4;
     QkArgs a{};
     a.part[0] = Heads{q, dq, q_weight, q_grad, q_weight_grad, strides[0], strides[1], strides[4], strides[5], strides[8], strides[9]};
