@@ -314,7 +314,8 @@ def hq_qk_norm_rope(q: torch.Tensor, k: torch.Tensor, q_weight: Optional[torch.T
                     ) -> Tuple[torch.Tensor, torch.Tensor]:
     """q [t, heads, d], k [t, kv_heads, d] fp16/bf16/fp32 with contiguous channels (views of a projection's result, say), weights
     [d], cos and sin fp32 [positions, rotary / 2], positions int32/int64 [t] (None: 0 .. t - 1; negative: padding) ->
-    both normalised head by head and rotated, contiguous or in `out`, which may be (q, k)."""
+    both normalised head by head and rotated, contiguous or in `out`, which may be (q, k); otherwise its two tensors share memory neither
+    with each other nor with an input."""
     return _native().qk_norm_rope(q, k, q_weight, k_weight, cos, sin, positions, eps, interleaved, out)
 
 
@@ -324,5 +325,6 @@ def hq_qk_norm_rope_backward(dq: torch.Tensor, dk: torch.Tensor, q: torch.Tensor
                              interleaved: bool = False, out: Optional[Tuple[torch.Tensor, torch.Tensor]] = None
                              ) -> Tuple[torch.Tensor, torch.Tensor, Optional[torch.Tensor], Optional[torch.Tensor]]:
     """Gradients of hq_qk_norm_rope: dq, dk of its results, its inputs -> (gradients of q and k, contiguous or in `out`; of the
-    weights, fp32 [d], None for a weight that is None)."""
+    weights, fp32 [d], None for a weight that is None).  out[0] may be dq or q, out[1] dk or k; otherwise they share memory with nothing
+    that is passed."""
     return _native().qk_norm_rope_backward(dq, dk, q, k, q_weight, k_weight, cos, sin, positions, eps, interleaved, out)

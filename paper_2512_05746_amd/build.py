@@ -13,6 +13,7 @@ CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libhq.so")
 MARSHAL = os.path.join(PKG, "_marshal.so")
 MARSHAL_SOURCE = os.path.join(CSRC, "marshal.cpp")
+MARSHAL_HEADERS = [os.path.join(CSRC, "hq_overlap.h")]
 SOURCES = ["hq_hadamard_quant.hip", "hq_int_gemm.hip", "hq_int_gemm_128x128.hip",
            "hq_int_gemm_64x128.hip", "hq_int_gemm_64x64.hip", "hq_conv3x3_wave.hip", "hq_conv3x3_fused.hip",
            "hq_resident.hip", "hq_resident_pertap.hip", "hq_resident_wholetaps.hip",
@@ -51,7 +52,7 @@ def _marshal_matches() -> bool:
 
 def is_stale() -> bool:
     abi = os.path.join(ROOT, "include", "hq.h")
-    deps = {LIB: sources() + [os.path.join(CSRC, h) for h in HEADERS] + [abi], MARSHAL: [MARSHAL_SOURCE, abi]}
+    deps = {LIB: sources() + [os.path.join(CSRC, h) for h in HEADERS] + [abi], MARSHAL: [MARSHAL_SOURCE, abi] + MARSHAL_HEADERS}
     return any(not os.path.exists(out) or any(os.path.getmtime(d) > os.path.getmtime(out) for d in ds)
                for out, ds in deps.items()) or not _marshal_matches()
 

@@ -20,6 +20,7 @@
 #include <string>
 
 #include "hq.h"
+#include "hq_overlap.h"
 
 // (build.py looks for this text in the file)
 extern "C" __attribute__((used, visibility("default"))) const char hq_marshal_built_for[] = HQ_BUILT_FOR;
@@ -713,6 +714,16 @@ void expect_distinct(const at::Tensor &t, const char *name) {
     if (!heads_inside && !tokens_inside) refuse(std::string(name) + " must not overlap itself");
 }
 
+// memory as the checks of results see it: a tensor [t, heads, d], and what lies in one piece
+hq::Rows2 memory_of(const at::Tensor &t) {
+    const int64_t size = static_cast<int64_t>(t.element_size());
+    return {reinterpret_cast<int64_t>(t.const_data_ptr()), {t.size(0), t.size(1)}, {t.stride(0) * size, t.stride(1) * size}, t.size(2) * size};
+}
+hq::Rows2 memory_of(const void *p, int64_t bytes) { return {reinterpret_cast<int64_t>(p), {1, 1}, {0, 0}, p ? bytes : 0}; }
+void expect_apart(const hq::Rows2 &a, const hq::Rows2 &b, const char *name, const char *other) {
+    if (hq::rows_overlap(a, b)) refuse(std::string(name) + " must not overlap " + other);
+}
+
 struct Qk {
     const at::Tensor &q, &k;
     hq_dtype type, weight_type;
@@ -761,10 +772,11 @@ Qk qk_of(Args &a) {
             narrow(cos.size(1) * 2), pos, pos_size, static_cast<float>(eps), interleaved ? 1 : 0};
 }
 
-// the results: new, or the caller's
+// The results: new, or the caller's.  Workgroups read their inputs while others write: a result may lie on the input that the same workgroup
+// reads (q, or dq where there is one, for that of q), and shares memory with nothing else.
 struct QkOut {
     at::Tensor q, k;
-    QkOut(PyObject *out, const Qk &in) {
+    QkOut(PyObject *out, const Qk &in, const at::Tensor *dq = nullptr, const at::Tensor *dk = nullptr) {
         if (out == Py_None) {
             q = empty(in.q.sizes(), in.q.scalar_type(), in.q);
             k = empty(in.k.sizes(), in.k.scalar_type(), in.k);
@@ -775,6 +787,30 @@ struct QkOut {
         k = heads_of(pair.b, "out[1]", &in.k);
         expect_distinct(q, "out[0]");
         expect_distinct(k, "out[1]");
+        const hq::Rows2 to_q = memory_of(q), to_k = memory_of(k);
+        expect_apart(to_q, to_k, "out[0]", "out[1]");
+        expect_inputs(to_q, "out[0]", in, in.q, dq, "q, unless it is q", "dq, unless it is dq", in.k, dk, "k", "dk");
+        expect_inputs(to_k, "out[1]", in, in.k, dk, "k, unless it is k", "dk, unless it is dk", in.q, dq, "q", "dq");
+    }
+
+private:
+    static void expect_inputs(const hq::Rows2 &to, const char *name, const Qk &in, const at::Tensor &own, const at::Tensor *own_grad,
+                              const char *own_name, const char *own_grad_name, const at::Tensor &other, const at::Tensor *other_grad,
+                              const char *other_name, const char *other_grad_name) {
+        const auto own_or_apart = [&](const at::Tensor &t, const char *text) {
+            const hq::Rows2 m = memory_of(t);
+            if (!hq::same_rows(to, m)) expect_apart(to, m, name, text);
+        };
+        own_or_apart(own, own_name);
+        if (own_grad) own_or_apart(*own_grad, own_grad_name);
+        expect_apart(to, memory_of(other), name, other_name);
+        if (other_grad) expect_apart(to, memory_of(*other_grad), name, other_grad_name);
+        const int64_t weight = in.q.size(2) * (in.weight_type == HQ_F32 ? 4 : 2), table = in.positions * in.rotary * 2;
+        expect_apart(to, memory_of(in.q_weight, weight), name, "q_weight");
+        expect_apart(to, memory_of(in.k_weight, weight), name, "k_weight");
+        expect_apart(to, memory_of(in.cos, table), name, "cos");
+        expect_apart(to, memory_of(in.sin, table), name, "sin");
+        expect_apart(to, memory_of(in.pos, in.q.size(0) * in.pos_size), name, "positions");
     }
 };
 
@@ -794,7 +830,7 @@ PyObject *qk_norm_rope_backward(Args a) {
     PyObject *dq_o = a.next(), *dk_o = a.next();
     const Qk in = qk_of(a);
     const at::Tensor &dq = heads_of(dq_o, "dq", &in.q), &dk = heads_of(dk_o, "dk", &in.k);
-    const QkOut out(a.next(), in);
+    const QkOut out(a.next(), in, &dq, &dk);
     at::Tensor qw, kw;
     if (in.q_weight) qw = empty({in.d()}, at::kFloat, in.q);
     if (in.k_weight) kw = empty({in.d()}, at::kFloat, in.q);

@@ -303,3 +303,56 @@ def test_refusals():
         assert e.value.code == code
     with pytest.raises(ValueError):
         hq.hq_qk_norm_rope_backward(c.dq[:, :3], c.dk, c.q, c.k, c.wq, c.wk, *c.tables())
+
+
+def test_results_that_share_memory():
+    """Results that lie on each other or on another input than their own are refused; views of one buffer that lie between each other are not."""
+    t, h, d = 50, 4, 64
+    c = Case(t, h, h, d, d, "f16", pos="random")
+    free = lambda: torch.empty((t, h, d), dtype=torch.float16, device="cuda")
+    flat = torch.zeros(t * h * d + 32, dtype=torch.float16, device="cuda")
+    table_f16 = c.cos_d.view(torch.float16).flatten()
+    one = c.cos_d.shape[0] * d // (h * d)   # tokens whose results would fit the table
+    bad = [(c.q, c.q), (c.k, c.q), (c.k, free()), (free(), c.q), (flat[:t * h * d].view(t, h, d), flat[32:].view(t, h, d)), (c.k, c.k),
+           (flat[:t * h * d].view(t, h, d), flat[:t * h * d].view(h, t, d).transpose(0, 1))]
+    keep = c.q.clone(), c.k.clone(), flat.clone()
+    for i, out in enumerate(bad):
+        with pytest.raises(ValueError, match="must not overlap"):
+            c.forward(out=out)
+            pytest.fail("case %d was not refused" % i)
+    for i, out in enumerate(bad + [(c.dk, c.dq), (c.dk, free()), (free(), c.dq), (c.dq, c.q)]):
+        with pytest.raises(ValueError, match="must not overlap"):
+            c.backward(out=out)
+            pytest.fail("case %d was not refused" % i)
+    # q moved on by a head, and onto the tables and the weights
+    wide = torch.zeros((t, (h + 1) * d), dtype=torch.float16, device="cuda")
+    for args, out in (((wide[:, :h * d].view(t, h, d), c.k), (wide[:, d:].view(t, h, d), free())),
+                      ((c.q[:one], c.k[:one]), (table_f16[:one * h * d].view(one, h, d), free()[:one])),
+                      ((c.q[:1, :1], c.k[:1, :1]), (free()[:1, :1], c.wk.view(1, 1, d)))):
+        n = args[0].shape[0]
+        with pytest.raises(ValueError, match="must not overlap"):
+            hq.hq_qk_norm_rope(*args, c.wq, c.wk, c.cos_d, c.sin_d, c.pos_d[:n], out=out)
+    assert all(torch.equal(a, b) for a, b in zip((c.q, c.k, flat), keep))
+
+    # accepted: in place in one projection's result, whose heads or parts follow one another; results between other results' rows
+    want, grads = c.forward(), c.backward()
+    for layout in ((t, 3, h, d), (t, h, 3, d)):
+        part = lambda b, i: b.select(layout.index(3), i)
+        qkv, dqkv = (torch.zeros(layout, dtype=torch.float16, device="cuda") for _ in range(2))
+        for b, x, y in ((qkv, c.q, c.k), (dqkv, c.dq, c.dk)):
+            part(b, 0).copy_(x)
+            part(b, 1).copy_(y)
+        args = (part(qkv, 0), part(qkv, 1), c.wq, c.wk, *c.tables())
+        got = hq.hq_qk_norm_rope_backward(part(dqkv, 0), part(dqkv, 1), *args, out=(part(dqkv, 0), part(dqkv, 1)))
+        assert torch.equal(part(dqkv, 0), grads[0]) and torch.equal(part(dqkv, 1), grads[1]) and torch.equal(got[2], grads[2])
+        assert not part(dqkv, 2).any()
+        hq.hq_qk_norm_rope_backward(c.dq, c.dk, *args, out=(part(dqkv, 2), part(dqkv, 1)))
+        assert torch.equal(part(dqkv, 2), grads[0])
+        hq.hq_qk_norm_rope(*args, out=args[:2])
+        assert torch.equal(part(qkv, 0), want[0]) and torch.equal(part(qkv, 1), want[1]) and not part(qkv, 2).any()
+    both = torch.empty((2 * h, t, d), dtype=torch.float16, device="cuda")
+    out = both[0::2].transpose(0, 1), both[1::2].transpose(0, 1)
+    c.forward(out=out)
+    assert torch.equal(out[0], want[0]) and torch.equal(out[1], want[1])
+    c.backward(out=(c.q, c.dk))
+    assert torch.equal(c.q, grads[0]) and torch.equal(c.dk, grads[1])
