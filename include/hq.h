@@ -413,7 +413,7 @@ hq_status hq_fp8_quantize_blocks(const void *w, hq_dtype w_dtype, int64_t n, int
 /*
  *   y[i, j] = sum_b x_scale[b, i] w_scale[j / 128, b] (sum over c in group b of xq[i, c] wq[j, c]) + bias[j]
  *
- * fp32 sums, rounded once to y_dtype.  bias [n] of y_dtype or NULL; y [m, n], dense.
+ * fp32 sums, rounded once to y_dtype.  bias [n] of y_dtype or NULL; y [m, n], dense, apart from all inputs (of the whole layer too).
  * w_scale_turned: w_scale is [ceil(k / 128), ceil(n / 128)] (codes of a transposed matrix with the scales of the matrix).
  */
 hq_status hq_fp8_linear(const uint8_t *xq, const float *x_scale, const uint8_t *wq, const float *w_scale,

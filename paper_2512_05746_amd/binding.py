@@ -275,13 +275,14 @@ def hq_fp8_linear(xq: torch.Tensor, x_scale: torch.Tensor, wq: torch.Tensor, w_s
                   bias: Optional[torch.Tensor] = None, y_dtype: torch.dtype = torch.float16,
                   out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """xq [..., kp], wq [n, kp] float8_e4m3fn codes as the quantisers write them, with their scales -> y [..., n].  w_scale may be
-    the transposed view of the scales of a matrix whose transposed codes wq holds."""
+    the transposed view of the scales of a matrix whose transposed codes wq holds.  out shares no memory with the inputs."""
     return _native().fp8_linear(xq, x_scale, wq, w_scale, bias, y_dtype, out)
 
 
 def hq_act_quant_fp8_linear(x: torch.Tensor, wq: torch.Tensor, w_scale: torch.Tensor, bias: Optional[torch.Tensor] = None,
                             y_dtype: torch.dtype = torch.float16, out: Optional[torch.Tensor] = None) -> torch.Tensor:
-    """The whole layer: x [..., k] fp16/bf16/fp32 -> y [..., n], as hq_fp8_quantize_rows and hq_fp8_linear give it."""
+    """The whole layer: x [..., k] fp16/bf16/fp32 -> y [..., n], as hq_fp8_quantize_rows and hq_fp8_linear give it.  out shares no
+    memory with the inputs."""
     return _native().act_quant_fp8_linear(x, wq, w_scale, bias, y_dtype, out)
 
 

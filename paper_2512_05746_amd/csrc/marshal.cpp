@@ -600,6 +600,31 @@ const float *block_scales(Args &a, const char *name, int64_t rows, int64_t colum
     return static_cast<const float *>(t.const_data_ptr());
 }
 
+// memory as the checks of results see it: a matrix of rows, a tensor [t, heads, d], and what lies in one piece
+hq::Rows2 memory_of(const Rows &r) {
+    const int64_t size = static_cast<int64_t>(r.t.element_size());
+    return {reinterpret_cast<int64_t>(r.t.const_data_ptr()), {r.m, 1}, {r.stride * size, 0}, r.k * size};
+}
+hq::Rows2 memory_of(const at::Tensor &t) {
+    const int64_t size = static_cast<int64_t>(t.element_size());
+    return {reinterpret_cast<int64_t>(t.const_data_ptr()), {t.size(0), t.size(1)}, {t.stride(0) * size, t.stride(1) * size}, t.size(2) * size};
+}
+hq::Rows2 memory_of(const void *p, int64_t bytes) { return {reinterpret_cast<int64_t>(p), {1, 1}, {0, 0}, p ? bytes : 0}; }
+void expect_apart(const hq::Rows2 &a, const hq::Rows2 &b, const char *name, const char *other) {
+    if (hq::rows_overlap(a, b)) refuse(std::string(name) + " must not overlap " + other);
+}
+hq::Rows2 piece_of(const at::Tensor &t) { return memory_of(t.const_data_ptr(), static_cast<int64_t>(t.nbytes())); }
+// A caller's buffer for y: the workgroups of one launch write it while others still read.
+void expect_result_apart(PyObject *out, const at::Tensor &y, const hq::Rows2 &x, const char *x_name, const at::Tensor &wq, const float *w_scale,
+                         int64_t scales, const void *bias, int64_t n) {
+    if (out == Py_None) return;
+    const hq::Rows2 to = piece_of(y);
+    expect_apart(to, x, "out", x_name);
+    expect_apart(to, piece_of(wq), "out", "wq");
+    expect_apart(to, memory_of(w_scale, scales * 4), "out", "w_scale");
+    expect_apart(to, memory_of(bias, n * static_cast<int64_t>(y.element_size())), "out", "bias");
+}
+
 PyObject *fp8_quantize_rows(Args a) {
     const Rows x = rows_of(a, "x");
     const at::Tensor xq = empty(with_last(x.t, pitch_of(x.k)), kE4m3, x.t);
@@ -642,7 +667,10 @@ PyObject *fp8_linear(Args a) {
     const at::ScalarType ydt = a.dtype();
     const hq_dtype dt = float_type(ydt, "y_dtype");
     const void *b = Args{&bias, 1}.vec(n, ydt, "bias");
-    const at::Tensor y = result(a.next(), with_last(xq, n), ydt, xq);
+    PyObject *out = a.next();
+    const at::Tensor y = result(out, with_last(xq, n), ydt, xq);
+    expect_result_apart(out, y, piece_of(xq), "xq", wq, sw, groups_of(n) * groups_of(kp), b, n);
+    if (out != Py_None) expect_apart(piece_of(y), piece_of(sx), "out", "x_scale");
     check("hq_fp8_linear", call(lib.hq_fp8_linear, u8(xq), f32(sx.const_data_ptr()), u8(wq), sw, turned, b, m, narrow(n), narrow(kp),
                                 y.data_ptr(), dt, stream()));
     return wrap(y);
@@ -661,7 +689,9 @@ PyObject *act_quant_fp8_linear(Args a) {
     const at::ScalarType ydt = a.dtype();
     const hq_dtype dt = float_type(ydt, "y_dtype");
     const void *b = Args{&bias, 1}.vec(n, ydt, "bias");
-    const at::Tensor y = result(a.next(), with_last(x.t, n), ydt, x.t);
+    PyObject *out = a.next();
+    const at::Tensor y = result(out, with_last(x.t, n), ydt, x.t);
+    expect_result_apart(out, y, memory_of(x), "x", wq, sw, groups_of(n) * groups_of(x.k), b, n);
     at::Tensor space;
     const int64_t bytes = lib.hq_act_quant_fp8_linear_workspace(x.type, x.m, narrow(n), narrow(x.k), dt);
     if (bytes) space = empty({bytes}, at::kByte, x.t);
@@ -712,16 +742,6 @@ void expect_distinct(const at::Tensor &t, const char *name) {
     const bool heads_inside = (n1 < 2 || s1 >= d) && (n0 < 2 || s0 >= (n1 - 1) * s1 + d);
     const bool tokens_inside = (n0 < 2 || s0 >= d) && (n1 < 2 || s1 >= (n0 - 1) * s0 + d);
     if (!heads_inside && !tokens_inside) refuse(std::string(name) + " must not overlap itself");
-}
-
-// memory as the checks of results see it: a tensor [t, heads, d], and what lies in one piece
-hq::Rows2 memory_of(const at::Tensor &t) {
-    const int64_t size = static_cast<int64_t>(t.element_size());
-    return {reinterpret_cast<int64_t>(t.const_data_ptr()), {t.size(0), t.size(1)}, {t.stride(0) * size, t.stride(1) * size}, t.size(2) * size};
-}
-hq::Rows2 memory_of(const void *p, int64_t bytes) { return {reinterpret_cast<int64_t>(p), {1, 1}, {0, 0}, p ? bytes : 0}; }
-void expect_apart(const hq::Rows2 &a, const hq::Rows2 &b, const char *name, const char *other) {
-    if (hq::rows_overlap(a, b)) refuse(std::string(name) + " must not overlap " + other);
 }
 
 struct Qk {

@@ -430,3 +430,35 @@ def test_refusals():
     with pytest.raises(hq.HqError) as e:
         hq.hq_fp8_linear(xq, sx, unaligned, sw)
     assert e.value.code == 5
+
+
+def test_results_that_share_memory_with_inputs():
+    """Refused: other workgroups may still read what one writes.  Columns of one matrix next to each other are no shared memory."""
+    x, _ = values((40, 128), "f32", 1)
+    w, _ = values((128, 128), "f32", 2)
+    wq, sw = hq.hq_fp8_quantize_blocks(w)
+    xq, sx = hq.hq_fp8_quantize_rows(x)
+    bias = torch.zeros(128, device="cuda")
+    keep = x.clone()
+    wide = torch.zeros((41, 128), device="cuda")
+    one_wq, one_sw = hq.hq_fp8_quantize_blocks(w[:1])
+    bad = [
+        lambda: hq.hq_act_quant_fp8_linear(x, wq, sw, y_dtype=torch.float32, out=x),
+        lambda: hq.hq_act_quant_fp8_linear(wide[1:], wq, sw, y_dtype=torch.float32, out=wide[:40]),
+        lambda: hq.hq_act_quant_fp8_linear(wide[:, :60], *hq.hq_fp8_quantize_blocks(w[:, :60]), y_dtype=torch.float32, out=wide),
+        lambda: hq.hq_act_quant_fp8_linear(x[:1], wq, sw, bias, y_dtype=torch.float32, out=bias),
+        lambda: hq.hq_act_quant_fp8_linear(x[:1], one_wq, one_sw, y_dtype=torch.float32, out=one_sw),
+        lambda: hq.hq_act_quant_fp8_linear(x[:32], wq, sw, y_dtype=torch.float32, out=wq.view(torch.float32)),
+        lambda: hq.hq_fp8_linear(xq[:8], sx[:, :8].contiguous(), wq, sw, y_dtype=torch.float32, out=xq.view(torch.float32).view(-1)[:1024].view(8, 128)),
+        lambda: hq.hq_fp8_linear(xq, sx, one_wq, one_sw, y_dtype=torch.float32, out=sx),
+    ]
+    for i, call in enumerate(bad):
+        with pytest.raises(ValueError, match="must not overlap"):
+            call()
+            pytest.fail("case %d was not refused" % i)
+    assert torch.equal(x, keep)
+    # rows of x with room for a row of results between them
+    beside = torch.zeros((1, 256), device="cuda")
+    beside[:, :128] = x[:1]
+    y = hq.hq_act_quant_fp8_linear(beside[:, :128], wq, sw, y_dtype=torch.float32, out=beside[:, 128:])
+    assert torch.equal(y, hq.hq_act_quant_fp8_linear(x[:1], wq, sw, y_dtype=torch.float32)) and torch.equal(beside[:, :128], x[:1])
