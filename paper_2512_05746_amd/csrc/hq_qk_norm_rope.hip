@@ -468,9 +468,10 @@ extern "C" hq_status hq_qk_norm_rope_backward(const void *dq, const void *dk, co
                                               int64_t positions, int rotary, int interleaved, const void *pos, int pos_size,
                                               float eps, void *workspace, void *q_grad, void *k_grad, float *q_weight_grad,
                                               float *k_weight_grad, void *stream) {
-    if ((t > 0 && (!dq || !dk || !q || !k || !q_grad || !k_grad || !workspace)) || !strides || (rotary > 0 && (!cos || !sin))) return HQ_ERR_NULL;
+    if ((t > 0 && (!dq || !dk || !q || !k || !q_grad || !k_grad)) || !strides || (rotary > 0 && (!cos || !sin))) return HQ_ERR_NULL;
     if (!hq::is_float(dtype) || (w_dtype != dtype && w_dtype != HQ_F32)) return HQ_ERR_DTYPE;
     if (const hq_status s = check_sizes(t, heads, kv_heads, d, rotary, positions, pos, pos_size, eps)) return s;
+    if (t > 0 && !workspace) return HQ_ERR_NULL;   // (sizes that are refused have a workspace of no bytes)
     const int size = hq::size_of(dtype);
     for (const void *p : {dq, dk, q, k, static_cast<const void *>(q_grad), static_cast<const void *>(k_grad)})
         if (!hq::aligned_to(p, size)) return HQ_ERR_ALIGN;

@@ -115,3 +115,18 @@ def test_binding_rejects_host_tensors():
     for call in (lambda: hq.hq_fp8_quantize_rows(None), lambda: hq.hq_qk_norm_rope(None, q, None, None, one, one)):
         with pytest.raises(TypeError):
             call()
+
+
+def test_gradients_of_heads_that_do_not_fit_name_the_reason(lib):
+    """Their workspace has no bytes, so it may be no memory at all: the sizes are what is wrong."""
+    strides = (ctypes.c_int64 * 12)(*([4096, 64] * 6))
+
+    def back(d=64, rotary=64, t=8, heads=4, space=None, positions=16):
+        return lib.hq_qk_norm_rope_backward(P, P, P, P, F16, t, heads, 2, d, strides, P, P, F16, P, P, positions, rotary, 0, P, 8, 1e-6, space, P, P, P, P,
+                                            None)
+
+    assert back(d=63, rotary=62) == SHAPE and back(rotary=66) == SHAPE and back(rotary=33) == SHAPE and back(positions=0) == SHAPE
+    assert back(d=1026) == UNSUPPORTED and back(t=1 << 29) == UNSUPPORTED
+    for d, rotary, t in ((63, 62, 8), (64, 66, 8), (1026, 64, 8), (64, 64, 1 << 29)):
+        assert lib.hq_qk_norm_rope_backward_workspace(F16, t, 4, 2, d, rotary) == 0
+    assert back() == NULL   # sizes that fit need it

@@ -356,3 +356,15 @@ def test_results_that_share_memory():
     assert torch.equal(out[0], want[0]) and torch.equal(out[1], want[1])
     c.backward(out=(c.q, c.dk))
     assert torch.equal(c.q, grads[0]) and torch.equal(c.dk, grads[1])
+
+
+def test_refusals_of_gradients():
+    c = Case(6, 4, 2, 64, 64, "f16", pos="random")
+    odd = [x[..., :63] for x in (c.dq, c.dk, c.q, c.k)]
+    wide = [torch.zeros((6, h, 1026), dtype=torch.float16, device="cuda") for h in (4, 2, 4, 2)]
+    whole = [c.dq, c.dk, c.q, c.k]
+    for tensors, tables, more, code in ((odd, c.tables(), {}, 2), (wide, c.tables(), {}, 6), (whole, [t.repeat(1, 2) for t in c.tables()[:2]], {}, 2),
+                                        (whole, [t[:5] for t in c.tables()[:2]], {}, 2), (whole, c.tables(), dict(eps=-1.0), 2)):
+        with pytest.raises(hq.HqError) as e:
+            hq.hq_qk_norm_rope_backward(*tensors, None, None, *tables, **more)
+        assert e.value.code == code
