@@ -462,3 +462,46 @@ def test_results_that_share_memory_with_inputs():
     beside[:, :128] = x[:1]
     y = hq.hq_act_quant_fp8_linear(beside[:, :128], wq, sw, y_dtype=torch.float32, out=beside[:, 128:])
     assert torch.equal(y, hq.hq_act_quant_fp8_linear(x[:1], wq, sw, y_dtype=torch.float32)) and torch.equal(beside[:, :128], x[:1])
+
+
+# ---- what sums are held in --------------------------------------------------------------------------------------
+
+def cut_sums(x, w):
+    """Sums of products of codes [m, k] and [n, k] (float64, on the device) with the products of each eight cut towards zero to multiples of 2^(e - 13),
+    e the largest sum of two exponents among those that are not zero, subnormal codes with -6; and the sums of magnitudes."""
+    exponent = lambda v: torch.floor(torch.log2(v.abs().clamp(min=2.0 ** -6)))
+    total, size = (torch.empty((x.shape[0], w.shape[0]), dtype=torch.float64, device="cuda") for _ in range(2))
+    for i in range(x.shape[0]):
+        p = x[i] * w
+        e = torch.where(p == 0, -100.0, exponent(x)[i] + exponent(w)).view(w.shape[0], -1, 8).amax(-1, keepdim=True)
+        unit, p = torch.exp2(e - 13), p.view(w.shape[0], -1, 8)
+        total[i], size[i] = (torch.trunc(p / unit) * unit).sum((-1, -2)), p.abs().sum((-1, -2))
+    return total, size
+
+
+@pytest.mark.parametrize("small", [False, True], ids=["normal", "subnormal"])
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("m,k,n", [(3, 128, 40), (300, 512, 700), (300, 512, 1030), (500, 2048, 2010), (1025, 512, 1030), (2049, 512, 4100),
+                                   (4096, 640, 1728), (2049, 896, 4100)])
+def test_what_results_of_16_bits_are_summed_in(m, k, n, dtype, small):
+    """The cut that the header describes and nothing else: what is left beside it is fp32 sums (the bound above) and one rounding.  Up to 24 rows
+    of the result are looked at; the sizes are those of different kernels."""
+    rng = np.random.default_rng(m + k + n + small)
+    value = lambda r: rng.standard_normal((r, k)) * (20 if not small else 2.0 ** rng.integers(-9, 3, (r, k)))
+    code = lambda v: torch.from_numpy(v.astype(np.float32)).clamp(-448, 448).to(torch.float8_e4m3fn).cuda()
+    x, w = code(value(m)), code(value(n))
+    sx, sw = torch.full((up(k, 128), m), 2.0 ** -7, device="cuda"), torch.full((up(n, 128), up(k, 128)), 2.0 ** -3, device="cuda")
+    y = hq.hq_fp8_linear(x, sx, w, sw, y_dtype=DTYPES[dtype])
+    rows = torch.from_numpy(np.unique(np.r_[0, m - 1, rng.integers(0, m, 22)])).cuda()
+    want, size = cut_sums(x.double()[rows], w.double())
+    close(y[rows], (want * 2.0 ** -10).cpu().numpy(), (size * (2.0 ** -10 * (128 + up(k, 128) + 4) * 2.0 ** -23)).cpu().numpy(), dtype)
+
+
+def test_products_that_cancel():
+    """1 - 1 + 2^-14 among eight neighbours: fp32 results have it, 16-bit ones keep 13 bits; across eights both have it."""
+    x, w = torch.zeros((2, 128)), torch.ones((1, 128))
+    x[:, 0], x[:, 1], x[0, 2], x[1, 8], w[0, 2], w[0, 8] = 1, -1, 2.0 ** -7, 2.0 ** -7, 2.0 ** -7, 2.0 ** -7
+    code = lambda v: v.to(torch.float8_e4m3fn).cuda()
+    sx, sw = torch.ones((1, 2), device="cuda"), torch.ones((1, 1), device="cuda")
+    for dtype, near in ((torch.float32, 2.0 ** -14), (torch.float16, 0.0), (torch.bfloat16, 0.0)):
+        assert hq.hq_fp8_linear(code(x), sx, code(w), sw, y_dtype=dtype).flatten().tolist() == [near, 2.0 ** -14]
