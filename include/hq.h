@@ -427,8 +427,9 @@ hq_status hq_fp8_linear(const uint8_t *xq, const float *x_scale, const uint8_t *
                         int w_scale_turned, const void *bias, int64_t m, int n, int k, void *y, hq_dtype y_dtype,
                         void *stream);
 /*
- * The whole layer, with the results of hq_fp8_quantize_rows and hq_fp8_linear; small ones are one launch.  workspace: device memory of
- * hq_act_quant_fp8_linear_workspace(..) bytes, 16-byte aligned, written and read by the call; NULL where that is 0.
+ * The whole layer: the codes and scales of hq_fp8_quantize_rows, multiplied as by hq_fp8_linear.  Small layers are one launch, whose waves
+ * split k: the groups of 128 may be added in another order than by the two calls, so the last bits of their fp32 sums can differ.
+ * workspace: device memory of hq_act_quant_fp8_linear_workspace(..) bytes, 16-byte aligned, written and read by the call; NULL where that is 0.
  */
 int64_t hq_act_quant_fp8_linear_workspace(hq_dtype x_dtype, int64_t m, int n, int k, hq_dtype y_dtype);
 hq_status hq_act_quant_fp8_linear(const void *x, hq_dtype x_dtype, int64_t row_stride, const uint8_t *wq,

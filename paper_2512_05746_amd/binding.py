@@ -284,8 +284,8 @@ def hq_fp8_linear(xq: torch.Tensor, x_scale: torch.Tensor, wq: torch.Tensor, w_s
 
 def hq_act_quant_fp8_linear(x: torch.Tensor, wq: torch.Tensor, w_scale: torch.Tensor, bias: Optional[torch.Tensor] = None,
                             y_dtype: torch.dtype = torch.float16, out: Optional[torch.Tensor] = None) -> torch.Tensor:
-    """The whole layer: x [..., k] fp16/bf16/fp32 -> y [..., n], as hq_fp8_quantize_rows and hq_fp8_linear give it.  out shares no
-    memory with the inputs."""
+    """The whole layer: x [..., k] fp16/bf16/fp32 -> y [..., n], with the codes of hq_fp8_quantize_rows and the sums of hq_fp8_linear
+    (in the order of another kernel where it is one launch: the last bits may differ).  out shares no memory with the inputs."""
     return _native().act_quant_fp8_linear(x, wq, w_scale, bias, y_dtype, out)
 
 

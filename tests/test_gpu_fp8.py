@@ -505,3 +505,36 @@ def test_products_that_cancel():
     sx, sw = torch.ones((1, 2), device="cuda"), torch.ones((1, 1), device="cuda")
     for dtype, near in ((torch.float32, 2.0 ** -14), (torch.float16, 0.0), (torch.bfloat16, 0.0)):
         assert hq.hq_fp8_linear(code(x), sx, code(w), sw, y_dtype=dtype).flatten().tolist() == [near, 2.0 ** -14]
+
+
+# ---- the layer and the two calls --------------------------------------------------------------------------------
+
+LAYERS = SHAPES + [(1, 4096, 1024), (16, 1000, 4100), (333, 1001, 777), (1025, 1000, 130), (4100, 100, 130), (2049, 900, 4100)]
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("m,k,n", LAYERS)
+def test_layer_and_the_two_calls(m, k, n, dtype):
+    """The same codes and the same terms: both sums are within the bound of sums in any order, so apart by twice that and two roundings; where the
+    sums are exact, on whole numbers that the codes hold (448 in every group makes its scale 1), the bits are the same."""
+    x, xf = values((m, k), dtype, 5 * m + k)
+    w, _ = values((n, k), "f32", n + k, 0.02)
+    b, _ = values((n,), dtype, n)
+    wq, sw = hq.hq_fp8_quantize_blocks(w)
+    layer = lambda *a: hq.hq_act_quant_fp8_linear(*a, y_dtype=DTYPES[dtype])
+    calls = lambda x, *a: hq.hq_fp8_linear(*hq.hq_fp8_quantize_rows(x), *a, y_dtype=DTYPES[dtype])
+    q, s = quantised(xf, 1)
+    xd, wd = q * spread(s, 1, m, k), held(wq)[:, :k] * spread(sw.cpu().numpy(), 128, n, k)
+    one, two = layer(x, wq, sw, b), calls(x, wq, sw, b)
+    # (the cut of 16-bit results is the same in both, but for it the bound of fp32 sums and the bias' addition)
+    size = np.abs(xd) @ np.abs(wd).T + np.abs(b.double().cpu().numpy())
+    a, c = one.double().cpu().numpy(), two.double().cpu().numpy()
+    assert (np.abs(a - c) <= 2 * size * (128 + up(k, 128) + 6) * 2.0 ** -23 + ULP[dtype] * (np.abs(a) + np.abs(c)) + 2 * TINY[dtype]).all()
+    rng = np.random.default_rng(m + k + n)
+    grid = lambda r: (rng.integers(-7, 8, (r, k)) * 64.0 * (rng.random((r, k)) < 0.2)).astype(np.float32)
+    xi, wi = grid(m), grid(n)
+    xi[:, 0::128], wi[:, 0::128] = 448, 448
+    x, (wq, sw) = torch.from_numpy(xi).to(DTYPES[dtype]).cuda(), hq.hq_fp8_quantize_blocks(torch.from_numpy(wi).cuda())
+    sw = sw * 2.0 ** -14   # (fp16 results stay inside its range; a power of two leaves every sum exact)
+    want = torch.from_numpy((xi.astype(np.float64) @ wi.T) * 2.0 ** -14).float().to(DTYPES[dtype])
+    assert torch.equal(layer(x, wq, sw).cpu(), want) and torch.equal(calls(x, wq, sw).cpu(), want)
