@@ -257,6 +257,8 @@ def hq_int_conv2d_i8(xq: torch.Tensor, x_scale: Optional[torch.Tensor], wq: torc
 
 
 # ---- 8-bit floats with block scales ---------------------------------------------------------------
+# The calls from here on record nothing for autograd.  Those that take activations refuse tensors that require a gradient while gradients
+# are recorded; under torch.no_grad(), or in an autograd function, with the _backward calls, they take them.
 
 def hq_fp8_quantize_rows(x: torch.Tensor) -> Tuple[torch.Tensor, torch.Tensor]:
     """x [..., k] fp16/bf16/fp32 -> (xq float8_e4m3fn [..., k up to a multiple of 16], x_scale fp32 [ceil(k / 128), rows]):

@@ -14,6 +14,7 @@
 #include <ATen/ATen.h>
 #include <ATen/EmptyTensor.h>
 #include <ATen/hip/EmptyTensor.h>
+#include <c10/core/GradMode.h>
 #include <c10/hip/HIPStream.h>
 
 #include <initializer_list>
@@ -561,6 +562,16 @@ bool truth(PyObject *o) {
     return v != 0;
 }
 
+// Calls that take activations record nothing for autograd: a tensor that needs a gradient would lose it without a word.
+void expect_no_gradient(const at::Tensor &t, const char *name) {
+    if (t.requires_grad() && c10::GradMode::is_enabled())
+        refuse(std::string(name) + " requires a gradient, which this call does not record: make it under torch.no_grad() (or in an autograd "
+                                   "function), with the _backward call for gradients");
+}
+void expect_no_gradient(PyObject *o, const char *name) {
+    if (THPVariable_Check(o)) expect_no_gradient(THPVariable_Unpack(o), name);
+}
+
 // A matrix of contiguous rows: a contiguous tensor, its leading axes taken together, or a matrix whose rows are apart.
 struct Rows {
     const at::Tensor &t;
@@ -627,6 +638,7 @@ void expect_result_apart(PyObject *out, const at::Tensor &y, const hq::Rows2 &x,
 
 PyObject *fp8_quantize_rows(Args a) {
     const Rows x = rows_of(a, "x");
+    expect_no_gradient(x.t, "x");
     const at::Tensor xq = empty(with_last(x.t, pitch_of(x.k)), kE4m3, x.t);
     const at::Tensor xs = empty({groups_of(x.k), x.m}, at::kFloat, x.t);
     check("hq_fp8_quantize_rows", call(lib.hq_fp8_quantize_rows, x.t.const_data_ptr(), x.type, x.m, narrow(x.k), x.stride,
@@ -664,6 +676,7 @@ PyObject *fp8_linear(Args a) {
     int turned = 0;
     const float *sw = block_scales(a, "w_scale", groups_of(n), groups_of(kp), &turned);
     PyObject *bias = a.next();
+    expect_no_gradient(bias, "bias");
     const at::ScalarType ydt = a.dtype();
     const hq_dtype dt = float_type(ydt, "y_dtype");
     const void *b = Args{&bias, 1}.vec(n, ydt, "bias");
@@ -678,6 +691,7 @@ PyObject *fp8_linear(Args a) {
 
 PyObject *act_quant_fp8_linear(Args a) {
     const Rows x = rows_of(a, "x");
+    expect_no_gradient(x.t, "x");
     const at::Tensor &wq = fp8_codes(a, "wq");
     if (wq.dim() != 2 || wq.size(1) != pitch_of(x.k)) refuse("wq does not match x in k");
     const int64_t n = wq.size(0);
@@ -686,6 +700,7 @@ PyObject *act_quant_fp8_linear(Args a) {
     const float *sw = block_scales(a, "w_scale", groups_of(n), groups_of(x.k), &turned);
     if (turned) refuse("w_scale must be contiguous");
     PyObject *bias = a.next();
+    expect_no_gradient(bias, "bias");
     const at::ScalarType ydt = a.dtype();
     const hq_dtype dt = float_type(ydt, "y_dtype");
     const void *b = Args{&bias, 1}.vec(n, ydt, "bias");
@@ -755,6 +770,7 @@ struct Qk {
     int pos_size;
     float eps;
     int interleaved;
+    PyObject *weights[2];
     int64_t t() const { return q.size(0); }
     int d() const { return narrow(q.size(2)); }
     int heads() const { return narrow(q.size(1)); }
@@ -789,7 +805,7 @@ Qk qk_of(Args &a) {
     if (eps == -1.0 && PyErr_Occurred()) throw PythonError();
     const bool interleaved = truth(a.next());
     return {q, k, type, float_type(wdt, "q_weight"), qw, kw, f32(cos.const_data_ptr()), f32(sin.const_data_ptr()), cos.size(0),
-            narrow(cos.size(1) * 2), pos, pos_size, static_cast<float>(eps), interleaved ? 1 : 0};
+            narrow(cos.size(1) * 2), pos, pos_size, static_cast<float>(eps), interleaved ? 1 : 0, {w[0], w[1]}};
 }
 
 // The results: new, or the caller's.  Workgroups read their inputs while others write: a result may lie on the input that the same workgroup
@@ -836,6 +852,10 @@ private:
 
 PyObject *qk_norm_rope(Args a) {
     const Qk in = qk_of(a);
+    expect_no_gradient(in.q, "q");
+    expect_no_gradient(in.k, "k");
+    expect_no_gradient(in.weights[0], "q_weight");
+    expect_no_gradient(in.weights[1], "k_weight");
     const QkOut out(a.next(), in);
     const int64_t strides[8] = {in.q.stride(0), in.q.stride(1), in.k.stride(0), in.k.stride(1),
                                 out.q.stride(0), out.q.stride(1), out.k.stride(0), out.k.stride(1)};

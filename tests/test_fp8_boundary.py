@@ -130,3 +130,35 @@ def test_gradients_of_heads_that_do_not_fit_name_the_reason(lib):
     for d, rotary, t in ((63, 62, 8), (64, 66, 8), (1026, 64, 8), (64, 64, 1 << 29)):
         assert lib.hq_qk_norm_rope_backward_workspace(F16, t, 4, 2, d, rotary) == 0
     assert back() == NULL   # sizes that fit need it
+
+
+def test_calls_that_record_no_gradient_refuse_tensors_that_need_one():
+    """While gradients are recorded; under no_grad, and for weights that are quantised, the tensors are taken.  (Fake device tensors: the call
+    ends with an error of another kind, since they have no memory.)"""
+    from torch._subclasses.fake_tensor import FakeTensor, FakeTensorMode
+    mode = FakeTensorMode()
+
+    def fake(*shape, dtype=torch.float16, grad=False):
+        t = FakeTensor(mode, torch.empty(shape, dtype=dtype, device="meta"), torch.device("cuda"))
+        return t.requires_grad_() if grad else t
+
+    codes = lambda *shape: fake(*shape, dtype=torch.float8_e4m3fn)
+    f32 = lambda *shape: fake(*shape, dtype=torch.float32)
+    layer = lambda x, b: hq.hq_act_quant_fp8_linear(x, codes(24, 208), f32(1, 2), b)
+    product = lambda b: hq.hq_fp8_linear(codes(8, 208), f32(2, 8), codes(24, 208), f32(1, 2), b)
+    heads = lambda q, k, a, b: hq.hq_qk_norm_rope(q, k, a, b, f32(8, 32), f32(8, 32))
+    x, b, q, k, w = (8, 200), (24,), (8, 4, 64), (8, 2, 64), (64,)
+    for name, call in (
+        ("x", lambda g: hq.hq_fp8_quantize_rows(fake(*x, grad=g))), ("x", lambda g: layer(fake(*x, grad=g), None)),
+        ("bias", lambda g: layer(fake(*x), fake(*b, grad=g))), ("bias", lambda g: product(fake(*b, grad=g))),
+        ("q", lambda g: heads(fake(*q, grad=g), fake(*k), None, None)), ("k", lambda g: heads(fake(*q), fake(*k, grad=g), None, None)),
+        ("q_weight", lambda g: heads(fake(*q), fake(*k), fake(*w, grad=g), fake(*w))),
+        ("k_weight", lambda g: heads(fake(*q), fake(*k), fake(*w), fake(*w, grad=g))),
+    ):
+        with pytest.raises(ValueError, match="^%s requires a gradient" % name):
+            call(True)
+        for grad, record in ((True, False), (False, True)):
+            with torch.set_grad_enabled(record), pytest.raises(RuntimeError):
+                call(grad)
+    with pytest.raises(RuntimeError):
+        hq.hq_fp8_quantize_blocks(fake(24, 200, grad=True))
