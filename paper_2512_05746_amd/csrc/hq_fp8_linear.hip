@@ -506,9 +506,10 @@ hq_status product_pair(const ProductArgs &a, const ProductArgs &b, const hq::Fp8
     return product(b, HQ_F32, st);
 }
 
-// Rows of codes whose tiles are addressed with 31-bit offsets, and tile counts that fit a grid.
+// Rows of codes whose tiles are addressed with 31-bit offsets, and tile counts that fit a grid (n is a size of 32 bits; m is bounded before
+// it is multiplied).
 bool product_fits(int64_t m, int64_t n, int64_t k) {
-    return k <= (int64_t{1} << 31) / 256 - 16 && ((m + 15) / 16) * ((n + 15) / 16) <= 0x7FFFFFFF;
+    return k <= (int64_t{1} << 31) / 256 - 16 && m <= int64_t{0x7FFFFFFF} * 16 && ((m + 15) / 16) * ((n + 15) / 16) <= 0x7FFFFFFF;
 }
 
 int64_t up256(int64_t v) { return (v + 255) & ~int64_t{255}; }

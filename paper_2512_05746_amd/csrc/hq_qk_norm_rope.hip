@@ -413,7 +413,7 @@ hq_status check_sizes(int64_t t, int heads, int kv_heads, int d, int rotary, int
     if ((d & 1) || (rotary & 1) || (!pos && t > positions)) return HQ_ERR_SHAPE;
     if (!(eps >= 0.0f)) return HQ_ERR_SHAPE;
     if (pos && pos_size != 4 && pos_size != 8) return HQ_ERR_DTYPE;
-    if (d > 1024 || t * std::max(heads, kv_heads) > 0x7FFF0000 || t > 0x7FFF0000) return HQ_ERR_UNSUPPORTED;
+    if (d > 1024 || t > 0x7FFF0000 || t * std::max(heads, kv_heads) > 0x7FFF0000) return HQ_ERR_UNSUPPORTED;
     return HQ_OK;
 }
 

@@ -162,3 +162,14 @@ def test_calls_that_record_no_gradient_refuse_tensors_that_need_one():
                 call(grad)
     with pytest.raises(RuntimeError):
         hq.hq_fp8_quantize_blocks(fake(24, 200, grad=True))
+
+
+def test_sizes_whose_products_wrap_are_refused(lib):
+    """Counts of tiles and of heads beyond 64 bits."""
+    for m, n in ((1 << 62, 1024), ((1 << 63) - 1, 16), (1 << 61, 128), ((1 << 63) - 1, 1), (1 << 40, 1)):
+        assert lib.hq_fp8_linear(P, P, P, P, 0, None, m, n, 200, P, BF16, None) == UNSUPPORTED
+        assert lib.hq_fp8_linear_kernel_name(I32, m, n, 200, BF16) == b"none"
+    strides = (ctypes.c_int64 * 12)(*([512, 64] * 6))
+    for t, heads in (((1 << 63) - 1, 4), (1 << 62, 4), (1 << 32, 1)):
+        assert lib.hq_qk_norm_rope(P, P, F16, t, heads, 2, 64, strides, P, P, F16, P, P, 16, 64, 0, P, 8, 1e-6, P, P, None) == UNSUPPORTED
+        assert lib.hq_qk_norm_rope_backward_workspace(F16, t, heads, 2, 64, 64) == 0
