@@ -387,8 +387,8 @@ hq_status hq_int_conv2d_i8(const int8_t *xq, const float *x_scale, const int8_t 
  * floating code loses no precision to a large neighbour.
  *
  * Values x, w, dy, y, dx: HQ_F16, HQ_F32 or HQ_BF16, a row's elements side by side, rows row_stride elements apart
- * (any number from 0 on; 0 repeats a row).  Their pointers need the alignment of an element only.  Codes are dense, 16-byte aligned, a row's length
- * rounded up to a multiple of 16 bytes, the end filled with zeros ("pitch" below).
+ * (any number from 0 on; 0 repeats a row).  Their pointers need the alignment of an element only.  Codes are dense, 16-byte aligned, a
+ * row's length rounded up to a multiple of 16 bytes, the end filled with zeros ("pitch" below).
  *
  *   amax  = max |x| over the scale's values
  *   scale = 1 if amax is 0, otherwise max(amax * c, 2^-126), c = 1/448 rounded to fp32
@@ -415,11 +415,11 @@ hq_status hq_fp8_quantize_blocks(const void *w, hq_dtype w_dtype, int64_t n, int
  *
  * The product of two scales is rounded to fp32 first (2^-126 .. 2^128 is its range), sums over groups are fp32, rounded once to y_dtype.
  * Sums inside a group: HQ_F32 results have fp32 sums of exact products.  For HQ_F16 and HQ_BF16 each eight neighbouring products
- * (c = 8 i .. 8 i + 7) are first cut towards zero to multiples of 2^(e - 13), e the largest sum of two codes' exponents among those that are
- * not zero (a subnormal code's is -6), then added in fp32: off by less than 2^-10 of the sum of the products' magnitudes, 2^-7 where an
- * eight holds nothing larger than a subnormal code's product.  Over normal values that is 1.5e-5 of the results' norm, and 6 in 100 fp16
- * results are the neighbour of the nearest number; where products cancel to 2^-10 of their size, take HQ_F32.  The same holds for the
- * layer and for dx below.
+ * (c = 8 i .. 8 i + 7) are first cut towards zero to multiples of 2^(e - 13), e the largest sum of two codes' exponents among those that
+ * are not zero (a subnormal code's is -6), then added in fp32: off by less than 2^-10 of the sum of the products' magnitudes, 2^-7 where
+ * an eight holds nothing larger than a subnormal code's product.  Over normal values that is 1.5e-5 of the results' norm, and 6 in 100
+ * fp16 results are the neighbour of the nearest number; where products cancel to 2^-10 of their size, take HQ_F32.  The same holds for
+ * the layer and for dx below.
  * bias [n] of y_dtype or NULL; y [m, n], dense, apart from all inputs (of the whole layer too).
  * w_scale_turned: w_scale is [ceil(k / 128), ceil(n / 128)] (codes of a transposed matrix with the scales of the matrix).
  */
@@ -429,7 +429,8 @@ hq_status hq_fp8_linear(const uint8_t *xq, const float *x_scale, const uint8_t *
 /*
  * The whole layer: the codes and scales of hq_fp8_quantize_rows, multiplied as by hq_fp8_linear.  Small layers are one launch, whose waves
  * split k: the groups of 128 may be added in another order than by the two calls, so the last bits of their fp32 sums can differ.
- * workspace: device memory of hq_act_quant_fp8_linear_workspace(..) bytes, 16-byte aligned, written and read by the call; NULL where that is 0.
+ * workspace: device memory of hq_act_quant_fp8_linear_workspace(..) bytes, 16-byte aligned, written and read by the call; NULL where that
+ * is 0.
  */
 int64_t hq_act_quant_fp8_linear_workspace(hq_dtype x_dtype, int64_t m, int n, int k, hq_dtype y_dtype);
 hq_status hq_act_quant_fp8_linear(const void *x, hq_dtype x_dtype, int64_t row_stride, const uint8_t *wq,
@@ -452,8 +453,8 @@ hq_status hq_fp8_linear_backward(const void *dy, int64_t dy_stride, const void *
                                  void *dx, float *dw, float *db, void *stream);
 
 /*
- * Diagnostics, host logic only: the kernel a layer takes (x_dtype HQ_I32: hq_fp8_linear, on codes), and the one that multiplies for both gradients
- * ("two launches": one each).  "split" and "one launch": the waves of a workgroup split k.
+ * Diagnostics, host logic only: the kernel a layer takes (x_dtype HQ_I32: hq_fp8_linear, on codes), and the one that multiplies for both
+ * gradients ("two launches": one each).  "split" and "one launch": the waves of a workgroup split k.
  */
 const char *hq_fp8_linear_kernel_name(hq_dtype x_dtype, int64_t m, int n, int k, hq_dtype y_dtype);
 const char *hq_fp8_linear_backward_kernel_name(hq_dtype dtype, int64_t m, int n, int k, int bias_grad);
@@ -473,8 +474,8 @@ const char *hq_fp8_linear_backward_kernel_name(hq_dtype dtype, int64_t m, int n,
  *   strides   HOST array, in elements, a head's channels side by side: q token, q head, k token, k head, then the results' in that order.
  *             A result may be its own input (the same memory with the same strides); any other overlap is not allowed.
  *   q_weight, k_weight  [d] of w_dtype (dtype or HQ_F32), or NULL for ones
- *   pos       [t] of pos_size bytes (4 or 8) each, or NULL for 0 .. t - 1 (then t <= positions).  A token with a negative position is padding: its
- *             results are zeros.  One at or beyond `positions` has NaN for results.
+ *   pos       [t] of pos_size bytes (4 or 8) each, or NULL for 0 .. t - 1 (then t <= positions).  A token with a negative position is
+ *             padding: its results are zeros.  One at or beyond `positions` has NaN for results.
  *   d, rotary even, rotary <= d <= 1024; t * heads below 2^31; eps >= 0
  *   t = 0 is no error.
  */

@@ -279,8 +279,9 @@ def hq_fp8_linear(xq: torch.Tensor, x_scale: torch.Tensor, wq: torch.Tensor, w_s
     """xq [..., kp], wq [n, kp] float8_e4m3fn codes as the quantisers write them, with their scales -> y [..., n].  w_scale may be
     the transposed view of the scales of a matrix whose transposed codes wq holds.  out shares no memory with the inputs.
 
-    Sums are fp32, but for fp16 and bf16 results eight neighbouring products are first cut 13 bits below the largest: at most 2^-10 of the sum
-    of magnitudes (2^-7 among products of subnormal codes), 1.5e-5 of the norm over normal values.  Where products cancel, take float32."""
+    Sums are fp32, but for fp16 and bf16 results eight neighbouring products are first cut 13 bits below the largest: at most 2^-10 of
+    the sum of magnitudes (2^-7 among products of subnormal codes), 1.5e-5 of the norm over normal values.  Where products cancel, take
+    float32."""
     return _native().fp8_linear(xq, x_scale, wq, w_scale, bias, y_dtype, out)
 
 

@@ -20,7 +20,8 @@ SOURCES = ["hq_hadamard_quant.hip", "hq_int_gemm.hip", "hq_int_gemm_128x128.hip"
            "hq_resident_wholetaps_ragged.hip", "hq_resident_sum.hip", "hq_resident_sum_ragged.hip",
            "hq_resident_planes.hip", "hq_resident_bytes.hip", "hq_linear_fp6.hip", "hq_linear_fused.hip",
            "hq_int_gemm_anyk.hip",
-           "hq_single_weights.hip", "hq_width_quant.hip", "hq_fp8_quant.hip", "hq_fp8_linear.hip", "hq_fp8_split.hip", "hq_qk_norm_rope.hip"]
+           "hq_single_weights.hip", "hq_width_quant.hip", "hq_fp8_quant.hip", "hq_fp8_linear.hip",
+           "hq_fp8_split.hip", "hq_qk_norm_rope.hip"]
 HEADERS = ["hq_common.h", "hq_int_gemm_kernel.h", "hq_hadamard_mfma.h", "hq_conv3x3_res_kernel.h",
            "hq_resident_kernel.h", "hq_fp6.h", "hq_buffer.h", "hq_floats.h", "hq_fp8.h",
            "hq_fp8_codes.h", "hq_fp8_product.h", "hq_qk_cut.h"]

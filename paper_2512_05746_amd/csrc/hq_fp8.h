@@ -27,14 +27,15 @@ inline bool fp8_fits(int64_t rows, int64_t columns) {
 hq_status fp8_rows(const void *x, hq_dtype dt, int64_t m, int k, int64_t row_stride, uint8_t *xq, float *scale, hipStream_t st);
 hq_status fp8_blocks(const void *x, hq_dtype dt, int64_t rows, int columns, int64_t row_stride, uint8_t *q, uint8_t *q_t, float *scale,
                      hipStream_t st);
-// What a backward pass quantises: dy [m, n] along its rows and along its columns, x [m, k] in blocks, transposed; the sums of 128 rows of dy.
+// What a backward pass quantises: dy [m, n] along its rows and along its columns, x [m, k] in blocks, transposed; the sums of 128 rows of
+// dy.
 struct Fp8Gradient {
     uint8_t *dyq, *dyq_t, *xq_t;              // [m, pitch of n], [n, pitch of m], [k, pitch of m]
     float *dy_scale, *dy_scale_t, *x_scale;   // [n / 128, m], [m / 128, n], [m / 128, k / 128]
     float *sums;                              // [m / 128, n], or null
 };
-hq_status fp8_gradient(const void *dy, int64_t dy_stride, const void *x, int64_t x_stride, hq_dtype dt, int64_t m, int n, int k, const Fp8Gradient &out,
-                       hipStream_t st);
+hq_status fp8_gradient(const void *dy, int64_t dy_stride, const void *x, int64_t x_stride, hq_dtype dt, int64_t m, int n, int k,
+                       const Fp8Gradient &out, hipStream_t st);
 
 // A product's arguments.
 struct Fp8Product {
@@ -54,7 +55,8 @@ struct Fp8Cut {
 };
 // the best cut; in: the type of rows that are quantised, or null for codes
 Fp8Cut fp8_split_cut(int64_t m, int64_t n, int64_t steps, const hq_dtype *in, hq_dtype out);
-hq_status fp8_split(const Fp8Product &p, Fp8Cut cut, const void *x, hq_dtype x_dtype, int64_t row_stride, int k, hq_dtype out, hipStream_t st);
+hq_status fp8_split(const Fp8Product &p, Fp8Cut cut, const void *x, hq_dtype x_dtype, int64_t row_stride, int k, hq_dtype out,
+                    hipStream_t st);
 
 // Two products in one launch, `a` with results of type out, `b` of fp32, and the sums over the rows of a matrix, both of a backward pass.
 struct Fp8Sums {

@@ -63,7 +63,9 @@ template <class T> struct Tops {
             t[i] = __builtin_elementwise_max(t[i], __builtin_bit_cast(u16x2, from(__builtin_bit_cast(int, t[i]))));
     }
     // as the bits of a float
-    __device__ __forceinline__ static uint32_t wide(unsigned short bits) { return __float_as_uint(static_cast<float>(__builtin_bit_cast(T, bits))); }
+    __device__ __forceinline__ static uint32_t wide(unsigned short bits) {
+        return __float_as_uint(static_cast<float>(__builtin_bit_cast(T, bits)));
+    }
     __device__ __forceinline__ uint32_t column(int i) const { return wide(t[i / 2][i & 1]); }
     __device__ __forceinline__ uint32_t all() const {
         const u16x2 m = __builtin_elementwise_max(__builtin_elementwise_max(t[0], t[1]), __builtin_elementwise_max(t[2], t[3]));

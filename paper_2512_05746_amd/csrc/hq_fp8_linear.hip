@@ -3,12 +3,13 @@
 //     y[i, j] = sum over blocks b of 128 of  sx[b, i] sw[j / 128, b] (sum over c in b of xq[i, c] wq[j, c])  + bias[j]
 //
 // The outer sum is fp32 fused multiply-adds.  The inner one is taken by matrix instructions started from zero, for results of 16 bits by
-// one of 8-bit floats (16 x 16 x 128).  That instruction cuts 8 neighbouring products towards zero to multiples of 2^(e - 13), e the largest
-// sum of two exponents among those that are not zero (subnormal codes count -6), and adds them in fp32 (measured on single products, and
-// sums of 128 .. 4096 of normal values agree with this in every fp16 result).  At most 7 products of an eight lose 2^-13 of the largest, 2^-10
-// of the sum of magnitudes, or 8 times that where the largest is a subnormal code's.  Over normal values the results are off by 1.5e-5 of their
-// norm (fp16 rounding: 2.1e-4) and 6 % of fp16 results are the neighbour of the nearest one: taken for twice the rate.  Not for
-// fp32 results (weight gradients among them): they use the bf16 instruction, which holds products of codes exactly and adds them in fp32.
+// one of 8-bit floats (16 x 16 x 128).  That instruction cuts 8 neighbouring products towards zero to multiples of 2^(e - 13), e the
+// largest sum of two exponents among those that are not zero (subnormal codes count -6), and adds them in fp32 (measured on single
+// products, and sums of 128 .. 4096 of normal values agree with this in every fp16 result).  At most 7 products of an eight lose 2^-13 of
+// the largest, 2^-10 of the sum of magnitudes, or 8 times that where the largest is a subnormal code's.  Over normal values the results
+// are off by 1.5e-5 of their norm (fp16 rounding: 2.1e-4) and 6 % of fp16 results are the neighbour of the nearest one: taken for twice
+// the rate.  Not for fp32 results (weight gradients among them): they use the bf16 instruction, which holds products of codes exactly and
+// adds them in fp32.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -24,23 +25,23 @@
 namespace {
 
 // A tile of BM tokens x BN channels; WM x WN waves.  Codes of one step, [row][8 pieces of 16 bytes], go from memory straight into LDS;
-// the pieces of a row are kept in an order that depends on the row, so that lanes that are served together read different banks.  Rows of weights
-// are kept so that a lane's channels in NG tiles of results are neighbours.
+// the pieces of a row are kept in an order that depends on the row, so that lanes that are served together read different banks.  Rows of
+// weights are kept so that a lane's channels in NG tiles of results are neighbours.
 //
 // A wave takes the products of a step in a fixed order, each with the fold of the one four before it (the multiply-adds issue while
-// the matrix pipe is busy): rows of its tiles, the last two rows together, column by column.  Each operand is read from LDS two rows ahead, and
-// the tokens' operands of the next step as soon as the last product with their predecessor has been issued, so that no step begins
-// with a wait.  The one barrier of a step stands before the last two rows: there all waves have read the buffer of this step, which is then
-// filled again, and the buffer of the next one has landed.  The loads of a step are dealt over the products, since a wave that issues them all at once
-// waits for the path to memory.
+// the matrix pipe is busy): rows of its tiles, the last two rows together, column by column.  Each operand is read from LDS two rows
+// ahead, and the tokens' operands of the next step as soon as the last product with their predecessor has been issued, so that no step
+// begins with a wait.  The one barrier of a step stands before the last two rows: there all waves have read the buffer of this step,
+// which is then filled again, and the buffer of the next one has landed.  The loads of a step are dealt over the products, since a wave
+// that issues them all at once waits for the path to memory.
 //
 // (The loads have to be those of hq_fp8_product.h, which the compiler does not wait for.)
 //
-// What bounds it: 8192 x 4096 -> 8192 with 256 x 256 tiles 239 us (2.3 PFLOP/s; a library product of the same codes with one scale for the tensor
-// 229 .. 231): the matrix pipe is busy in 62 % of the cycles and the clock is at 1.73 of 2.4 GHz, so it is power; at few workgroups LDS (192 KB
-// of reads and 64 KB of loads a step, 128 bytes a cycle, against 2048 cycles of the matrix pipe).  fp32 results: 4096 x 8192 -> 4096 239 us (1.15
-// PFLOP/s; bf16 products of a library 1.42).  Small K (4096 x 576 -> 1728 12.2 us, 8.2 with K = 128): launch, first loads and results (14 MB)
-// of one round of workgroups.
+// What bounds it: 8192 x 4096 -> 8192 with 256 x 256 tiles 239 us (2.3 PFLOP/s; a library product of the same codes with one scale for
+// the tensor 229 .. 231): the matrix pipe is busy in 62 % of the cycles and the clock is at 1.73 of 2.4 GHz, so it is power; at few
+// workgroups LDS (192 KB of reads and 64 KB of loads a step, 128 bytes a cycle, against 2048 cycles of the matrix pipe).  fp32 results:
+// 4096 x 8192 -> 4096 239 us (1.15 PFLOP/s; bf16 products of a library 1.42).  Small K (4096 x 576 -> 1728 12.2 us, 8.2 with K = 128):
+// launch, first loads and results (14 MB) of one round of workgroups.
 template <int OUT, int BM, int BN, int WM, int WN, int STAGES>
 struct Product {
     using Out = typename Float<OUT>::type;
@@ -76,7 +77,8 @@ struct Product {
     uint32_t x_at[2], w_at[2], s_at;         // of the lane's two pieces of its first rows, and of its first scale, in a buffer
     v8i x[MT], w[4];
     f32x4 acc[NT][MT], p[RING];
-    float s[MT], s_old[2], s_new[MT], s_w;   // scales of this step, of the columns whose products of the step before are not folded yet, of the next step
+    // scales of this step, of the columns whose products of the step before are not folded yet, of the next step
+    float s[MT], s_old[2], s_new[MT], s_w;
 
     __device__ __forceinline__ Product(const ProductArgs &args, uint32_t tile_m, uint32_t tile_n) : a(args) {
         const int tid = threadIdx.x;
@@ -130,8 +132,10 @@ struct Product {
             // (channels of a tile beyond the last block are not stored)
             const int block = n0 / kStep + i - SX, last = (a.n - 1) / kStep;
             const float *from = tokens ? a.sx + static_cast<int64_t>(step) * a.m + m0
-                                       : a.sw + static_cast<int64_t>(block < last ? block : last) * a.sw_block + static_cast<int64_t>(step) * a.sw_step;
-            load4_to_lds(words_of(from, step >= a.steps ? 0 : tokens ? sx_bytes : 4), tokens ? (i * 64 + lane) * 4 : 0, fill + kCodes + i * 256);
+                                       : a.sw + static_cast<int64_t>(block < last ? block : last) * a.sw_block +
+                                             static_cast<int64_t>(step) * a.sw_step;
+            load4_to_lds(words_of(from, step >= a.steps ? 0 : tokens ? sx_bytes : 4), tokens ? (i * 64 + lane) * 4 : 0,
+                         fill + kCodes + i * 256);
         }
     }
     __device__ __forceinline__ void request(uint32_t lds) {
@@ -148,8 +152,12 @@ struct Product {
     __device__ __forceinline__ static v8i fetch(const uint8_t *lo, const uint8_t *hi) {
         return __builtin_shufflevector(*reinterpret_cast<const v4i *>(lo), *reinterpret_cast<const v4i *>(hi), 0, 1, 2, 3, 4, 5, 6, 7);
     }
-    __device__ __forceinline__ void fetch_x(const uint8_t *lds, int j) { x[j] = fetch(lds + x_at[0] + j * 16 * kStep, lds + x_at[1] + j * 16 * kStep); }
-    __device__ __forceinline__ void fetch_w(const uint8_t *lds, int i) { w[i & 3] = fetch(lds + w_at[0] + i * 16 * kStep, lds + w_at[1] + i * 16 * kStep); }
+    __device__ __forceinline__ void fetch_x(const uint8_t *lds, int j) {
+        x[j] = fetch(lds + x_at[0] + j * 16 * kStep, lds + x_at[1] + j * 16 * kStep);
+    }
+    __device__ __forceinline__ void fetch_w(const uint8_t *lds, int i) {
+        w[i & 3] = fetch(lds + w_at[0] + i * 16 * kStep, lds + w_at[1] + i * 16 * kStep);
+    }
     __device__ __forceinline__ void fetch_scales(const uint8_t *lds) {
         s_w = *reinterpret_cast<const float *>(lds + kCodes + (SX + wn * TN / kStep) * 256);
 #pragma unroll
@@ -196,7 +204,8 @@ struct Product {
         if (NT == 2 && t >= T - 2) fetch_w(next, t - (T - 2));
     }
     // loads that go with product t: a request begins after the barrier and goes on in the next step
-    static constexpr int OVER = T < 16 ? T : 16, kFirst = (2 * MT < OVER ? 2 * MT : OVER) * kLoads / OVER;   // parts of a request before the next step
+    static constexpr int OVER = T < 16 ? T : 16;
+    static constexpr int kFirst = (2 * MT < OVER ? 2 * MT : OVER) * kLoads / OVER;   // parts of a request before the next step
     __device__ __forceinline__ void deal(int t) const {
         const int slot = t >= kBody ? t - kBody : t + 2 * MT;
         if (slot < OVER) {
@@ -285,8 +294,8 @@ struct Product {
     }
 };
 
-// Neighbouring workgroups share tiles' codes in the L2 of their XCD: workgroup b runs on XCD b % 8, each XCD takes a contiguous run of tiles,
-// and those go through bands of 4 tiles of tokens.
+// Neighbouring workgroups share tiles' codes in the L2 of their XCD: workgroup b runs on XCD b % 8, each XCD takes a contiguous run of
+// tiles, and those go through bands of 4 tiles of tokens.
 struct Tiles {
     uint32_t m, n;   // counts
 };
@@ -329,7 +338,8 @@ __global__ __launch_bounds__(WM *WN * 64) void product_kernel(ProductArgs a, Til
 
 // Two products, `b` with fp32 results, and sums: workgroups of b first, then of a, then of the sums.
 template <int OUT, int BM, int BN, int WM, int WN, int STAGES>
-__global__ __launch_bounds__(WM *WN * 64) void product_pair_kernel(ProductArgs a, Tiles a_count, ProductArgs b, Tiles b_count, hq::Fp8Sums sums) {
+__global__ __launch_bounds__(WM *WN * 64) void product_pair_kernel(ProductArgs a, Tiles a_count, ProductArgs b, Tiles b_count,
+                                                                   hq::Fp8Sums sums) {
     extern __shared__ __attribute__((aligned(1024))) uint8_t lds[];
     const uint32_t na = a_count.m * a_count.n, nb = b_count.m * b_count.n;
     if (blockIdx.x < nb) product_tile<HQ_F32, BM, BN, WM, WN, STAGES>(b, b_count, blockIdx.x, lds);
@@ -374,11 +384,11 @@ hq_status launch_pair(const ProductArgs &a, const ProductArgs &b, const hq::Fp8S
 }
 
 // The tiles of the product, for 16-bit results first, then for 32-bit ones.  A step of a lone workgroup takes `round` us, a CU's share of a
-// step `each` us a tile when it has several; measured with 8192 x 4096 -> 8192 and 4096 x 8192 -> 4096 (shares), 2048 x 3840 -> 960, 1024 x 1024
-// -> 1024 and 256 x 4096 -> 4096 (rounds); begin: launch, first loads and results (300 x 100 -> 4100, 1025 x 500 -> 1030), again: those of a CU's further
-// tiles (2048 x 512 -> 2048, 4096 x 256 -> 1024).  Tiles of 128 x 128, two workgroups a CU, are not among them: 335 us for 8192 x 4096 -> 8192 where
-// 256 x 128 takes 302 and 256 x 256 257; with fp32 results 246 us for 4096 x 8192 -> 4096 where 256 x 128 takes 239 (the card's power is the limit
-// there, and larger tiles move less through LDS).
+// step `each` us a tile when it has several; measured with 8192 x 4096 -> 8192 and 4096 x 8192 -> 4096 (shares), 2048 x 3840 -> 960, 1024
+// x 1024 -> 1024 and 256 x 4096 -> 4096 (rounds); begin: launch, first loads and results (300 x 100 -> 4100, 1025 x 500 -> 1030), again:
+// those of a CU's further tiles (2048 x 512 -> 2048, 4096 x 256 -> 1024).  Tiles of 128 x 128, two workgroups a CU, are not among them:
+// 335 us for 8192 x 4096 -> 8192 where 256 x 128 takes 302 and 256 x 256 257; with fp32 results 246 us for 4096 x 8192 -> 4096 where 256
+// x 128 takes 239 (the card's power is the limit there, and larger tiles move less through LDS).
 enum Tile { kTile256, kTile128, kTile64x128, kTile64 };
 struct TileCost {
     Tile tile;
@@ -403,7 +413,8 @@ TileChoice choose_tile(int64_t m, int64_t n, int64_t steps, hq_dtype out) {
     TileChoice best{kTile64, 1e30f};
     for (const TileCost &c : kTiles) {
         const int o = out == HQ_F32;
-        const float tiles = ceilf(tiles_per_cu(c, m, n, cu)), us = c.begin + (tiles - 1.0f) * c.again + steps * std::max(c.round[o], tiles * c.each[o]);
+        const float tiles = ceilf(tiles_per_cu(c, m, n, cu));
+        const float us = c.begin + (tiles - 1.0f) * c.again + steps * std::max(c.round[o], tiles * c.each[o]);
         if (us < best.us) best = {c.tile, us};
     }
     return best;
@@ -415,7 +426,8 @@ TileChoice choose_pair(const ProductArgs &a, const ProductArgs &b, hq_dtype out)
         if (c.tile == kTile256) continue;
         const int o = out == HQ_F32;
         const float share = a.steps * tiles_per_cu(c, a.m, a.n, cu) * c.each[o] + b.steps * tiles_per_cu(c, b.m, b.n, cu) * c.each[1];
-        // (the last round is only partly filled: half of the longer tile)
+        // (the last round is only partly filled: half of the longer tile; charged where there is one round, too: 2048 x 960 -> 3840 is
+        // estimated at 45.7 us for 184 workgroups of 256 x 128, 32.1 without it, and takes 64 x 128, 34.4)
         const float longest = std::max(a.steps * c.each[o], b.steps * c.each[1]);
         const float us = c.begin + std::max(std::max(a.steps * c.round[o], b.steps * c.round[1]), share + 0.5f * longest);
         if (us < best.us) best = {c.tile, us};
@@ -427,7 +439,8 @@ template <int OUT>
 hq_status launch(const ProductArgs &a, Tile tile, hipStream_t st) {
     switch (tile) {
         case kTile256:
-            if constexpr (OUT != HQ_F32) return launch_tiles<OUT, 256, 256, 4, 2, 2>(a, st);   // (not with fp32 results: too many registers)
+            // (not with fp32 results: too many registers)
+            if constexpr (OUT != HQ_F32) return launch_tiles<OUT, 256, 256, 4, 2, 2>(a, st);
             [[fallthrough]];
         case kTile128: return launch_tiles<OUT, 256, 128, 4, 2, 3>(a, st);
         case kTile64x128: return launch_tiles<OUT, 64, 128, 2, 2, 3>(a, st);
@@ -444,8 +457,8 @@ hq_status launch_pair(const ProductArgs &a, const ProductArgs &b, const hq::Fp8S
     }
 }
 
-ProductArgs product_args(const uint8_t *xq, const float *x_scale, const uint8_t *wq, const float *w_scale, bool scale_turned, const void *bias,
-                         int64_t m, int n, int k, void *y) {
+ProductArgs product_args(const uint8_t *xq, const float *x_scale, const uint8_t *wq, const float *w_scale, bool scale_turned,
+                         const void *bias, int64_t m, int n, int k, void *y) {
     const int steps = static_cast<int>(hq::fp8_groups(k)), blocks = static_cast<int>(hq::fp8_groups(n));
     return {xq, wq, x_scale, w_scale, bias, y, m, n, hq::fp8_pitch(k), steps, scale_turned ? 1 : steps, scale_turned ? blocks : 1};
 }
@@ -483,7 +496,8 @@ PairChoice choose_pair_launch(const ProductArgs &a, const ProductArgs &b, bool s
     const hq::Fp8Cut cut = hq::fp8_split_pair_cut(a, b, dt);
     const TileChoice tile = choose_pair(a, b, dt);
     const float alone = choose(a.m, a.n, a.steps, dt).us() + choose(b.m, b.n, b.steps, HQ_F32).us() + (sums ? 2.0f : 0.0f);
-    return {cut.us < tile.us && cut.us < alone ? PairChoice::kSplit : tile.us < alone ? PairChoice::kTiles : PairChoice::kAlone, cut, tile.tile};
+    const auto how = cut.us < tile.us && cut.us < alone ? PairChoice::kSplit : tile.us < alone ? PairChoice::kTiles : PairChoice::kAlone;
+    return {how, cut, tile.tile};
 }
 
 // a with results of type dt, b with fp32 ones, and sums
@@ -548,7 +562,8 @@ extern "C" hq_status hq_fp8_linear(const uint8_t *xq, const float *x_scale, cons
         return HQ_ERR_ALIGN;
     if (!product_fits(m, n, k)) return HQ_ERR_UNSUPPORTED;
     if (m == 0) return HQ_OK;
-    return product(product_args(xq, x_scale, wq, w_scale, w_scale_turned != 0, bias, m, n, k, y), y_dtype, static_cast<hipStream_t>(stream));
+    return product(product_args(xq, x_scale, wq, w_scale, w_scale_turned != 0, bias, m, n, k, y), y_dtype,
+                   static_cast<hipStream_t>(stream));
 }
 
 namespace {
@@ -560,8 +575,8 @@ struct LayerChoice {
 LayerChoice choose_layer(hq_dtype x_dtype, int64_t m, int n, int k, hq_dtype y_dtype) {
     const int64_t steps = hq::fp8_groups(k);
     const hq::Fp8Cut fused = hq::fp8_split_cut(m, n, steps, &x_dtype, y_dtype);
-    // us of quantising them by themselves: 2.2 on the card, and a launch more on the host, which counts where calls follow one another (16 x 4096 -> 4096: 6.8
-    // against 8.4 us of one launch in a graph, called one by one 9.6 against 9.1)
+    // us of quantising them by themselves: 2.2 on the card, and a launch more on the host, which counts where calls follow one another
+    // (16 x 4096 -> 4096: 6.8 against 8.4 us of one launch in a graph, called one by one 9.6 against 9.1)
     const float rows = 3.2f + static_cast<float>(m) * k * (hq::size_of(x_dtype) + 1) / 4.5e6f;
     return {fused.us < rows + choose(m, n, steps, y_dtype).us(), fused};
 }
@@ -598,7 +613,11 @@ extern "C" hq_status hq_act_quant_fp8_linear(const void *x, hq_dtype x_dtype, in
 
 namespace {
 const char *name_of(const hq::Fp8Cut &c, bool one_launch) {
-    if (one_launch) return c.nt == 1 ? "one launch (16 x 16)" : c.nt == 2 ? "one launch (16 x 32)" : c.nt == 4 ? "one launch (16 x 64)" : "one launch (16 x 128)";
+    if (one_launch)
+        return c.nt == 1   ? "one launch (16 x 16)"
+               : c.nt == 2 ? "one launch (16 x 32)"
+               : c.nt == 4 ? "one launch (16 x 64)"
+                           : "one launch (16 x 128)";
     return c.mt == 4 ? "split (64 x 64)" : c.mt == 2 ? "split (32 x 32)" : c.nt == 2 ? "split (16 x 32)" : "split (16 x 16)";
 }
 const char *name_of(Tile t) {
@@ -642,7 +661,8 @@ extern "C" hq_status hq_fp8_linear_backward(const void *dy, int64_t dy_stride, c
     hipStream_t st = static_cast<hipStream_t>(stream);
     if (m == 0) {
         const hq::LaunchCheck check;
-        zero_kernel<<<static_cast<uint32_t>(std::min<int64_t>(1024, (static_cast<int64_t>(n) * k + 255) / 256)), 256, 0, st>>>(dw, static_cast<int64_t>(n) * k);
+        const int64_t count = static_cast<int64_t>(n) * k;
+        zero_kernel<<<static_cast<uint32_t>(std::min<int64_t>(1024, (count + 255) / 256)), 256, 0, st>>>(dw, count);
         if (db) zero_kernel<<<std::min<uint32_t>(1024, (n + 255) / 256), 256, 0, st>>>(db, n);
         return check.status();
     }

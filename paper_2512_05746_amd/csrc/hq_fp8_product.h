@@ -44,7 +44,8 @@ __device__ __forceinline__ Halves halves_of(const v8i &codes) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         const uint32_t w = static_cast<uint32_t>(codes[i]);
-        const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, false), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, true);
+        const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, false);
+        const bf16x2 b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, true);
         const int at = (i & 1) * 4;
         h.v[i / 2][at] = a[0], h.v[i / 2][at + 1] = a[1], h.v[i / 2][at + 2] = b[0], h.v[i / 2][at + 3] = b[1];
     }

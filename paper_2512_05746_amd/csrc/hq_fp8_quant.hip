@@ -4,16 +4,17 @@
 //     amax = max |x| over the tile;  s = 1 if amax is 0, else max(amax * c, 2^-126);  code = E4M3(x * (1 / s))
 //
 // c is 1/448 in fp32, and products and quotient are rounded to nearest, so that the codes are a function of the inputs alone; the
-// conversion rounds to nearest, ties to even.  |x (1 / s)| is at most 448 (1 + 2^-22), which rounds to 448.  A tile that holds an infinity or a NaN gets
-// a NaN for its scale and zeros for codes: every product that uses it is NaN.
+// conversion rounds to nearest, ties to even.  |x (1 / s)| is at most 448 (1 + 2^-22), which rounds to 448.  A tile that holds an
+// infinity or a NaN gets a NaN for its scale and zeros for codes: every product that uses it is NaN.
 //
 // Bound by memory: a value is read once and written as one byte, or as two bytes where codes along rows and along columns are wanted.
 // rows_kernel: 16 lanes own 128 values of a row, 8 each; 8192 x 4096 in bf16 20.5 us (4.9 TB/s).
-// tile: a workgroup of 256 threads owns a tile of 128 x 128; a thread holds 8 rows x 8 columns as they came from memory, so a maximum along a row is
-// one over 16 lanes, along a column one over 16 threads at the same columns (4 lanes of each wave, then LDS), and the codes of a column leave
-// through LDS as whole pieces of 128 bytes.  Values of 16 bits are compared two at a time by their bits; the scales of a wave's 8 rows are
-// taken in 8 lanes at once (a division each), not in every lane for every row; tiles that lie inside have no bounds to check: together 79 -> 41 us for
-// the gradient and the activations of 8192 x (4096 + 4096) in bf16 (224 MB, 5.4 TB/s), 15.6 -> 9.7 for 2048 x (3840 + 960) in fp16.
+// tile: a workgroup of 256 threads owns a tile of 128 x 128; a thread holds 8 rows x 8 columns as they came from memory, so a maximum
+// along a row is one over 16 lanes, along a column one over 16 threads at the same columns (4 lanes of each wave, then LDS), and the
+// codes of a column leave through LDS as whole pieces of 128 bytes.  Values of 16 bits are compared two at a time by their bits; the
+// scales of a wave's 8 rows are taken in 8 lanes at once (a division each), not in every lane for every row; tiles that lie inside have
+// no bounds to check: together 79 -> 41 us for the gradient and the activations of 8192 x (4096 + 4096) in bf16 (224 MB, 5.4 TB/s), 15.6
+// -> 9.7 for 2048 x (3840 + 960) in fp16.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -193,7 +194,8 @@ __device__ __forceinline__ void tile_body(const TileArgs &a, TileSpace &lds, uin
     for (int i = 0; i < 8; ++i, to += 16 * a.pitch_t) {
         const int column = i * 16 + part;
         if (WHOLE || (column0 + column < a.columns && row0 + lane16 * 8 < a.pitch_t))
-            *reinterpret_cast<uint2 *>(to) = *reinterpret_cast<const uint2 *>(lds.turned + column * kGroup + ((lane16 ^ (column >> 3)) * 8));
+            *reinterpret_cast<uint2 *>(to) =
+                *reinterpret_cast<const uint2 *>(lds.turned + column * kGroup + ((lane16 ^ (column >> 3)) * 8));
     }
 }
 template <int DT, bool BLOCKS>
@@ -258,8 +260,8 @@ hq_status fp8_blocks(const void *x, hq_dtype dt, int64_t rows, int columns, int6
     });
 }
 
-hq_status fp8_gradient(const void *dy, int64_t dy_stride, const void *x, int64_t x_stride, hq_dtype dt, int64_t m, int n, int k, const Fp8Gradient &out,
-                       hipStream_t st) {
+hq_status fp8_gradient(const void *dy, int64_t dy_stride, const void *x, int64_t x_stride, hq_dtype dt, int64_t m, int n, int k,
+                       const Fp8Gradient &out, hipStream_t st) {
     const TileArgs g{dy, m, dy_stride, n, fp8_pitch(n), fp8_pitch64(m), out.dyq, out.dyq_t, out.dy_scale, out.dy_scale_t, out.sums};
     const TileArgs b{x, m, x_stride, k, fp8_pitch(k), fp8_pitch64(m), nullptr, out.xq_t, out.x_scale, nullptr, nullptr};
     const int64_t down = fp8_groups(m), dy_across = fp8_groups(n), x_across = fp8_groups(k);

@@ -1,17 +1,20 @@
 // Product of E4M3 codes for few tokens or few tiles: the waves of a workgroup share one small tile of results and split K.
 //
-// A wave takes every NW-th step of 128 codes.  They go from memory into LDS that the wave has to itself, from there into its registers, and while it
-// multiplies them the next ones are on their way; there is no barrier before the end, where the waves' sums meet in LDS, in the order of the waves.
-// Activations come as codes with their scales, or as 16- or 32-bit floats, which the wave then quantises itself (16 lanes to a token, 8 neighbours to a
-// lane), so that a whole layer is one launch; each workgroup of the same tokens quantises them anew.
+// A wave takes every NW-th step of 128 codes.  They go from memory into LDS that the wave has to itself, from there into its registers,
+// and while it multiplies them the next ones are on their way; there is no barrier before the end, where the waves' sums meet in LDS, in
+// the order of the waves.  Activations come as codes with their scales, or as 16- or 32-bit floats, which the wave then quantises itself
+// (16 lanes to a token, 8 neighbours to a lane), so that a whole layer is one launch; each workgroup of the same tokens quantises them
+// anew.
 //
-// Why LDS, where every byte is read once: a matrix instruction wants neighbouring lanes to hold neighbouring rows, and loads for which they are
-// take the path to memory 64 cycles each (16 bytes a cycle and CU), loads whose neighbouring lanes read 128 neighbouring bytes a quarter of that.
-// Straight into registers 64 tokens of 4096 -> 4096 took 10.1 us on codes, 512 of 4096 -> 512 9.7, 16 of 4096 -> 8192 7.9; so 6.3, 5.6 and 5.3.
+// Why LDS, where every byte is read once: a matrix instruction wants neighbouring lanes to hold neighbouring rows, and loads for which
+// they are take the path to memory 64 cycles each (16 bytes a cycle and CU), loads whose neighbouring lanes read 128 neighbouring bytes a
+// quarter of that.  Straight into registers 64 tokens of 4096 -> 4096 took 10.1 us on codes, 512 of 4096 -> 512 9.7, 16 of 4096 -> 8192
+// 7.9; so 6.3, 5.6 and 5.3.
 //
-// Bound by latency (launch, one round of loads for each step of a wave, the exchange), for many channels and few tokens by reading the weights: us in
-// a graph, bf16 on codes: 960 -> 3840 for 1 token 2.6, for 64 3.3; 16 tokens of 4096 -> 4096 4.3, 1 token of 4096 -> 8192 4.6 (tiles: 4.8, 5.1,
-// 11.9 and 11.9).  As a layer in one launch, fp16: 3.2, 4.7, 8.4 and 6.3.
+// Bound by latency (launch, one round of loads for each step of a wave, the exchange), for many channels and few tokens by reading the
+// weights: us in a graph, bf16 on codes: 960 -> 3840 for 1 token 2.6, for 64 3.3; 16 tokens of 4096 -> 4096 4.3, 1 token of 4096 -> 8192
+// 4.6 (tiles: 4.8, 5.1, 11.9 and 11.9).  As a layer in one launch, fp16: 3.2, 4.7, 8.4 and 6.3.  (The estimates below charge that form
+// for 16 tokens whatever their count, so one token of 4096 -> 8192 takes two launches: 7.0 in a graph, 7.3 called one by one.)
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -59,8 +62,8 @@ __device__ __forceinline__ void split(const SplitArgs &a, uint32_t bx, uint32_t 
     const uint32_t mine_at = lds_address(lds) + wave * AREA;
 
     // A load brings 8 rows, lane = (row, piece): the lanes of a row read 128 neighbouring bytes.  Row r of tile i holds channel
-    // 4 NT (r / 4) + 4 i + r % 4, which makes a lane's channels neighbours; pieces are in an order that depends on the row (key), so that reads of a
-    // column of rows use all banks.  Rows beyond the last, and pieces beyond a row's end, are zeros from beyond the buffer.
+    // 4 NT (r / 4) + 4 i + r % 4, which makes a lane's channels neighbours; pieces are in an order that depends on the row (key), so that
+    // reads of a column of rows use all banks.  Rows beyond the last, and pieces beyond a row's end, are zeros from beyond the buffer.
     const int r8 = lane >> 3;
     const uint32_t piece = ((lane & 7) ^ (r8 >> 1)) * 16, x_off = static_cast<uint32_t>(r8) * pitch,
                    w_off = static_cast<uint32_t>((r8 >> 2) * (4 * NT) + (r8 & 3)) * pitch;
@@ -71,7 +74,8 @@ __device__ __forceinline__ void split(const SplitArgs &a, uint32_t bx, uint32_t 
             if constexpr (IN == kCodes) {
 #pragma unroll
                 for (int j = 0; j < MT; ++j)
-                    load16_to_lds(xb, beyond ? beyond : x_off + static_cast<uint32_t>(j * 16 + h * 8) * pitch + c, mine_at + (j * 2 + h) * 1024);
+                    load16_to_lds(xb, beyond ? beyond : x_off + static_cast<uint32_t>(j * 16 + h * 8) * pitch + c,
+                                  mine_at + (j * 2 + h) * 1024);
             }
 #pragma unroll
             for (int i = 0; i < NT; ++i)
@@ -107,8 +111,8 @@ __device__ __forceinline__ void split(const SplitArgs &a, uint32_t bx, uint32_t 
     // the lane's two pieces of row l16 of a tile
     const uint32_t at0 = l16 * kStep + ((quarter * 2) ^ (l16 >> 1)) * 16, at1 = at0 ^ 16;
     const auto fetch = [&](int tile) {
-        return __builtin_shufflevector(*reinterpret_cast<const v4i *>(mine + tile * 2048 + at0), *reinterpret_cast<const v4i *>(mine + tile * 2048 + at1), 0, 1, 2,
-                                       3, 4, 5, 6, 7);
+        return __builtin_shufflevector(*reinterpret_cast<const v4i *>(mine + tile * 2048 + at0),
+                                       *reinterpret_cast<const v4i *>(mine + tile * 2048 + at1), 0, 1, 2, 3, 4, 5, 6, 7);
     };
 
     f32x4 acc[NT][MT];
@@ -151,8 +155,9 @@ __device__ __forceinline__ void split(const SplitArgs &a, uint32_t bx, uint32_t 
             }
             const float its_scale = scale_of(top);
             const int its_inverse = __float_as_int(inverse_of(its_scale));
+            // of the quad's lanes 0 .. 3
             const float inverse[4] = {__int_as_float(dpp<0x00>(its_inverse)), __int_as_float(dpp<0x55>(its_inverse)),
-                                      __int_as_float(dpp<0xAA>(its_inverse)), __int_as_float(dpp<0xFF>(its_inverse))};   // of the quad's lanes 0 .. 3
+                                      __int_as_float(dpp<0xAA>(its_inverse)), __int_as_float(dpp<0xFF>(its_inverse))};
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 if (i * 4 < rows_x) {
@@ -248,8 +253,8 @@ __global__ __launch_bounds__(NW * 64) void split_kernel(SplitArgs a) {
 
 // Two products of codes, `b` with fp32 results, and sums: workgroups of b first, then of a, then of the sums.
 template <int OUT, int MT, int NT>
-__global__ __launch_bounds__(NW * 64) void pair_kernel(SplitArgs a, SplitArgs b, hq::Fp8Sums sums, uint32_t a_across, uint32_t b_across, uint32_t a_groups,
-                                                       uint32_t b_groups) {
+__global__ __launch_bounds__(NW * 64) void pair_kernel(SplitArgs a, SplitArgs b, hq::Fp8Sums sums, uint32_t a_across, uint32_t b_across,
+                                                       uint32_t a_groups, uint32_t b_groups) {
     extern __shared__ __attribute__((aligned(1024))) uint8_t lds[];
     if (blockIdx.x < b_groups) {
         split<kCodes, HQ_F32, MT, NT>(b, blockIdx.x % b_across, blockIdx.x / b_across, lds);
@@ -309,7 +314,9 @@ hq_status with_cut(const SplitArgs &a, hq::Fp8Cut cut, hipStream_t st) {
 }
 template <int IN>
 hq_status with_out(const SplitArgs &a, hq::Fp8Cut cut, hq_dtype out, hipStream_t st) {
-    return out == HQ_F16 ? with_cut<IN, HQ_F16>(a, cut, st) : out == HQ_BF16 ? with_cut<IN, HQ_BF16>(a, cut, st) : with_cut<IN, HQ_F32>(a, cut, st);
+    return out == HQ_F16    ? with_cut<IN, HQ_F16>(a, cut, st)
+           : out == HQ_BF16 ? with_cut<IN, HQ_BF16>(a, cut, st)
+                            : with_cut<IN, HQ_F32>(a, cut, st);
 }
 
 }  // namespace
@@ -317,18 +324,20 @@ hq_status with_out(const SplitArgs &a, hq::Fp8Cut cut, hq_dtype out, hipStream_t
 namespace hq {
 
 namespace {
-// A launch takes `begin` us, one round of a wave `round` (latency), a workgroup `fixed` and `each` for a step of a CU that has several; measured
-// with 1 and 16 x 960 -> 3840, 16 and 64 x 4096 -> 4096 (rounds), 512 x 4096 -> 512 and 2048, 512 x 1024 -> 2048, 2048 x 2048 -> 2048 and
-// 2048 x 512 -> 2048 (shares), us in a graph; fp32: what a workgroup takes longer with fp32 results.  On codes a cut of 64 x 64 is for products that give
-// every CU one of them (512 x 4096 -> 2048 10.3 us, 32 x 32 13.9, 64 x 64 tiles 13.0); between those 32 x 64 is no faster than the better of its neighbours by
-// more than 6 %.  Activations that are quantised: there a workgroup takes more channels (16 x 64:
-// 333 x 1024 -> 768 4.6 us, 16 x 32 5.4, 16 x 128 5.2; 16 x 128 where these are more than the CUs: 512 x 1024 -> 1024 5.5, 16 x 64 6.1, 32-bit 6.4 and 8.4).
+// A launch takes `begin` us, one round of a wave `round` (latency), a workgroup `fixed` and `each` for a step of a CU that has several;
+// measured with 1 and 16 x 960 -> 3840, 16 and 64 x 4096 -> 4096 (rounds), 512 x 4096 -> 512 and 2048, 512 x 1024 -> 2048, 2048 x 2048 ->
+// 2048 and 2048 x 512 -> 2048 (shares), us in a graph; fp32: what a workgroup takes longer with fp32 results.  On codes a cut of 64 x 64
+// is for products that give every CU one of them (512 x 4096 -> 2048 10.3 us, 32 x 32 13.9, 64 x 64 tiles 13.0); between those 32 x 64 is
+// no faster than the better of its neighbours by more than 6 %.  Activations that are quantised: there a workgroup takes more channels
+// (16 x 64: 333 x 1024 -> 768 4.6 us, 16 x 32 5.4, 16 x 128 5.2; 16 x 128 where these are more than the CUs: 512 x 1024 -> 1024 5.5, 16 x
+// 64 6.1, 32-bit 6.4 and 8.4).
 struct Cost {
     int mt, nt;
     float begin, fp32, fixed[3], round[3], each[3];   // codes; 16-bit, 32-bit activations
 
     int64_t groups(int64_t m, int64_t n) const { return ((m + 16 * mt - 1) / (16 * mt)) * ((n + 16 * nt - 1) / (16 * nt)); }
-    // (of two products the one with fewer steps has waves that only wait: 1.8 times the fixed part, 2048 x 512 -> 2048 with 8 waves 16.0 us, with 4 11.5)
+    // (of two products the one with fewer steps has waves that only wait: 1.8 times the fixed part, 2048 x 512 -> 2048 with 8 waves 16.0
+    // us, with 4 11.5)
     float workgroup(int64_t steps, int kind, hq_dtype out, bool pair = false) const {
         return (fixed[kind] * (pair ? 1.8f : 1.0f) + steps * each[kind]) * (out == HQ_F32 && !kind ? fp32 : 1.0f);
     }
@@ -349,13 +358,16 @@ Fp8Cut fp8_split_cut(int64_t m, int64_t n, int64_t steps, const hq_dtype *in, hq
     Fp8Cut best{1, 1, 1e30f};
     for (const Cost &c : costs) {
         if ((m + 16 * c.mt - 1) / (16 * c.mt) > 65535) continue;   // (the grid's limit in y)
-        // Fewer workgroups than CUs: each has a CU of its own.  Those that quantise keep a CU's vector units busy, so that a second one on it waits (333 x
-        // 1024 -> 768, 252 of them, 4.5 us, 512 x 1024 -> 1024, 512, 6.1); those on codes wait for loads.  64 x 64 and 16 x 128 fill a CU's LDS: no
-        // more than one for each CU (2048 x 3840 -> 960, 480 of 64 x 64, 24 us, 64 x 128 tiles 16; 1024 x 1024 -> 1024, 512 of 16 x 128, 9.9, two launches 7.7).
+        // Fewer workgroups than CUs: each has a CU of its own.  Those that quantise keep a CU's vector units busy, so that a second one
+        // on it waits (333 x 1024 -> 768, 252 of them, 4.5 us, 512 x 1024 -> 1024, 512, 6.1); those on codes wait for loads.  64 x 64 and
+        // 16 x 128 fill a CU's LDS: no more than one for each CU (2048 x 3840 -> 960, 480 of 64 x 64, 24 us, 64 x 128 tiles 16; 1024 x
+        // 1024 -> 1024, 512 of 16 x 128, 9.9, two launches 7.7).
         const float groups = static_cast<float>(c.groups(m, n)) / cu;
         float share = kind ? ceilf(groups) : std::max(groups, 1.0f);
-        // (32 x 32 in eight waves: LDS for two on a CU, and a last round that is partly filled takes as long; 1429 x 2543 -> 393, 585 of them, 12.5 us)
-        if (c.mt == 2 && groups > 2.0f && 3 * std::min<int64_t>(NW, steps) * wave_bytes(2, 2) > kLdsPerCu) share = 2.0f * ceilf(groups / 2.0f);
+        // (32 x 32 in eight waves: LDS for two on a CU, and a last round that is partly filled takes as long; 1429 x 2543 -> 393, 585 of
+        // them, 12.5 us)
+        if (c.mt == 2 && groups > 2.0f && 3 * std::min<int64_t>(NW, steps) * wave_bytes(2, 2) > kLdsPerCu)
+            share = 2.0f * ceilf(groups / 2.0f);
         if (groups > 1.0f && 2 * NW * wave_bytes(c.mt, c.nt) > kLdsPerCu) continue;
         const float us = c.begin + std::max(c.rounds(steps, kind), share * c.workgroup(steps, kind, out));
         if (us < best.us) best = {c.mt, c.nt, us};
@@ -382,7 +394,8 @@ hq_status fp8_split_pair(const Fp8Product &a, const Fp8Product &b, const Fp8Sums
                                                                                       : pair_with_cut<HQ_F32>(x, y, sums, cut, st);
 }
 
-hq_status fp8_split(const Fp8Product &p, Fp8Cut cut, const void *x, hq_dtype x_dtype, int64_t row_stride, int k, hq_dtype out, hipStream_t st) {
+hq_status fp8_split(const Fp8Product &p, Fp8Cut cut, const void *x, hq_dtype x_dtype, int64_t row_stride, int k, hq_dtype out,
+                    hipStream_t st) {
     const SplitArgs a{p, x, row_stride, k};
     if (!x) return with_out<kCodes>(a, cut, out, st);
     switch (x_dtype) {

@@ -2,8 +2,8 @@
 //
 //     r = (mean x^2 + eps)^-1/2,   n = x r w,   y = R(position) n
 //
-// R turns the channel pairs (i, i + R/2), or (2i, 2i + 1), of the first R = rotary channels by the angles of the token's position; the other channels
-// pass.  Backwards, with g = R^T dy (the opposite angles):
+// R turns the channel pairs (i, i + R/2), or (2i, 2i + 1), of the first R = rotary channels by the angles of the token's position; the
+// other channels pass.  Backwards, with g = R^T dy (the opposite angles):
 //
 //     dw_i = sum over tokens and heads of g_i x_i r,     dx = r (g w - x r mean(g w x r))
 //
@@ -11,13 +11,13 @@
 //
 // All sums in fp32; one rounding, of the result.
 //
-// Bound by memory (two passes over q and k, three backwards).  A head is owned by G neighbouring lanes, a lane owns C channel pairs: it loads C channels of
-// each half of the head (or 2 C neighbours, where these are the pairs), so that both channels of a pair meet in one lane and only
-// the sum of squares crosses lanes (permutes inside a row of 16).  Heads that no such cut fits (more than 64 lanes of the pairs that divide
-// both their rotated and their other channels) take a wave each, whose lanes have pairs 64 apart.
-// 65536 tokens of 32 + 8 heads of 128 in bf16: 252 us (5.3 TB/s, a large copy 5.15); backwards, 32768 tokens: 191 us and 4.5 for the weights' sums
-// (5.2 TB/s).  Few tokens are bound by latency: launch, the position, the tables' row that it names, results (1 token 2.5 us, 1021 tokens of
-// 32 heads of 72 in fp16 5.7).
+// Bound by memory (two passes over q and k, three backwards).  A head is owned by G neighbouring lanes, a lane owns C channel pairs: it
+// loads C channels of each half of the head (or 2 C neighbours, where these are the pairs), so that both channels of a pair meet in one
+// lane and only the sum of squares crosses lanes (permutes inside a row of 16).  Heads that no such cut fits (more than 64 lanes of the
+// pairs that divide both their rotated and their other channels) take a wave each, whose lanes have pairs 64 apart.
+// 65536 tokens of 32 + 8 heads of 128 in bf16: 252 us (5.3 TB/s, a large copy 5.15); backwards, 32768 tokens: 191 us and 4.5 for the
+// weights' sums (5.2 TB/s).  Few tokens are bound by latency: launch, the position, the tables' row that it names, results (1 token 2.5
+// us, 1021 tokens of 32 heads of 72 in fp16 5.7).
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -228,8 +228,8 @@ __global__ __launch_bounds__(256) void heads_kernel(QkArgs a) {
     }
 }
 
-// Any even number of channels up to 1024: a wave for each head, a lane's pairs 64 apart (4096 tokens of 16 heads of 514 in bf16 118 us, of 1024 271, where the
-// kernel above takes 62).
+// Any even number of channels up to 1024: a wave for each head, a lane's pairs 64 apart (4096 tokens of 16 + 1 heads in bf16: of 514
+// channels, 258 of them turned, 96 us, of 1024, 66 turned, 154; 1024 all turned, which the kernel above takes, 56).
 constexpr int kMostPairs = 8;   // of a lane
 template <int DT, bool BACK>
 __global__ __launch_bounds__(256) void wave_kernel(QkArgs a) {
@@ -323,9 +323,9 @@ __global__ __launch_bounds__(256) void wave_kernel(QkArgs a) {
     }
 }
 
-// dw of queries (workgroups of the first half) and keys: the workgroups' parts, of which there are up to 1024.  8 channels a workgroup, 128 threads
-// to a channel with 8 loads under way each: one round of them, where the parts come from other XCDs' caches (1024 parts of 128 channels:
-// 22 us with 16 threads and one load after the other, 13 with 32 and 4 loads).
+// dw of queries (workgroups of the first half) and keys: the workgroups' parts, of which there are up to 1024.  8 channels a workgroup,
+// 128 threads to a channel with 8 loads under way each: one round of them, where the parts come from other XCDs' caches (1024 parts of
+// 128 channels: 22 us with 16 threads and one load after the other, 13 with 32 and 4 loads).
 __global__ __launch_bounds__(1024) void weight_sums_kernel(QkArgs a) {
     __shared__ float s[128][8];
     const uint32_t half = gridDim.x >> 1;
@@ -363,8 +363,8 @@ __global__ __launch_bounds__(1024) void weight_sums_kernel(QkArgs a) {
     }
 }
 
-// Forwards 24 workgroups a CU (65536 tokens of 40 heads of 128 in 16 bits: 252 us, 290 with a workgroup for every 32 heads, 259 with 8 a CU);
-// backwards, where a workgroup keeps sums, 4 (2 to 8 within 1 %).
+// Forwards 24 workgroups a CU (65536 tokens of 40 heads of 128 in 16 bits: 252 us, 290 with a workgroup for every 32 heads, 259 with 8 a
+// CU); backwards, where a workgroup keeps sums, 4 (2 to 8 within 1 %).
 uint32_t blocks_for(uint32_t items, int slots, bool back) {
     const uint32_t all = (items + slots - 1) / slots;
     return std::min<uint32_t>(all, static_cast<uint32_t>(hq::compute_units()) * (back ? 4 : 24));

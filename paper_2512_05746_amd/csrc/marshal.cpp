@@ -565,8 +565,8 @@ bool truth(PyObject *o) {
 // Calls that take activations record nothing for autograd: a tensor that needs a gradient would lose it without a word.
 void expect_no_gradient(const at::Tensor &t, const char *name) {
     if (t.requires_grad() && c10::GradMode::is_enabled())
-        refuse(std::string(name) + " requires a gradient, which this call does not record: make it under torch.no_grad() (or in an autograd "
-                                   "function), with the _backward call for gradients");
+        refuse(std::string(name) + " requires a gradient, which this call does not record: make it under torch.no_grad() (or in an "
+                                   "autograd function), with the _backward call for gradients");
 }
 void expect_no_gradient(PyObject *o, const char *name) {
     if (THPVariable_Check(o)) expect_no_gradient(THPVariable_Unpack(o), name);
@@ -618,7 +618,8 @@ hq::Rows2 memory_of(const Rows &r) {
 }
 hq::Rows2 memory_of(const at::Tensor &t) {
     const int64_t size = static_cast<int64_t>(t.element_size());
-    return {reinterpret_cast<int64_t>(t.const_data_ptr()), {t.size(0), t.size(1)}, {t.stride(0) * size, t.stride(1) * size}, t.size(2) * size};
+    const int64_t at = reinterpret_cast<int64_t>(t.const_data_ptr());
+    return {at, {t.size(0), t.size(1)}, {t.stride(0) * size, t.stride(1) * size}, t.size(2) * size};
 }
 hq::Rows2 memory_of(const void *p, int64_t bytes) { return {reinterpret_cast<int64_t>(p), {1, 1}, {0, 0}, p ? bytes : 0}; }
 void expect_apart(const hq::Rows2 &a, const hq::Rows2 &b, const char *name, const char *other) {
@@ -626,8 +627,8 @@ void expect_apart(const hq::Rows2 &a, const hq::Rows2 &b, const char *name, cons
 }
 hq::Rows2 piece_of(const at::Tensor &t) { return memory_of(t.const_data_ptr(), static_cast<int64_t>(t.nbytes())); }
 // A caller's buffer for y: the workgroups of one launch write it while others still read.
-void expect_result_apart(PyObject *out, const at::Tensor &y, const hq::Rows2 &x, const char *x_name, const at::Tensor &wq, const float *w_scale,
-                         int64_t scales, const void *bias, int64_t n) {
+void expect_result_apart(PyObject *out, const at::Tensor &y, const hq::Rows2 &x, const char *x_name, const at::Tensor &wq,
+                         const float *w_scale, int64_t scales, const void *bias, int64_t n) {
     if (out == Py_None) return;
     const hq::Rows2 to = piece_of(y);
     expect_apart(to, x, "out", x_name);
@@ -710,8 +711,8 @@ PyObject *act_quant_fp8_linear(Args a) {
     at::Tensor space;
     const int64_t bytes = lib.hq_act_quant_fp8_linear_workspace(x.type, x.m, narrow(n), narrow(x.k), dt);
     if (bytes) space = empty({bytes}, at::kByte, x.t);
-    check("hq_act_quant_fp8_linear", call(lib.hq_act_quant_fp8_linear, x.t.const_data_ptr(), x.type, x.stride, u8(wq), sw, b, x.m, narrow(n),
-                                          narrow(x.k), bytes ? space.data_ptr() : nullptr, y.data_ptr(), dt, stream()));
+    check("hq_act_quant_fp8_linear", call(lib.hq_act_quant_fp8_linear, x.t.const_data_ptr(), x.type, x.stride, u8(wq), sw, b, x.m,
+                                          narrow(n), narrow(x.k), bytes ? space.data_ptr() : nullptr, y.data_ptr(), dt, stream()));
     return wrap(y);
 }
 
@@ -808,8 +809,8 @@ Qk qk_of(Args &a) {
             narrow(cos.size(1) * 2), pos, pos_size, static_cast<float>(eps), interleaved ? 1 : 0, {w[0], w[1]}};
 }
 
-// The results: new, or the caller's.  Workgroups read their inputs while others write: a result may lie on the input that the same workgroup
-// reads (q, or dq where there is one, for that of q), and shares memory with nothing else.
+// The results: new, or the caller's.  Workgroups read their inputs while others write: a result may lie on the input that the same
+// workgroup reads (q, or dq where there is one, for that of q), and shares memory with nothing else.
 struct QkOut {
     at::Tensor q, k;
     QkOut(PyObject *out, const Qk &in, const at::Tensor *dq = nullptr, const at::Tensor *dk = nullptr) {
