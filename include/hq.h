@@ -58,7 +58,7 @@ typedef enum {
     HQ_F16 = 0, /* IEEE half */
     HQ_F32 = 1, /* IEEE single */
     HQ_I32 = 2, /* raw int32 accumulators: outputs of the integer stage only */
-    HQ_BF16 = 3 /* bfloat16: the calls on 8-bit floats and on query and key heads only */
+    HQ_BF16 = 3 /* bfloat16: the calls on 8-bit floats, on query and key heads and on 4-bit caches only */
 } hq_dtype;
 
 /* Static, NUL-terminated description of a status code. */
@@ -497,6 +497,83 @@ hq_status hq_qk_norm_rope_backward(const void *dq, const void *dk, const void *q
                                    int64_t positions, int rotary, int interleaved, const void *pos, int pos_size, float eps,
                                    void *workspace, void *q_grad, void *k_grad, float *q_weight_grad,
                                    float *k_weight_grad, void *stream);
+
+/*
+ * ---- a key/value cache in 4 bits ----------------------------------------------------------
+ *
+ * Keys and values of an attention block, kept in pages of page_size tokens.  A head x of a token is kept as H x, H the orthonormal
+ * block-diagonal Hadamard matrix of blocks of had_block channels (symmetric and its own inverse), in E2M1 codes (0, 0.5, 1, 1.5, 2, 3, 4, 6;
+ * bit 3 the sign) with one fp32 scale for each token and head:
+ *
+ *   scale = max |H x| / 6, 1 if that is 0, at least 2^-126;   code = E2M1(H x * (1 / scale)), to nearest, ties to even
+ *
+ * A head that is not finite has a scale of NaN and codes of 0.
+ *
+ *   k        [pages, kv_heads, page_size, pitch / 2] bytes, pitch = d rounded up to a multiple of 32; channel 2 i in the low bits of byte i
+ *   v        [pages, kv_heads, page_size / 8, pitch, 4] bytes: a channel's codes of 8 tokens, token 2 i in the low bits of byte i
+ *   k_scale, v_scale   [pages, kv_heads, page_size]
+ * Channels from d to pitch are not used.
+ *
+ * A call is about t tokens of `batch` sequences, those of sequence b from begins[b] to begins[b + 1] (begins[0] is 0; begins rises to
+ * begins[batch] <= t), or t / batch each where begins is NULL.  They are the newest of the lengths[b] tokens of the sequence: their
+ * places are lengths[b] - n .. lengths[b] - 1, n of them.  Tokens of no sequence (from begins[batch] on), and those whose place would be
+ * negative (lengths[b] < n), are padding.  Place p of sequence b is slot p % page_size of page page_table[b, p / page_size].
+ * Several sequences may share pages that are only read.
+ *
+ *   page_size power of two from 8 on;  d a multiple of 8 up to 256;  had_block power of two up to 128 that divides d;
+ *   table_pages * page_size, t * heads below 2^31.
+ * page_table, lengths and begins are on the device: what they hold is read when the kernel runs.  A place without a page (an entry that is
+ * negative or not below `pages`, a place beyond the table) is never written; what is read there is NaN.  k and v: 16-byte aligned, the
+ * scales too.
+ */
+typedef struct {
+    uint8_t *k, *v;
+    float *k_scale, *v_scale;
+    const int32_t *page_table; /* [batch, table_pages] */
+    const int32_t *lengths;    /* [batch]: tokens of each sequence, those of this call among them */
+    const int32_t *begins;     /* [batch + 1], or NULL */
+    int64_t pages, t;
+    int page_size, kv_heads, d, had_block, batch, table_pages;
+} hq_kv4; /* on the HOST; read before the call returns */
+
+/*
+ * What follows the query/key/value projection, with keys and values going into the cache: the norm and the rotation of hq_qk_norm_rope
+ * (norm = 0: no norm, and no weights) for q [t, heads, d] and k [t, kv_heads, d]; v [t, kv_heads, d] goes in as it is.
+ *
+ *   strides   HOST array, in elements: q token, q head, k token, k head, v token, v head, q_out token, q_out head.  q_out may be q (the
+ *             same memory, the same strides), and shares memory with nothing else.
+ *   cos, sin  [positions, rotary / 2];  pos: the position of each token for its rotation, of pos_size bytes (4 or 8), or NULL for its place in
+ *             the sequence.  At or beyond `positions`: q_out and the token's keys are NaN (rotary = 0: no tables).  Negative: padding.
+ * Padding gets zeros in q_out and is not stored.  No two tokens of a call may have one slot (sequences that share a page they write).
+ */
+hq_status hq_kv4_append(const hq_kv4 *cache, const void *q, const void *k, const void *v, hq_dtype dtype, int heads,
+                        const int64_t *strides, const void *q_weight, const void *k_weight, hq_dtype w_dtype, const float *cos,
+                        const float *sin, int64_t positions, int rotary, int interleaved, const void *pos, int pos_size, int norm,
+                        float eps, void *q_out, void *stream);
+/*
+ * Attention of each token's query heads over its sequence in the cache, query head h over key head h / (heads / kv_heads):
+ *
+ *   out[i, h] = sum_j p_j v_j,   p = softmax over the visible j of scale * q[i, h] . k_j
+ *
+ * Visible to a token at place p: places j <= p, of them, where window is not 0, those with j > p - window or j < sinks.  Without a visible
+ * token, and for padding, out is zeros; where lengths[b] is beyond the table, NaN.
+ *
+ *   strides   HOST array, in elements: q token, q head, out token, out head; channels side by side.  out shares no memory with the inputs.
+ *   scale     finite, magnitude up to 2^100
+ *   workspace hq_kv4_attention_workspace(..) bytes, 16-byte aligned; NULL where that is 0
+ *
+ * Sums and the softmax are fp32.  H q and the weights (1 the largest) times the scales of v are rounded to half, in units of powers of two:
+ * by 2^-11 of each, products below 2^-14 of the largest scale by 2^-25 of that; HQ_F32: in two halves, by 2^-22.  The order of every
+ * sum is fixed by the sizes and what lengths and begins hold: the same inputs give the same bits.
+ */
+int64_t hq_kv4_attention_workspace(const hq_kv4 *cache, hq_dtype dtype, int heads, int window, int sinks);
+hq_status hq_kv4_attention(const hq_kv4 *cache, const void *q, hq_dtype dtype, int heads, const int64_t *strides, float scale,
+                           int window, int sinks, void *workspace, void *out, void *stream);
+/*
+ * The numbers that the cache holds for the call's tokens: k, v [t, kv_heads, d] of `dtype`, dense.  Padding: zeros.  A place without a page:
+ * NaN.  (All tokens of the sequences: begins = the running sums of lengths.)
+ */
+hq_status hq_kv4_read(const hq_kv4 *cache, void *k, void *v, hq_dtype dtype, void *stream);
 
 #ifdef __cplusplus
 }

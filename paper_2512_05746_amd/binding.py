@@ -8,7 +8,7 @@ cannot be loaded or a call is refused, an exception is raised.
 from __future__ import annotations
 
 import ctypes
-from typing import Optional, Tuple
+from typing import NamedTuple, Optional, Tuple, Union
 
 import torch
 
@@ -22,12 +22,20 @@ SYMBOLS = ("hq_status_string", "hq_quantize_weights", "hq_act_hadamard_quant",
            "hq_int_linear_i8", "hq_int_conv2d_i8", "hq_act_hadamard_quant_i8",
            "hq_act_quant_int_conv2d", "hq_act_quant_int_linear",
            "hq_fp8_quantize_rows", "hq_fp8_quantize_blocks", "hq_fp8_linear", "hq_act_quant_fp8_linear",
-           "hq_fp8_linear_backward", "hq_qk_norm_rope", "hq_qk_norm_rope_backward")
+           "hq_fp8_linear_backward", "hq_qk_norm_rope", "hq_qk_norm_rope_backward",
+           "hq_kv4_append", "hq_kv4_attention", "hq_kv4_read")
 # entry points that return the bytes of a workspace
 WORKSPACE_SYMBOLS = ("hq_act_quant_fp8_linear_workspace", "hq_fp8_linear_backward_workspace",
-                     "hq_qk_norm_rope_backward_workspace")
+                     "hq_qk_norm_rope_backward_workspace", "hq_kv4_attention_workspace")
 # entry points that do not return a status
 INFO_SYMBOLS = ("hq_int_conv2d_kernel_name", "hq_fp8_linear_kernel_name", "hq_fp8_linear_backward_kernel_name") + WORKSPACE_SYMBOLS
+
+
+class _Kv4(ctypes.Structure):
+    """hq_kv4 of include/hq.h."""
+    _fields_ = [(n, ctypes.c_void_p) for n in ("k", "v", "k_scale", "v_scale", "page_table", "lengths", "begins")] + [
+        ("pages", ctypes.c_int64), ("t", ctypes.c_int64)] + [
+        (n, ctypes.c_int) for n in ("page_size", "kv_heads", "d", "had_block", "batch", "table_pages")]
 
 
 class HqError(RuntimeError):
@@ -90,6 +98,11 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
     lib.hq_act_quant_fp8_linear_workspace.argtypes = [i32, i64, i32, i32, i32]
     lib.hq_fp8_linear_backward_workspace.argtypes = [i64, i32, i32]
     lib.hq_qk_norm_rope_backward_workspace.argtypes = [i32, i64, i32, i32, i32, i32]
+    cache = ctypes.POINTER(_Kv4)
+    lib.hq_kv4_append.argtypes = [cache, vp, vp, vp, i32, i32, vp, vp, vp, i32, vp, vp, i64, i32, i32, vp, i32, i32, f32, vp, vp]
+    lib.hq_kv4_attention.argtypes = [cache, vp, i32, i32, vp, f32, i32, i32, vp, vp, vp]
+    lib.hq_kv4_attention_workspace.argtypes = [cache, i32, i32, i32, i32]
+    lib.hq_kv4_read.argtypes = [cache, vp, vp, i32, vp]
     for name in SYMBOLS[1:]:
         getattr(lib, name).restype = i32
     for name in WORKSPACE_SYMBOLS:
@@ -335,3 +348,57 @@ def hq_qk_norm_rope_backward(dq: torch.Tensor, dk: torch.Tensor, q: torch.Tensor
     weights, fp32 [d], None for a weight that is None).  out[0] may be dq or q, out[1] dk or k; otherwise they share memory with nothing
     that is passed."""
     return _native().qk_norm_rope_backward(dq, dk, q, k, q_weight, k_weight, cos, sin, positions, eps, interleaved, out)
+
+
+# ---- a key/value cache in 4 bits ---------------------------------------------------------------------
+
+class Kv4Cache(NamedTuple):
+    """Pages of keys and values: each head of each token through the Hadamard transform (blocks of had_block channels, by default the
+    largest power of two that divides d, up to 128), in 4-bit codes with one scale; the layout is in include/hq.h."""
+    k: torch.Tensor
+    v: torch.Tensor
+    k_scale: torch.Tensor
+    v_scale: torch.Tensor
+    d: int
+    had_block: Optional[int] = None
+
+
+def hq_kv4_cache(pages: int, page_size: int, kv_heads: int, d: int, had_block: Optional[int] = None,
+                 device: Union[str, torch.device] = "cuda") -> Kv4Cache:
+    """An empty cache of `pages` pages of page_size tokens (a power of two from 8 on) for kv_heads heads of d channels (a multiple of 8 up
+    to 256)."""
+    pitch = -(-d // 32) * 32
+    zeros = lambda shape, dt: torch.zeros(shape, dtype=dt, device=device)
+    return Kv4Cache(zeros((pages, kv_heads, page_size, pitch // 2), torch.uint8), zeros((pages, kv_heads, page_size // 8, pitch, 4), torch.uint8),
+                    zeros((pages, kv_heads, page_size), torch.float32), zeros((pages, kv_heads, page_size), torch.float32), d, had_block)
+
+
+def hq_kv4_append(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, q_weight: Optional[torch.Tensor], k_weight: Optional[torch.Tensor],
+                  cos: torch.Tensor, sin: torch.Tensor, cache: Kv4Cache, page_table: torch.Tensor, lengths: torch.Tensor,
+                  begins: Optional[torch.Tensor] = None, positions: Optional[torch.Tensor] = None, eps: Optional[float] = 1e-6,
+                  interleaved: bool = False, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """q [t, heads, d] normalised head by head and rotated, returned (or in `out`, which may be q); k [t, kv_heads, d] likewise and v
+    [t, kv_heads, d] as it is into the cache.  Weights, cos and sin as in hq_qk_norm_rope; eps None: no norm, no weights.
+
+    The tokens of sequence b are rows begins[b] .. begins[b + 1] - 1 (int32 [sequences + 1]; None: as many for each), the newest of its
+    lengths[b] (int32) tokens; page_table int32 [sequences, pages of the longest].  positions: int32/int64 [t] for the rotation (None:
+    the place in the sequence; negative: padding).  Tokens of no sequence are padding: zeros, not stored.  No two tokens may have one slot."""
+    return _native().kv4_append(q, k, v, q_weight, k_weight, cos, sin, *cache, page_table, lengths, begins, positions, eps, interleaved, out)
+
+
+def hq_kv4_attention(q: torch.Tensor, cache: Kv4Cache, page_table: torch.Tensor, lengths: torch.Tensor,
+                     begins: Optional[torch.Tensor] = None, scale: Optional[float] = None, window: int = 0, sinks: int = 0,
+                     out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Each of q's [t, heads, d] tokens over the places of its sequence up to its own, in the cache; the tokens are described as in
+    hq_kv4_append, which has stored them.  heads is a multiple of kv_heads.  scale None: d^-1/2.  window: only the last `window` places,
+    its own among them, and the first `sinks` ones (0: all).  Padding, and rows that see nothing: zeros.  `out` [t, heads, d] shares no
+    memory with the inputs."""
+    return _native().kv4_attention(q, *cache, page_table, lengths, begins, scale, window, sinks, out)
+
+
+def hq_kv4_read(cache: Kv4Cache, page_table: torch.Tensor, lengths: torch.Tensor, tokens: int, begins: Optional[torch.Tensor] = None,
+                y_dtype: torch.dtype = torch.float16, out: Optional[Tuple[torch.Tensor, torch.Tensor]] = None
+                ) -> Tuple[torch.Tensor, torch.Tensor]:
+    """(k, v) [tokens, kv_heads, d]: the numbers that the cache holds for a call's tokens (rotated keys), described as in hq_kv4_append;
+    for all tokens of the sequences begins is the running sum of lengths.  Padding: zeros."""
+    return _native().kv4_read(tokens, *cache, page_table, lengths, begins, y_dtype, out)

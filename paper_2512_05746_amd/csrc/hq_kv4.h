@@ -1,0 +1,120 @@
+// A paged key/value cache in 4 bits: where a token's codes lie, which tokens a call is about, and how attention cuts its work.  Host and
+// device arithmetic; what a caller's arrays on the device say (page_table, lengths, begins) is checked here before it becomes an address.
+#pragma once
+#include <stdint.h>
+
+#include "hq.h"
+
+namespace hq {
+
+__host__ __device__ __forceinline__ int kv4_pitch(int d) { return (d + 31) & ~31; }
+__host__ __device__ __forceinline__ int kv4_min(int a, int b) { return a < b ? a : b; }
+__host__ __device__ __forceinline__ int kv4_max(int a, int b) { return a > b ? a : b; }
+
+struct Kv4 {
+    uint8_t *k, *v;             // [pages, kv_heads, page_size, pitch / 2], [pages, kv_heads, page_size / 8, pitch, 4]
+    float *k_scale, *v_scale;   // [pages, kv_heads, page_size]
+    const int32_t *table, *lengths, *begins;
+    int64_t pages;
+    int page_log2, kv_heads, d, pitch, block_log2, batch, table_pages, t, each;   // each: tokens of a sequence where begins is null
+
+    // The first token of sequence s; of `batch`: the end of the last.  In 0 .. t whatever begins holds.
+    __host__ __device__ __forceinline__ int begin(int s) const {
+        if (s == 0) return 0;
+        if (!begins) return s * each;
+        return kv4_max(0, kv4_min(begins[s], t));
+    }
+    __host__ __device__ __forceinline__ int capacity() const { return table_pages << page_log2; }   // (tokens; the host checks that it fits)
+    // The page of a position of sequence s; -1 for a position without one.
+    __host__ __device__ __forceinline__ int64_t page(int s, int position) const {
+        if (position < 0 || position >= capacity()) return -1;
+        const int64_t p = table[static_cast<int64_t>(s) * table_pages + (position >> page_log2)];
+        return p < pages ? (p < 0 ? -1 : p) : -1;
+    }
+    // The first slot of a head of a page: slots are tokens (scales), pitch / 2 bytes of k, a group of 8 of them 4 pitch bytes of v.
+    __host__ __device__ __forceinline__ int64_t slots(int64_t page, int head) const { return (page * kv_heads + head) << page_log2; }
+    __host__ __device__ __forceinline__ int slot(int position) const { return position & ((1 << page_log2) - 1); }
+    __host__ __device__ __forceinline__ int64_t row_bytes() const { return pitch >> 1; }
+};
+
+// Positions are worked on in aligned groups of 8 (a channel's codes of a group share a dword of v), a workgroup each.  Sequence s has the
+// groups from group_begin(s) on, at least as many as its tokens touch; behind the last sequence come groups of tokens of none.
+__host__ __device__ __forceinline__ int kv4_group_begin(int first_token, int s) { return (first_token >> 3) + 2 * s; }
+__host__ __device__ __forceinline__ int kv4_groups(int t, int batch) { return (t >> 3) + 2 * batch + 2; }
+
+// The tokens of a group: `count` rows from token `row` on, at positions from `position` on, which are all in one group of 8.
+struct Kv4Group {
+    int s;           // sequence; batch: none
+    int row, count;
+    int position;    // (of tokens of no sequence: meaningless)
+};
+__host__ __device__ __forceinline__ Kv4Group kv4_group(const Kv4 &c, int s, int index) {
+    const int begin = c.begin(s), j = index - kv4_group_begin(begin, s);
+    if (s >= c.batch) {
+        const int64_t row = begin + int64_t{8} * j;
+        return row < c.t ? Kv4Group{s, static_cast<int>(row), kv4_min(8, c.t - static_cast<int>(row)), 0} : Kv4Group{s, 0, 0, 0};
+    }
+    const int n = c.begin(s + 1) - begin, length = kv4_max(0, c.lengths[s]);
+    const int64_t first = int64_t{length} - n;                       // position of the sequence's first token; negative: no place for it
+    const int64_t group = ((first >> 3) + j) * 8;
+    const int64_t from = group > first ? group : first, to = group + 8 < length ? group + 8 : length;
+    if (n <= 0 || j < 0 || from >= to) return {s, 0, 0, 0};
+    return {s, begin + static_cast<int>(from - first), static_cast<int>(to - from), static_cast<int>(from)};
+}
+
+// The positions that a query at `position` sees: those below `sinks`, and from `from` to itself.
+struct Kv4Seen {
+    int sinks, from;
+};
+__host__ __device__ __forceinline__ Kv4Seen kv4_seen(int position, int window, int sinks) {
+    const int from = window > 0 && position >= window ? position - window + 1 : 0;
+    return {kv4_min(sinks, from), from};
+}
+
+// Attention's rows: row r of a sequence and key head is its new token r / group under query head r % group of that key head; a workgroup
+// takes `rows` of them over a part of their tokens.  Parts are cut so that about `target` workgroups share the tokens of all rows, none of
+// fewer than `least` tokens; a part is a multiple of 32 tokens.
+struct Kv4Cut {
+    int rows, group, target, least, step, window, sinks;
+};
+struct Kv4Span {        // of a sequence: blocks of rows, and the tokens that the largest of them looks at
+    int begin, n, length, blocks, tokens;
+};
+__host__ __device__ __forceinline__ Kv4Span kv4_span(const Kv4 &c, const Kv4Cut &cut, int s) {
+    const int begin = c.begin(s), n = kv4_max(0, c.begin(s + 1) - begin), length = kv4_max(0, c.lengths[s]);
+    const int blocks = static_cast<int>((int64_t{n} * cut.group + cut.rows - 1) / cut.rows);
+    int64_t tokens = kv4_min(length, c.capacity());
+    if (cut.window > 0) {
+        const int64_t most = int64_t{cut.window} + cut.sinks + (cut.rows + cut.group - 1) / cut.group + 64;   // (64: both ranges' ragged ends)
+        tokens = tokens < most ? tokens : most;
+    }
+    return {begin, n, length, blocks, static_cast<int>(tokens)};
+}
+constexpr int kKv4Undivided = 0x7FFFFFFF;   // no sequence has more tokens than a part
+// work: tokens times blocks of rows of all sequences, for one key head
+__host__ __device__ __forceinline__ int kv4_part(const Kv4Cut &cut, int64_t work, int kv_heads) {
+    const int64_t share = (work * kv_heads + cut.target - 1) / cut.target;
+    const int64_t part = share > cut.least ? share : cut.least;
+    const int64_t whole = (part + cut.step - 1) / cut.step * cut.step;
+    return whole < kKv4Undivided ? static_cast<int>(whole) : kKv4Undivided;
+}
+__host__ __device__ __forceinline__ int kv4_parts(const Kv4Span &p, int part) { return p.tokens > part ? (p.tokens + part - 1) / part : 1; }
+
+// The tokens that a block of rows looks at, in tiles of 32 positions: those of the sinks (tiles 0 .. sinks - 1) and those from `from` to `to`.
+struct Kv4Tiles {
+    int sinks, from, to;
+    __host__ __device__ __forceinline__ int count() const { return sinks + (to - from); }
+    __host__ __device__ __forceinline__ int tile(int i) const { return i < sinks ? i : from + (i - sinks); }
+};
+// first, last: positions of the block's first and last row (the last may be negative: nothing is seen)
+__host__ __device__ __forceinline__ Kv4Tiles kv4_tiles(int first, int last, int window, int sinks) {
+    if (last < 0) return {0, 0, 0};
+    const int to = (last >> 5) + 1;
+    const Kv4Seen s = kv4_seen(kv4_max(first, 0), window, sinks);
+    const int from = s.from >> 5;
+    // (a later row of the block can see sinks that the first one has in its window: tiles before `from` are enough)
+    const int before = kv4_min((kv4_seen(last, window, sinks).sinks + 31) >> 5, from);
+    return {before, from, to};
+}
+
+}  // namespace hq

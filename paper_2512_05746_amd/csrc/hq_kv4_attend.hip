@@ -1,0 +1,90 @@
+// Attention over a 4-bit cache: the entry point, and how its work is cut.
+#include <hip/hip_runtime.h>
+#include <math.h>
+#include <stdint.h>
+
+#include <algorithm>
+
+#include "hq_common.h"
+#include "hq_fp8.h"
+#include "hq_kv4_attend.h"
+#include "hq_kv4_check.h"
+
+namespace {
+
+struct Plan {
+    hq::Kv4Shape shape;
+    hq::Kv4Cut cut;
+    bool split;
+    int64_t blocks, slots;
+};
+// Few rows for each key head: the waves of a workgroup take tokens apart.  Otherwise rows of their own.
+Plan plan_of(const hq::Kv4 &c, int heads, hq_dtype dtype, int window, int sinks) {
+    const int group = heads / c.kv_heads, cus = hq::compute_units();
+    const int64_t rows = c.batch ? (int64_t{c.t} * group + c.batch - 1) / c.batch : 0;   // of a sequence, on average
+    Plan p;
+    p.shape.apart = rows <= 64;
+    p.shape.tiles = rows <= 16 || c.d > 128 ? 1 : 2;
+    const int64_t most = int64_t{c.kv_heads} * (int64_t{c.t} * group / p.shape.rows() + c.batch);   // blocks of rows
+    const int target = 4 * cus, step = p.shape.apart ? 128 : 32;
+    const int64_t tokens = window > 0 ? std::min<int64_t>(c.capacity(), int64_t{window} + sinks + 64) : c.capacity();
+    p.cut = hq::Kv4Cut{p.shape.rows(), group, target, p.shape.apart ? 512 : 256, step, window, sinks};
+    p.split = tokens > p.cut.least && most < target;
+    p.blocks = most + (p.split ? target : 0) + 1;
+    p.slots = p.split ? 2 * (target + int64_t{c.kv_heads}) : 0;
+    return p;
+}
+int64_t bytes_of(const Plan &p, int d) { return p.slots * p.shape.rows() * (hq::kv4_pitch(d) + 2) * 4; }
+
+}  // namespace
+
+extern "C" int64_t hq_kv4_attention_workspace(const hq_kv4 *cache, hq_dtype dtype, int heads, int window, int sinks) {
+    hq::Kv4 c;
+    if (!cache || !hq::is_float(dtype) || hq::kv4_check(*cache, heads, &c) != HQ_OK || window < 0 || sinks < 0) return 0;
+    return bytes_of(plan_of(c, heads, dtype, window, sinks), c.d);
+}
+
+extern "C" hq_status hq_kv4_attention(const hq_kv4 *cache, const void *q, hq_dtype dtype, int heads, const int64_t *strides, float scale,
+                                      int window, int sinks, void *workspace, void *out, void *stream) {
+    if (!cache || !strides) return HQ_ERR_NULL;
+    if (!hq::is_float(dtype)) return HQ_ERR_DTYPE;
+    hq::Kv4 c;
+    if (const hq_status s = hq::kv4_check(*cache, heads, &c)) return s;
+    if (c.t > 0 && (!q || !out)) return HQ_ERR_NULL;
+    if (window < 0 || sinks < 0 || !(fabsf(scale) <= 0x1p100f)) return HQ_ERR_SHAPE;
+    if (!hq::aligned_to(q, hq::size_of(dtype)) || !hq::aligned_to(out, hq::size_of(dtype))) return HQ_ERR_ALIGN;
+    if (c.t == 0) return HQ_OK;
+    if (window == 0) sinks = 0;
+    const Plan p = plan_of(c, heads, dtype, window, sinks);
+    if (p.blocks > 0x7FFFFFFF) return HQ_ERR_UNSUPPORTED;
+    if (p.slots && !workspace) return HQ_ERR_NULL;
+    if (!hq::aligned16(workspace)) return HQ_ERR_ALIGN;
+    hq::Kv4Attend a{};
+    a.c = c;
+    a.cut = p.cut;
+    a.q = q;
+    a.out = out;
+    a.q_token = strides[0], a.q_head = strides[1], a.out_token = strides[2], a.out_head = strides[3];
+    a.dtype = dtype;
+    a.heads = heads;
+    a.scale = static_cast<float>(fabs(static_cast<double>(scale)) * 1.4426950408889634 * pow(2.0, -0.5 * c.block_log2));
+    a.negative = scale < 0.0f;
+    a.split = p.split;
+    a.slots = static_cast<int>(p.slots);
+    a.sums = static_cast<float *>(workspace);
+    a.tops = a.sums + p.slots * p.shape.rows() * c.pitch;
+    const hq::LaunchCheck check;
+    const auto st = static_cast<hipStream_t>(stream);
+    const auto blocks = static_cast<unsigned>(p.blocks);
+    switch (c.pitch / 32) {
+        case 1: hq::kv4_attend_launch<1>(a, p.shape, blocks, st); break;
+        case 2: hq::kv4_attend_launch<2>(a, p.shape, blocks, st); break;
+        case 3: hq::kv4_attend_launch<3>(a, p.shape, blocks, st); break;
+        case 4: hq::kv4_attend_launch<4>(a, p.shape, blocks, st); break;
+        case 5: hq::kv4_attend_launch<5>(a, p.shape, blocks, st); break;
+        case 6: hq::kv4_attend_launch<6>(a, p.shape, blocks, st); break;
+        case 7: hq::kv4_attend_launch<7>(a, p.shape, blocks, st); break;
+        default: hq::kv4_attend_launch<8>(a, p.shape, blocks, st); break;
+    }
+    return check.status();
+}

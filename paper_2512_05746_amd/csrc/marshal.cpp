@@ -17,6 +17,8 @@
 #include <c10/core/GradMode.h>
 #include <c10/hip/HIPStream.h>
 
+#include <algorithm>
+#include <cmath>
 #include <initializer_list>
 #include <string>
 
@@ -36,7 +38,8 @@ namespace {
     X(hq_int_conv2d_i8) X(hq_act_hadamard_quant_i8) X(hq_act_quant_int_conv2d) X(hq_act_quant_int_linear) \
     X(hq_fp8_quantize_rows) X(hq_fp8_quantize_blocks) X(hq_fp8_linear) X(hq_act_quant_fp8_linear)                    \
     X(hq_act_quant_fp8_linear_workspace) X(hq_fp8_linear_backward) X(hq_fp8_linear_backward_workspace)               \
-    X(hq_qk_norm_rope) X(hq_qk_norm_rope_backward) X(hq_qk_norm_rope_backward_workspace)
+    X(hq_qk_norm_rope) X(hq_qk_norm_rope_backward) X(hq_qk_norm_rope_backward_workspace)                             \
+    X(hq_kv4_append) X(hq_kv4_attention) X(hq_kv4_attention_workspace) X(hq_kv4_read)
 
 struct Library {
 #define X(name) decltype(&::name) name;
@@ -888,6 +891,198 @@ PyObject *qk_norm_rope_backward(Args a) {
     return wrap({out.q, out.k, qw, kw});
 }
 
+// ---- a key/value cache in 4 bits -----------------------------------------------------------------------------------
+// The cache and a call's sequences: k, v, k_scale, v_scale, d, had_block, page_table, lengths, begins.
+struct Kv4 {
+    hq_kv4 c{};
+    const at::Tensor *k = nullptr;
+    hq::Rows2 memory[7];   // as the checks of results see it
+    static constexpr const char *kNames[7] = {"the cache's k", "the cache's v", "the cache's k_scale", "the cache's v_scale", "page_table", "lengths", "begins"};
+    void expect_apart_from(const hq::Rows2 &m, const char *name) const {
+        for (int i = 0; i < 7; ++i) expect_apart(m, memory[i], name, kNames[i]);
+    }
+};
+const at::Tensor &shaped(Args &a, at::ScalarType dt, at::IntArrayRef shape, const char *name) {
+    const at::Tensor &t = a.device(name);
+    if (t.scalar_type() != dt || t.sizes() != shape) {
+        std::string text = std::string(name) + " must be " + c10::toString(dt) + ", [";
+        for (size_t i = 0; i < shape.size(); ++i) text += (i ? ", " : "") + std::to_string(shape[i]);
+        refuse(text + "]");
+    }
+    return t;
+}
+Kv4 kv4_of(Args &a, int64_t t) {
+    Kv4 r;
+    const at::Tensor &k = a.device("the cache's k");
+    if (k.scalar_type() != at::kByte || k.dim() != 4) refuse("the cache's k must be torch.uint8, [pages, kv_heads, page_size, bytes]");
+    const int64_t pages = k.size(0), heads = k.size(1), page = k.size(2);
+    expect_32bit({heads, page});
+    PyObject *const v_o = a.next(), *const ks_o = a.next(), *const vs_o = a.next();
+    const int d = a.integer();
+    const int block = a.none() ? (a.next(), d > 0 ? std::min(128, d & -d) : 0) : a.integer();
+    if (d <= 0 || block <= 0) refuse("d and had_block must be positive");
+    const int64_t pitch = (int64_t{d} + 31) / 32 * 32;
+    Args from_v{&v_o, 1}, from_ks{&ks_o, 1}, from_vs{&vs_o, 1};
+    if (k.size(3) != pitch / 2 || page % 8) refuse("the cache's k does not match d, or its pages are not a multiple of 8 tokens");
+    const at::Tensor &v = shaped(from_v, at::kByte, {pages, heads, page / 8, pitch, 4}, "the cache's v");
+    const at::Tensor &ks = shaped(from_ks, at::kFloat, {pages, heads, page}, "the cache's k_scale");
+    const at::Tensor &vs = shaped(from_vs, at::kFloat, {pages, heads, page}, "the cache's v_scale");
+    const at::Tensor &table = a.device("page_table");
+    if (table.scalar_type() != at::kInt || table.dim() != 2) refuse("page_table must be torch.int32, [sequences, pages]");
+    const int64_t batch = table.size(0);
+    expect_32bit({batch, table.size(1)});
+    const at::Tensor &lengths = shaped(a, at::kInt, {batch}, "lengths");
+    const at::Tensor *begins = nullptr;
+    if (a.none()) a.next();
+    else begins = &shaped(a, at::kInt, {batch + 1}, "begins");
+    for (const at::Tensor *o : {&v, &ks, &vs, &table, &lengths})
+        if (o->device() != k.device()) refuse("the cache, page_table and lengths must be on one device");
+    if (begins && begins->device() != k.device()) refuse("begins must be on the cache's device");
+    r.k = &k;
+    r.c.k = const_cast<uint8_t *>(u8(k));
+    r.c.v = const_cast<uint8_t *>(u8(v));
+    r.c.k_scale = const_cast<float *>(f32(ks.const_data_ptr()));
+    r.c.v_scale = const_cast<float *>(f32(vs.const_data_ptr()));
+    r.c.page_table = static_cast<const int32_t *>(table.const_data_ptr());
+    r.c.lengths = static_cast<const int32_t *>(lengths.const_data_ptr());
+    r.c.begins = begins ? static_cast<const int32_t *>(begins->const_data_ptr()) : nullptr;
+    r.c.pages = pages;
+    r.c.t = t;
+    r.c.page_size = narrow(page);
+    r.c.kv_heads = narrow(heads);
+    r.c.d = d;
+    r.c.had_block = block;
+    r.c.batch = narrow(batch);
+    r.c.table_pages = narrow(table.size(1));
+    const at::Tensor *all[7] = {&k, &v, &ks, &vs, &table, &lengths, begins};
+    for (int i = 0; i < 7; ++i) r.memory[i] = all[i] ? piece_of(*all[i]) : hq::Rows2{};
+    return r;
+}
+void expect_one_device(const at::Tensor &t, const Kv4 &c, const char *name) {
+    if (t.device() != c.k->device()) refuse(std::string(name) + " must be on the cache's device");
+}
+// q's result: new, or the caller's, which may be q where a workgroup reads what it writes.
+at::Tensor heads_result(PyObject *out, const at::Tensor &q, const Kv4 &c, bool may_be_q) {
+    if (out == Py_None) return empty(q.sizes(), q.scalar_type(), q);
+    const at::Tensor &t = heads_of(out, "out", &q);
+    expect_distinct(t, "out");
+    expect_one_device(t, c, "out");
+    const hq::Rows2 to = memory_of(t), from = memory_of(q);
+    if (!may_be_q || !hq::same_rows(to, from)) expect_apart(to, from, "out", may_be_q ? "q, unless it is q" : "q");
+    c.expect_apart_from(to, "out");
+    return t;
+}
+double real(PyObject *o) {
+    const double v = PyFloat_AsDouble(o);
+    if (v == -1.0 && PyErr_Occurred()) throw PythonError();
+    return v;
+}
+
+PyObject *kv4_append(Args a) {
+    const at::Tensor &q = heads_of(a.next(), "q", nullptr), &k = heads_of(a.next(), "k", nullptr), &v = heads_of(a.next(), "v", nullptr);
+    const hq_dtype type = float_type(q.scalar_type(), "q");
+    for (const at::Tensor *t : {&k, &v})
+        if (t->scalar_type() != q.scalar_type() || t->size(0) != q.size(0) || t->size(2) != q.size(2) || t->size(1) != k.size(1))
+            refuse("k and v must match q in type, tokens and channels, and each other in heads");
+    expect_32bit({q.size(1), k.size(1), q.size(2)});
+    PyObject *w[2] = {a.next(), a.next()};
+    at::ScalarType wdt = q.scalar_type();
+    for (PyObject *o : w)
+        if (THPVariable_Check(o) && THPVariable_Unpack(o).scalar_type() == at::kFloat) wdt = at::kFloat;
+    const void *qw = Args{&w[0], 1}.vec(q.size(2), wdt, "q_weight"), *kw = Args{&w[1], 1}.vec(q.size(2), wdt, "k_weight");
+    const at::Tensor &cos = a.device("cos"), &sin = a.device("sin");
+    if (cos.scalar_type() != at::kFloat || sin.scalar_type() != at::kFloat || cos.dim() != 2 || cos.sizes() != sin.sizes())
+        refuse("cos and sin must be Float, [positions, rotary / 2]");
+    expect_32bit({cos.size(1) * 2});
+    const Kv4 c = kv4_of(a, q.size(0));
+    const at::Tensor *pos = nullptr;
+    if (a.none()) {
+        a.next();
+    } else {
+        pos = &a.device("positions");
+        if ((pos->scalar_type() != at::kInt && pos->scalar_type() != at::kLong) || pos->numel() != q.size(0))
+            refuse("positions must hold one torch.int32 or torch.int64 for each token");
+    }
+    const bool norm = !a.none();
+    const double eps = norm ? real(a.next()) : (a.next(), 0.0);
+    const bool interleaved = truth(a.next());
+    if (k.size(1) != c.c.kv_heads || k.size(2) != c.c.d) refuse("k does not match the cache in heads or channels");
+    for (const at::Tensor *t : {&q, &k, &v, &cos, &sin}) expect_one_device(*t, c, "q, k, v, cos and sin each");
+    for (PyObject *o : w)
+        if (THPVariable_Check(o)) expect_one_device(THPVariable_Unpack(o), c, "a weight");
+    if (pos) expect_one_device(*pos, c, "positions");
+    expect_no_gradient(q, "q");
+    expect_no_gradient(k, "k");
+    expect_no_gradient(v, "v");
+    expect_no_gradient(w[0], "q_weight");
+    expect_no_gradient(w[1], "k_weight");
+    // Workgroups write the cache while others still read: what goes in shares no memory with it.
+    const int64_t weight = q.size(2) * (wdt == at::kFloat ? 4 : static_cast<int64_t>(q.element_size()));
+    const hq::Rows2 in[8] = {memory_of(q), memory_of(k), memory_of(v), memory_of(qw, weight), memory_of(kw, weight), piece_of(cos), piece_of(sin),
+                             pos ? piece_of(*pos) : hq::Rows2{}};
+    static const char *const names[8] = {"q", "k", "v", "q_weight", "k_weight", "cos", "sin", "positions"};
+    for (int i = 0; i < 8; ++i)
+        for (int j = 0; j < 4; ++j) expect_apart(c.memory[j], in[i], Kv4::kNames[j], names[i]);
+    for (int i = 0; i < 4; ++i)
+        for (int j = i + 1; j < 7; ++j) expect_apart(c.memory[i], c.memory[j], Kv4::kNames[i], Kv4::kNames[j]);
+    PyObject *out_o = a.next();
+    const at::Tensor out = heads_result(out_o, q, c, true);
+    if (out_o != Py_None)
+        for (int i = 1; i < 8; ++i) expect_apart(memory_of(out), in[i], "out", names[i]);
+    const int64_t strides[8] = {q.stride(0), q.stride(1), k.stride(0), k.stride(1), v.stride(0), v.stride(1), out.stride(0), out.stride(1)};
+    check("hq_kv4_append",
+          call(lib.hq_kv4_append, &c.c, q.const_data_ptr(), k.const_data_ptr(), v.const_data_ptr(), type, narrow(q.size(1)),
+               static_cast<const int64_t *>(strides), qw, kw, float_type(wdt, "q_weight"), f32(cos.const_data_ptr()), f32(sin.const_data_ptr()),
+               cos.size(0), narrow(cos.size(1) * 2), interleaved ? 1 : 0, pos ? pos->const_data_ptr() : nullptr,
+               pos && pos->scalar_type() == at::kLong ? 8 : 4, norm ? 1 : 0, static_cast<float>(eps), out.data_ptr(), stream()));
+    return wrap(out);
+}
+
+PyObject *kv4_attention(Args a) {
+    const at::Tensor &q = heads_of(a.next(), "q", nullptr);
+    const hq_dtype type = float_type(q.scalar_type(), "q");
+    expect_32bit({q.size(1), q.size(2)});
+    const Kv4 c = kv4_of(a, q.size(0));
+    const float scale = a.none() ? (a.next(), static_cast<float>(1.0 / std::sqrt(static_cast<double>(c.c.d)))) : static_cast<float>(real(a.next()));
+    const int window = a.integer(), sinks = a.integer();
+    if (q.size(2) != c.c.d) refuse("q does not match the cache in channels");
+    expect_one_device(q, c, "q");
+    expect_no_gradient(q, "q");
+    const at::Tensor out = heads_result(a.next(), q, c, false);
+    at::Tensor space;
+    const int heads = narrow(q.size(1));
+    const int64_t bytes = lib.hq_kv4_attention_workspace(&c.c, type, heads, window, sinks);
+    if (bytes) space = empty({bytes}, at::kByte, q);
+    const int64_t strides[4] = {q.stride(0), q.stride(1), out.stride(0), out.stride(1)};
+    check("hq_kv4_attention", call(lib.hq_kv4_attention, &c.c, q.const_data_ptr(), type, heads, static_cast<const int64_t *>(strides), scale, window,
+                                   sinks, bytes ? space.data_ptr() : nullptr, out.data_ptr(), stream()));
+    return wrap(out);
+}
+
+PyObject *kv4_read(Args a) {
+    PyObject *t_o = a.next();
+    const long long t = PyLong_AsLongLong(t_o);
+    if (t == -1 && PyErr_Occurred()) throw PythonError();
+    if (t < 0) refuse("tokens must not be negative");
+    const Kv4 c = kv4_of(a, t);
+    const at::ScalarType dt = a.dtype();
+    const hq_dtype type = float_type(dt, "y_dtype");
+    expect_32bit({t});
+    PyObject *out = a.next();
+    const Pair pair(out);
+    const int64_t shape[3] = {t, c.c.kv_heads, c.c.d};
+    const at::Tensor k = result(pair.a, shape, dt, *c.k), v = result(pair.b, shape, dt, *c.k);
+    if (out != Py_None) {
+        expect_one_device(k, c, "out[0]");
+        expect_one_device(v, c, "out[1]");
+        expect_apart(piece_of(k), piece_of(v), "out[0]", "out[1]");
+        c.expect_apart_from(piece_of(k), "out[0]");
+        c.expect_apart_from(piece_of(v), "out[1]");
+    }
+    check("hq_kv4_read", call(lib.hq_kv4_read, &c.c, k.data_ptr(), v.data_ptr(), type, stream()));
+    return wrap(k, v);
+}
+
 // ---- module -----------------------------------------------------------------------------------------------------
 template <PyObject *(*F)(Args)>
 PyObject *entry(PyObject *, PyObject *const *args, Py_ssize_t n) {
@@ -936,6 +1131,7 @@ PyMethodDef methods[] = {
     HQ_METHOD(act_hadamard_quant_width), HQ_METHOD(conv2d_width),
     HQ_METHOD(fp8_quantize_rows), HQ_METHOD(fp8_quantize_blocks), HQ_METHOD(fp8_linear), HQ_METHOD(act_quant_fp8_linear),
     HQ_METHOD(fp8_linear_backward), HQ_METHOD(qk_norm_rope), HQ_METHOD(qk_norm_rope_backward),
+    HQ_METHOD(kv4_append), HQ_METHOD(kv4_attention), HQ_METHOD(kv4_read),
     {"bind", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(bind)), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 
