@@ -21,8 +21,8 @@ SOURCES = ["hq_hadamard_quant.hip", "hq_int_gemm.hip", "hq_int_gemm_128x128.hip"
            "hq_resident_planes.hip", "hq_resident_bytes.hip", "hq_linear_fp6.hip", "hq_linear_fused.hip",
            "hq_int_gemm_anyk.hip",
            "hq_single_weights.hip", "hq_width_quant.hip", "hq_fp8_quant.hip", "hq_fp8_linear.hip",
-           "hq_fp8_split.hip", "hq_qk_norm_rope.hip", "hq_kv4_cache.hip", "hq_kv4_attend.hip", "hq_kv4_attend_12.hip",
-           "hq_kv4_attend_34.hip", "hq_kv4_attend_56.hip", "hq_kv4_attend_78.hip"]
+           "hq_fp8_split.hip", "hq_qk_norm_rope.hip", "hq_kv4_cache.hip", "hq_kv4_attend.hip"] + [
+           "hq_kv4_attend_%d.hip" % k for k in range(1, 9)]
 HEADERS = ["hq_common.h", "hq_int_gemm_kernel.h", "hq_hadamard_mfma.h", "hq_conv3x3_res_kernel.h",
            "hq_resident_kernel.h", "hq_fp6.h", "hq_buffer.h", "hq_floats.h", "hq_fp8.h",
            "hq_fp8_codes.h", "hq_fp8_product.h", "hq_qk_cut.h", "hq_kv4.h", "hq_kv4_check.h", "hq_kv4_lanes.h", "hq_kv4_attend.h",

@@ -11,6 +11,9 @@ __host__ __device__ __forceinline__ int kv4_pitch(int d) { return (d + 31) & ~31
 __host__ __device__ __forceinline__ int kv4_min(int a, int b) { return a < b ? a : b; }
 __host__ __device__ __forceinline__ int kv4_max(int a, int b) { return a > b ? a : b; }
 
+// (the first page in place of none: what is read there is dropped)
+__host__ __device__ __forceinline__ int64_t kv4_readable(int64_t page) { return page < 0 ? 0 : page; }
+
 struct Kv4 {
     uint8_t *k, *v;             // [pages, kv_heads, page_size, pitch / 2], [pages, kv_heads, page_size / 8, pitch, 4]
     float *k_scale, *v_scale;   // [pages, kv_heads, page_size]
@@ -25,11 +28,14 @@ struct Kv4 {
         return kv4_max(0, kv4_min(begins[s], t));
     }
     __host__ __device__ __forceinline__ int capacity() const { return table_pages << page_log2; }   // (tokens; the host checks that it fits)
-    // The page of a position of sequence s; -1 for a position without one.
-    __host__ __device__ __forceinline__ int64_t page(int s, int position) const {
+    // The page of a position; -1 for a position without one.  entry: reads an entry of the sequence's table.
+    template <class F> __host__ __device__ __forceinline__ int64_t checked(int position, F entry) const {
         if (position < 0 || position >= capacity()) return -1;
-        const int64_t p = table[static_cast<int64_t>(s) * table_pages + (position >> page_log2)];
+        const int64_t p = entry(position >> page_log2);
         return p < pages ? (p < 0 ? -1 : p) : -1;
+    }
+    __host__ __device__ __forceinline__ int64_t page(int s, int position) const {
+        return checked(position, [&](int column) { return table[static_cast<int64_t>(s) * table_pages + column]; });
     }
     // The first slot of a head of a page: slots are tokens (scales), pitch / 2 bytes of k, a group of 8 of them 4 pitch bytes of v.
     __host__ __device__ __forceinline__ int64_t slots(int64_t page, int head) const { return (page * kv_heads + head) << page_log2; }
@@ -91,11 +97,12 @@ __host__ __device__ __forceinline__ Kv4Span kv4_span(const Kv4 &c, const Kv4Cut 
     return {begin, n, length, blocks, static_cast<int>(tokens)};
 }
 constexpr int kKv4Undivided = 0x7FFFFFFF;   // no sequence has more tokens than a part
-// work: tokens times blocks of rows of all sequences, for one key head
-__host__ __device__ __forceinline__ int kv4_part(const Kv4Cut &cut, int64_t work, int kv_heads) {
-    const int64_t share = (work * kv_heads + cut.target - 1) / cut.target;
-    const int64_t part = share > cut.least ? share : cut.least;
-    const int64_t whole = (part + cut.step - 1) / cut.step * cut.step;
+// work: tokens times blocks of rows of all sequences, for one key head, by a sum of up to 2^18 floats: the share is enlarged by more than that
+// sum can be too small
+__host__ __device__ __forceinline__ int kv4_part(const Kv4Cut &cut, float work, int kv_heads) {
+    const float share = work * static_cast<float>(kv_heads) / static_cast<float>(cut.target) * 1.03125f + 1.0f;
+    const int64_t part = share < 0x1p31f ? kv4_max(static_cast<int>(share < 0x1p30f ? share : 0x1p30f), cut.least) : kKv4Undivided;
+    const int64_t whole = share < 0x1p30f ? (part + cut.step - 1) / cut.step * cut.step : kKv4Undivided;
     return whole < kKv4Undivided ? static_cast<int>(whole) : kKv4Undivided;
 }
 __host__ __device__ __forceinline__ int kv4_parts(const Kv4Span &p, int part) { return p.tokens > part ? (p.tokens + part - 1) / part : 1; }

@@ -22,11 +22,10 @@ struct Kv4Attend {
     float *tops;     // [slots, rows, 2]: the reference that a part's sums are relative to, the sum of its weights
 };
 
-// Waves of a workgroup: on the same rows with tokens apart (`apart`), or on rows of their own; row tiles of 16 for each.
+// Tiles of 16 rows a wave, waves a workgroup.
 struct Kv4Shape {
-    int tiles;
-    bool apart;
-    int rows() const { return 16 * tiles * (apart ? 1 : 4); }
+    int tiles, waves;
+    int rows() const { return 16 * tiles * waves; }
 };
 // One launch for heads of up to 32 KS channels (hq_kv4_attend_<..>.hip).
 template <int KS> void kv4_attend_launch(const Kv4Attend &a, Kv4Shape shape, unsigned blocks, hipStream_t st);

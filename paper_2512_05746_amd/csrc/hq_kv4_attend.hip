@@ -18,17 +18,17 @@ struct Plan {
     bool split;
     int64_t blocks, slots;
 };
-// Few rows for each key head: the waves of a workgroup take tokens apart.  Otherwise rows of their own.
 Plan plan_of(const hq::Kv4 &c, int heads, hq_dtype dtype, int window, int sinks) {
     const int group = heads / c.kv_heads, cus = hq::compute_units();
     const int64_t rows = c.batch ? (int64_t{c.t} * group + c.batch - 1) / c.batch : 0;   // of a sequence, on average
     Plan p;
-    p.shape.apart = rows <= 64;
-    p.shape.tiles = rows <= 16 || c.d > 128 ? 1 : 2;
+    const bool few = rows <= 16 || c.pitch > 128;
+    const int64_t items = int64_t{c.kv_heads} * std::max<int64_t>(1, c.batch);
+    p.shape = few ? hq::Kv4Shape{1, items * c.capacity() <= 65536 ? 8 : 4} : hq::Kv4Shape{2, 4};
     const int64_t most = int64_t{c.kv_heads} * (int64_t{c.t} * group / p.shape.rows() + c.batch);   // blocks of rows
-    const int target = 4 * cus, step = p.shape.apart ? 128 : 32;
+    const int target = 4 * cus;
     const int64_t tokens = window > 0 ? std::min<int64_t>(c.capacity(), int64_t{window} + sinks + 64) : c.capacity();
-    p.cut = hq::Kv4Cut{p.shape.rows(), group, target, p.shape.apart ? 512 : 256, step, window, sinks};
+    p.cut = hq::Kv4Cut{p.shape.rows(), group, target, 1024, 32 * p.shape.waves, window, sinks};
     p.split = tokens > p.cut.least && most < target;
     p.blocks = most + (p.split ? target : 0) + 1;
     p.slots = p.split ? 2 * (target + int64_t{c.kv_heads}) : 0;

@@ -11,8 +11,9 @@
 // 16 tokens is token 8 (m / 4) + m % 4 and of the second 4 further on.  v is kept channel by channel for 8 tokens, the order of its operand.
 //
 // Roundings: H q to half (2^-11 of an element), in units of a power of two that leaves the row's largest below 2^12; weights times v_scale to
-// half, in units of the power of two next to the largest v_scale so far (2^-11; below 2^-14 of it, 2^-25 of it).  With WIDE (32-bit
-// results) both are two halves, 2^-22.  Codes are exact, sums are 32 bits.
+// half, in units of the power of two next to the largest v_scale so far (2^-11; below 2^-14 of it, 2^-25 of it).  For half and 32-bit
+// results H q is two halves (2^-22; a rounding of q moves every score of its row, and results were off by twice their own rounding), for
+// 32-bit ones the weights too.  Codes are exact, sums are 32 bits.
 //
 // The reference moves only where s would exceed it by 8 (2^8 times 2 is far inside a half), so most turns leave the sums alone.
 #pragma once
@@ -27,35 +28,46 @@ namespace {
 
 typedef float float4v __attribute__((ext_vector_type(4)));
 
-__device__ __forceinline__ int64_t wave_sum(int64_t v) {
-#pragma unroll
-    for (int i = 1; i < 64; i *= 2) v += __shfl_xor(static_cast<long long>(v), i);
+// Sums over the lanes before and with one, by moves inside rows of 16 lanes and from a row's last lane on.
+template <class T, int CTRL, int ROWS>
+__device__ __forceinline__ T moved(T v) {
+    return __builtin_bit_cast(T, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, ROWS, 0xF, false));
+}
+template <class T>
+__device__ __forceinline__ T wave_prefix(T v) {
+    v += moved<T, 0x111, 0xF>(v);
+    v += moved<T, 0x112, 0xF>(v);
+    v += moved<T, 0x114, 0xF>(v);
+    v += moved<T, 0x118, 0xF>(v);
+    v += moved<T, 0x142, 0xA>(v);
+    v += moved<T, 0x143, 0xC>(v);
     return v;
 }
-__device__ __forceinline__ int wave_prefix(int v, int lane) {   // with its own
-#pragma unroll
-    for (int i = 1; i < 64; i *= 2) {
-        const int o = __shfl_up(v, i);
-        v += lane >= i ? o : 0;
-    }
-    return v;
+template <class T>
+__device__ __forceinline__ T lane_value(T v, int lane) {
+    return __builtin_bit_cast(T, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), lane));
 }
+template <class T>
+__device__ __forceinline__ T wave_sum(T v) { return lane_value(wave_prefix(v), 63); }
 // What the wave's lanes wrote to LDS, to be read by each other.
 __device__ __forceinline__ void wave_sync() {
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
     __builtin_amdgcn_wave_barrier();
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 }
-// Tokens of a part.
+// Tokens of a part: every wave adds up the work by itself, in the same order.
 __device__ __forceinline__ int part_of(const hq::Kv4Attend &a, int lane) {
     if (!a.split) return hq::kKv4Undivided;
-    int64_t work = 0;
-    for (int base = 0; base < a.c.batch; base += 64)
+    float work = 0.0f;
+    for (int base = 0; base < a.c.batch; base += 64) {
+        float mine = 0.0f;
         if (base + lane < a.c.batch) {
             const hq::Kv4Span p = hq::kv4_span(a.c, a.cut, base + lane);
-            work += int64_t{p.blocks} * p.tokens;
+            mine = static_cast<float>(p.blocks) * static_cast<float>(p.tokens);
         }
-    return hq::kv4_part(a.cut, wave_sum(work), a.c.kv_heads);
+        work += wave_sum(mine);
+    }
+    return hq::kv4_part(a.cut, work, a.c.kv_heads);
 }
 
 // What a workgroup works on: a part of the tokens of a block of rows of one key head.
@@ -73,23 +85,23 @@ __device__ __forceinline__ Task task_of(const hq::Kv4Attend &a, int id, int lane
             parts = hq::kv4_parts(p, part);
         }
         const int count = p.blocks * parts * a.c.kv_heads, mine = parts > 1 ? count : 0;
-        const int to = wave_prefix(count, lane), slot_to = wave_prefix(mine, lane);
+        const int to = wave_prefix(count), slot_to = wave_prefix(mine);
         const uint64_t behind = __ballot(base + to > id);
         if (behind) {
             const int at = __ffsll(static_cast<unsigned long long>(behind)) - 1;
-            const int in = id - base - __shfl(to - count, at), blocks = __shfl(p.blocks, at);
-            parts = __shfl(parts, at);
+            const unsigned in = id - base - lane_value(to - count, at), blocks = lane_value(p.blocks, at), of = lane_value(parts, at);
+            const unsigned row_blocks = in / of;
             Task t;
             t.s = from + at;
-            t.slot = slots + __shfl(slot_to - mine, at) + in;
-            t.parts = parts;
-            t.part = in % parts;
-            t.block = in / parts % blocks;
-            t.head = in / parts / blocks;
+            t.slot = slots + lane_value(slot_to - mine, at) + in;
+            t.parts = of;
+            t.part = in - row_blocks * of;
+            t.head = row_blocks / blocks;
+            t.block = row_blocks - t.head * blocks;
             return t;
         }
-        base += __shfl(to, 63);
-        slots += __shfl(slot_to, 63);
+        base += lane_value(to, 63);
+        slots += lane_value(slot_to, 63);
     }
     return {-1, 0, id - base, 0, 1, 0};
 }
@@ -122,10 +134,10 @@ __device__ __forceinline__ void store_all(const hq::Kv4Attend &a, float value, i
 constexpr int lanes_of(int ks) { return ks <= 1 ? 4 : ks <= 2 ? 8 : ks <= 4 ? 16 : 32; }   // that own a row, 8 channels each
 
 // 32 tokens as they are in memory.
-template <int KS> struct Turn32 {
+template <int KS> struct Turn {
     uint32_t k[2][KS], v[2 * KS];
     float4v ks[2], vs[2];
-    bool bad;   // its group of tokens has no page
+    bool bad;   // the lane's group of tokens has no page
 };
 template <int N>
 __device__ __forceinline__ void load_words(const uint8_t *p, uint32_t *w) {
@@ -139,54 +151,152 @@ __device__ __forceinline__ void load_words(const uint8_t *p, uint32_t *w) {
     }
     if constexpr (N > STEP) load_words<N - STEP>(p + 4 * STEP, w + STEP);
 }
+// Waves a SIMD for which registers are kept: loads of other waves and conversions beside products need them.
+constexpr int waves_of(int ks, int r, int qh) { return r == 1 && ks <= 4 ? 3 : ks <= 6 ? 2 : 1; }
+// Conversions and products in the order in which they are written: four conversions, then the products that take them.  (Left to itself the
+// compiler converts everything first, in registers that the sums need.)
+template <int N, int PRODUCTS>
+__device__ __forceinline__ void order() {
+    if constexpr (N > 0) {
+        __builtin_amdgcn_sched_group_barrier(0x2, 4, 0);
+        __builtin_amdgcn_sched_group_barrier(0x8, PRODUCTS, 0);
+        order<N - 1, PRODUCTS>();
+    }
+}
+template <bool B> using Flag = std::integral_constant<bool, B>;
 
-template <int KS, int R, bool APART, bool WIDE>
-__global__ __launch_bounds__(256) void attend_kernel(hq::Kv4Attend a) {
+// R tiles of 16 rows a wave, WAVES waves a workgroup.  Rows that fill more than one wave's tiles: rows of its own for each wave.  Otherwise all
+// waves have the same rows, and tiles of 32 tokens in turn.  QH, PH: halves for an element of H q, for a weight.  WIDE_PAGES: pages of 32
+// tokens or more, so that a tile's place is one number for the wave.
+template <int KS, int R, int WAVES, int QH, int PH, bool WIDE_PAGES>
+__global__ __launch_bounds__(64 * WAVES, waves_of(KS, R, QH)) void attend_kernel(hq::Kv4Attend a) {
     constexpr int DP = 32 * KS, LP = lanes_of(KS), STAGE = DP + 8, ROW = DP + 4;
-    // per wave: a tile of rows as halves (two planes where WIDE), and later their sums
-    constexpr int WAVE_BYTES = 16 * ROW * 4 > 16 * STAGE * 2 * (1 + WIDE) ? 16 * ROW * 4 : 16 * STAGE * 2 * (1 + WIDE);
-    __shared__ __attribute__((aligned(16))) uint8_t lds[4][WAVE_BYTES];
-    __shared__ float row_factor[4][16], row_top[4][16], row_sum[4][16];
+    // per wave: a tile of rows as halves, and later their sums
+    constexpr int WAVE_BYTES = 16 * ROW * 4 > 16 * STAGE * 2 * QH ? 16 * ROW * 4 : 16 * STAGE * 2 * QH;
+    __shared__ __attribute__((aligned(16))) uint8_t lds[WAVES][WAVE_BYTES];
+    __shared__ float row_factor[WAVES][16], row_top[WAVES][16], row_sum[WAVES][16];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), m = lane & 15, g = lane >> 4;
     const Task task = task_of(a, blockIdx.x, lane);
     const int in = lane % LP;
     if (task.s < 0) {
         // rows of no sequence: zeros
         const int begin = a.c.begin(a.c.batch), rows = (a.c.t - begin) * a.heads, from = blockIdx.x - task.block;
-        const int step = (gridDim.x - from) * (256 / LP);
-        for (int r = task.block * (256 / LP) + threadIdx.x / LP; r < rows; r += step)
+        const int step = (gridDim.x - from) * (64 * WAVES / LP);
+        for (int r = task.block * (64 * WAVES / LP) + threadIdx.x / LP; r < rows; r += step)
             store_all<KS>(a, 0.0f, in, (begin + r / a.heads) * a.out_token + r % a.heads * a.out_head);
         return;
     }
-    const int s = __builtin_amdgcn_readfirstlane(task.s), head = __builtin_amdgcn_readfirstlane(task.head);
+    const int s = task.s, head = task.head;
     const hq::Kv4Span span = hq::kv4_span(a.c, a.cut, s);
     if (head >= a.c.kv_heads || (task.parts > 1 && task.slot >= a.slots)) return;
     const int group = a.cut.group, rows = span.n * group;   // (below 2^31: the host checks t x heads)
-    const int row0 = task.block * a.cut.rows + (APART ? 0 : wave * 16 * R);
+    const bool apart = rows - task.block * a.cut.rows <= 16 * R;   // tokens are apart, not rows
+    const int row0 = task.block * a.cut.rows + (apart ? 0 : wave * 16 * R);
+    const int by = apart ? 64 * WAVES / LP : 64 / LP, mine_at = apart ? threadIdx.x / LP : lane / LP;   // rows at once, this lane's
     const auto at_of = [&](int row, int64_t by_token, int64_t by_head) {
-        return (span.begin + row / group) * by_token + (head * group + row % group) * by_head;
+        const int token = row / group;
+        return (span.begin + token) * by_token + (head * group + row - token * group) * by_head;
     };
     if (span.length > a.c.capacity()) {   // the sequence says that it has tokens that no page holds
         if (task.part == 0)
-            for (int r = APART ? wave * (64 / LP) + lane / LP : lane / LP; r < 16 * R && row0 + r < rows; r += (APART ? 256 : 64) / LP)
+            for (int r = mine_at; r < 16 * R && row0 + r < rows; r += by)
                 store_all<KS>(a, __builtin_nanf(""), in, at_of(row0 + r, a.out_token, a.out_head));
         return;
     }
+    // ---- the tokens: the first of them are asked for before the rows are prepared
+    const int last_row = hq::kv4_min(row0 + 16 * R, rows) - 1;
+    const int first_position = span.length - span.n + row0 / group, last_position = row0 < rows ? span.length - span.n + last_row / group : -1;
+    const hq::Kv4Tiles tiles = hq::kv4_tiles(first_position, last_position, a.cut.window, a.cut.sinks);
+    const int seen_from = hq::kv4_seen(last_position, a.cut.window, a.cut.sinks).from;
+    const int step = apart ? WAVES : 1;
+    int share = tiles.count();
+    if (task.parts > 1) share = (share + task.parts * step - 1) / (task.parts * step) * step;
+    const int end = hq::kv4_min(tiles.count(), (task.part + 1) * share);
+    int i = task.part * share + (apart ? wave : 0);
+
+    // Pages of a tile, by scalar loads: vector loads arrive in order, so that waiting for one of these would mean waiting for every k and v
+    // that was asked for before it.
+    constexpr int PAGES = WIDE_PAGES ? 1 : 4;
+    struct Pages {
+        int64_t of[PAGES];   // -1: none
+        __device__ __forceinline__ int64_t at(int part) const {
+            if constexpr (PAGES == 1) return of[0];
+            else return part & 2 ? (part & 1 ? of[3] : of[2]) : (part & 1 ? of[1] : of[0]);
+        }
+    };
+    const auto *const table = reinterpret_cast<const __attribute__((address_space(4))) int32_t *>(
+        reinterpret_cast<uint64_t>(a.c.table + static_cast<int64_t>(s) * a.c.table_pages));
+    const auto pages_of = [&](int index) {
+        const int first = tiles.tile(index) * 32;
+        Pages p;
+#pragma unroll
+        for (int e = 0; e < PAGES; ++e) p.of[e] = a.c.checked(first + 8 * e, [&](int column) { return table[column]; });
+        return p;
+    };
+    Turn<KS> turn;
+    const uint32_t k_lane = (8 * (m >> 2) + (m & 3)) * (DP / 2) + g * (KS * 4), v_lane = g * (DP * 4) + m * (KS * 8);
+    const auto load_k = [&](int index, const Pages &p) {
+        const int first = tiles.tile(index) * 32;
+        const uint8_t *k;
+        const float *ks;
+        if constexpr (WIDE_PAGES) {
+            const int64_t at = a.c.slots(hq::kv4_readable(p.of[0]), head) + a.c.slot(first);
+            k = a.c.k + at * (DP / 2) + k_lane;
+            ks = a.c.k_scale + at + static_cast<uint32_t>(g * 8);
+        } else {
+            const int64_t at = a.c.slots(hq::kv4_readable(p.at(m >> 2)), head) + a.c.slot(first + 8 * (m >> 2)) + (m & 3);
+            k = a.c.k + at * (DP / 2) + g * (KS * 4);
+            ks = a.c.k_scale + a.c.slots(hq::kv4_readable(p.at(g)), head) + a.c.slot(first + 8 * g);
+        }
+        turn.bad = p.at(g) < 0;
+        load_words<KS>(k, turn.k[0]);
+        load_words<KS>(k + 4 * (DP / 2), turn.k[1]);
+#pragma unroll
+        for (int e = 0; e < 2; ++e) turn.ks[e] = reinterpret_cast<const float4v *>(ks)[e];
+    };
+    const auto load_v = [&](int index, const Pages &p) {
+        const int first = tiles.tile(index) * 32;
+        const uint8_t *v;
+        const float *vs;
+        if constexpr (WIDE_PAGES) {
+            const int64_t at = a.c.slots(hq::kv4_readable(p.of[0]), head) + a.c.slot(first);
+            v = a.c.v + at * (DP / 2) + v_lane;
+            vs = a.c.v_scale + at + static_cast<uint32_t>(g * 8);
+        } else {
+            const int64_t at = a.c.slots(hq::kv4_readable(p.at(g)), head) + a.c.slot(first + 8 * g);
+            v = a.c.v + at * (DP / 2) + m * (KS * 8);
+            vs = a.c.v_scale + at;
+        }
+        load_words<2 * KS>(v, turn.v);
+#pragma unroll
+        for (int e = 0; e < 2; ++e) turn.vs[e] = reinterpret_cast<const float4v *>(vs)[e];
+    };
+    // k of a turn is asked for when the products with k of the turn before are done, v likewise; pages a turn before that
+    Pages pages{};
+    if (i < end) {
+        pages = pages_of(i);
+        load_k(i, pages);
+        load_v(i, pages);
+        pages = pages_of(i + step < end ? i + step : i);
+    }
     // ---- the rows: through the transform, to halves, to the lanes of the matrix instruction
-    half8v q[R][KS], q_low[R][WIDE ? KS : 1];
+    half8v q[R][QH][KS];
     float factor[R];
     int position[R];
 #pragma unroll
     for (int r = 0; r < R; ++r) {
-        if (APART && r) __syncthreads();
-        uint8_t *const stage = lds[APART ? 0 : wave];
-        for (int i = APART ? threadIdx.x / LP : lane / LP; i < 16; i += (APART ? 256 : 64) / LP) {
-            const int row = row0 + 16 * r + i;
+        if (apart && r) __syncthreads();
+        const int owner = apart ? 0 : wave;
+        uint8_t *const stage = lds[owner];
+        for (int i2 = mine_at; i2 < 16; i2 += by) {
+            const int row = row0 + 16 * r + i2;
             float x[8];
 #pragma unroll
             for (int e = 0; e < 8; ++e) x[e] = 0.0f;
-            if (row < rows && in * 8 < a.c.d)
-                with_type(a.dtype, [&](auto *t) { load8(static_cast<decltype(t)>(const_cast<void *>(a.q)) + at_of(row, a.q_token, a.q_head) + in * 8, x); });
+            if (row < rows && in * 8 < a.c.d) {
+                const int64_t at = at_of(row, a.q_token, a.q_head) + in * 8;
+                with_type(a.dtype, [&](auto *t) { load8(static_cast<decltype(t)>(const_cast<void *>(a.q)) + at, x); });
+            }
             walsh(x, in, a.c.block_log2);
             uint32_t top = 0;
 #pragma unroll
@@ -206,51 +316,25 @@ __global__ __launch_bounds__(256) void attend_kernel(hq::Kv4Attend a) {
                 lo[e] = static_cast<_Float16>(y - static_cast<float>(hi[e]));
             }
             if (in * 8 < DP) {
-                *reinterpret_cast<half8v *>(stage + (i * STAGE + in * 8) * 2) = hi;
-                if constexpr (WIDE) *reinterpret_cast<half8v *>(stage + (16 * STAGE + i * STAGE + in * 8) * 2) = lo;
+                *reinterpret_cast<half8v *>(stage + (i2 * STAGE + in * 8) * 2) = hi;
+                if constexpr (QH > 1) *reinterpret_cast<half8v *>(stage + (16 * STAGE + i2 * STAGE + in * 8) * 2) = lo;
             }
-            if (in == 0) row_factor[APART ? 0 : wave][i] = f;
+            if (in == 0) row_factor[owner][i2] = f;
         }
-        if constexpr (APART) __syncthreads();
+        if (apart) __syncthreads();
         else wave_sync();
 #pragma unroll
-        for (int e = 0; e < KS; ++e) {
-            q[r][e] = *reinterpret_cast<const half8v *>(stage + (m * STAGE + g * (DP / 4) + e * 8) * 2);
-            if constexpr (WIDE) q_low[r][e] = *reinterpret_cast<const half8v *>(stage + (16 * STAGE + m * STAGE + g * (DP / 4) + e * 8) * 2);
-        }
-        factor[r] = row_factor[APART ? 0 : wave][m];
+        for (int h = 0; h < QH; ++h)
+#pragma unroll
+            for (int e = 0; e < KS; ++e) q[r][h][e] = *reinterpret_cast<const half8v *>(stage + (h * 16 * STAGE + m * STAGE + g * (DP / 4) + e * 8) * 2);
+        factor[r] = row_factor[owner][m];
         const int row = row0 + 16 * r + m;
         position[r] = row < rows ? span.length - span.n + row / group : -1;
-        if constexpr (!APART) wave_sync();
+        if (!apart) wave_sync();
     }
-    // ---- the tokens
-    const int last_row = hq::kv4_min(row0 + 16 * R, rows) - 1;
-    const int first_position = span.length - span.n + row0 / group, last_position = row0 < rows ? span.length - span.n + last_row / group : -1;
-    const hq::Kv4Tiles tiles = hq::kv4_tiles(first_position, last_position, a.cut.window, a.cut.sinks);
-    const int seen_from = hq::kv4_seen(last_position, a.cut.window, a.cut.sinks).from;
-    const int share = ((tiles.count() + task.parts - 1) / task.parts + (APART ? 3 : 0)) & (APART ? ~3 : ~0);
-    const int end = hq::kv4_min(tiles.count(), (task.part + 1) * share);
-    int i = task.part * share + (APART ? wave : 0);
-    constexpr int STEP = APART ? 4 : 1;
-
-    const auto page_of = [&](int tile, int part) { return a.c.page(s, tile * 32 + 8 * part); };
-    const auto load = [&](Turn32<KS> &t, int tile, int64_t k_page, int64_t v_page) {
-        const int k_slot = a.c.slot(tile * 32 + 8 * (m >> 2)) + (m & 3), v_slot = a.c.slot(tile * 32 + 8 * g);
-        t.bad = v_page < 0;
-        const int64_t k_at = a.c.slots(k_page < 0 ? 0 : k_page, head), v_at = a.c.slots(v_page < 0 ? 0 : v_page, head) + v_slot;
-        const uint8_t *k = a.c.k + (k_at + k_slot) * (DP / 2) + g * (KS * 4);
-        load_words<KS>(k, t.k[0]);
-        load_words<KS>(k + 4 * (DP / 2), t.k[1]);
-        load_words<2 * KS>(a.c.v + v_at * (DP / 2) + m * (KS * 8), t.v);
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            t.ks[e] = *reinterpret_cast<const float4v *>(a.c.k_scale + v_at + 4 * e);
-            t.vs[e] = *reinterpret_cast<const float4v *>(a.c.v_scale + v_at + 4 * e);
-        }
-    };
 
     float4v o[R][2 * KS];
-    float top[R], sum[R];            // the reference, this lane's sum of weights
+    float top[R], sum[R];                  // the reference, this lane's sum of weights
     float limit = 0.0f, power = -100.0f;   // the largest v_scale that the reference allows for, its power of two
 #pragma unroll
     for (int r = 0; r < R; ++r) {
@@ -259,141 +343,122 @@ __global__ __launch_bounds__(256) void attend_kernel(hq::Kv4Attend a) {
 #pragma unroll
         for (int e = 0; e < 2 * KS; ++e) o[r][e] = float4v{0.0f, 0.0f, 0.0f, 0.0f};
     }
-    Turn32<KS> next;
-    int64_t k_page = -1, v_page = -1;
-    if (i < end) {
-        const int tile = tiles.tile(i);
-        load(next, tile, page_of(tile, m >> 2), page_of(tile, g));
-        if (i + STEP < end) {
-            k_page = page_of(tiles.tile(i + STEP), m >> 2);
-            v_page = page_of(tiles.tile(i + STEP), g);
-        }
-    }
-    for (; i < end; i += STEP) {
-        const int tile = tiles.tile(i);
-        Turn32<KS> now = next;
-        if (i + STEP < end) {
-            load(next, tiles.tile(i + STEP), k_page, v_page);
-            if (i + 2 * STEP < end) {
-                k_page = page_of(tiles.tile(i + 2 * STEP), m >> 2);
-                v_page = page_of(tiles.tile(i + 2 * STEP), g);
-            }
-        }
+    for (; i < end; i += step) {
+        const int first = tiles.tile(i) * 32, next = i + step < end ? i + step : i;   // (the last turn asks for its own tile again)
         float4v t[R][2];
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
+        for (int r = 0; r < R; ++r) t[r][0] = t[r][1] = float4v{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-            for (int r = 0; r < R; ++r) t[r][h] = float4v{0.0f, 0.0f, 0.0f, 0.0f};
+        for (int e = 0; e < KS; ++e)
 #pragma unroll
-            for (int e = 0; e < KS; ++e) {
-                const half8v k = kv4_halves(now.k[h][e]);
+            for (int h = 0; h < 2; ++h) {
+                const half8v k = kv4_halves(turn.k[h][e]);
 #pragma unroll
-                for (int r = 0; r < R; ++r) {
-                    if constexpr (WIDE) t[r][h] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, q_low[r][e], t[r][h], 0, 0, 0);
-                    t[r][h] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, q[r][e], t[r][h], 0, 0, 0);
-                }
+                for (int r = 0; r < R; ++r)
+#pragma unroll
+                    for (int l = QH - 1; l >= 0; --l) t[r][h] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, q[r][l][e], t[r][h], 0, 0, 0);
             }
-        }
-        if (now.bad) now.ks[0] = now.ks[1] = float4v{1.0f, 1.0f, 1.0f, 1.0f} * __builtin_nanf("");
-        const int first = tile * 32;
-        const bool whole = first + 31 <= first_position && (first >= seen_from || first + 32 <= a.cut.sinks);
-        const int token = first + 8 * g;
-        if (!whole) {
-            // scales behind the sequence's end are whatever the page held
-#pragma unroll
-            for (int h = 0; h < 2; ++h)
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    if (token + 4 * h + e >= span.length) now.ks[h][e] = now.vs[h][e] = 0.0f;
-        }
-        uint32_t seen[R];   // a bit for each of the lane's 8 tokens
-        float most[R];
-        bool move = false;
-        float v_top = 0.0f;
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) v_top = fmaxf(v_top, now.vs[h][e]);
-        move = v_top >= limit;
+        order<2 * KS, R * QH>();
 #pragma unroll
         for (int r = 0; r < R; ++r) {
-            seen[r] = 0xFFu;
-            if (!whole) {
+            t[r][0] *= turn.ks[0];
+            t[r][1] *= turn.ks[1];
+        }
+        const bool bad = turn.bad;
+        __builtin_amdgcn_sched_barrier(0);
+        load_k(next, pages);
+        __builtin_amdgcn_sched_barrier(0);
+        float scale_v[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) scale_v[e] = turn.vs[e >> 2][e & 3];
+        const bool whole = first + 31 <= first_position && (first >= seen_from || first + 32 <= a.cut.sinks) && !__any(bad);
+        if (!whole) {
+            const int token = first + 8 * g;
+            // A scale of v that is not finite makes the scores of the rows that see its token NaN instead, so that it does not meet the weight 0
+            // of those that do not; behind the sequence's end scales are whatever the page held.
+            uint32_t odd = bad ? 0xFFu : 0;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                float &x = scale_v[e];
+                if (!(fabsf(x) < __builtin_inff())) odd |= 1u << e;
+                if (odd >> e & 1 || token + e >= span.length) x = 0.0f;
+            }
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
                 const int from = a.cut.window > 0 && position[r] >= a.cut.window ? position[r] - a.cut.window + 1 : 0;
-                seen[r] = 0;
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
                     const int j = token + e;
-                    if (j <= position[r] && (j >= from || j < a.cut.sinks)) seen[r] |= 1u << e;
+                    const bool seen = j <= position[r] && (j >= from || j < a.cut.sinks);
+                    t[r][e >> 2][e & 3] = seen ? odd >> e & 1 ? __builtin_nanf("") : t[r][e >> 2][e & 3] : -__builtin_inff();
                 }
             }
-            most[r] = -__builtin_inff();
+        }
+        float most[R];
+        const float v_most = fmaxf(fmaxf(fmaxf(scale_v[0], scale_v[1]), fmaxf(scale_v[2], scale_v[3])),
+                                   fmaxf(fmaxf(scale_v[4], scale_v[5]), fmaxf(scale_v[6], scale_v[7])));
+        bool move = v_most >= limit;
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                t[r][h] *= now.ks[h];
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    if (!whole && !(seen[r] >> (4 * h + e) & 1)) t[r][h][e] = -__builtin_inff();
-                    most[r] = fmaxf(most[r], t[r][h][e]);
-                }
-            }
+        for (int r = 0; r < R; ++r) {
+            most[r] = fmaxf(fmaxf(fmaxf(t[r][0][0], t[r][0][1]), fmaxf(t[r][0][2], t[r][0][3])), fmaxf(fmaxf(t[r][1][0], t[r][1][1]), fmaxf(t[r][1][2], t[r][1][3])));
             most[r] *= factor[r];
             move |= most[r] > top[r] - power + 8.0f;
         }
         if (__any(move)) {
-            v_top = fmaxf(v_top, __shfl_xor(v_top, 16));
+            float v_top = fmaxf(v_most, __shfl_xor(v_most, 16));
             v_top = fmaxf(v_top, __shfl_xor(v_top, 32));
             const float before = power;
             if (v_top >= limit && v_top > 0.0f) {
                 const int p = hq::kv4_max(-100, hq::kv4_min(100, __builtin_amdgcn_frexp_expf(v_top) - 1));
                 power = fmaxf(power, static_cast<float>(p));
-                limit = __builtin_ldexpf(2.0f, static_cast<int>(power));
-                if (power == 100.0f) limit = __builtin_inff();
+                limit = power == 100.0f ? __builtin_inff() : __builtin_ldexpf(2.0f, static_cast<int>(power));
             }
 #pragma unroll
             for (int r = 0; r < R; ++r) {
-                float top_here = fmaxf(most[r], __shfl_xor(most[r], 16));
-                top_here = fmaxf(top_here, __shfl_xor(top_here, 32));
-                const float moved = fmaxf(top[r] - before, top_here) + power;
-                const float by = top[r] == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(top[r] - moved);
-                top[r] = moved;
-                sum[r] *= by;
+                float here = fmaxf(most[r], __shfl_xor(most[r], 16));
+                here = fmaxf(here, __shfl_xor(here, 32));
+                const float to = fmaxf(top[r] - before, here) + power;
+                const float f = top[r] == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(top[r] - to);
+                top[r] = to;
+                sum[r] *= f;
 #pragma unroll
-                for (int e = 0; e < 2 * KS; ++e) o[r][e] *= by;
+                for (int e = 0; e < 2 * KS; ++e) o[r][e] *= f;
             }
         }
-        half8v p[R], p_low[WIDE ? R : 1];
+        half8v p[R][PH];
 #pragma unroll
         for (int r = 0; r < R; ++r) {
             const float reference = top[r] == -__builtin_inff() ? 0.0f : top[r];
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    float w = __builtin_amdgcn_exp2f(fmaf(t[r][h][e], factor[r], -reference));
-                    float y = w * now.vs[h][e];
-                    if (!whole && !(seen[r] >> (4 * h + e) & 1)) w = y = 0.0f;
-                    sum[r] += w;
-                    p[r][4 * h + e] = static_cast<_Float16>(y);
-                    if constexpr (WIDE) p_low[r][4 * h + e] = static_cast<_Float16>(y - static_cast<float>(p[r][4 * h + e]));
-                }
-        }
-#pragma unroll
-        for (int e = 0; e < 2 * KS; ++e) {
-            const half8v v = kv4_halves(now.v[e]);
-#pragma unroll
-            for (int r = 0; r < R; ++r) {
-                if constexpr (WIDE) o[r][e] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, p_low[r], o[r][e], 0, 0, 0);
-                o[r][e] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, p[r], o[r][e], 0, 0, 0);
+            for (int e = 0; e < 8; ++e) {
+                const float w = __builtin_amdgcn_exp2f(fmaf(t[r][e >> 2][e & 3], factor[r], -reference));
+                const float y = w * scale_v[e];
+                sum[r] += w;
+                p[r][0][e] = static_cast<_Float16>(y);
+                if constexpr (PH > 1) p[r][1][e] = static_cast<_Float16>(y - static_cast<float>(p[r][0][e]));
             }
         }
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int e = 0; e < 2 * KS; ++e) {
+            const half8v v = kv4_halves(turn.v[e]);
+#pragma unroll
+            for (int r = 0; r < R; ++r)
+#pragma unroll
+                for (int l = PH - 1; l >= 0; --l) o[r][e] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, p[r][l], o[r][e], 0, 0, 0);
+        }
+        order<2 * KS, R * PH>();
+        __builtin_amdgcn_sched_barrier(0);
+        load_v(next, pages);
+        __builtin_amdgcn_sched_barrier(0);
+        pages = pages_of(i + 2 * step < end ? i + 2 * step : next);
     }
     // ---- the waves' sums together, and out
 #pragma unroll
     for (int r = 0; r < R; ++r) {
         sum[r] += __shfl_xor(sum[r], 16);
         sum[r] += __shfl_xor(sum[r], 32);
-        if constexpr (APART) __syncthreads();
+        if (apart) __syncthreads();
         else wave_sync();
         float *const mine = reinterpret_cast<float *>(lds[wave]);
         // lane (m, g) has channels 2 KS (4 g + i) + e of row m
@@ -408,24 +473,26 @@ __global__ __launch_bounds__(256) void attend_kernel(hq::Kv4Attend a) {
             row_top[wave][m] = top[r];
             row_sum[wave][m] = sum[r];
         }
-        if constexpr (APART) __syncthreads();
+        if (apart) __syncthreads();
         else wave_sync();
-        for (int i2 = APART ? threadIdx.x / LP : lane / LP; i2 < 16; i2 += (APART ? 256 : 64) / LP) {
+        for (int i2 = mine_at; i2 < 16; i2 += by) {
             const int row = row0 + 16 * r + i2;
             if (row >= rows) continue;
             float x[8], weight, reference;
-            if constexpr (APART) {
-                reference = fmaxf(fmaxf(row_top[0][i2], row_top[1][i2]), fmaxf(row_top[2][i2], row_top[3][i2]));
+            if (apart) {
+                reference = row_top[0][i2];
+#pragma unroll
+                for (int w = 1; w < WAVES; ++w) reference = fmaxf(reference, row_top[w][i2]);
                 weight = 0.0f;
 #pragma unroll
                 for (int e = 0; e < 8; ++e) x[e] = 0.0f;
 #pragma unroll
-                for (int w = 0; w < 4; ++w) {
-                    const float by = row_top[w][i2] == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(row_top[w][i2] - reference);
-                    weight += by * row_sum[w][i2];
+                for (int w = 0; w < WAVES; ++w) {
+                    const float f = row_top[w][i2] == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(row_top[w][i2] - reference);
+                    weight += f * row_sum[w][i2];
                     if (in * 8 < DP) {
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) x[e] += by * reinterpret_cast<const float *>(lds[w])[i2 * ROW + in * 8 + e];
+                        for (int e = 0; e < 8; ++e) x[e] += f * reinterpret_cast<const float *>(lds[w])[i2 * ROW + in * 8 + e];
                     }
                 }
             } else {
@@ -434,10 +501,11 @@ __global__ __launch_bounds__(256) void attend_kernel(hq::Kv4Attend a) {
 #pragma unroll
                 for (int e = 0; e < 8; ++e) x[e] = in * 8 < DP ? mine[i2 * ROW + in * 8 + e] : 0.0f;
             }
+            if (span.length - span.n + row / group < 0) weight = 0.0f;   // (it sees nothing, whatever its query is)
             if (task.parts == 1) {
                 store_row<KS>(a, x, weight, in, at_of(row, a.out_token, a.out_head));
             } else {
-                const int64_t at = int64_t{task.slot} * a.cut.rows + (APART ? 0 : wave * 16 * R) + 16 * r + i2;
+                const int64_t at = int64_t{task.slot} * a.cut.rows + (apart ? 0 : wave * 16 * R) + 16 * r + i2;
                 if (in * 8 < DP) store8(a.sums + at * DP + in * 8, x);
                 if (in == 0) {
                     a.tops[2 * at] = reference;
@@ -470,7 +538,7 @@ __global__ __launch_bounds__(256) void join_kernel(hq::Kv4Attend a) {
             const int parts = hq::kv4_parts(p, part);
             mine = parts > 1 ? p.blocks * parts * a.c.kv_heads : 0;
         }
-        slots += static_cast<int>(wave_sum(mine));
+        slots += wave_sum(mine);
     }
     const hq::Kv4Span span = hq::kv4_span(a.c, a.cut, s);
     const int parts = hq::kv4_parts(span, part);
@@ -492,13 +560,19 @@ __global__ __launch_bounds__(256) void join_kernel(hq::Kv4Attend a) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) x[e] = x[e] * mine + other[e] * by;
     };
-    for (int p = slot; p < parts; p += SLOTS) {
-        const int64_t at = first + int64_t{p} * a.cut.rows;
-        float y[8];
+    // four parts at a time: their loads are under way together
+    for (int p = slot; p < parts; p += 4 * SLOTS) {
+        float y[4][8], tops[4], sums[4];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) y[e] = 0.0f;
-        if (in * 8 < DP) load8(a.sums + at * DP + in * 8, y);
-        add(a.tops[2 * at], a.tops[2 * at + 1], y);
+        for (int i = 0; i < 4; ++i) {
+            const int there = p + i * SLOTS < parts ? p + i * SLOTS : p;
+            const int64_t at = first + int64_t{there} * a.cut.rows;
+            tops[i] = a.tops[2 * at];
+            sums[i] = there == p && i ? 0.0f : a.tops[2 * at + 1];
+            load8(a.sums + at * DP + (in * 8 < DP ? in * 8 : 0), y[i]);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) add(tops[i], sums[i], y[i]);
     }
 #pragma unroll
     for (int e = 0; e < 8; ++e) x_of[slot][in * 8 + e] = x[e];
@@ -523,19 +597,24 @@ namespace hq {
 
 template <int KS>
 void kv4_attend_launch(const Kv4Attend &a, Kv4Shape shape, unsigned blocks, hipStream_t st) {
-    const auto go = [&](auto tiles, auto apart, auto wide) {
-        attend_kernel<KS, decltype(tiles)::value, decltype(apart)::value, decltype(wide)::value><<<blocks, 256, 0, st>>>(a);
+    const auto go = [&](auto tiles, auto waves, auto q_halves, auto p_halves, auto wide_pages) {
+        constexpr int R = decltype(tiles)::value, WAVES = decltype(waves)::value;
+        attend_kernel<KS, R, WAVES, decltype(q_halves)::value, decltype(p_halves)::value, decltype(wide_pages)::value><<<blocks, 64 * WAVES, 0, st>>>(a);
     };
-    const auto with_wide = [&](auto tiles, auto apart) {
-        if (a.dtype == HQ_F32) go(tiles, apart, std::true_type{});
-        else go(tiles, apart, std::false_type{});
+    const auto with_pages = [&](auto tiles, auto waves, auto q_halves, auto p_halves) {
+        if (a.c.page_log2 >= 5) go(tiles, waves, q_halves, p_halves, Flag<true>{});
+        else go(tiles, waves, q_halves, p_halves, Flag<false>{});
     };
-    if (shape.apart && shape.tiles == 1) with_wide(std::integral_constant<int, 1>{}, std::true_type{});
-    else if (shape.tiles == 1) with_wide(std::integral_constant<int, 1>{}, std::false_type{});
-    else if constexpr (KS <= 4) {
-        if (shape.apart) with_wide(std::integral_constant<int, 2>{}, std::true_type{});
-        else with_wide(std::integral_constant<int, 2>{}, std::false_type{});
-    }
+    const auto with_halves = [&](auto tiles, auto waves) {
+        const std::integral_constant<int, 1> one;
+        const std::integral_constant<int, 2> two;
+        if (a.dtype == HQ_F32) with_pages(tiles, waves, two, two);
+        else if (a.dtype == HQ_F16) with_pages(tiles, waves, two, one);
+        else with_pages(tiles, waves, one, one);
+    };
+    if (shape.tiles == 1 && shape.waves == 8) with_halves(std::integral_constant<int, 1>{}, std::integral_constant<int, 8>{});
+    else if (shape.tiles == 1) with_halves(std::integral_constant<int, 1>{}, std::integral_constant<int, 4>{});
+    else if constexpr (KS <= 4) with_halves(std::integral_constant<int, 2>{}, std::integral_constant<int, 4>{});
     if (a.split) join_kernel<KS><<<static_cast<unsigned>(a.c.t) * a.heads, 256, 0, st>>>(a);
 }
 

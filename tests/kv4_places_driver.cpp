@@ -57,11 +57,11 @@ static void groups(const Call &call, bool sound) {
 // tasks stay below what the host allots; every row's visible tokens are in its tiles
 static void tasks(const Call &call, const Kv4Cut &cut, bool sound) {
     const Kv4 &c = call.c;
-    int64_t work = 0;
+    float work = 0.0f;
     for (int s = 0; s < c.batch; ++s) {
         const Kv4Span p = kv4_span(c, cut, s);
         EXPECT(p.begin >= 0 && p.n >= 0 && p.begin + int64_t{p.n} <= c.t && p.tokens >= 0 && p.tokens <= c.capacity(), "span");
-        work += int64_t{p.blocks} * p.tokens;
+        work += static_cast<float>(p.blocks) * static_cast<float>(p.tokens);
     }
     const int part = kv4_part(cut, work, c.kv_heads);
     EXPECT(part == kKv4Undivided || part % cut.step == 0, "part %d", part);
