@@ -78,34 +78,45 @@ __host__ __device__ __forceinline__ Kv4Seen kv4_seen(int position, int window, i
 }
 
 // Attention's rows: row r of a sequence and key head is its new token r / group under query head r % group of that key head; a workgroup
-// takes `rows` of them over a part of their tokens.  Parts are cut so that about `target` workgroups share the tokens of all rows, none of
-// fewer than `least` tokens; a part is a multiple of 32 tokens.
+// takes rows() of them over a part of their tokens, in steps of 32 tokens for a wave.  Parts are cut so that about `target` workgroups share
+// the steps of all rows, none much shorter than `least` steps.
 struct Kv4Cut {
-    int rows, group, target, least, step, window, sinks;
+    int rows_log2, waves_log2, group, target, least, window, sinks;
+    int reach;                                                  // tokens that a block of rows sees at most; window and sinks with ragged ends
+    uint32_t magic, shift;                                      // exact division by group
+    __host__ __device__ __forceinline__ int token_of(int row) const {
+        return group == 1 ? row : static_cast<int>(static_cast<uint32_t>(uint64_t{static_cast<uint32_t>(row)} * magic >> 32) >> shift);
+    }
+    __host__ __device__ __forceinline__ int rows() const { return 1 << rows_log2; }
 };
-struct Kv4Span {        // of a sequence: blocks of rows, and the tokens that the largest of them looks at
-    int begin, n, length, blocks, tokens;
+inline int kv4_reach(int window, int sinks, int rows, int group) {
+    const int64_t most = int64_t{window} + sinks + (rows + group - 1) / group + 64;   // (64: the ragged ends of both ranges)
+    return window > 0 && most < 0x7FFFFFFF ? static_cast<int>(most) : 0x7FFFFFFF;
+}
+struct Kv4Span {        // of a sequence: blocks of rows, and the steps through the tokens that the largest of them looks at
+    int begin, n, length, blocks, steps;
 };
 __host__ __device__ __forceinline__ Kv4Span kv4_span(const Kv4 &c, const Kv4Cut &cut, int s) {
     const int begin = c.begin(s), n = kv4_max(0, c.begin(s + 1) - begin), length = kv4_max(0, c.lengths[s]);
-    const int blocks = static_cast<int>((int64_t{n} * cut.group + cut.rows - 1) / cut.rows);
-    int64_t tokens = kv4_min(length, c.capacity());
-    if (cut.window > 0) {
-        const int64_t most = int64_t{cut.window} + cut.sinks + (cut.rows + cut.group - 1) / cut.group + 64;   // (64: both ranges' ragged ends)
-        tokens = tokens < most ? tokens : most;
-    }
-    return {begin, n, length, blocks, static_cast<int>(tokens)};
+    const int blocks = static_cast<int>((static_cast<uint32_t>(n) * cut.group + cut.rows() - 1) >> cut.rows_log2);   // (t x heads is below 2^31)
+    const int tokens = kv4_min(kv4_min(length, c.capacity()), cut.reach);
+    // rows for one wave are given to all waves, which share the tokens
+    const bool apart = static_cast<uint32_t>(n) * cut.group <= static_cast<uint32_t>(cut.rows() >> cut.waves_log2);
+    return {begin, n, length, blocks, static_cast<int>((static_cast<uint32_t>(tokens) + 31) >> (apart ? 5 + cut.waves_log2 : 5))};
 }
-constexpr int kKv4Undivided = 0x7FFFFFFF;   // no sequence has more tokens than a part
-// work: tokens times blocks of rows of all sequences, for one key head, by a sum of up to 2^18 floats: the share is enlarged by more than that
+constexpr int kKv4Undivided = 0x7FFFFFFF;   // no sequence has more steps than a part
+// work: steps times blocks of rows of all sequences, for one key head, by a sum of up to 2^18 floats: the share is enlarged by more than that
 // sum can be too small
 __host__ __device__ __forceinline__ int kv4_part(const Kv4Cut &cut, float work, int kv_heads) {
     const float share = work * static_cast<float>(kv_heads) / static_cast<float>(cut.target) * 1.03125f + 1.0f;
-    const int64_t part = share < 0x1p31f ? kv4_max(static_cast<int>(share < 0x1p30f ? share : 0x1p30f), cut.least) : kKv4Undivided;
-    const int64_t whole = share < 0x1p30f ? (part + cut.step - 1) / cut.step * cut.step : kKv4Undivided;
-    return whole < kKv4Undivided ? static_cast<int>(whole) : kKv4Undivided;
+    if (!(share < 0x1p30f)) return kKv4Undivided;
+    return kv4_max(static_cast<int>(share), cut.least);
 }
-__host__ __device__ __forceinline__ int kv4_parts(const Kv4Span &p, int part) { return p.tokens > part ? (p.tokens + part - 1) / part : 1; }
+// (to the nearest: no part of less than two thirds)
+__host__ __device__ __forceinline__ int kv4_parts(const Kv4Span &p, int part) {
+    const uint32_t parts = (static_cast<uint32_t>(p.steps) + (static_cast<uint32_t>(part) >> 1)) / static_cast<uint32_t>(part);
+    return parts > 1 ? static_cast<int>(parts) : 1;
+}
 
 // The tokens that a block of rows looks at, in tiles of 32 positions: those of the sinks (tiles 0 .. sinks - 1) and those from `from` to `to`.
 struct Kv4Tiles {

@@ -28,8 +28,10 @@ Plan plan_of(const hq::Kv4 &c, int heads, hq_dtype dtype, int window, int sinks)
     const int64_t most = int64_t{c.kv_heads} * (int64_t{c.t} * group / p.shape.rows() + c.batch);   // blocks of rows
     const int target = 4 * cus;
     const int64_t tokens = window > 0 ? std::min<int64_t>(c.capacity(), int64_t{window} + sinks + 64) : c.capacity();
-    p.cut = hq::Kv4Cut{p.shape.rows(), group, target, 1024, 32 * p.shape.waves, window, sinks};
-    p.split = tokens > p.cut.least && most < target;
+    const hq::Magic31 m = hq::magic31(group);
+    p.cut = hq::Kv4Cut{hq::ilog2(p.shape.rows()), hq::ilog2(p.shape.waves), group, target, 8, window, sinks,
+                       hq::kv4_reach(window, sinks, p.shape.rows(), group), m.m, m.s};
+    p.split = tokens > 12 * 32 * (p.shape.tiles == 1 && rows <= 16 ? p.shape.waves : 1) && most < target;
     p.blocks = most + (p.split ? target : 0) + 1;
     p.slots = p.split ? 2 * (target + int64_t{c.kv_heads}) : 0;
     return p;

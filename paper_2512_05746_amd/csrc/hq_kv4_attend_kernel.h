@@ -55,7 +55,7 @@ __device__ __forceinline__ void wave_sync() {
     __builtin_amdgcn_wave_barrier();
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 }
-// Tokens of a part: every wave adds up the work by itself, in the same order.
+// Steps of a part: every wave adds up the work by itself, in the same order.
 __device__ __forceinline__ int part_of(const hq::Kv4Attend &a, int lane) {
     if (!a.split) return hq::kKv4Undivided;
     float work = 0.0f;
@@ -63,7 +63,7 @@ __device__ __forceinline__ int part_of(const hq::Kv4Attend &a, int lane) {
         float mine = 0.0f;
         if (base + lane < a.c.batch) {
             const hq::Kv4Span p = hq::kv4_span(a.c, a.cut, base + lane);
-            mine = static_cast<float>(p.blocks) * static_cast<float>(p.tokens);
+            mine = static_cast<float>(p.blocks) * static_cast<float>(p.steps);
         }
         work += wave_sum(mine);
     }
@@ -152,7 +152,7 @@ __device__ __forceinline__ void load_words(const uint8_t *p, uint32_t *w) {
     if constexpr (N > STEP) load_words<N - STEP>(p + 4 * STEP, w + STEP);
 }
 // Waves a SIMD for which registers are kept: loads of other waves and conversions beside products need them.
-constexpr int waves_of(int ks, int r, int qh) { return r == 1 && ks <= 4 ? 3 : ks <= 6 ? 2 : 1; }
+constexpr int waves_of(int ks, int r, int qh) { return r == 1 && ks <= 4 ? qh == 1 ? 4 : 3 : ks <= 6 ? 2 : 1; }
 // Conversions and products in the order in which they are written: four conversions, then the products that take them.  (Left to itself the
 // compiler converts everything first, in registers that the sums need.)
 template <int N, int PRODUCTS>
@@ -190,11 +190,11 @@ __global__ __launch_bounds__(64 * WAVES, waves_of(KS, R, QH)) void attend_kernel
     const hq::Kv4Span span = hq::kv4_span(a.c, a.cut, s);
     if (head >= a.c.kv_heads || (task.parts > 1 && task.slot >= a.slots)) return;
     const int group = a.cut.group, rows = span.n * group;   // (below 2^31: the host checks t x heads)
-    const bool apart = rows - task.block * a.cut.rows <= 16 * R;   // tokens are apart, not rows
-    const int row0 = task.block * a.cut.rows + (apart ? 0 : wave * 16 * R);
+    const bool apart = rows - (task.block << a.cut.rows_log2) <= 16 * R;   // tokens are apart, not rows (in a sequence's last block too)
+    const int row0 = (task.block << a.cut.rows_log2) + (apart ? 0 : wave * 16 * R);
     const int by = apart ? 64 * WAVES / LP : 64 / LP, mine_at = apart ? threadIdx.x / LP : lane / LP;   // rows at once, this lane's
     const auto at_of = [&](int row, int64_t by_token, int64_t by_head) {
-        const int token = row / group;
+        const int token = a.cut.token_of(row);
         return (span.begin + token) * by_token + (head * group + row - token * group) * by_head;
     };
     if (span.length > a.c.capacity()) {   // the sequence says that it has tokens that no page holds
@@ -205,7 +205,8 @@ __global__ __launch_bounds__(64 * WAVES, waves_of(KS, R, QH)) void attend_kernel
     }
     // ---- the tokens: the first of them are asked for before the rows are prepared
     const int last_row = hq::kv4_min(row0 + 16 * R, rows) - 1;
-    const int first_position = span.length - span.n + row0 / group, last_position = row0 < rows ? span.length - span.n + last_row / group : -1;
+    const int first_position = span.length - span.n + a.cut.token_of(row0),
+              last_position = row0 < rows ? span.length - span.n + a.cut.token_of(last_row) : -1;
     const hq::Kv4Tiles tiles = hq::kv4_tiles(first_position, last_position, a.cut.window, a.cut.sinks);
     const int seen_from = hq::kv4_seen(last_position, a.cut.window, a.cut.sinks).from;
     const int step = apart ? WAVES : 1;
@@ -329,7 +330,7 @@ __global__ __launch_bounds__(64 * WAVES, waves_of(KS, R, QH)) void attend_kernel
             for (int e = 0; e < KS; ++e) q[r][h][e] = *reinterpret_cast<const half8v *>(stage + (h * 16 * STAGE + m * STAGE + g * (DP / 4) + e * 8) * 2);
         factor[r] = row_factor[owner][m];
         const int row = row0 + 16 * r + m;
-        position[r] = row < rows ? span.length - span.n + row / group : -1;
+        position[r] = row < rows ? span.length - span.n + a.cut.token_of(row) : -1;
         if (!apart) wave_sync();
     }
 
@@ -501,11 +502,11 @@ __global__ __launch_bounds__(64 * WAVES, waves_of(KS, R, QH)) void attend_kernel
 #pragma unroll
                 for (int e = 0; e < 8; ++e) x[e] = in * 8 < DP ? mine[i2 * ROW + in * 8 + e] : 0.0f;
             }
-            if (span.length - span.n + row / group < 0) weight = 0.0f;   // (it sees nothing, whatever its query is)
+            if (span.length - span.n + a.cut.token_of(row) < 0) weight = 0.0f;   // (it sees nothing, whatever its query is)
             if (task.parts == 1) {
                 store_row<KS>(a, x, weight, in, at_of(row, a.out_token, a.out_head));
             } else {
-                const int64_t at = int64_t{task.slot} * a.cut.rows + (apart ? 0 : wave * 16 * R) + 16 * r + i2;
+                const int64_t at = (int64_t{task.slot} << a.cut.rows_log2) + (apart ? 0 : wave * 16 * R) + 16 * r + i2;
                 if (in * 8 < DP) store8(a.sums + at * DP + in * 8, x);
                 if (in == 0) {
                     a.tops[2 * at] = reference;
@@ -516,12 +517,13 @@ __global__ __launch_bounds__(64 * WAVES, waves_of(KS, R, QH)) void attend_kernel
     }
 }
 
-// The parts of a row's tokens together: a workgroup for each row of a call whose tokens may be apart.
-template <int KS>
+// The parts of rows' tokens together: a workgroup for a token and as many heads as it has slots of lanes (EACH), or for one of them, whose
+// parts the slots share.
+template <int KS, bool EACH>
 __global__ __launch_bounds__(256) void join_kernel(hq::Kv4Attend a) {
     constexpr int DP = 32 * KS, LP = lanes_of(KS), SLOTS = 256 / LP;
-    __shared__ float x_of[SLOTS][LP * 8 + 4], top_of[SLOTS], sum_of[SLOTS];
-    const int lane = threadIdx.x & 63, token = blockIdx.x / a.heads, q_head = blockIdx.x % a.heads;
+    const int lane = threadIdx.x & 63, token = blockIdx.x, in = threadIdx.x % LP, slot = threadIdx.x / LP;
+    const int q_head = EACH ? blockIdx.y * SLOTS + slot : blockIdx.y;
     const int part = part_of(a, lane);
     int s = -1, slots = 0;
     for (int from = 0; from <= a.c.batch; from += 64) {
@@ -531,23 +533,23 @@ __global__ __launch_bounds__(256) void join_kernel(hq::Kv4Attend a) {
     }
     if (s >= a.c.batch) return;
     // (of sequences without tokens the last one that begins here)
+    const hq::Kv4Span span = hq::kv4_span(a.c, a.cut, s);
+    const int parts = hq::kv4_parts(span, part);
+    if (parts == 1 || span.length > a.c.capacity()) return;
     for (int from = 0; from < s; from += 64) {
         int mine = 0;
         if (from + lane < s) {
             const hq::Kv4Span p = hq::kv4_span(a.c, a.cut, from + lane);
-            const int parts = hq::kv4_parts(p, part);
-            mine = parts > 1 ? p.blocks * parts * a.c.kv_heads : 0;
+            const int of = hq::kv4_parts(p, part);
+            mine = of > 1 ? p.blocks * of * a.c.kv_heads : 0;
         }
         slots += wave_sum(mine);
     }
-    const hq::Kv4Span span = hq::kv4_span(a.c, a.cut, s);
-    const int parts = hq::kv4_parts(span, part);
-    if (parts == 1 || span.length > a.c.capacity()) return;
-    const int group = a.cut.group, row = (token - span.begin) * group + q_head % group, block = row / a.cut.rows;
-    const int64_t before = int64_t{slots} + (int64_t{q_head / group} * span.blocks + block) * parts;
+    if (q_head >= a.heads) return;   // (EACH: no lane waits for another slot's)
+    const int group = a.cut.group, head = a.cut.token_of(q_head), row = (token - span.begin) * group + q_head - head * group;
+    const int64_t before = int64_t{slots} + (int64_t{head} * span.blocks + (row >> a.cut.rows_log2)) * parts;
     if (before < 0 || before + parts > a.slots) return;
-    const int64_t first = before * a.cut.rows + row % a.cut.rows;
-    const int in = threadIdx.x % LP, slot = threadIdx.x / LP;
+    const int64_t first = (before << a.cut.rows_log2) + (row & (a.cut.rows() - 1));
     float x[8], top = -__builtin_inff(), sum = 0.0f;
 #pragma unroll
     for (int e = 0; e < 8; ++e) x[e] = 0.0f;
@@ -561,12 +563,13 @@ __global__ __launch_bounds__(256) void join_kernel(hq::Kv4Attend a) {
         for (int e = 0; e < 8; ++e) x[e] = x[e] * mine + other[e] * by;
     };
     // four parts at a time: their loads are under way together
-    for (int p = slot; p < parts; p += 4 * SLOTS) {
+    constexpr int STEP = EACH ? 1 : SLOTS;
+    for (int p = EACH ? 0 : slot; p < parts; p += 4 * STEP) {
         float y[4][8], tops[4], sums[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const int there = p + i * SLOTS < parts ? p + i * SLOTS : p;
-            const int64_t at = first + int64_t{there} * a.cut.rows;
+            const int there = p + i * STEP < parts ? p + i * STEP : p;
+            const int64_t at = first + (int64_t{there} << a.cut.rows_log2);
             tops[i] = a.tops[2 * at];
             sums[i] = there == p && i ? 0.0f : a.tops[2 * at + 1];
             load8(a.sums + at * DP + (in * 8 < DP ? in * 8 : 0), y[i]);
@@ -574,19 +577,22 @@ __global__ __launch_bounds__(256) void join_kernel(hq::Kv4Attend a) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) add(tops[i], sums[i], y[i]);
     }
+    if constexpr (!EACH) {
+        __shared__ float x_of[SLOTS][LP * 8 + 4], top_of[SLOTS], sum_of[SLOTS];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) x_of[slot][in * 8 + e] = x[e];
-    if (in == 0) {
-        top_of[slot] = top;
-        sum_of[slot] = sum;
-    }
-    __syncthreads();
-    if (slot) return;
-    for (int p = 1; p < SLOTS && p < parts; ++p) {
-        float y[8];
+        for (int e = 0; e < 8; ++e) x_of[slot][in * 8 + e] = x[e];
+        if (in == 0) {
+            top_of[slot] = top;
+            sum_of[slot] = sum;
+        }
+        __syncthreads();
+        if (slot) return;
+        for (int p = 1; p < SLOTS && p < parts; ++p) {
+            float y[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) y[e] = x_of[p][in * 8 + e];
-        add(top_of[p], sum_of[p], y);
+            for (int e = 0; e < 8; ++e) y[e] = x_of[p][in * 8 + e];
+            add(top_of[p], sum_of[p], y);
+        }
     }
     store_row<KS>(a, x, sum, in, token * a.out_token + q_head * a.out_head);
 }
@@ -615,7 +621,11 @@ void kv4_attend_launch(const Kv4Attend &a, Kv4Shape shape, unsigned blocks, hipS
     if (shape.tiles == 1 && shape.waves == 8) with_halves(std::integral_constant<int, 1>{}, std::integral_constant<int, 8>{});
     else if (shape.tiles == 1) with_halves(std::integral_constant<int, 1>{}, std::integral_constant<int, 4>{});
     else if constexpr (KS <= 4) with_halves(std::integral_constant<int, 2>{}, std::integral_constant<int, 4>{});
-    if (a.split) join_kernel<KS><<<static_cast<unsigned>(a.c.t) * a.heads, 256, 0, st>>>(a);
+    if (!a.split) return;
+    // (2177 tokens of 16 heads whose parts are 2 to 4: a workgroup for a row 45 us)
+    constexpr int SLOTS = 256 / lanes_of(KS);
+    if (int64_t{a.c.t} * a.heads > 8192) join_kernel<KS, true><<<dim3(a.c.t, (a.heads + SLOTS - 1) / SLOTS), 256, 0, st>>>(a);
+    else join_kernel<KS, false><<<dim3(a.c.t, a.heads), 256, 0, st>>>(a);
 }
 
 }  // namespace hq

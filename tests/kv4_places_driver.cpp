@@ -30,6 +30,17 @@ static int sequence_of(const Kv4 &c, int index) {   // as a wave counts it
     return std::max(s, 0);
 }
 
+static void finish(Kv4Cut &cut) {
+    cut.reach = kv4_reach(cut.window, cut.sinks, cut.rows(), cut.group);
+    // as the host's exact division of numbers below 2^31: m = ceil(2^(31 + l) / d), l = ceil(log2 d)
+    uint32_t l = 0;
+    while ((1ull << l) < static_cast<uint64_t>(cut.group)) ++l;
+    cut.magic = cut.group > 1 ? static_cast<uint32_t>(((1ull << (31 + l)) + cut.group - 1) / cut.group) : 0;
+    cut.shift = l ? l - 1 : 0;
+    for (const int row : {0, 1, cut.group - 1, cut.group, 1000003, 0x7FFEFFFF, 0x7FFFFFFF})
+        EXPECT(cut.token_of(row) == row / cut.group, "row %d of groups of %d", row, cut.group);
+}
+
 // every group lies inside the call; a token is in one group where begins rises
 static void groups(const Call &call, bool sound) {
     const Kv4 &c = call.c;
@@ -60,11 +71,11 @@ static void tasks(const Call &call, const Kv4Cut &cut, bool sound) {
     float work = 0.0f;
     for (int s = 0; s < c.batch; ++s) {
         const Kv4Span p = kv4_span(c, cut, s);
-        EXPECT(p.begin >= 0 && p.n >= 0 && p.begin + int64_t{p.n} <= c.t && p.tokens >= 0 && p.tokens <= c.capacity(), "span");
-        work += static_cast<float>(p.blocks) * static_cast<float>(p.tokens);
+        EXPECT(p.begin >= 0 && p.n >= 0 && p.begin + int64_t{p.n} <= c.t && p.steps >= 0 && p.steps <= c.capacity() / 32 + 1, "span");
+        work += static_cast<float>(p.blocks) * static_cast<float>(p.steps);
     }
     const int part = kv4_part(cut, work, c.kv_heads);
-    EXPECT(part == kKv4Undivided || part % cut.step == 0, "part %d", part);
+    EXPECT(part >= cut.least, "part %d", part);
     int64_t blocks = 0, slots = 0;
     for (int s = 0; s < c.batch; ++s) {
         const Kv4Span p = kv4_span(c, cut, s);
@@ -75,8 +86,8 @@ static void tasks(const Call &call, const Kv4Cut &cut, bool sound) {
         if (p.length > c.capacity()) continue;   // (answered with NaN)
         const int rows = p.n * cut.group;
         for (int b = 0; b < p.blocks; ++b)
-            for (const int per : {cut.rows, cut.rows / 4}) {   // a workgroup's rows, and a wave's
-                for (int row0 = b * cut.rows; row0 < std::min((b + 1) * cut.rows, rows); row0 += per) {
+            for (const int per : {cut.rows(), cut.rows() >> cut.waves_log2}) {   // a workgroup's rows, and a wave's
+                for (int row0 = b * cut.rows(); row0 < std::min((b + 1) * cut.rows(), rows); row0 += per) {
                     const int last_row = std::min(row0 + per, rows) - 1, base = p.length - p.n;
                     const Kv4Tiles t = kv4_tiles(base + row0 / cut.group, base + last_row / cut.group, cut.window, cut.sinks);
                     EXPECT(t.sinks >= 0 && t.sinks <= t.from + (t.count() == 0) && t.from <= t.to && t.to * int64_t{32} < int64_t{p.length} + 32, "tiles %d %d %d of %d", t.sinks, t.from, t.to, p.length);
@@ -99,7 +110,7 @@ static void tasks(const Call &call, const Kv4Cut &cut, bool sound) {
             }
     }
     if (sound) {
-        const int64_t most = int64_t{c.kv_heads} * (int64_t{c.t} * cut.group / cut.rows + c.batch);
+        const int64_t most = int64_t{c.kv_heads} * (int64_t{c.t} * cut.group / cut.rows() + c.batch);
         EXPECT(blocks <= most + cut.target, "%lld workgroups, %lld allotted", static_cast<long long>(blocks), static_cast<long long>(most + cut.target));
         EXPECT(slots <= 2 * int64_t{cut.target}, "%lld slots of %d", static_cast<long long>(slots), 2 * cut.target);
     }
@@ -132,8 +143,9 @@ int main() {
         c.table = call.table.data(), c.lengths = call.lengths.data(), c.begins = uniform ? nullptr : call.begins.data();
         groups(call, sound || uniform);
         Kv4Cut cut{};
-        cut.rows = 16 << below(4), cut.group = 1 + below(9), cut.target = 1 + below(64), cut.least = 32 * (1 + below(4)), cut.step = below(2) ? 32 : 128;
+        cut.waves_log2 = 2 + below(2), cut.rows_log2 = 4 + cut.waves_log2 + below(2), cut.group = 1 + below(9), cut.target = 1 + below(64), cut.least = 1 + below(8);
         cut.window = below(2) ? 1 + below(100) : 0, cut.sinks = cut.window ? below(70) : 0;
+        finish(cut);
         tasks(call, cut, sound || uniform);
     }
     // the ends of the range: lengths near 2^31, a table that does not reach
@@ -144,7 +156,9 @@ int main() {
         c.table = call.table.data(), c.lengths = call.lengths.data(), c.begins = call.begins.data();
         c.page_log2 = 4, c.batch = 1, c.table_pages = 1, c.pages = 1, c.kv_heads = 1, c.d = 64, c.pitch = 64, c.t = 16;
         groups(call, true);
-        tasks(call, Kv4Cut{16, 4, 8, 32, 32, 0, 0}, true);
+        Kv4Cut cut{6, 2, 4, 8, 1, 0, 0, 0, 0, 0};
+        finish(cut);
+        tasks(call, cut, true);
     }
     // places beyond 32 bits of bytes
     Kv4 c{};
