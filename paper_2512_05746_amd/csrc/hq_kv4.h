@@ -54,13 +54,22 @@ struct Kv4Group {
     int row, count;
     int position;    // (of tokens of no sequence: meaningless)
 };
-__host__ __device__ __forceinline__ Kv4Group kv4_group(const Kv4 &c, int s, int index) {
+// The sequence that group `index` belongs to where begins is null: the last s with s each / 8 + 2 s <= index, at most `batch`.
+__host__ __device__ __forceinline__ int kv4_sequence(const Kv4 &c, int index) {
+    // s (each / 8 + 2) is between the left side and one less, so the quotient is s or one too small
+    int s = kv4_min(static_cast<int>(static_cast<uint32_t>(index) * 8u / static_cast<uint32_t>(c.each + 16)), c.batch);
+    while (s < c.batch && kv4_group_begin(c.begin(s + 1), s + 1) <= index) ++s;
+    return s;
+}
+// read: reads a number of lengths.
+template <class F>
+__host__ __device__ __forceinline__ Kv4Group kv4_group(const Kv4 &c, int s, int index, F read) {
     const int begin = c.begin(s), j = index - kv4_group_begin(begin, s);
     if (s >= c.batch) {
         const int64_t row = begin + int64_t{8} * j;
         return row < c.t ? Kv4Group{s, static_cast<int>(row), kv4_min(8, c.t - static_cast<int>(row)), 0} : Kv4Group{s, 0, 0, 0};
     }
-    const int n = c.begin(s + 1) - begin, length = kv4_max(0, c.lengths[s]);
+    const int n = c.begin(s + 1) - begin, length = kv4_max(0, read(c.lengths + s));
     const int64_t first = int64_t{length} - n;                       // position of the sequence's first token; negative: no place for it
     const int64_t group = ((first >> 3) + j) * 8;
     const int64_t from = group > first ? group : first, to = group + 8 < length ? group + 8 : length;

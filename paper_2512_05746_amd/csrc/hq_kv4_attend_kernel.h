@@ -177,7 +177,7 @@ __global__ __launch_bounds__(64 * WAVES, waves_of(KS, R, QH)) void attend_kernel
     __shared__ float row_factor[WAVES][16], row_top[WAVES][16], row_sum[WAVES][16];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), m = lane & 15, g = lane >> 4;
     const Task task = task_of(a, blockIdx.x, lane);
-    const int in = lane % LP;
+    const int in = kv4_block(lane % LP);   // the 8 channels that the lane has where a row is dealt to lanes
     if (task.s < 0) {
         // rows of no sequence: zeros
         const int begin = a.c.begin(a.c.batch), rows = (a.c.t - begin) * a.heads, from = blockIdx.x - task.block;
@@ -467,7 +467,6 @@ __global__ __launch_bounds__(64 * WAVES, waves_of(KS, R, QH)) void attend_kernel
         for (int e = 0; e < 4; ++e)
 #pragma unroll
             for (int c = 0; c < 2 * KS; c += 2) {
-                typedef float float2v __attribute__((ext_vector_type(2)));
                 *reinterpret_cast<float2v *>(mine + m * ROW + 2 * KS * (4 * g + e) + c) = float2v{o[r][c][e], o[r][c + 1][e]};
             }
         if (g == 0) {
@@ -522,7 +521,7 @@ __global__ __launch_bounds__(64 * WAVES, waves_of(KS, R, QH)) void attend_kernel
 template <int KS, bool EACH>
 __global__ __launch_bounds__(256) void join_kernel(hq::Kv4Attend a) {
     constexpr int DP = 32 * KS, LP = lanes_of(KS), SLOTS = 256 / LP;
-    const int lane = threadIdx.x & 63, token = blockIdx.x, in = threadIdx.x % LP, slot = threadIdx.x / LP;
+    const int lane = threadIdx.x & 63, token = blockIdx.x, in = kv4_block(threadIdx.x % LP), slot = threadIdx.x / LP;
     const int q_head = EACH ? blockIdx.y * SLOTS + slot : blockIdx.y;
     const int part = part_of(a, lane);
     int s = -1, slots = 0;

@@ -8,8 +8,9 @@
 //
 // A workgroup takes the tokens of one group of 8 positions, because a dword of the cache's v holds the codes of a channel for 8 tokens: it
 // is then written by one workgroup, whole where all 8 tokens are new, around what it held where they are not.  A head is owned by LP
-// neighbouring lanes, 8 channels each; a lane keeps its token's cosines, sines and both channels' weights over all heads of the token.  The
-// other channel of a pair comes from memory a second time (a cache line that the wave has just read) instead of through LDS.
+// neighbouring lanes, 8 channels each; a lane keeps its token's cosines, sines and weights over all heads of the token.  The other
+// channel of a pair is in the lane, or in a lane that one permute reaches, or comes from memory a second time (a cache line that
+// the wave has just read).
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -24,16 +25,30 @@
 
 namespace {
 
+// What a caller's arrays on the device hold, by scalar loads: they are not written while a call runs.
+__device__ __forceinline__ int32_t constant(const int32_t *p) {
+    return *reinterpret_cast<const __attribute__((address_space(4))) int32_t *>(reinterpret_cast<uint64_t>(p));
+}
 // The group of tokens that a workgroup works on: every wave looks for the sequence by itself.
 __device__ __forceinline__ hq::Kv4Group group_of(const hq::Kv4 &c, int index) {
-    const int lane = threadIdx.x & 63;
     int s = -1;
-    for (int base = 0; base <= c.batch; base += 64) {
-        const int at = base + lane;
-        const bool before = at <= c.batch && hq::kv4_group_begin(c.begin(at), at) <= index;
-        s += __popcll(__ballot(before));
+    if (c.begins) {
+        const int lane = threadIdx.x & 63;
+        for (int base = 0; base <= c.batch; base += 64) {
+            const int at = base + lane;
+            const bool before = at <= c.batch && hq::kv4_group_begin(c.begin(at), at) <= index;
+            s += __popcll(__ballot(before));
+        }
+        s = __builtin_amdgcn_readfirstlane(hq::kv4_max(s, 0));
+    } else {
+        s = hq::kv4_sequence(c, index);
     }
-    return hq::kv4_group(c, __builtin_amdgcn_readfirstlane(hq::kv4_max(s, 0)), index);
+    return hq::kv4_group(c, s, index, [](const int32_t *p) { return constant(p); });
+}
+__device__ __forceinline__ int64_t page_of(const hq::Kv4 &c, const hq::Kv4Group &g) {
+    if (g.s >= c.batch) return -1;
+    const int32_t *const table = c.table + static_cast<int64_t>(g.s) * c.table_pages;
+    return c.checked(g.position, [&](int column) { return constant(table + column); });
 }
 
 // ---- append -----------------------------------------------------------------------------------------------------------
@@ -47,8 +62,17 @@ struct AppendArgs {
     int64_t positions;
     int heads, rotary, pos_wide, interleaved, w_float, norm;
     float eps;
+    hq::Magic31 d_magic;
+    int q_parts, k_parts;
 };
 
+// Where the other channel of a pair is.
+enum Pairs {
+    kNeighbours,   // in the lane (or nothing is rotated)
+    kLanes,        // in a lane whose block of channels differs in one bit: halves of 8, 16, 32 or 64 channels
+    kQuads,        // in memory: runs of 4 channels have theirs in runs of 4
+    kSingle        // in memory, one by one
+};
 // What a lane does to each head of its token.
 struct Turn {
     bool pad, beyond;
@@ -82,63 +106,90 @@ __device__ __forceinline__ Turn turn_of(const AppendArgs &a, int row, int64_t pl
     }
     return t;
 }
-// A lane's 8 channels as they are, and those of their pairs' other channels.  QUADS: runs of 4 channels have theirs in runs of 4.
-template <class T, bool QUADS>
-__device__ __forceinline__ void load_partners(const T *x, int c0, int rotary, float (&v)[8]) {
-    if constexpr (QUADS) {
+// A lane's 8 channels of a head, and those of their pairs' other channels where these come from memory.
+template <class T, int PAIRS> struct Raw {
+    typename Vec<T, 8>::type v;
+    T p[PAIRS >= kQuads ? 8 : 1];
+    __device__ __forceinline__ void load(const T *x, int c0, int rotary) {
+        v = load_vec<T, 8>(x + c0);
+        if constexpr (PAIRS == kQuads) {
 #pragma unroll
-        for (int i = 0; i < 8; i += 4) {
-            const typename Vec<T, 4>::type t = load_vec<T, 4>(x + partner_of(c0 + i, rotary));
+            for (int i = 0; i < 8; i += 4) {
+                const typename Vec<T, 4>::type t = load_vec<T, 4>(x + partner_of(c0 + i, rotary));
 #pragma unroll
-            for (int e = 0; e < 4; ++e) v[i + e] = static_cast<float>(t[e]);
+                for (int e = 0; e < 4; ++e) p[i + e] = t[e];
+            }
+        } else if constexpr (PAIRS == kSingle) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) p[i] = x[partner_of(c0 + i, rotary)];
         }
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = static_cast<float>(x[partner_of(c0 + i, rotary)]);
     }
-}
-template <class T, bool QUADS>
-__device__ __forceinline__ void weights_of(const AppendArgs &a, const void *w, int c0, float (&own)[8], float (&other)[8]) {
+};
+template <class T, int PAIRS>
+__device__ __forceinline__ Raw<float, PAIRS> weights_of(const AppendArgs &a, const void *w, int c0) {
+    Raw<float, PAIRS> r;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) own[i] = other[i] = 1.0f;
-    if (!w) return;
+    for (int i = 0; i < 8; ++i) r.v[i] = 1.0f;
+#pragma unroll
+    for (float &x : r.p) x = 1.0f;
+    if (!w) return r;
     if (a.w_float) {
-        load8(static_cast<const float *>(w) + c0, own);
-        if (!a.interleaved) load_partners<float, QUADS>(static_cast<const float *>(w), c0, a.rotary, other);
+        r.load(static_cast<const float *>(w), c0, a.rotary);
     } else {
-        load8(static_cast<const T *>(w) + c0, own);
-        if (!a.interleaved) load_partners<T, QUADS>(static_cast<const T *>(w), c0, a.rotary, other);
+        Raw<T, PAIRS> t;
+        t.load(static_cast<const T *>(w), c0, a.rotary);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) r.v[i] = static_cast<float>(t.v[i]);
+        if constexpr (PAIRS >= kQuads) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) r.p[i] = static_cast<float>(t.p[i]);
+        }
     }
+    return r;
 }
 // A head normalised and turned.
-template <class T, int LP, bool QUADS>
-__device__ __forceinline__ void head(const AppendArgs &a, const T *x, int c0, bool live, const Turn &t, const float (&own)[8],
-                                     const float (&other)[8], float (&v)[8]) {
-    float p[8];
-    load8(x + c0, v);
-    if (!a.interleaved && a.rotary) load_partners<T, QUADS>(x, c0, a.rotary, p);
+template <class T, int LP, int PAIRS>
+__device__ __forceinline__ void head(const AppendArgs &a, const Raw<T, PAIRS> &x, int c0, bool live, const Turn &t, const Raw<float, PAIRS> &w,
+                                     float (&v)[8]) {
     float r = 1.0f;
     if (a.norm) {
         float sum = 0.0f;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) sum += v[i] * v[i];
-        sum = sum_lanes<LP>(live ? sum : 0.0f);
-        r = 1.0f / sqrtf(sum * (1.0f / static_cast<float>(a.c.d)) + a.eps);
+        for (int i = 0; i < 8; ++i) sum += static_cast<float>(x.v[i]) * static_cast<float>(x.v[i]);
+        sum = sum_lanes<LP>(live ? sum : 0.0f) * (1.0f / static_cast<float>(a.c.d)) + a.eps;
+        r = __builtin_amdgcn_rsqf(sum);                       // (off by one step at most)
+        if (sum < 0x1p-120f) r = 1.0f / sqrtf(sum);           // (which it takes for 0 where it is not a normal number)
     }
     if (t.beyond) r = __builtin_nanf("");
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] *= r * own[i];
+    for (int i = 0; i < 8; ++i) v[i] = static_cast<float>(x.v[i]) * (r * w.v[i]);
     if (!a.rotary) return;
-    if (a.interleaved) {
+    float p[8];
+    if constexpr (PAIRS == kLanes) {
+        const auto other = [&](auto bit) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) p[i] = v[i ^ 1];
+            for (int i = 0; i < 8; ++i) p[i] = lane_of_bit<decltype(bit)::value>(v[i]);
+        };
+        const int half = a.rotary >> 4;   // in blocks
+        if (half == 8) other(std::integral_constant<int, 3>{});
+        else if (half == 4) other(std::integral_constant<int, 2>{});
+        else if (half == 2) other(std::integral_constant<int, 1>{});
+        else other(std::integral_constant<int, 0>{});
     } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) p[i] *= r * other[i];
+        for (int i = 0; i < 8; ++i) {
+            if constexpr (PAIRS == kNeighbours) p[i] = v[i ^ 1];
+            else p[i] = static_cast<float>(x.p[i]) * (r * w.p[i]);
+        }
     }
+    if (a.rotary == a.c.d) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
-        if (c0 + i < a.rotary) v[i] = v[i] * t.cos[i] + p[i] * t.sin[i];
+        for (int i = 0; i < 8; ++i) v[i] = v[i] * t.cos[i] + p[i] * t.sin[i];
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (c0 + i < a.rotary) v[i] = v[i] * t.cos[i] + p[i] * t.sin[i];
+    }
 }
 // Its transform in codes.
 template <int LP>
@@ -157,7 +208,10 @@ __device__ __forceinline__ uint32_t coded(float (&v)[8], int in, bool live, int 
     return kv4_codes(v, scale == scale ? __fdiv_rn(1.0f, scale) : 0.0f);
 }
 
-template <int DT, int LP, bool QUADS>
+constexpr int kAtOnce = 4;   // heads of a slot whose loads are under way together
+
+// Workgroups of a group, by blockIdx.y: q_parts for the queries, then k_parts for the keys, the rest for the values.
+template <int DT, int LP, int PAIRS>
 __global__ __launch_bounds__(256) void append_kernel(AppendArgs a) {
     using T = typename Float<DT>::type;
     constexpr int SLOTS = 256 / LP;
@@ -165,66 +219,96 @@ __global__ __launch_bounds__(256) void append_kernel(AppendArgs a) {
     if (g.count == 0) return;
     // slots: tokens, a power of two of them, times heads at once
     const int log2 = g.count > 4 ? 3 : g.count > 2 ? 2 : g.count - 1, at_once = SLOTS >> log2;
-    const int in = threadIdx.x % LP, slot = threadIdx.x / LP, token = slot & ((1 << log2) - 1), first = slot >> log2;
+    const int in = kv4_block(threadIdx.x % LP), slot = threadIdx.x / LP, token = slot & ((1 << log2) - 1), first = slot >> log2;
     const bool live = in * 8 < a.c.d, mine = token < g.count;
     const int c0 = live ? in * 8 : 0, row = g.row + (mine ? token : 0);
     const int64_t place = g.s < a.c.batch ? g.position + (mine ? token : 0) : -1;
-    const Turn turn = turn_of(a, row, place, c0);
-    const int part = blockIdx.y, parts = gridDim.y;
-    float own[8], other[8], x[8];
-    weights_of<T, QUADS>(a, a.q_weight, c0, own, other);
-    for (int h = part * at_once + first; h < a.heads; h += parts * at_once) {
-        const T *q = static_cast<const T *>(a.q) + row * a.q_token + h * a.q_head;
-        head<T, LP, QUADS>(a, q, c0, live, turn, own, other, x);
-        if (turn.pad) {
+    int part = blockIdx.y;
+    if (part < a.q_parts + a.k_parts) {
+        const bool keys = part >= a.q_parts;
+        if (keys) part -= a.q_parts;
+        const int heads = keys ? a.c.kv_heads : a.heads, step = (keys ? a.k_parts : a.q_parts) * at_once;
+        // (positions of a group of 8 are all negative, without a page, or none is)
+        const int64_t page = keys ? page_of(a.c, g) : 0;
+        if (page < 0) return;
+        const int64_t by_head = keys ? a.k_head : a.q_head;
+        const T *x = static_cast<const T *>(keys ? a.k : a.q) + row * (keys ? a.k_token : a.q_token);
+        const auto load = [&](Raw<T, PAIRS> (&raw)[kAtOnce], int h) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) x[i] = 0.0f;
+            for (int e = 0; e < kAtOnce; ++e)
+                if (h + e * step < heads) raw[e].load(x + (h + e * step) * by_head, c0, a.rotary);
+        };
+        const int from = part * at_once + first;
+        Raw<T, PAIRS> raw[kAtOnce];
+        load(raw, from);
+        const Raw<float, PAIRS> w = weights_of<T, PAIRS>(a, keys ? a.k_weight : a.q_weight, c0);
+        const Turn turn = turn_of(a, row, place, c0);
+        const int64_t at = keys ? a.c.slots(page, 0) + a.c.slot(static_cast<int>(place)) : 0;
+        const auto work = [&](const Raw<T, PAIRS> &now, int h) {
+            float v[8];
+            head<T, LP, PAIRS>(a, now, c0, live, turn, w, v);
+            if (!keys) {
+                if (__any(turn.pad)) {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) v[i] = turn.pad ? 0.0f : v[i];
+                }
+                if (live && mine) store8(static_cast<T *>(a.q_out) + row * a.out_token + h * a.out_head + c0, v);
+            } else {
+                float scale;
+                const uint32_t code = coded<LP>(v, in, live, a.c.block_log2, scale);
+                if (!mine || turn.pad) return;
+                const int64_t to = at + (static_cast<int64_t>(h) << a.c.page_log2);
+                if (live) *reinterpret_cast<uint32_t *>(a.c.k + to * a.c.row_bytes() + in * 4) = code;
+                if (in == 0) a.c.k_scale[to] = scale;
+            }
+        };
+        for (int h = from; h < heads; h += kAtOnce * step) {
+#pragma unroll
+            for (int e = 0; e < kAtOnce; ++e)
+                if (h + e * step < heads) work(raw[e], h + e * step);
+            load(raw, h + kAtOnce * step);
         }
-        if (live && mine) store8(static_cast<T *>(a.q_out) + row * a.out_token + h * a.out_head + c0, x);
+        return;
     }
-    if (g.s >= a.c.batch) return;
-    // (positions of a group of 8 are all negative, without a page, or none is)
-    const int64_t page = a.c.page(g.s, g.position);
+    part -= a.q_parts + a.k_parts;
+    const int parts = gridDim.y - a.q_parts - a.k_parts;
+    const int64_t page = page_of(a.c, g);
     if (page < 0) return;
-    const bool stored = mine && !turn.pad;
-    weights_of<T, QUADS>(a, a.k_weight, c0, own, other);
-    for (int h = part * at_once + first; h < a.c.kv_heads; h += parts * at_once) {
-        const T *k = static_cast<const T *>(a.k) + row * a.k_token + h * a.k_head;
-        head<T, LP, QUADS>(a, k, c0, live, turn, own, other, x);
-        float scale;
-        const uint32_t w = coded<LP>(x, in, live, a.c.block_log2, scale);
-        if (!stored) continue;
-        const int64_t at = a.c.slots(page, h) + a.c.slot(static_cast<int>(place));
-        if (live) *reinterpret_cast<uint32_t *>(a.c.k + at * a.c.row_bytes() + in * 4) = w;
-        if (in == 0) a.c.k_scale[at] = scale;
-    }
     __shared__ uint32_t codes[SLOTS][LP + 1];
     __shared__ uint32_t new_tokens;   // four bits for each token of the group that is stored
     if (threadIdx.x == 0) new_tokens = 0;
+    bool stored = mine;
+    if (a.pos && (a.pos_wide ? static_cast<const int64_t *>(a.pos)[row] : static_cast<const int32_t *>(a.pos)[row]) < 0) stored = false;
+    const T *x = static_cast<const T *>(a.v) + row * a.v_token + c0;
+    const int64_t at = a.c.slots(page, 0);
+    float next[8];
+    if (part * at_once + first < a.c.kv_heads) load8(x + (part * at_once + first) * a.v_head, next);
     __syncthreads();
     if (first == 0 && in == 0 && stored) atomicOr(&new_tokens, 15u << (4 * (static_cast<int>(place) & 7)));
     for (int base = part * at_once; base < a.c.kv_heads; base += parts * at_once) {
         const int h = base + first;
         if (h < a.c.kv_heads) {
-            load8(static_cast<const T *>(a.v) + row * a.v_token + h * a.v_head + c0, x);
-            float scale;
-            codes[slot][in] = coded<LP>(x, in, live, a.c.block_log2, scale);
-            if (stored && in == 0) a.c.v_scale[a.c.slots(page, h) + a.c.slot(static_cast<int>(place))] = scale;
+            float v[8], scale;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = next[i];
+            if (h + parts * at_once < a.c.kv_heads) load8(x + (h + parts * at_once) * a.v_head, next);
+            codes[slot][in] = coded<LP>(v, in, live, a.c.block_log2, scale);
+            if (stored && in == 0) a.c.v_scale[at + (static_cast<int64_t>(h) << a.c.page_log2) + a.c.slot(static_cast<int>(place))] = scale;
         }
         __syncthreads();
         const uint32_t mask = new_tokens;
-        const int skip = g.position & 7, ahead = g.position & ~7;
+        const int skip = g.position & 7, ahead = a.c.slot(g.position & ~7);
         for (int e = threadIdx.x; e < at_once * a.c.d; e += 256) {
-            const int local = e / a.c.d, c = e - local * a.c.d;
+            const int local = hq::div_magic31(e, a.c.d, a.d_magic.m, a.d_magic.s), c = e - local * a.c.d;
             if (base + local >= a.c.kv_heads) break;
+            uint32_t *to = reinterpret_cast<uint32_t *>(a.c.v + (at + (static_cast<int64_t>(base + local) << a.c.page_log2) + ahead) * a.c.row_bytes()) + c;
             uint32_t w = 0;
+            if (mask != 0xFFFFFFFFu) w = *to & ~mask;
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const int from = i - skip;
-                if (from >= 0 && from < g.count) w |= (codes[(local << log2) + from][c >> 3] >> (4 * (c & 7)) & 15u) << (4 * i);
+                if (from >= 0 && from < g.count && (mask >> (4 * i) & 1)) w |= (codes[(local << log2) + from][c >> 3] >> (4 * (c & 7)) & 15u) << (4 * i);
             }
-            uint32_t *to = reinterpret_cast<uint32_t *>(a.c.v + (a.c.slots(page, base + local) + a.c.slot(ahead)) * a.c.row_bytes()) + c;
-            if (mask != 0xFFFFFFFFu) w = (w & mask) | (*to & ~mask);
             if (mask) *to = w;
         }
         __syncthreads();
@@ -237,6 +321,8 @@ struct ReadArgs {
     void *k, *v;   // [t, kv_heads, d], dense
 };
 
+// Workgroups of a group: the first half by blockIdx.y reads keys, the other values.  A slot has a row; of v it reads the dwords of its
+// channels, which hold 8 tokens (the other slots that want them find them in the first-level cache).
 template <int DT, int LP>
 __global__ __launch_bounds__(256) void read_kernel(ReadArgs a) {
     using T = typename Float<DT>::type;
@@ -244,83 +330,109 @@ __global__ __launch_bounds__(256) void read_kernel(ReadArgs a) {
     const hq::Kv4Group g = group_of(a.c, blockIdx.x);
     if (g.count == 0) return;
     const int log2 = g.count > 4 ? 3 : g.count > 2 ? 2 : g.count - 1, at_once = SLOTS >> log2;
-    const int in = threadIdx.x % LP, slot = threadIdx.x / LP, token = slot & ((1 << log2) - 1), first = slot >> log2;
-    const bool live = in * 8 < a.c.d && token < g.count;
+    const int in = kv4_block(threadIdx.x % LP), slot = threadIdx.x / LP, token = slot & ((1 << log2) - 1), first = slot >> log2;
+    if (token >= g.count) return;   // (whole heads: no lane waits for another head's)
+    const bool live = in * 8 < a.c.d;
     const int row = g.row + token, place = g.s < a.c.batch ? g.position + token : -1;
-    const int64_t page = g.s < a.c.batch ? a.c.page(g.s, g.position) : -1;
-    const float factor = walsh_factor(a.c.block_log2), nothing = place < 0 ? 0.0f : __builtin_nanf("");
-    const int ahead = g.position & ~7;
-    __shared__ uint32_t codes[256];   // v's dwords of one turn: [heads at once, d]
-    for (int base = blockIdx.y * at_once; base < a.c.kv_heads; base += gridDim.y * at_once) {
-        const int h = base + first;
-        const bool mine = live && h < a.c.kv_heads;
-        for (int v = 0; v < 2; ++v) {
-            float x[8];
-            float scale = 0.0f;
-            uint32_t w = 0;
-            const int64_t at = page < 0 || place < 0 || !mine ? 0 : a.c.slots(page, h) + a.c.slot(place);
-            if (mine && page >= 0 && place >= 0) scale = (v ? a.c.v_scale : a.c.k_scale)[at];
-            if (v == 0) {
-                if (mine && page >= 0 && place >= 0) w = *reinterpret_cast<const uint32_t *>(a.c.k + at * a.c.row_bytes() + in * 4);
-            } else {
-                for (int part = 0; part < at_once * a.c.d; part += 256) {
-                    const int e = part + threadIdx.x, local = e / a.c.d, c = e - local * a.c.d;
-                    __syncthreads();
-                    if (e < at_once * a.c.d && base + local < a.c.kv_heads && page >= 0)
-                        codes[threadIdx.x] =
-                            *(reinterpret_cast<const uint32_t *>(a.c.v + (a.c.slots(page, base + local) + a.c.slot(ahead)) * a.c.row_bytes()) + c);
-                    __syncthreads();
+    const int64_t page = page_of(a.c, g);
+    const float factor = walsh_factor(a.c.block_log2);
+    const int parts = gridDim.y >> 1;
+    const bool values = static_cast<int>(blockIdx.y) >= parts;
+    const int part = values ? blockIdx.y - parts : blockIdx.y, step = parts * at_once;
+    T *const out = static_cast<T *>(values ? a.v : a.k) + static_cast<int64_t>(row) * a.c.kv_heads * a.c.d + in * 8;
+    if (page < 0) {
+        float x[8];
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const int from = first * a.c.d + in * 8 + i - part;
-                        if (mine && page >= 0 && from >= 0 && from < 256) w |= (codes[from] >> (4 * (place & 7)) & 15u) << (4 * i);
-                    }
+        for (int i = 0; i < 8; ++i) x[i] = place < 0 ? 0.0f : __builtin_nanf("");
+        for (int h = part * at_once + first; h < a.c.kv_heads; h += step)
+            if (live) store8(out + h * a.c.d, x);
+        return;
+    }
+    const int64_t at = a.c.slots(page, 0) + a.c.slot(place), by_head = int64_t{1} << a.c.page_log2;
+    const float *const scales = (values ? a.c.v_scale : a.c.k_scale) + at;
+    const uint8_t *const codes = values ? a.c.v + (a.c.slots(page, 0) + a.c.slot(place & ~7)) * a.c.row_bytes() + (live ? in * 32 : 0)
+                                        : a.c.k + at * a.c.row_bytes() + (live ? in * 4 : 0);
+    const int shift = 4 * (place & 7);
+    typedef uint32_t words4 __attribute__((ext_vector_type(4)));
+    words4 raw[kAtOnce][2] = {};
+    float raw_scale[kAtOnce] = {};
+    const auto load = [&](int h) {
+#pragma unroll
+        for (int e = 0; e < kAtOnce; ++e)
+            if (h + e * step < a.c.kv_heads) {
+                const uint8_t *p = codes + (h + e * step) * (by_head * a.c.row_bytes());
+                raw_scale[e] = scales[(h + e * step) * by_head];
+                if (values) {
+                    raw[e][0] = reinterpret_cast<const words4 *>(p)[0];
+                    raw[e][1] = reinterpret_cast<const words4 *>(p)[1];
+                } else {
+                    raw[e][0][0] = *reinterpret_cast<const uint32_t *>(p);
                 }
             }
-            const half8v n = kv4_halves(w);
+    };
+    const auto work = [&](const words4 (&now)[2], float scale, int h) {
+        const float f = scale * factor;
+        uint32_t w = now[0][0];
+        if (values) {
+            w = 0;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) x[i] = static_cast<float>(n[i]);
-            walsh(x, in, a.c.block_log2);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) x[i] = page < 0 || place < 0 ? nothing : x[i] * (scale * factor);
-            if (mine) store8(static_cast<T *>(v ? a.v : a.k) + (static_cast<int64_t>(row) * a.c.kv_heads + h) * a.c.d + in * 8, x);
+            for (int i = 0; i < 8; ++i) w = __builtin_amdgcn_alignbit(now[i >> 2][i & 3] >> shift, w, 4);   // (its low 4 bits on top)
         }
+        float x[8];
+        kv4_floats(live ? w : 0u, x);
+        walsh(x, in, a.c.block_log2);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] *= f;
+        if (live) store8(out + h * a.c.d, x);
+    };
+    const int from = part * at_once + first;
+    load(from);
+    for (int h = from; h < a.c.kv_heads; h += kAtOnce * step) {
+#pragma unroll
+        for (int e = 0; e < kAtOnce; ++e)
+            if (h + e * step < a.c.kv_heads) work(raw[e], raw_scale[e], h + e * step);
+        load(h + kAtOnce * step);
     }
 }
 
-// Workgroups beside each other share a group's heads where there are few groups.
-uint32_t parts_for(int groups, int most, int lanes) {
-    const int turns = std::max(1, (most + 256 / lanes / 8 - 1) / (256 / lanes / 8));
-    const int wanted = (4 * hq::compute_units() + groups - 1) / groups;
-    return static_cast<uint32_t>(std::max(1, std::min({wanted, turns, 64})));
+// Workgroups that share a group's heads where there are few groups: one for each turn of 8 tokens, or of one where tokens come singly.
+int parts_for(const hq::Kv4 &c, int groups, int heads, int lanes, int wanted) {
+    const int slots = 256 / lanes, at_once = c.each == 1 && !c.begins ? slots : slots / 8;
+    const int turns = (heads + at_once - 1) / at_once, more = (wanted * hq::compute_units() + groups - 1) / groups;
+    return std::max(1, std::min({more, turns, 32}));
 }
 
+template <class F>
+void with_lanes(int d, F f) {
+    if (d <= 32) f(std::integral_constant<int, 4>{});
+    else if (d <= 64) f(std::integral_constant<int, 8>{});
+    else if (d <= 128) f(std::integral_constant<int, 16>{});
+    else f(std::integral_constant<int, 32>{});
+}
 template <int DT>
-void launch_append(const AppendArgs &a, hipStream_t st) {
-    const int groups = hq::kv4_groups(a.c.t, a.c.batch);
-    const bool quads = (a.rotary >> 1) % 4 == 0;
-    const auto go = [&](auto lp) {
+void launch_append(AppendArgs a, hipStream_t st) {
+    const int groups = hq::kv4_groups(a.c.t, a.c.batch), half = a.rotary >> 1;
+    const Pairs pairs = a.interleaved || !a.rotary ? kNeighbours : half <= 64 && half >= 8 && hq::is_pow2(half) ? kLanes : half % 4 == 0 ? kQuads : kSingle;
+    with_lanes(a.c.d, [&](auto lp) {
         constexpr int LP = decltype(lp)::value;
-        const dim3 grid(groups, parts_for(groups, std::max(a.heads, a.c.kv_heads), LP));
-        if (quads) append_kernel<DT, LP, true><<<grid, 256, 0, st>>>(a);
-        else append_kernel<DT, LP, false><<<grid, 256, 0, st>>>(a);
-    };
-    if (a.c.d <= 32) go(std::integral_constant<int, 4>{});
-    else if (a.c.d <= 64) go(std::integral_constant<int, 8>{});
-    else if (a.c.d <= 128) go(std::integral_constant<int, 16>{});
-    else go(std::integral_constant<int, 32>{});
+        a.q_parts = parts_for(a.c, groups, a.heads, LP, 8);
+        a.k_parts = parts_for(a.c, groups, a.c.kv_heads, LP, 8);
+        const dim3 grid(groups, a.q_parts + 2 * a.k_parts);
+        switch (pairs) {
+            case kNeighbours: append_kernel<DT, LP, kNeighbours><<<grid, 256, 0, st>>>(a); break;
+            case kLanes: append_kernel<DT, LP, kLanes><<<grid, 256, 0, st>>>(a); break;
+            case kQuads: append_kernel<DT, LP, kQuads><<<grid, 256, 0, st>>>(a); break;
+            default: append_kernel<DT, LP, kSingle><<<grid, 256, 0, st>>>(a); break;
+        }
+    });
 }
 template <int DT>
 void launch_read(const ReadArgs &a, hipStream_t st) {
     const int groups = hq::kv4_groups(a.c.t, a.c.batch);
-    const auto go = [&](auto lp) {
+    with_lanes(a.c.d, [&](auto lp) {
         constexpr int LP = decltype(lp)::value;
-        read_kernel<DT, LP><<<dim3(groups, parts_for(groups, a.c.kv_heads, LP)), 256, 0, st>>>(a);
-    };
-    if (a.c.d <= 32) go(std::integral_constant<int, 4>{});
-    else if (a.c.d <= 64) go(std::integral_constant<int, 8>{});
-    else if (a.c.d <= 128) go(std::integral_constant<int, 16>{});
-    else go(std::integral_constant<int, 32>{});
+        read_kernel<DT, LP><<<dim3(groups, 2 * parts_for(a.c, groups, a.c.kv_heads, LP, 8)), 256, 0, st>>>(a);
+    });
 }
 
 }  // namespace
@@ -346,7 +458,7 @@ extern "C" hq_status hq_kv4_append(const hq_kv4 *cache, const void *q, const voi
     if (c.t == 0) return HQ_OK;
     const AppendArgs a{c, q, k, v, q_weight, k_weight, q_out, strides[0], strides[1], strides[2], strides[3], strides[4], strides[5],
                        strides[6], strides[7], cos, sin, pos, positions, heads, rotary, pos_size == 8, interleaved != 0, w_dtype == HQ_F32,
-                       norm != 0, eps};
+                       norm != 0, eps, hq::magic31(c.d), 0, 0};
     const hq::LaunchCheck check;
     const auto st = static_cast<hipStream_t>(stream);
     switch (dtype) {

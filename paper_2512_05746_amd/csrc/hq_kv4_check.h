@@ -13,7 +13,7 @@ inline hq_status kv4_check(const hq_kv4 &a, int heads, Kv4 *out) {
     if (heads % a.kv_heads || !is_pow2(a.page_size) || !is_pow2(a.had_block) || a.d % a.had_block) return HQ_ERR_SHAPE;
     if (a.batch == 0 ? a.t != 0 : !a.begins && a.t % a.batch) return HQ_ERR_SHAPE;
     if (a.d > 256 || a.page_size < 8 || a.had_block > 128) return HQ_ERR_UNSUPPORTED;
-    if (a.table_pages > 0x7FFF0000 / a.page_size || a.t > 0x7FFF0000 / (heads + 1) || a.batch > 0x0FFFFFFF || a.t > 0x3FFFFFFF)
+    if (a.table_pages > 0x7FFF0000 / a.page_size || a.t > 0x7FFF0000 / (heads + 1) || a.batch > 0x03FFFFFF || a.t > 0x3FFFFFFF)
         return HQ_ERR_UNSUPPORTED;
     // (bytes of k below 2^62: places are counted in 64 bits)
     if (a.pages > (int64_t{1} << 62) / (int64_t{a.page_size} * 256) / a.kv_heads) return HQ_ERR_UNSUPPORTED;

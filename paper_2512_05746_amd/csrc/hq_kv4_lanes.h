@@ -7,20 +7,23 @@
 
 namespace {
 
-// the value of lane i ^ 4, i ^ 8 (inside a row of 16)
-__device__ __forceinline__ float lane_xor4(float v) {
-    const int x = __float_as_int(v);
-    const int up = __builtin_amdgcn_update_dpp(x, x, 0x104, 0xF, 0x5, false);       // lanes 0 .. 3, 8 .. 11 from 4 further on
-    return __int_as_float(__builtin_amdgcn_update_dpp(up, x, 0x114, 0xF, 0xA, false));   // the others from 4 before
-}
-__device__ __forceinline__ float lane_xor8(float v) { return __int_as_float(dpp<0x128>(__float_as_int(v))); }   // row turned by 8
+// Which 8 channels of a head a lane has: block number kv4_block(in), so that blocks whose numbers differ in one bit are in lanes that one
+// permute exchanges: bits 0 and 1 inside quads, bit 2 in a mirrored half row (lane i ^ 7), bit 3 in a mirrored row (i ^ 15).  Heads begin at a
+// lane that is a multiple of their lanes, a power of two.
+__host__ __device__ __forceinline__ int kv4_block(int in) { return (in & 19) ^ (in & 4 ? 7 : 0) ^ (in & 8 ? 12 : 0); }
 
+// the value of the lane whose block differs in bit BIT
+template <int BIT>
+__device__ __forceinline__ float lane_of_bit(float v) {
+    constexpr int CTRL = BIT == 0 ? 0xB1 : BIT == 1 ? 0x4E : BIT == 2 ? 0x141 : 0x140;
+    return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xF, 0xF, true));
+}
 // One step between lanes: sums in the lanes whose bit is 0, differences in the others.
-template <class F>
-__device__ __forceinline__ void walsh_lanes(float (&v)[8], int bit, F other) {
-    const float sign = bit ? -1.0f : 1.0f;
+template <int BIT>
+__device__ __forceinline__ void walsh_lanes(float (&v)[8], int block) {
+    const float sign = block >> BIT & 1 ? -1.0f : 1.0f;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = fmaf(v[i], sign, other(v[i]));
+    for (int i = 0; i < 8; ++i) v[i] = lane_of_bit<BIT>(v[i]) + v[i] * sign;   // (the product is exact)
 }
 template <int STEP>
 __device__ __forceinline__ void walsh_own(float (&v)[8]) {
@@ -32,16 +35,15 @@ __device__ __forceinline__ void walsh_own(float (&v)[8]) {
             v[i + STEP] = a - b;
         }
 }
-// The transform of blocks of 2^log2 channels (up to 128: 16 lanes), without its factor 2^(-log2 / 2).  Lane `in` of a head has channels
-// 8 in .. 8 in + 7; heads begin at a lane that is a multiple of their lanes, a power of two.
-__device__ __forceinline__ void walsh(float (&v)[8], int in, int log2) {
+// The transform of blocks of 2^log2 channels (up to 128: 16 lanes), without its factor 2^(-log2 / 2); `block`: the lane's 8 channels.
+__device__ __forceinline__ void walsh(float (&v)[8], int block, int log2) {
     if (log2 > 0) walsh_own<1>(v);
     if (log2 > 1) walsh_own<2>(v);
     if (log2 > 2) walsh_own<4>(v);
-    if (log2 > 3) walsh_lanes(v, in & 1, [](float x) { return __int_as_float(dpp<0xB1>(__float_as_int(x))); });
-    if (log2 > 4) walsh_lanes(v, in & 2, [](float x) { return __int_as_float(dpp<0x4E>(__float_as_int(x))); });
-    if (log2 > 5) walsh_lanes(v, in & 4, lane_xor4);
-    if (log2 > 6) walsh_lanes(v, in & 8, lane_xor8);
+    if (log2 > 3) walsh_lanes<0>(v, block);
+    if (log2 > 4) walsh_lanes<1>(v, block);
+    if (log2 > 5) walsh_lanes<2>(v, block);
+    if (log2 > 6) walsh_lanes<3>(v, block);
 }
 __device__ __forceinline__ float walsh_factor(int log2) {
     return __builtin_ldexpf(log2 & 1 ? 0.70710678118654752f : 1.0f, -(log2 >> 1));
@@ -70,6 +72,14 @@ __device__ __forceinline__ half8v kv4_halves(uint32_t w) {
     const half2v a = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, 1.0f, 0), b = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, 1.0f, 1),
                  c = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, 1.0f, 2), d = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, 1.0f, 3);
     return half8v{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+}
+
+// The numbers of 8 codes as floats.
+typedef float float2v __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ void kv4_floats(uint32_t w, float (&v)[8]) {
+    const float2v a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.0f, 0), b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.0f, 1),
+                  c = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.0f, 2), d = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.0f, 3);
+    v[0] = a[0], v[1] = a[1], v[2] = b[0], v[3] = b[1], v[4] = c[0], v[5] = c[1], v[6] = d[0], v[7] = d[1];
 }
 
 template <class T>
