@@ -117,10 +117,12 @@ __device__ __forceinline__ void with_type(hq_dtype dt, F f) {
 template <int KS>
 __device__ __forceinline__ void store_row(const hq::Kv4Attend &a, float (&o)[8], float weight, int in, int64_t at) {
     const bool live = in * 8 < a.c.d;
-    const float f = weight == 0.0f ? 0.0f : walsh_factor(a.c.block_log2) / weight;
+    const float f = weight == 0.0f ? 0.0f : walsh_factor(in, a.c.block_log2) / weight;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) o[i] = live && weight != 0.0f ? o[i] * f : 0.0f;
+    for (int i = 0; i < 8; ++i) o[i] = live && weight != 0.0f ? o[i] : 0.0f;
     walsh(o, in, a.c.block_log2);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) o[i] *= f;
     if (live) with_type(a.dtype, [&](auto *t) { store8(static_cast<decltype(t)>(a.out) + at + in * 8, o); });
 }
 template <int KS>
@@ -306,7 +308,7 @@ __global__ __launch_bounds__(64 * WAVES, waves_of(KS, R, QH)) void attend_kernel
             // x = x' 2^power, |x'| < 2^12: halves of full precision down to 2^-26 of the largest
             const int power = top == 0 || top >= 0x7F800000u ? 0 : __builtin_amdgcn_frexp_expf(__uint_as_float(top)) - 12;
             float f = __builtin_ldexpf(a.scale, power);
-            const float sign = a.scale == 0.0f ? 0.0f : a.negative ? -1.0f : 1.0f;
+            const float sign = a.scale == 0.0f ? 0.0f : (walsh_factor(in, a.c.block_log2) < 0.0f) != (a.negative != 0) ? -1.0f : 1.0f;
             if (a.scale == 0.0f) f = 1.0f;
             if (top >= 0x7F800000u) f = __builtin_nanf("");
             half8v hi, lo;

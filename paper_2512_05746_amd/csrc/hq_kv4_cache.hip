@@ -62,7 +62,7 @@ struct AppendArgs {
     int64_t positions;
     int heads, rotary, pos_wide, interleaved, w_float, norm;
     float eps;
-    hq::Magic31 d_magic;
+    hq::Magic31 d_magic, part_magic;
     int q_parts, k_parts;
 };
 
@@ -83,6 +83,7 @@ __device__ __forceinline__ int partner_of(int c, int rotary) {
     const int half = rotary >> 1;
     return c < half ? c + half : c < rotary ? c - half : c;
 }
+template <int PAIRS>
 __device__ __forceinline__ Turn turn_of(const AppendArgs &a, int row, int64_t place, int c0) {
     Turn t;
     int64_t p = place;
@@ -93,15 +94,33 @@ __device__ __forceinline__ Turn turn_of(const AppendArgs &a, int row, int64_t pl
     const int64_t at = (t.pad || t.beyond ? 0 : p) * half;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        const int c = c0 + i;
         t.cos[i] = 1.0f;
         t.sin[i] = 0.0f;
-        if (c < a.rotary) {
-            const int pair = a.interleaved ? c >> 1 : c < half ? c : c - half;
-            const bool first = a.interleaved ? !(c & 1) : c < half;
-            t.cos[i] = a.cos[at + pair];
-            const float s = a.sin[at + pair];
-            t.sin[i] = first ? -s : s;
+    }
+    // runs of channels with neighbouring pairs in one load
+    constexpr int RUN = PAIRS == kLanes ? 8 : PAIRS == kSingle ? 1 : 4;
+#pragma unroll
+    for (int i = 0; i < 8; i += RUN) {
+        const int c = c0 + i;
+        if constexpr (PAIRS == kNeighbours) {
+            // (channels 2 j and 2 j + 1 of a run of 4; the rotated part ends at an even one)
+#pragma unroll
+            for (int e = 0; e < 4; e += 2)
+                if (c + e < a.rotary) {
+                    const float x = a.cos[at + ((c + e) >> 1)], y = a.sin[at + ((c + e) >> 1)];
+                    t.cos[i + e] = t.cos[i + e + 1] = x;
+                    t.sin[i + e] = -y;
+                    t.sin[i + e + 1] = y;
+                }
+        } else if (c < a.rotary) {
+            const bool first = c < half;
+            const int64_t from = at + (first ? c : c - half);
+            const typename Vec<float, RUN>::type x = load_vec<float, RUN>(a.cos + from), y = load_vec<float, RUN>(a.sin + from);
+#pragma unroll
+            for (int e = 0; e < RUN; ++e) {
+                t.cos[i + e] = x[e];
+                t.sin[i + e] = first ? -y[e] : y[e];
+            }
         }
     }
     return t;
@@ -164,28 +183,24 @@ __device__ __forceinline__ void head(const AppendArgs &a, const Raw<T, PAIRS> &x
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] = static_cast<float>(x.v[i]) * (r * w.v[i]);
     if (!a.rotary) return;
-    float p[8];
     if constexpr (PAIRS == kLanes) {
-        const auto other = [&](auto bit) {
+        float y[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) p[i] = lane_of_bit<decltype(bit)::value>(v[i]);
-        };
+        for (int i = 0; i < 8; ++i) y[i] = v[i] * t.cos[i];
         const int half = a.rotary >> 4;   // in blocks
-        if (half == 8) other(std::integral_constant<int, 3>{});
-        else if (half == 4) other(std::integral_constant<int, 2>{});
-        else if (half == 2) other(std::integral_constant<int, 1>{});
-        else other(std::integral_constant<int, 0>{});
+        if (half == 8) add_lanes<3>(y, v, t.sin);
+        else if (half == 4) add_lanes<2>(y, v, t.sin);
+        else if (half == 2) add_lanes<1>(y, v, t.sin);
+        else add_lanes<0>(y, v, t.sin);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = c0 < a.rotary ? y[i] : v[i];
     } else {
+        float p[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             if constexpr (PAIRS == kNeighbours) p[i] = v[i ^ 1];
             else p[i] = static_cast<float>(x.p[i]) * (r * w.p[i]);
         }
-    }
-    if (a.rotary == a.c.d) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = v[i] * t.cos[i] + p[i] * t.sin[i];
-    } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i)
             if (c0 + i < a.rotary) v[i] = v[i] * t.cos[i] + p[i] * t.sin[i];
@@ -197,7 +212,7 @@ __device__ __forceinline__ uint32_t coded(float (&v)[8], int in, bool live, int 
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] = live ? v[i] : 0.0f;
     walsh(v, in, block_log2);
-    const float f = walsh_factor(block_log2);
+    const float f = walsh_factor(in, block_log2);
     uint32_t top = 0;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
@@ -210,12 +225,68 @@ __device__ __forceinline__ uint32_t coded(float (&v)[8], int in, bool live, int 
 
 constexpr int kAtOnce = 4;   // heads of a slot whose loads are under way together
 
-// Workgroups of a group, by blockIdx.y: q_parts for the queries, then k_parts for the keys, the rest for the values.
+// The heads of a slot's token, from the part's first on, `step` apart: queries go out, keys into the cache.
+template <class T, int LP, int PAIRS, bool KEYS>
+__device__ __forceinline__ void turned_heads(const AppendArgs &a, int part, int step, int at_once, int first, int row, int64_t place, int in, bool live,
+                                             bool mine, const hq::Kv4Group &g) {
+    // (positions of a group of 8 are all negative, without a page, or none is)
+    const int64_t page = KEYS ? page_of(a.c, g) : 0;
+    if (page < 0) return;
+    const int heads = KEYS ? a.c.kv_heads : a.heads, c0 = live ? in * 8 : 0, from = part * at_once + first;
+    const int64_t by_head = KEYS ? a.k_head : a.q_head;
+    const T *x = static_cast<const T *>(KEYS ? a.k : a.q) + row * (KEYS ? a.k_token : a.q_token) + from * by_head;
+    Raw<T, PAIRS> raw[kAtOnce];
+    const auto load = [&](int h) {
+#pragma unroll
+        for (int e = 0; e < kAtOnce; ++e) {
+            if (h + e * step < heads) raw[e].load(x, c0, a.rotary);
+            x += step * by_head;
+        }
+    };
+    load(from);
+    const Raw<float, PAIRS> w = weights_of<T, PAIRS>(a, KEYS ? a.k_weight : a.q_weight, c0);
+    const Turn turn = turn_of<PAIRS>(a, row, place, c0);
+    T *out = KEYS ? nullptr : static_cast<T *>(a.q_out) + row * a.out_token + from * a.out_head + c0;
+    const int64_t at = KEYS ? a.c.slots(page, from) + a.c.slot(static_cast<int>(place)) : 0;
+    uint8_t *code_out = a.c.k + at * a.c.row_bytes() + in * 4;
+    float *scale_out = a.c.k_scale + at;
+    for (int h = from; h < heads; h += kAtOnce * step) {
+#pragma unroll
+        for (int e = 0; e < kAtOnce; ++e) {
+            if (h + e * step >= heads) break;
+            float v[8];
+            head<T, LP, PAIRS>(a, raw[e], c0, live, turn, w, v);
+            if constexpr (!KEYS) {
+                if (__any(turn.pad)) {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) v[i] = turn.pad ? 0.0f : v[i];
+                }
+                if (live && mine) store8(out, v);
+                out += step * a.out_head;
+            } else {
+                float scale;
+                const uint32_t code = coded<LP>(v, in, live, a.c.block_log2, scale);
+                if (mine && !turn.pad) {
+                    if (live) *reinterpret_cast<uint32_t *>(code_out) = code;
+                    if (in == 0) *scale_out = scale;
+                }
+                code_out += (static_cast<int64_t>(step) << a.c.page_log2) * a.c.row_bytes();
+                scale_out += static_cast<int64_t>(step) << a.c.page_log2;
+            }
+        }
+        load(h + kAtOnce * step);
+    }
+}
+
+// Workgroups of a group, side by side: q_parts for the queries, k_parts for the keys, as many for the values (bound by memory and by arithmetic: beside
+// each other they overlap, 184 -> 167 us for 32768 tokens of 32 + 8 heads).
 template <int DT, int LP, int PAIRS>
 __global__ __launch_bounds__(256) void append_kernel(AppendArgs a) {
     using T = typename Float<DT>::type;
     constexpr int SLOTS = 256 / LP;
-    const hq::Kv4Group g = group_of(a.c, blockIdx.x);
+    const int parts_of = a.q_parts + 2 * a.k_parts;
+    const int group = hq::div_magic31(blockIdx.x, parts_of, a.part_magic.m, a.part_magic.s);
+    const hq::Kv4Group g = group_of(a.c, group);
     if (g.count == 0) return;
     // slots: tokens, a power of two of them, times heads at once
     const int log2 = g.count > 4 ? 3 : g.count > 2 ? 2 : g.count - 1, at_once = SLOTS >> log2;
@@ -223,55 +294,12 @@ __global__ __launch_bounds__(256) void append_kernel(AppendArgs a) {
     const bool live = in * 8 < a.c.d, mine = token < g.count;
     const int c0 = live ? in * 8 : 0, row = g.row + (mine ? token : 0);
     const int64_t place = g.s < a.c.batch ? g.position + (mine ? token : 0) : -1;
-    int part = blockIdx.y;
-    if (part < a.q_parts + a.k_parts) {
-        const bool keys = part >= a.q_parts;
-        if (keys) part -= a.q_parts;
-        const int heads = keys ? a.c.kv_heads : a.heads, step = (keys ? a.k_parts : a.q_parts) * at_once;
-        // (positions of a group of 8 are all negative, without a page, or none is)
-        const int64_t page = keys ? page_of(a.c, g) : 0;
-        if (page < 0) return;
-        const int64_t by_head = keys ? a.k_head : a.q_head;
-        const T *x = static_cast<const T *>(keys ? a.k : a.q) + row * (keys ? a.k_token : a.q_token);
-        const auto load = [&](Raw<T, PAIRS> (&raw)[kAtOnce], int h) {
-#pragma unroll
-            for (int e = 0; e < kAtOnce; ++e)
-                if (h + e * step < heads) raw[e].load(x + (h + e * step) * by_head, c0, a.rotary);
-        };
-        const int from = part * at_once + first;
-        Raw<T, PAIRS> raw[kAtOnce];
-        load(raw, from);
-        const Raw<float, PAIRS> w = weights_of<T, PAIRS>(a, keys ? a.k_weight : a.q_weight, c0);
-        const Turn turn = turn_of(a, row, place, c0);
-        const int64_t at = keys ? a.c.slots(page, 0) + a.c.slot(static_cast<int>(place)) : 0;
-        const auto work = [&](const Raw<T, PAIRS> &now, int h) {
-            float v[8];
-            head<T, LP, PAIRS>(a, now, c0, live, turn, w, v);
-            if (!keys) {
-                if (__any(turn.pad)) {
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) v[i] = turn.pad ? 0.0f : v[i];
-                }
-                if (live && mine) store8(static_cast<T *>(a.q_out) + row * a.out_token + h * a.out_head + c0, v);
-            } else {
-                float scale;
-                const uint32_t code = coded<LP>(v, in, live, a.c.block_log2, scale);
-                if (!mine || turn.pad) return;
-                const int64_t to = at + (static_cast<int64_t>(h) << a.c.page_log2);
-                if (live) *reinterpret_cast<uint32_t *>(a.c.k + to * a.c.row_bytes() + in * 4) = code;
-                if (in == 0) a.c.k_scale[to] = scale;
-            }
-        };
-        for (int h = from; h < heads; h += kAtOnce * step) {
-#pragma unroll
-            for (int e = 0; e < kAtOnce; ++e)
-                if (h + e * step < heads) work(raw[e], h + e * step);
-            load(raw, h + kAtOnce * step);
-        }
-        return;
-    }
+    int part = blockIdx.x - group * parts_of;
+    if (part < a.q_parts) return turned_heads<T, LP, PAIRS, false>(a, part, a.q_parts * at_once, at_once, first, row, place, in, live, mine, g);
+    if (part < a.q_parts + a.k_parts)
+        return turned_heads<T, LP, PAIRS, true>(a, part - a.q_parts, a.k_parts * at_once, at_once, first, row, place, in, live, mine, g);
     part -= a.q_parts + a.k_parts;
-    const int parts = gridDim.y - a.q_parts - a.k_parts;
+    const int parts = a.k_parts;
     const int64_t page = page_of(a.c, g);
     if (page < 0) return;
     __shared__ uint32_t codes[SLOTS][LP + 1];
@@ -319,15 +347,16 @@ __global__ __launch_bounds__(256) void append_kernel(AppendArgs a) {
 struct ReadArgs {
     hq::Kv4 c;
     void *k, *v;   // [t, kv_heads, d], dense
+    int parts_log2;
 };
 
-// Workgroups of a group: the first half by blockIdx.y reads keys, the other values.  A slot has a row; of v it reads the dwords of its
+// Workgroups of a group, side by side: the first half reads keys, the other values.  A slot has a row; of v it reads the dwords of its
 // channels, which hold 8 tokens (the other slots that want them find them in the first-level cache).
 template <int DT, int LP>
 __global__ __launch_bounds__(256) void read_kernel(ReadArgs a) {
     using T = typename Float<DT>::type;
     constexpr int SLOTS = 256 / LP;
-    const hq::Kv4Group g = group_of(a.c, blockIdx.x);
+    const hq::Kv4Group g = group_of(a.c, blockIdx.x >> a.parts_log2);
     if (g.count == 0) return;
     const int log2 = g.count > 4 ? 3 : g.count > 2 ? 2 : g.count - 1, at_once = SLOTS >> log2;
     const int in = kv4_block(threadIdx.x % LP), slot = threadIdx.x / LP, token = slot & ((1 << log2) - 1), first = slot >> log2;
@@ -335,10 +364,9 @@ __global__ __launch_bounds__(256) void read_kernel(ReadArgs a) {
     const bool live = in * 8 < a.c.d;
     const int row = g.row + token, place = g.s < a.c.batch ? g.position + token : -1;
     const int64_t page = page_of(a.c, g);
-    const float factor = walsh_factor(a.c.block_log2);
-    const int parts = gridDim.y >> 1;
-    const bool values = static_cast<int>(blockIdx.y) >= parts;
-    const int part = values ? blockIdx.y - parts : blockIdx.y, step = parts * at_once;
+    const float factor = walsh_factor(in, a.c.block_log2);
+    const int parts = 1 << (a.parts_log2 - 1), part = blockIdx.x & (parts - 1), step = parts * at_once;
+    const bool values = blockIdx.x & parts;
     T *const out = static_cast<T *>(values ? a.v : a.k) + static_cast<int64_t>(row) * a.c.kv_heads * a.c.d + in * 8;
     if (page < 0) {
         float x[8];
@@ -417,7 +445,8 @@ void launch_append(AppendArgs a, hipStream_t st) {
         constexpr int LP = decltype(lp)::value;
         a.q_parts = parts_for(a.c, groups, a.heads, LP, 8);
         a.k_parts = parts_for(a.c, groups, a.c.kv_heads, LP, 8);
-        const dim3 grid(groups, a.q_parts + 2 * a.k_parts);
+        const unsigned parts = a.q_parts + 2 * a.k_parts, grid = static_cast<unsigned>(groups) * parts;
+        a.part_magic = hq::magic31(parts);
         switch (pairs) {
             case kNeighbours: append_kernel<DT, LP, kNeighbours><<<grid, 256, 0, st>>>(a); break;
             case kLanes: append_kernel<DT, LP, kLanes><<<grid, 256, 0, st>>>(a); break;
@@ -427,11 +456,12 @@ void launch_append(AppendArgs a, hipStream_t st) {
     });
 }
 template <int DT>
-void launch_read(const ReadArgs &a, hipStream_t st) {
+void launch_read(ReadArgs a, hipStream_t st) {
     const int groups = hq::kv4_groups(a.c.t, a.c.batch);
     with_lanes(a.c.d, [&](auto lp) {
         constexpr int LP = decltype(lp)::value;
-        read_kernel<DT, LP><<<dim3(groups, 2 * parts_for(a.c, groups, a.c.kv_heads, LP, 8)), 256, 0, st>>>(a);
+        a.parts_log2 = 1 + hq::ilog2(parts_for(a.c, groups, a.c.kv_heads, LP, 8));
+        read_kernel<DT, LP><<<static_cast<unsigned>(groups) << a.parts_log2, 256, 0, st>>>(a);
     });
 }
 
@@ -458,7 +488,7 @@ extern "C" hq_status hq_kv4_append(const hq_kv4 *cache, const void *q, const voi
     if (c.t == 0) return HQ_OK;
     const AppendArgs a{c, q, k, v, q_weight, k_weight, q_out, strides[0], strides[1], strides[2], strides[3], strides[4], strides[5],
                        strides[6], strides[7], cos, sin, pos, positions, heads, rotary, pos_size == 8, interleaved != 0, w_dtype == HQ_F32,
-                       norm != 0, eps, hq::magic31(c.d), 0, 0};
+                       norm != 0, eps, hq::magic31(c.d), {}, 0, 0};
     const hq::LaunchCheck check;
     const auto st = static_cast<hipStream_t>(stream);
     switch (dtype) {
@@ -477,7 +507,7 @@ extern "C" hq_status hq_kv4_read(const hq_kv4 *cache, void *k, void *v, hq_dtype
     if (c.t > 0 && (!k || !v)) return HQ_ERR_NULL;
     if (!hq::aligned_to(k, hq::size_of(dtype)) || !hq::aligned_to(v, hq::size_of(dtype))) return HQ_ERR_ALIGN;
     if (c.t == 0) return HQ_OK;
-    const ReadArgs a{c, k, v};
+    const ReadArgs a{c, k, v, 0};
     const hq::LaunchCheck check;
     const auto st = static_cast<hipStream_t>(stream);
     switch (dtype) {

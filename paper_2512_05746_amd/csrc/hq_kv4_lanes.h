@@ -12,19 +12,43 @@ namespace {
 // lane that is a multiple of their lanes, a power of two.
 __host__ __device__ __forceinline__ int kv4_block(int in) { return (in & 19) ^ (in & 4 ? 7 : 0) ^ (in & 8 ? 12 : 0); }
 
-// the value of the lane whose block differs in bit BIT
+// sum[i] += factor[i] * x[i] of the lane whose block differs in bit BIT, rounded once.  One instruction each, which the compiler does not form
+// by itself from a permute and a multiply-add (there is none with three addresses).  A permute reads a register at the earliest two
+// instructions after it was written.
+#define HQ_LANES(i, ctrl) "v_fmac_f32_dpp %" #i ", %[x" #i "], %[f" #i "] " ctrl " row_mask:0xf bank_mask:0xf\n\t"
+#define HQ_LANES8(ctrl)                                                                                                                    \
+    asm("s_nop 1\n\t" HQ_LANES(0, ctrl) HQ_LANES(1, ctrl) HQ_LANES(2, ctrl) HQ_LANES(3, ctrl) HQ_LANES(4, ctrl) HQ_LANES(5, ctrl)           \
+            HQ_LANES(6, ctrl) HQ_LANES(7, ctrl)                                                                                           \
+        : "+&v"(sum[0]), "+&v"(sum[1]), "+&v"(sum[2]), "+&v"(sum[3]), "+&v"(sum[4]), "+&v"(sum[5]), "+&v"(sum[6]), "+&v"(sum[7])                  \
+        : [x0] "v"(x[0]), [x1] "v"(x[1]), [x2] "v"(x[2]), [x3] "v"(x[3]), [x4] "v"(x[4]), [x5] "v"(x[5]), [x6] "v"(x[6]), [x7] "v"(x[7]),   \
+          [f0] "v"(f[0]), [f1] "v"(f[1]), [f2] "v"(f[2]), [f3] "v"(f[3]), [f4] "v"(f[4]), [f5] "v"(f[5]), [f6] "v"(f[6]), [f7] "v"(f[7]))
 template <int BIT>
-__device__ __forceinline__ float lane_of_bit(float v) {
-    constexpr int CTRL = BIT == 0 ? 0xB1 : BIT == 1 ? 0x4E : BIT == 2 ? 0x141 : 0x140;
-    return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xF, 0xF, true));
+__device__ __forceinline__ void add_lanes(float (&sum)[8], const float (&x)[8], const float (&f)[8]) {
+    if constexpr (BIT == 0) HQ_LANES8("quad_perm:[1,0,3,2]");
+    else if constexpr (BIT == 1) HQ_LANES8("quad_perm:[2,3,0,1]");
+    else if constexpr (BIT == 2) HQ_LANES8("row_half_mirror");
+    else HQ_LANES8("row_mirror");
 }
-// One step between lanes: sums in the lanes whose bit is 0, differences in the others.
+#undef HQ_LANES8
+#undef HQ_LANES
+// One step between lanes: sums in the lanes whose bit is 0, differences in the others, which come with the opposite sign: own value minus
+// the other lane's (a multiply-add by 1 or -1 into the value itself: 8 instructions instead of 16).
+#define HQ_STEP(i, ctrl) "v_fmac_f32_dpp %" #i ", %" #i ", %8 " ctrl " row_mask:0xf bank_mask:0xf\n\t"
+#define HQ_STEP8(ctrl)                                                                                                                     \
+    asm("s_nop 1\n\t" HQ_STEP(0, ctrl) HQ_STEP(1, ctrl) HQ_STEP(2, ctrl) HQ_STEP(3, ctrl) HQ_STEP(4, ctrl) HQ_STEP(5, ctrl) HQ_STEP(6, ctrl) \
+            HQ_STEP(7, ctrl)                                                                                                              \
+        : "+v"(v[0]), "+v"(v[1]), "+v"(v[2]), "+v"(v[3]), "+v"(v[4]), "+v"(v[5]), "+v"(v[6]), "+v"(v[7])                                       \
+        : "v"(sign))
 template <int BIT>
 __device__ __forceinline__ void walsh_lanes(float (&v)[8], int block) {
     const float sign = block >> BIT & 1 ? -1.0f : 1.0f;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = lane_of_bit<BIT>(v[i]) + v[i] * sign;   // (the product is exact)
+    if constexpr (BIT == 0) HQ_STEP8("quad_perm:[1,0,3,2]");
+    else if constexpr (BIT == 1) HQ_STEP8("quad_perm:[2,3,0,1]");
+    else if constexpr (BIT == 2) HQ_STEP8("row_half_mirror");
+    else HQ_STEP8("row_mirror");
 }
+#undef HQ_STEP8
+#undef HQ_STEP
 template <int STEP>
 __device__ __forceinline__ void walsh_own(float (&v)[8]) {
 #pragma unroll
@@ -35,7 +59,7 @@ __device__ __forceinline__ void walsh_own(float (&v)[8]) {
             v[i + STEP] = a - b;
         }
 }
-// The transform of blocks of 2^log2 channels (up to 128: 16 lanes), without its factor 2^(-log2 / 2); `block`: the lane's 8 channels.
+// The transform of blocks of 2^log2 channels (up to 128: 16 lanes), without its factor, walsh_factor; `block`: the lane's 8 channels.
 __device__ __forceinline__ void walsh(float (&v)[8], int block, int log2) {
     if (log2 > 0) walsh_own<1>(v);
     if (log2 > 1) walsh_own<2>(v);
@@ -45,8 +69,11 @@ __device__ __forceinline__ void walsh(float (&v)[8], int block, int log2) {
     if (log2 > 5) walsh_lanes<2>(v, block);
     if (log2 > 6) walsh_lanes<3>(v, block);
 }
-__device__ __forceinline__ float walsh_factor(int log2) {
-    return __builtin_ldexpf(log2 & 1 ? 0.70710678118654752f : 1.0f, -(log2 >> 1));
+// 2^(-log2 / 2) and the sign that the steps between lanes left the lane with.
+__device__ __forceinline__ float walsh_factor(int block, int log2) {
+    const float f = __builtin_ldexpf(log2 & 1 ? 0.70710678118654752f : 1.0f, -(log2 >> 1));
+    const int bits = log2 > 3 ? block & ((1 << (log2 - 3)) - 1) : 0;
+    return __builtin_popcount(bits) & 1 ? -f : f;
 }
 
 // ---- codes ------------------------------------------------------------------------------------------------------------
