@@ -61,15 +61,15 @@ __host__ __device__ __forceinline__ int kv4_sequence(const Kv4 &c, int index) {
     while (s < c.batch && kv4_group_begin(c.begin(s + 1), s + 1) <= index) ++s;
     return s;
 }
-// read: reads a number of lengths.
+// begin, end: of sequence s; read: reads a number of lengths.
 template <class F>
-__host__ __device__ __forceinline__ Kv4Group kv4_group(const Kv4 &c, int s, int index, F read) {
-    const int begin = c.begin(s), j = index - kv4_group_begin(begin, s);
+__host__ __device__ __forceinline__ Kv4Group kv4_group(const Kv4 &c, int s, int begin, int end, int index, F read) {
+    const int j = index - kv4_group_begin(begin, s);
     if (s >= c.batch) {
         const int64_t row = begin + int64_t{8} * j;
         return row < c.t ? Kv4Group{s, static_cast<int>(row), kv4_min(8, c.t - static_cast<int>(row)), 0} : Kv4Group{s, 0, 0, 0};
     }
-    const int n = c.begin(s + 1) - begin, length = kv4_max(0, read(c.lengths + s));
+    const int n = end - begin, length = kv4_max(0, read(c.lengths + s));
     const int64_t first = int64_t{length} - n;                       // position of the sequence's first token; negative: no place for it
     const int64_t group = ((first >> 3) + j) * 8;
     const int64_t from = group > first ? group : first, to = group + 8 < length ? group + 8 : length;
@@ -106,7 +106,7 @@ struct Kv4Span {        // of a sequence: blocks of rows, and the steps through 
     int begin, n, length, blocks, steps;
 };
 __host__ __device__ __forceinline__ Kv4Span kv4_span(const Kv4 &c, const Kv4Cut &cut, int s) {
-    const int begin = c.begin(s), n = kv4_max(0, c.begin(s + 1) - begin), length = kv4_max(0, c.lengths[s]);
+    const int length = kv4_max(0, c.lengths[s]), begin = c.begin(s), n = kv4_max(0, c.begin(s + 1) - begin);
     const int blocks = static_cast<int>((static_cast<uint32_t>(n) * cut.group + cut.rows() - 1) >> cut.rows_log2);   // (t x heads is below 2^31)
     const int tokens = kv4_min(kv4_min(length, c.capacity()), cut.reach);
     // rows for one wave are given to all waves, which share the tokens

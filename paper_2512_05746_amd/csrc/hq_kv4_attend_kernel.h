@@ -55,55 +55,68 @@ __device__ __forceinline__ void wave_sync() {
     __builtin_amdgcn_wave_barrier();
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 }
-// Steps of a part: every wave adds up the work by itself, in the same order.
-__device__ __forceinline__ int part_of(const hq::Kv4Attend &a, int lane) {
-    if (!a.split) return hq::kKv4Undivided;
-    float work = 0.0f;
-    for (int base = 0; base < a.c.batch; base += 64) {
-        float mine = 0.0f;
-        if (base + lane < a.c.batch) {
-            const hq::Kv4Span p = hq::kv4_span(a.c, a.cut, base + lane);
-            mine = static_cast<float>(p.blocks) * static_cast<float>(p.steps);
-        }
-        work += wave_sum(mine);
+// The sequences' spans, a lane each; the first 64 are kept.
+struct Spans {
+    const hq::Kv4Attend &a;
+    const int lane;
+    const hq::Kv4Span first;
+    __device__ __forceinline__ Spans(const hq::Kv4Attend &a, int lane) : a(a), lane(lane), first(read(0)) {}
+    __device__ __forceinline__ hq::Kv4Span read(int from) const {
+        return from + lane < a.c.batch ? hq::kv4_span(a.c, a.cut, from + lane) : hq::Kv4Span{};
     }
-    return hq::kv4_part(a.cut, work, a.c.kv_heads);
+    __device__ __forceinline__ hq::Kv4Span at(int from) const { return from ? read(from) : first; }
+    // Steps of a part: every wave adds up the work by itself, in the same order.
+    __device__ __forceinline__ int part() const {
+        if (!a.split) return hq::kKv4Undivided;
+        float work = 0.0f;
+        for (int from = 0; from < a.c.batch; from += 64) {
+            const hq::Kv4Span p = at(from);
+            work += wave_sum(static_cast<float>(p.blocks) * static_cast<float>(p.steps));
+        }
+        return hq::kv4_part(a.cut, work, a.c.kv_heads);
+    }
+};
+__device__ __forceinline__ hq::Kv4Span of_lane(const hq::Kv4Span &p, int lane) {
+    return {lane_value(p.begin, lane), lane_value(p.n, lane), lane_value(p.length, lane), lane_value(p.blocks, lane), lane_value(p.steps, lane)};
 }
 
-// What a workgroup works on: a part of the tokens of a block of rows of one key head.
+// What a workgroup works on: a part of the tokens of a block of rows of one key head.  The last blocks of a sequence, which see most, come
+// first; the heads of a block follow one another, so that eight heads go to the eight XCDs and each finds its own in its cache.
 struct Task {
     int s, head, block, part, parts, slot;   // slot: its place among the parts' sums; s = -1: none, and `block` counts up from 0
+    hq::Kv4Span span;
 };
 __device__ __forceinline__ Task task_of(const hq::Kv4Attend &a, int id, int lane) {
-    const int part = part_of(a, lane);
+    const Spans spans(a, lane);
+    const int part = spans.part();
     int base = 0, slots = 0;
     for (int from = 0; from < a.c.batch; from += 64) {
-        hq::Kv4Span p{};
-        int parts = 1;
-        if (from + lane < a.c.batch) {
-            p = hq::kv4_span(a.c, a.cut, from + lane);
-            parts = hq::kv4_parts(p, part);
-        }
+        const hq::Kv4Span p = spans.at(from);
+        const int parts = a.split ? hq::kv4_parts(p, part) : 1;
         const int count = p.blocks * parts * a.c.kv_heads, mine = parts > 1 ? count : 0;
-        const int to = wave_prefix(count), slot_to = wave_prefix(mine);
+        const int to = wave_prefix(count), slot_to = a.split ? wave_prefix(mine) : 0;
         const uint64_t behind = __ballot(base + to > id);
         if (behind) {
             const int at = __ffsll(static_cast<unsigned long long>(behind)) - 1;
-            const unsigned in = id - base - lane_value(to - count, at), blocks = lane_value(p.blocks, at), of = lane_value(parts, at);
-            const unsigned row_blocks = in / of;
             Task t;
+            t.span = of_lane(p, at);
+            const unsigned in = id - base - lane_value(to - count, at), of = lane_value(parts, at), row_blocks = of == 1 ? in : in / of;
             t.s = from + at;
             t.slot = slots + lane_value(slot_to - mine, at) + in;
             t.parts = of;
             t.part = in - row_blocks * of;
-            t.head = row_blocks / blocks;
-            t.block = row_blocks - t.head * blocks;
+            const unsigned turn = row_blocks / static_cast<unsigned>(a.c.kv_heads);
+            t.head = row_blocks - turn * a.c.kv_heads;
+            t.block = t.span.blocks - 1 - turn;
             return t;
         }
         base += lane_value(to, 63);
         slots += lane_value(slot_to, 63);
     }
-    return {-1, 0, id - base, 0, 1, 0};
+    Task none{};
+    none.s = -1;
+    none.block = id - base;
+    return none;
 }
 
 template <class F>
@@ -153,8 +166,18 @@ __device__ __forceinline__ void load_words(const uint8_t *p, uint32_t *w) {
     }
     if constexpr (N > STEP) load_words<N - STEP>(p + 4 * STEP, w + STEP);
 }
+// The largest of 8 numbers that are not NaN, by instructions that take three (written out: fmaxf comes with an instruction more for each
+// operand, in case it is a signalling NaN).
+__device__ __forceinline__ float largest(const float (&v)[8]) {
+    float x, y;
+    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(x) : "v"(v[0]), "v"(v[1]), "v"(v[2]));
+    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(y) : "v"(v[3]), "v"(v[4]), "v"(v[5]));
+    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(x) : "v"(x), "v"(v[6]), "v"(v[7]));
+    asm("v_max_f32 %0, %1, %2" : "=v"(x) : "v"(x), "v"(y));
+    return x;
+}
 // Waves a SIMD for which registers are kept: loads of other waves and conversions beside products need them.
-constexpr int waves_of(int ks, int r, int qh) { return r == 1 && ks <= 4 ? qh == 1 ? 4 : 3 : ks <= 6 ? 2 : 1; }
+constexpr int waves_of(int ks, int r, int qh, int waves) { return waves == 16 ? 4 : r == 1 && ks <= 4 ? qh == 1 ? 4 : 3 : ks <= 6 ? 2 : 1; }
 // Conversions and products in the order in which they are written: four conversions, then the products that take them.  (Left to itself the
 // compiler converts everything first, in registers that the sums need.)
 template <int N, int PRODUCTS>
@@ -171,7 +194,7 @@ template <bool B> using Flag = std::integral_constant<bool, B>;
 // waves have the same rows, and tiles of 32 tokens in turn.  QH, PH: halves for an element of H q, for a weight.  WIDE_PAGES: pages of 32
 // tokens or more, so that a tile's place is one number for the wave.
 template <int KS, int R, int WAVES, int QH, int PH, bool WIDE_PAGES>
-__global__ __launch_bounds__(64 * WAVES, waves_of(KS, R, QH)) void attend_kernel(hq::Kv4Attend a) {
+__global__ __launch_bounds__(64 * WAVES, waves_of(KS, R, QH, WAVES)) void attend_kernel(hq::Kv4Attend a) {
     constexpr int DP = 32 * KS, LP = lanes_of(KS), STAGE = DP + 8, ROW = DP + 4;
     // per wave: a tile of rows as halves, and later their sums
     constexpr int WAVE_BYTES = 16 * ROW * 4 > 16 * STAGE * 2 * QH ? 16 * ROW * 4 : 16 * STAGE * 2 * QH;
@@ -189,7 +212,7 @@ __global__ __launch_bounds__(64 * WAVES, waves_of(KS, R, QH)) void attend_kernel
         return;
     }
     const int s = task.s, head = task.head;
-    const hq::Kv4Span span = hq::kv4_span(a.c, a.cut, s);
+    const hq::Kv4Span &span = task.span;
     if (head >= a.c.kv_heads || (task.parts > 1 && task.slot >= a.slots)) return;
     const int group = a.cut.group, rows = span.n * group;   // (below 2^31: the host checks t x heads)
     const bool apart = rows - (task.block << a.cut.rows_log2) <= 16 * R;   // tokens are apart, not rows (in a sequence's last block too)
@@ -338,11 +361,12 @@ __global__ __launch_bounds__(64 * WAVES, waves_of(KS, R, QH)) void attend_kernel
 
     float4v o[R][2 * KS];
     float top[R], sum[R];                  // the reference, this lane's sum of weights
+    float most_allowed[R], minus[R];       // what moves the reference, its negative (0 for none)
     float limit = 0.0f, power = -100.0f;   // the largest v_scale that the reference allows for, its power of two
 #pragma unroll
     for (int r = 0; r < R; ++r) {
-        top[r] = -__builtin_inff();
-        sum[r] = 0.0f;
+        top[r] = most_allowed[r] = -__builtin_inff();
+        minus[r] = sum[r] = 0.0f;
 #pragma unroll
         for (int e = 0; e < 2 * KS; ++e) o[r][e] = float4v{0.0f, 0.0f, 0.0f, 0.0f};
     }
@@ -398,14 +422,13 @@ __global__ __launch_bounds__(64 * WAVES, waves_of(KS, R, QH)) void attend_kernel
             }
         }
         float most[R];
-        const float v_most = fmaxf(fmaxf(fmaxf(scale_v[0], scale_v[1]), fmaxf(scale_v[2], scale_v[3])),
-                                   fmaxf(fmaxf(scale_v[4], scale_v[5]), fmaxf(scale_v[6], scale_v[7])));
+        const float v_most = largest(scale_v);
         bool move = v_most >= limit;
 #pragma unroll
         for (int r = 0; r < R; ++r) {
-            most[r] = fmaxf(fmaxf(fmaxf(t[r][0][0], t[r][0][1]), fmaxf(t[r][0][2], t[r][0][3])), fmaxf(fmaxf(t[r][1][0], t[r][1][1]), fmaxf(t[r][1][2], t[r][1][3])));
-            most[r] *= factor[r];
-            move |= most[r] > top[r] - power + 8.0f;
+            const float all[8] = {t[r][0][0], t[r][0][1], t[r][0][2], t[r][0][3], t[r][1][0], t[r][1][1], t[r][1][2], t[r][1][3]};
+            most[r] = largest(all) * factor[r];
+            move |= most[r] > most_allowed[r];
         }
         if (__any(move)) {
             float v_top = fmaxf(v_most, __shfl_xor(v_most, 16));
@@ -423,6 +446,8 @@ __global__ __launch_bounds__(64 * WAVES, waves_of(KS, R, QH)) void attend_kernel
                 const float to = fmaxf(top[r] - before, here) + power;
                 const float f = top[r] == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(top[r] - to);
                 top[r] = to;
+                most_allowed[r] = to - power + 8.0f;
+                minus[r] = to == -__builtin_inff() ? 0.0f : -to;
                 sum[r] *= f;
 #pragma unroll
                 for (int e = 0; e < 2 * KS; ++e) o[r][e] *= f;
@@ -431,10 +456,9 @@ __global__ __launch_bounds__(64 * WAVES, waves_of(KS, R, QH)) void attend_kernel
         half8v p[R][PH];
 #pragma unroll
         for (int r = 0; r < R; ++r) {
-            const float reference = top[r] == -__builtin_inff() ? 0.0f : top[r];
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                const float w = __builtin_amdgcn_exp2f(fmaf(t[r][e >> 2][e & 3], factor[r], -reference));
+                const float w = __builtin_amdgcn_exp2f(fmaf(t[r][e >> 2][e & 3], factor[r], minus[r]));
                 const float y = w * scale_v[e];
                 sum[r] += w;
                 p[r][0][e] = static_cast<_Float16>(y);
@@ -525,7 +549,8 @@ __global__ __launch_bounds__(256) void join_kernel(hq::Kv4Attend a) {
     constexpr int DP = 32 * KS, LP = lanes_of(KS), SLOTS = 256 / LP;
     const int lane = threadIdx.x & 63, token = blockIdx.x, in = kv4_block(threadIdx.x % LP), slot = threadIdx.x / LP;
     const int q_head = EACH ? blockIdx.y * SLOTS + slot : blockIdx.y;
-    const int part = part_of(a, lane);
+    const Spans spans(a, lane);
+    const int part = spans.part();
     int s = -1, slots = 0;
     for (int from = 0; from <= a.c.batch; from += 64) {
         const int at = from + lane;
@@ -533,22 +558,19 @@ __global__ __launch_bounds__(256) void join_kernel(hq::Kv4Attend a) {
         s += __popcll(__ballot(before));
     }
     if (s >= a.c.batch) return;
+    s = __builtin_amdgcn_readfirstlane(s);
     // (of sequences without tokens the last one that begins here)
-    const hq::Kv4Span span = hq::kv4_span(a.c, a.cut, s);
+    const hq::Kv4Span span = s < 64 ? of_lane(spans.first, s) : hq::kv4_span(a.c, a.cut, s);
     const int parts = hq::kv4_parts(span, part);
     if (parts == 1 || span.length > a.c.capacity()) return;
     for (int from = 0; from < s; from += 64) {
-        int mine = 0;
-        if (from + lane < s) {
-            const hq::Kv4Span p = hq::kv4_span(a.c, a.cut, from + lane);
-            const int of = hq::kv4_parts(p, part);
-            mine = of > 1 ? p.blocks * of * a.c.kv_heads : 0;
-        }
-        slots += wave_sum(mine);
+        const hq::Kv4Span p = spans.at(from);
+        const int of = hq::kv4_parts(p, part);
+        slots += wave_sum(from + lane < s && of > 1 ? p.blocks * of * a.c.kv_heads : 0);
     }
     if (q_head >= a.heads) return;   // (EACH: no lane waits for another slot's)
     const int group = a.cut.group, head = a.cut.token_of(q_head), row = (token - span.begin) * group + q_head - head * group;
-    const int64_t before = int64_t{slots} + (int64_t{head} * span.blocks + (row >> a.cut.rows_log2)) * parts;
+    const int64_t before = int64_t{slots} + ((span.blocks - 1 - (row >> a.cut.rows_log2)) * int64_t{a.c.kv_heads} + head) * parts;
     if (before < 0 || before + parts > a.slots) return;
     const int64_t first = (before << a.cut.rows_log2) + (row & (a.cut.rows() - 1));
     float x[8], top = -__builtin_inff(), sum = 0.0f;
@@ -619,7 +641,8 @@ void kv4_attend_launch(const Kv4Attend &a, Kv4Shape shape, unsigned blocks, hipS
         else if (a.dtype == HQ_F16) with_pages(tiles, waves, two, one);
         else with_pages(tiles, waves, one, one);
     };
-    if (shape.tiles == 1 && shape.waves == 8) with_halves(std::integral_constant<int, 1>{}, std::integral_constant<int, 8>{});
+    constexpr int MOST = KS <= 4 ? 16 : 8;   // (their sums have to fit the 160 KB of LDS)
+    if (shape.waves > 4) with_halves(std::integral_constant<int, 1>{}, std::integral_constant<int, MOST>{});
     else if (shape.tiles == 1) with_halves(std::integral_constant<int, 1>{}, std::integral_constant<int, 4>{});
     else if constexpr (KS <= 4) with_halves(std::integral_constant<int, 2>{}, std::integral_constant<int, 4>{});
     if (!a.split) return;

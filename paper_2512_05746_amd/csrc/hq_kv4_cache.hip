@@ -31,19 +31,22 @@ __device__ __forceinline__ int32_t constant(const int32_t *p) {
 }
 // The group of tokens that a workgroup works on: every wave looks for the sequence by itself.
 __device__ __forceinline__ hq::Kv4Group group_of(const hq::Kv4 &c, int index) {
-    int s = -1;
-    if (c.begins) {
-        const int lane = threadIdx.x & 63;
-        for (int base = 0; base <= c.batch; base += 64) {
-            const int at = base + lane;
-            const bool before = at <= c.batch && hq::kv4_group_begin(c.begin(at), at) <= index;
-            s += __popcll(__ballot(before));
-        }
-        s = __builtin_amdgcn_readfirstlane(hq::kv4_max(s, 0));
-    } else {
-        s = hq::kv4_sequence(c, index);
+    const auto length = [](const int32_t *p) { return constant(p); };
+    if (!c.begins) {
+        const int s = hq::kv4_sequence(c, index);
+        return hq::kv4_group(c, s, c.begin(s), c.begin(s + 1), index, length);
     }
-    return hq::kv4_group(c, s, index, [](const int32_t *p) { return constant(p); });
+    const int lane = threadIdx.x & 63;
+    int s = -1, mine = 0;
+    for (int base = 0; base <= c.batch; base += 64) {
+        const int at = base + lane;
+        mine = at <= c.batch ? c.begin(at) : 0;
+        s += __popcll(__ballot(at <= c.batch && hq::kv4_group_begin(mine, at) <= index));
+    }
+    s = __builtin_amdgcn_readfirstlane(hq::kv4_max(s, 0));
+    if (c.batch < 64)   // (they are in the lanes)
+        return hq::kv4_group(c, s, __builtin_amdgcn_readlane(mine, s), __builtin_amdgcn_readlane(mine, hq::kv4_min(s + 1, c.batch)), index, length);
+    return hq::kv4_group(c, s, c.begin(s), c.begin(hq::kv4_min(s + 1, c.batch)), index, length);
 }
 __device__ __forceinline__ int64_t page_of(const hq::Kv4 &c, const hq::Kv4Group &g) {
     if (g.s >= c.batch) return -1;
@@ -460,7 +463,10 @@ void launch_read(ReadArgs a, hipStream_t st) {
     const int groups = hq::kv4_groups(a.c.t, a.c.batch);
     with_lanes(a.c.d, [&](auto lp) {
         constexpr int LP = decltype(lp)::value;
-        a.parts_log2 = 1 + hq::ilog2(parts_for(a.c, groups, a.c.kv_heads, LP, 8));
+        // (2366 tokens of 16 heads of 80: 16 workgroups a group 13 us, TWO)
+        const int parts = parts_for(a.c, groups, a.c.kv_heads, LP, 3);
+        a.parts_log2 = 1;
+        while (2 << (a.parts_log2 - 1) <= parts) ++a.parts_log2;
         read_kernel<DT, LP><<<static_cast<unsigned>(groups) << a.parts_log2, 256, 0, st>>>(a);
     });
 }

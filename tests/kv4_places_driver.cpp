@@ -49,7 +49,7 @@ static void groups(const Call &call, bool sound) {
         const int s = sequence_of(c, i);
         EXPECT(s <= c.batch, "%d", s);
         if (!c.begins) EXPECT(kv4_sequence(c, i) == s, "group %d: sequence %d, not %d", i, kv4_sequence(c, i), s);
-        const Kv4Group g = kv4_group(c, s, i, [](const int32_t *p) { return *p; });
+        const Kv4Group g = kv4_group(c, s, c.begin(s), c.begin(std::min(s + 1, c.batch)), i, [](const int32_t *p) { return *p; });
         EXPECT(g.count >= 0 && g.count <= 8 && g.row >= 0 && g.row + g.count <= c.t, "row %d, count %d of %d", g.row, g.count, c.t);
         if (g.count <= 0 || g.row < 0 || g.row + g.count > c.t) continue;
         for (int r = 0; r < g.count; ++r) ++seen[g.row + r];
