@@ -240,70 +240,70 @@ __global__ __launch_bounds__(64 * WAVES, waves_of(KS, R, QH, WAVES)) void attend
     const int end = hq::kv4_min(tiles.count(), (task.part + 1) * share);
     int i = task.part * share + (apart ? wave : 0);
 
-    // Pages of a tile, by scalar loads: vector loads arrive in order, so that waiting for one of these would mean waiting for every k and v
-    // that was asked for before it.
-    constexpr int PAGES = WIDE_PAGES ? 1 : 4;
-    struct Pages {
-        int64_t of[PAGES];   // -1: none
-        __device__ __forceinline__ int64_t at(int part) const {
-            if constexpr (PAGES == 1) return of[0];
-            else return part & 2 ? (part & 1 ? of[3] : of[2]) : (part & 1 ? of[1] : of[0]);
+    // Where the tokens of a tile are (slots), by scalar loads of the table: vector loads arrive in order, so that waiting for one of these would
+    // mean waiting for every k and v that was asked for before it.  Groups of 8 tokens have one place each, tiles of wide pages one.
+    constexpr int GROUPS = WIDE_PAGES ? 1 : 4;
+    struct Place {
+        int64_t at[GROUPS];
+        bool none[GROUPS];   // without a page: the first page is read, and dropped
+        __device__ __forceinline__ int64_t of(int part) const {
+            if constexpr (GROUPS == 1) return at[0];
+            else return part & 2 ? (part & 1 ? at[3] : at[2]) : (part & 1 ? at[1] : at[0]);
+        }
+        __device__ __forceinline__ bool missing(int part) const {
+            if constexpr (GROUPS == 1) return none[0];
+            else return part & 2 ? (part & 1 ? none[3] : none[2]) : (part & 1 ? none[1] : none[0]);
         }
     };
     const auto *const table = reinterpret_cast<const __attribute__((address_space(4))) int32_t *>(
         reinterpret_cast<uint64_t>(a.c.table + static_cast<int64_t>(s) * a.c.table_pages));
-    const auto pages_of = [&](int index) {
+    // An entry is asked for a turn before it is looked at.
+    struct Entries {
+        int32_t of[GROUPS];
+    };
+    const auto entries_of = [&](int index) {
         const int first = tiles.tile(index) * 32;
-        Pages p;
+        Entries p;
 #pragma unroll
-        for (int e = 0; e < PAGES; ++e) p.of[e] = a.c.checked(first + 8 * e, [&](int column) { return table[column]; });
+        for (int e = 0; e < GROUPS; ++e) p.of[e] = table[hq::kv4_min((first + 8 * e) >> a.c.page_log2, a.c.table_pages - 1)];
+        return p;
+    };
+    const auto place_of = [&](int index, const Entries &entries) {
+        const int first = tiles.tile(index) * 32;
+        Place p;
+#pragma unroll
+        for (int e = 0; e < GROUPS; ++e) {
+            const int64_t page = a.c.checked(first + 8 * e, [&](int) { return entries.of[e]; });
+            p.none[e] = page < 0;
+            p.at[e] = a.c.slots(hq::kv4_readable(page), head) + a.c.slot(first + 8 * e);
+        }
         return p;
     };
     Turn<KS> turn;
     const uint32_t k_lane = (8 * (m >> 2) + (m & 3)) * (DP / 2) + g * (KS * 4), v_lane = g * (DP * 4) + m * (KS * 8);
-    const auto load_k = [&](int index, const Pages &p) {
-        const int first = tiles.tile(index) * 32;
-        const uint8_t *k;
-        const float *ks;
-        if constexpr (WIDE_PAGES) {
-            const int64_t at = a.c.slots(hq::kv4_readable(p.of[0]), head) + a.c.slot(first);
-            k = a.c.k + at * (DP / 2) + k_lane;
-            ks = a.c.k_scale + at + static_cast<uint32_t>(g * 8);
-        } else {
-            const int64_t at = a.c.slots(hq::kv4_readable(p.at(m >> 2)), head) + a.c.slot(first + 8 * (m >> 2)) + (m & 3);
-            k = a.c.k + at * (DP / 2) + g * (KS * 4);
-            ks = a.c.k_scale + a.c.slots(hq::kv4_readable(p.at(g)), head) + a.c.slot(first + 8 * g);
-        }
-        turn.bad = p.at(g) < 0;
+    const auto load_k = [&](const Place &p) {
+        const uint8_t *const k = WIDE_PAGES ? a.c.k + p.at[0] * (DP / 2) + k_lane : a.c.k + (p.of(m >> 2) + (m & 3)) * (DP / 2) + g * (KS * 4);
+        const float *const ks = a.c.k_scale + p.of(g) + (WIDE_PAGES ? static_cast<uint32_t>(g * 8) : 0u);
+        turn.bad = p.missing(g);
         load_words<KS>(k, turn.k[0]);
         load_words<KS>(k + 4 * (DP / 2), turn.k[1]);
 #pragma unroll
         for (int e = 0; e < 2; ++e) turn.ks[e] = reinterpret_cast<const float4v *>(ks)[e];
     };
-    const auto load_v = [&](int index, const Pages &p) {
-        const int first = tiles.tile(index) * 32;
-        const uint8_t *v;
-        const float *vs;
-        if constexpr (WIDE_PAGES) {
-            const int64_t at = a.c.slots(hq::kv4_readable(p.of[0]), head) + a.c.slot(first);
-            v = a.c.v + at * (DP / 2) + v_lane;
-            vs = a.c.v_scale + at + static_cast<uint32_t>(g * 8);
-        } else {
-            const int64_t at = a.c.slots(hq::kv4_readable(p.at(g)), head) + a.c.slot(first + 8 * g);
-            v = a.c.v + at * (DP / 2) + m * (KS * 8);
-            vs = a.c.v_scale + at;
-        }
+    const auto load_v = [&](const Place &p) {
+        const uint8_t *const v = WIDE_PAGES ? a.c.v + p.at[0] * (DP / 2) + v_lane : a.c.v + p.of(g) * (DP / 2) + m * (KS * 8);
+        const float *const vs = a.c.v_scale + p.of(g) + (WIDE_PAGES ? static_cast<uint32_t>(g * 8) : 0u);
         load_words<2 * KS>(v, turn.v);
 #pragma unroll
         for (int e = 0; e < 2; ++e) turn.vs[e] = reinterpret_cast<const float4v *>(vs)[e];
     };
-    // k of a turn is asked for when the products with k of the turn before are done, v likewise; pages a turn before that
-    Pages pages{};
+    // k of a turn is asked for when the products with k of the turn before are done, v likewise; its place a turn before that
+    Entries entries{};
     if (i < end) {
-        pages = pages_of(i);
-        load_k(i, pages);
-        load_v(i, pages);
-        pages = pages_of(i + step < end ? i + step : i);
+        const Place place = place_of(i, entries_of(i));
+        load_k(place);
+        load_v(place);
+        entries = entries_of(i + step < end ? i + step : i);
     }
     // ---- the rows: through the transform, to halves, to the lanes of the matrix instruction
     half8v q[R][QH][KS];
@@ -393,7 +393,8 @@ __global__ __launch_bounds__(64 * WAVES, waves_of(KS, R, QH, WAVES)) void attend
         }
         const bool bad = turn.bad;
         __builtin_amdgcn_sched_barrier(0);
-        load_k(next, pages);
+        const Place place = place_of(next, entries);
+        load_k(place);
         __builtin_amdgcn_sched_barrier(0);
         float scale_v[8];
 #pragma unroll
@@ -476,9 +477,9 @@ __global__ __launch_bounds__(64 * WAVES, waves_of(KS, R, QH, WAVES)) void attend
         }
         order<2 * KS, R * PH>();
         __builtin_amdgcn_sched_barrier(0);
-        load_v(next, pages);
+        load_v(place);
         __builtin_amdgcn_sched_barrier(0);
-        pages = pages_of(i + 2 * step < end ? i + 2 * step : next);
+        entries = entries_of(i + 2 * step < end ? i + 2 * step : next);
     }
     // ---- the waves' sums together, and out
 #pragma unroll
