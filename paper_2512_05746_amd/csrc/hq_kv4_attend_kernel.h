@@ -178,6 +178,24 @@ __device__ __forceinline__ float largest(const float (&v)[8]) {
 }
 // Waves a SIMD for which registers are kept: loads of other waves and conversions beside products need them.
 constexpr int waves_of(int ks, int r, int qh, int waves) { return waves == 16 ? 4 : r == 1 && ks <= 4 ? qh == 1 ? 4 : 3 : ks <= 6 ? 2 : 1; }
+// Of a tile's groups of 8 tokens the lane's: one for all, or one of four.
+template <class T, int N>
+__device__ __forceinline__ T of_group(const T (&x)[N], int part) {
+    if constexpr (N == 1) return x[0];
+    else return part & 2 ? (part & 1 ? x[3] : x[2]) : (part & 1 ? x[1] : x[0]);
+}
+// Row m of the products with v has, of each 64 channels, 4 (2 in a last part of 32): lanes that follow one another read what follows one another.
+// Lane m's channel number e.
+template <int KS>
+__device__ __forceinline__ constexpr int channel_of(int m, int e) {
+    return e / 4 * 64 + (2 * KS - e / 4 * 4 < 4 ? 2 : 4) * m + e % 4;
+}
+template <int N>
+__device__ __forceinline__ void load_channels(const uint8_t *p, int m, uint32_t *w) {
+    constexpr int STEP = N < 4 ? N : 4;
+    load_words<STEP>(p + m * (4 * STEP), w);
+    if constexpr (N > STEP) load_channels<N - STEP>(p + 256, m, w + STEP);
+}
 // Conversions and products in the order in which they are written: four conversions, then the products that take them.  (Left to itself the
 // compiler converts everything first, in registers that the sums need.)
 template <int N, int PRODUCTS>
@@ -240,32 +258,32 @@ __global__ __launch_bounds__(64 * WAVES, waves_of(KS, R, QH, WAVES)) void attend
     const int end = hq::kv4_min(tiles.count(), (task.part + 1) * share);
     int i = task.part * share + (apart ? wave : 0);
 
-    // Where the tokens of a tile are (slots), by scalar loads of the table: vector loads arrive in order, so that waiting for one of these would
-    // mean waiting for every k and v that was asked for before it.  Groups of 8 tokens have one place each, tiles of wide pages one.
+    // Where the tokens of a tile are, by scalar loads of the table: vector loads arrive in order, so that waiting for one of these would
+    // mean waiting for every k and v that was asked for before it.  Groups of 8 tokens have one place each, tiles of wide pages one.  (Scalar
+    // instructions take the wave's turns too: a place is two multiplications of 32 bits, from what one head's page begins with.)
     constexpr int GROUPS = WIDE_PAGES ? 1 : 4;
+    const uint32_t page_slots = static_cast<uint32_t>(a.c.kv_heads) << a.c.page_log2, page_bytes = page_slots * (DP / 2), pages = static_cast<uint32_t>(a.c.pages);
+    const int64_t head_slot = static_cast<int64_t>(head) << a.c.page_log2;
+    const uint8_t *const k_head = a.c.k + head_slot * (DP / 2), *const v_head = a.c.v + head_slot * (DP / 2);
+    const uint8_t *const ks_head = reinterpret_cast<const uint8_t *>(a.c.k_scale + head_slot), *const vs_head = reinterpret_cast<const uint8_t *>(a.c.v_scale + head_slot);
     struct Place {
-        int64_t at[GROUPS];
-        bool none[GROUPS];   // without a page: the first page is read, and dropped
-        __device__ __forceinline__ int64_t of(int part) const {
-            if constexpr (GROUPS == 1) return at[0];
-            else return part & 2 ? (part & 1 ? at[3] : at[2]) : (part & 1 ? at[1] : at[0]);
-        }
-        __device__ __forceinline__ bool missing(int part) const {
-            if constexpr (GROUPS == 1) return none[0];
-            else return part & 2 ? (part & 1 ? none[3] : none[2]) : (part & 1 ? none[1] : none[0]);
-        }
+        uint64_t codes[GROUPS], scales[GROUPS];   // in bytes
+        bool none[GROUPS];                        // without a page: the first page is read, and dropped
     };
     const auto *const table = reinterpret_cast<const __attribute__((address_space(4))) int32_t *>(
         reinterpret_cast<uint64_t>(a.c.table + static_cast<int64_t>(s) * a.c.table_pages));
     // An entry is asked for a turn before it is looked at.
     struct Entries {
-        int32_t of[GROUPS];
+        uint32_t of[GROUPS];
     };
     const auto entries_of = [&](int index) {
         const int first = tiles.tile(index) * 32;
         Entries p;
 #pragma unroll
-        for (int e = 0; e < GROUPS; ++e) p.of[e] = table[hq::kv4_min((first + 8 * e) >> a.c.page_log2, a.c.table_pages - 1)];
+        for (int e = 0; e < GROUPS; ++e) {
+            const int column = (first + 8 * e) >> a.c.page_log2;
+            p.of[e] = table[WIDE_PAGES ? column : hq::kv4_min(column, a.c.table_pages - 1)];   // (a wide tile begins inside the sequence)
+        }
         return p;
     };
     const auto place_of = [&](int index, const Entries &entries) {
@@ -273,27 +291,29 @@ __global__ __launch_bounds__(64 * WAVES, waves_of(KS, R, QH, WAVES)) void attend
         Place p;
 #pragma unroll
         for (int e = 0; e < GROUPS; ++e) {
-            const int64_t page = a.c.checked(first + 8 * e, [&](int) { return entries.of[e]; });
-            p.none[e] = page < 0;
-            p.at[e] = a.c.slots(hq::kv4_readable(page), head) + a.c.slot(first + 8 * e);
+            const uint32_t slot = a.c.slot(first + 8 * e);
+            p.none[e] = entries.of[e] >= pages || (!WIDE_PAGES && first + 8 * e >= a.c.capacity());   // (a negative one is large)
+            const uint32_t page = p.none[e] ? 0 : entries.of[e];
+            p.codes[e] = static_cast<uint64_t>(page) * page_bytes + slot * (DP / 2);
+            p.scales[e] = static_cast<uint64_t>(page) * (page_slots * 4) + slot * 4;
         }
         return p;
     };
     Turn<KS> turn;
-    const uint32_t k_lane = (8 * (m >> 2) + (m & 3)) * (DP / 2) + g * (KS * 4), v_lane = g * (DP * 4) + m * (KS * 8);
+    const uint32_t k_lane = ((WIDE_PAGES ? 8 * (m >> 2) : 0) + (m & 3)) * (DP / 2) + g * (KS * 4);
+    const uint32_t v_lane = WIDE_PAGES ? g * (DP * 4) : 0, scale_lane = WIDE_PAGES ? g * 32 : 0;
     const auto load_k = [&](const Place &p) {
-        const uint8_t *const k = WIDE_PAGES ? a.c.k + p.at[0] * (DP / 2) + k_lane : a.c.k + (p.of(m >> 2) + (m & 3)) * (DP / 2) + g * (KS * 4);
-        const float *const ks = a.c.k_scale + p.of(g) + (WIDE_PAGES ? static_cast<uint32_t>(g * 8) : 0u);
-        turn.bad = p.missing(g);
+        const uint8_t *const k = k_head + of_group(p.codes, m >> 2) + k_lane;
+        const uint8_t *const ks = ks_head + of_group(p.scales, g) + scale_lane;
+        turn.bad = of_group(p.none, g);
         load_words<KS>(k, turn.k[0]);
         load_words<KS>(k + 4 * (DP / 2), turn.k[1]);
 #pragma unroll
         for (int e = 0; e < 2; ++e) turn.ks[e] = reinterpret_cast<const float4v *>(ks)[e];
     };
     const auto load_v = [&](const Place &p) {
-        const uint8_t *const v = WIDE_PAGES ? a.c.v + p.at[0] * (DP / 2) + v_lane : a.c.v + p.of(g) * (DP / 2) + m * (KS * 8);
-        const float *const vs = a.c.v_scale + p.of(g) + (WIDE_PAGES ? static_cast<uint32_t>(g * 8) : 0u);
-        load_words<2 * KS>(v, turn.v);
+        const uint8_t *const vs = vs_head + of_group(p.scales, g) + scale_lane;
+        load_channels<2 * KS>(v_head + of_group(p.codes, g) + v_lane, m, turn.v);
 #pragma unroll
         for (int e = 0; e < 2; ++e) turn.vs[e] = reinterpret_cast<const float4v *>(vs)[e];
     };
@@ -489,12 +509,12 @@ __global__ __launch_bounds__(64 * WAVES, waves_of(KS, R, QH, WAVES)) void attend
         if (apart) __syncthreads();
         else wave_sync();
         float *const mine = reinterpret_cast<float *>(lds[wave]);
-        // lane (m, g) has channels 2 KS (4 g + i) + e of row m
+        // lane (m, g) has, of row m, the channels of rows 4 g + e of the products
 #pragma unroll
         for (int e = 0; e < 4; ++e)
 #pragma unroll
             for (int c = 0; c < 2 * KS; c += 2) {
-                *reinterpret_cast<float2v *>(mine + m * ROW + 2 * KS * (4 * g + e) + c) = float2v{o[r][c][e], o[r][c + 1][e]};
+                *reinterpret_cast<float2v *>(mine + m * ROW + channel_of<KS>(4 * g + e, c)) = float2v{o[r][c][e], o[r][c + 1][e]};
             }
         if (g == 0) {
             row_top[wave][m] = top[r];

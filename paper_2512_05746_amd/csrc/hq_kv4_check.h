@@ -15,8 +15,8 @@ inline hq_status kv4_check(const hq_kv4 &a, int heads, Kv4 *out) {
     if (a.d > 256 || a.page_size < 8 || a.had_block > 128) return HQ_ERR_UNSUPPORTED;
     if (a.table_pages > 0x7FFF0000 / a.page_size || a.t > 0x7FFF0000 / (heads + 1) || a.batch > 0x03FFFFFF || a.t > 0x3FFFFFFF)
         return HQ_ERR_UNSUPPORTED;
-    // (bytes of k below 2^62: places are counted in 64 bits)
-    if (a.pages > (int64_t{1} << 62) / (int64_t{a.page_size} * 256) / a.kv_heads) return HQ_ERR_UNSUPPORTED;
+    // (a page's place is its number times what a page takes of codes, both of 32 bits)
+    if (a.pages > 0x7FFFFFFF || int64_t{a.page_size} * a.kv_heads > 0xFFFFFFFFll / 128) return HQ_ERR_UNSUPPORTED;
     if (a.t > 0 && (!a.k || !a.v || !a.k_scale || !a.v_scale || !a.page_table || !a.lengths)) return HQ_ERR_NULL;
     if (!aligned16(a.k) || !aligned16(a.v) || !aligned16(a.k_scale) || !aligned16(a.v_scale)) return HQ_ERR_ALIGN;
     if (!aligned_to(a.page_table, 4) || !aligned_to(a.lengths, 4) || !aligned_to(a.begins, 4)) return HQ_ERR_ALIGN;
