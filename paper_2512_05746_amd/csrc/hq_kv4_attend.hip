@@ -24,9 +24,9 @@ Plan plan_of(const hq::Kv4 &c, int heads, hq_dtype dtype, int window, int sinks)
     Plan p;
     const bool few = rows <= 16 || c.pitch > 128;
     const int64_t items = int64_t{c.kv_heads} * std::max<int64_t>(1, c.batch);
-    p.shape = few ? hq::Kv4Shape{1, items <= cus && rows <= 16 && c.capacity() <= 4096 ? (c.pitch <= 128 ? 16 : 8) : 4} : hq::Kv4Shape{2, 4};
+    p.shape = few ? hq::Kv4Shape{1, items <= cus && rows <= 16 && c.capacity() <= 2048 ? 8 : 4} : hq::Kv4Shape{2, 4};
     const int64_t most = int64_t{c.kv_heads} * (int64_t{c.t} * group / p.shape.rows() + c.batch);   // blocks of rows
-    const int target = 4 * cus;
+    const int target = (p.shape.tiles == 1 ? 3 : 2) * cus;   // workgroups of 4 waves that a CU holds
     const int64_t tokens = window > 0 ? std::min<int64_t>(c.capacity(), int64_t{window} + sinks + 64) : c.capacity();
     const hq::Magic31 m = hq::magic31(group);
     p.cut = hq::Kv4Cut{hq::ilog2(p.shape.rows()), hq::ilog2(p.shape.waves), group, target, 8, window, sinks,

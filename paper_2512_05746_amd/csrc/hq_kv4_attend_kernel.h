@@ -177,7 +177,7 @@ __device__ __forceinline__ float largest(const float (&v)[8]) {
     return x;
 }
 // Waves a SIMD for which registers are kept: loads of other waves and conversions beside products need them.
-constexpr int waves_of(int ks, int r, int qh, int waves) { return waves == 16 ? 4 : r == 1 && ks <= 4 ? qh == 1 ? 4 : 3 : ks <= 6 ? 2 : 1; }
+constexpr int waves_of(int ks, int r, int qh, int waves) { return waves == 8 ? 2 : r == 1 && ks <= 4 ? qh == 1 ? 4 : 3 : ks <= 6 ? 2 : 1; }
 // Of a tile's groups of 8 tokens the lane's: one for all, or one of four.
 template <class T, int N>
 __device__ __forceinline__ T of_group(const T (&x)[N], int part) {
@@ -326,6 +326,17 @@ __global__ __launch_bounds__(64 * WAVES, waves_of(KS, R, QH, WAVES)) void attend
         entries = entries_of(i + step < end ? i + step : i);
     }
     // ---- the rows: through the transform, to halves, to the lanes of the matrix instruction
+    using T = std::conditional_t<(PH > 1), float, std::conditional_t<(QH > 1), _Float16, __bf16>>;
+    constexpr int PASSES = LP / 4;   // of a wave through a tile's rows; of all waves fewer
+    typename Vec<T, 8>::type raw[R][PASSES];
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+#pragma unroll
+        for (int pass = 0; pass < PASSES; ++pass) {   // (all rows asked for before the first is looked at)
+            const int i2 = mine_at + pass * by, row = row0 + 16 * r + i2;
+            raw[r][pass] = typename Vec<T, 8>::type{};
+            if (i2 < 16 && row < rows && in * 8 < a.c.d) raw[r][pass] = load_vec<T, 8>(static_cast<const T *>(a.q) + at_of(row, a.q_token, a.q_head) + in * 8);
+        }
     half8v q[R][QH][KS];
     float factor[R];
     int position[R];
@@ -334,15 +345,13 @@ __global__ __launch_bounds__(64 * WAVES, waves_of(KS, R, QH, WAVES)) void attend
         if (apart && r) __syncthreads();
         const int owner = apart ? 0 : wave;
         uint8_t *const stage = lds[owner];
-        for (int i2 = mine_at; i2 < 16; i2 += by) {
-            const int row = row0 + 16 * r + i2;
+#pragma unroll
+        for (int pass = 0; pass < PASSES; ++pass) {
+            const int i2 = mine_at + pass * by;
+            if (i2 >= 16) break;
             float x[8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] = 0.0f;
-            if (row < rows && in * 8 < a.c.d) {
-                const int64_t at = at_of(row, a.q_token, a.q_head) + in * 8;
-                with_type(a.dtype, [&](auto *t) { load8(static_cast<decltype(t)>(const_cast<void *>(a.q)) + at, x); });
-            }
+            for (int e = 0; e < 8; ++e) x[e] = static_cast<float>(raw[r][pass][e]);
             walsh(x, in, a.c.block_log2);
             uint32_t top = 0;
 #pragma unroll
@@ -662,8 +671,7 @@ void kv4_attend_launch(const Kv4Attend &a, Kv4Shape shape, unsigned blocks, hipS
         else if (a.dtype == HQ_F16) with_pages(tiles, waves, two, one);
         else with_pages(tiles, waves, one, one);
     };
-    constexpr int MOST = KS <= 4 ? 16 : 8;   // (their sums have to fit the 160 KB of LDS)
-    if (shape.waves > 4) with_halves(std::integral_constant<int, 1>{}, std::integral_constant<int, MOST>{});
+    if (shape.waves == 8) with_halves(std::integral_constant<int, 1>{}, std::integral_constant<int, 8>{});
     else if (shape.tiles == 1) with_halves(std::integral_constant<int, 1>{}, std::integral_constant<int, 4>{});
     else if constexpr (KS <= 4) with_halves(std::integral_constant<int, 2>{}, std::integral_constant<int, 4>{});
     if (!a.split) return;
