@@ -521,7 +521,8 @@ hq_status hq_qk_norm_rope_backward(const void *dq, const void *dk, const void *q
  * Several sequences may share pages that are only read.
  *
  *   page_size power of two from 8 on;  d a multiple of 8 up to 256;  had_block power of two up to 128 that divides d;
- *   table_pages * page_size, t * heads, pages below 2^31; page_size * kv_heads up to 2^25 (half of a page with its heads is below 4 GiB).
+ *   table_pages * page_size, t * heads, pages below 2^31; page_size * kv_heads up to 2^25 (half of a page with its heads is below 4 GiB);
+ *   t / 8 + 2 batch up to 5 * 2^20, and of attention what one launch holds (HQ_ERR_UNSUPPORTED beyond).
  * page_table, lengths and begins are on the device: what they hold is read when the kernel runs.  A place without a page (an entry that is
  * negative or not below `pages`, a place beyond the table) is never written; what is read there is NaN.  k and v: 16-byte aligned, the
  * scales too.

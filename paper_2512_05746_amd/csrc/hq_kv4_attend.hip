@@ -58,7 +58,7 @@ extern "C" hq_status hq_kv4_attention(const hq_kv4 *cache, const void *q, hq_dty
     if (c.t == 0) return HQ_OK;
     if (window == 0) sinks = 0;
     const Plan p = plan_of(c, heads, dtype, window, sinks);
-    if (p.blocks > 0x7FFFFFFF) return HQ_ERR_UNSUPPORTED;
+    if (p.blocks * 64 * p.shape.waves > 0xFFFFFFFFll) return HQ_ERR_UNSUPPORTED;   // lanes of a launch
     if (p.slots && !workspace) return HQ_ERR_NULL;
     if (!hq::aligned16(workspace)) return HQ_ERR_ALIGN;
     hq::Kv4Attend a{};

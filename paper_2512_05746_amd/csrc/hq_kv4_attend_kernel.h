@@ -11,11 +11,11 @@
 // 16 tokens is token 8 (m / 4) + m % 4 and of the second 4 further on.  v is kept channel by channel for 8 tokens, the order of its operand.
 //
 // Roundings: H q to half (2^-11 of an element), in units of a power of two that leaves the row's largest below 2^12; weights times v_scale to
-// half, in units of the power of two next to the largest v_scale so far (2^-11; below 2^-14 of it, 2^-25 of it).  For half and 32-bit
+// half, the largest v_scale so far times the weight of the reference as 2^6 to 2^7 (2^-11; below 2^-20 of it, 2^-31 of it).  For half and 32-bit
 // results H q is two halves (2^-22; a rounding of q moves every score of its row, and results were off by twice their own rounding), for
 // 32-bit ones the weights too.  Codes are exact, sums are 32 bits.
 //
-// The reference moves only where s would exceed it by 8 (2^8 times 2 is far inside a half), so most turns leave the sums alone.
+// The reference moves only where s would exceed it by 8, so most turns leave the sums alone.
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -206,6 +206,9 @@ __device__ __forceinline__ void order() {
         order<N - 1, PRODUCTS>();
     }
 }
+// Weights times v_scale are kept 2^kRoom times as large as the reference says, next to the end of a half (2^6 2 2^8 = 2^15): below 2^-14 a half
+// has fewer bits, and over long sequences most weights are small.
+constexpr int kRoom = 6;
 template <bool B> using Flag = std::integral_constant<bool, B>;
 
 // R tiles of 16 rows a wave, WAVES waves a workgroup.  Rows that fill more than one wave's tiles: rows of its own for each wave.  Otherwise all
@@ -223,10 +226,13 @@ __global__ __launch_bounds__(64 * WAVES, waves_of(KS, R, QH, WAVES)) void attend
     const int in = kv4_block(lane % LP);   // the 8 channels that the lane has where a row is dealt to lanes
     if (task.s < 0) {
         // rows of no sequence: zeros
-        const int begin = a.c.begin(a.c.batch), rows = (a.c.t - begin) * a.heads, from = blockIdx.x - task.block;
-        const int step = (gridDim.x - from) * (64 * WAVES / LP);
-        for (int r = task.block * (64 * WAVES / LP) + threadIdx.x / LP; r < rows; r += step)
-            store_all<KS>(a, 0.0f, in, (begin + r / a.heads) * a.out_token + r % a.heads * a.out_head);
+        if (task.block < 0) return;   // (begins that do not rise can ask for more work than can be counted)
+        const int begin = a.c.begin(a.c.batch), rows = (a.c.t - begin) * a.heads;
+        const int64_t from = int64_t{blockIdx.x} - task.block, step = (int64_t{gridDim.x} - from) * (64 * WAVES / LP);
+        for (int64_t r = int64_t{task.block} * (64 * WAVES / LP) + threadIdx.x / LP; r < rows; r += step) {
+            const int row = static_cast<int>(r);
+            store_all<KS>(a, 0.0f, in, (begin + row / a.heads) * a.out_token + row % a.heads * a.out_head);
+        }
         return;
     }
     const int s = task.s, head = task.head;
@@ -391,7 +397,7 @@ __global__ __launch_bounds__(64 * WAVES, waves_of(KS, R, QH, WAVES)) void attend
     float4v o[R][2 * KS];
     float top[R], sum[R];                  // the reference, this lane's sum of weights
     float most_allowed[R], minus[R];       // what moves the reference, its negative (0 for none)
-    float limit = 0.0f, power = -100.0f;   // the largest v_scale that the reference allows for, its power of two
+    float limit = 0.0f, power = -100.0f;   // the largest v_scale that the reference allows for, its power of two less kRoom
 #pragma unroll
     for (int r = 0; r < R; ++r) {
         top[r] = most_allowed[r] = -__builtin_inff();
@@ -465,9 +471,9 @@ __global__ __launch_bounds__(64 * WAVES, waves_of(KS, R, QH, WAVES)) void attend
             v_top = fmaxf(v_top, __shfl_xor(v_top, 32));
             const float before = power;
             if (v_top >= limit && v_top > 0.0f) {
-                const int p = hq::kv4_max(-100, hq::kv4_min(100, __builtin_amdgcn_frexp_expf(v_top) - 1));
+                const int p = hq::kv4_max(-100, hq::kv4_min(100, __builtin_amdgcn_frexp_expf(v_top) - 1 - kRoom));
                 power = fmaxf(power, static_cast<float>(p));
-                limit = power == 100.0f ? __builtin_inff() : __builtin_ldexpf(2.0f, static_cast<int>(power));
+                limit = power == 100.0f ? __builtin_inff() : __builtin_ldexpf(2.0f, static_cast<int>(power) + kRoom);
             }
 #pragma unroll
             for (int r = 0; r < R; ++r) {

@@ -15,6 +15,7 @@ inline hq_status kv4_check(const hq_kv4 &a, int heads, Kv4 *out) {
     if (a.d > 256 || a.page_size < 8 || a.had_block > 128) return HQ_ERR_UNSUPPORTED;
     if (a.table_pages > 0x7FFF0000 / a.page_size || a.t > 0x7FFF0000 / (heads + 1) || a.batch > 0x03FFFFFF || a.t > 0x3FFFFFFF)
         return HQ_ERR_UNSUPPORTED;
+    if (a.t / 8 + 2 * int64_t{a.batch} > 0x500000) return HQ_ERR_UNSUPPORTED;   // groups: three workgroups each are one launch
     // (a page's place is its number times what a page takes of codes, both of 32 bits)
     if (a.pages > 0x7FFFFFFF || int64_t{a.page_size} * a.kv_heads > 0xFFFFFFFFll / 128) return HQ_ERR_UNSUPPORTED;
     if (a.t > 0 && (!a.k || !a.v || !a.k_scale || !a.v_scale || !a.page_table || !a.lengths)) return HQ_ERR_NULL;

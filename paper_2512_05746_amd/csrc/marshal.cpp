@@ -938,6 +938,7 @@ Kv4 kv4_of(Args &a, int64_t t) {
     for (const at::Tensor *o : {&v, &ks, &vs, &table, &lengths})
         if (o->device() != k.device()) refuse("the cache, page_table and lengths must be on one device");
     if (begins && begins->device() != k.device()) refuse("begins must be on the cache's device");
+    if (k.get_device() != c10::hip::current_device()) refuse("the cache must be on the current device");   // (whose stream the call uses)
     r.k = &k;
     r.c.k = const_cast<uint8_t *>(u8(k));
     r.c.v = const_cast<uint8_t *>(u8(v));

@@ -58,6 +58,14 @@ def test_cache_arguments(lib):
         assert call(dt=I32) == DTYPE and call(dt=9) == DTYPE
 
 
+def test_more_than_a_launch_holds(lib):
+    many = dict(t=8 * 0x500000 + 8, kv_heads=1)
+    for call in calls(lib):
+        assert call(**many) == UNSUPPORTED and call(t=8, batch=0x300000) == UNSUPPORTED
+    _, attention, _ = calls(lib)
+    assert attention(heads=32, t=40_000_000, d=256, had_block=128) == UNSUPPORTED   # 16 x 40e6 rows of 2 heads, 64 to 256 lanes
+
+
 def test_append_arguments(lib):
     append, _, _ = calls(lib)
     assert lib.hq_kv4_append(None, P, P, P, F16, 4, STRIDES, None, None, F16, P, P, 8, 64, 0, None, 0, 1, 1e-6, P, None) == NULL
