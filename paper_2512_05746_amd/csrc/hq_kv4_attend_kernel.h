@@ -43,6 +43,16 @@ __device__ __forceinline__ T wave_prefix(T v) {
     v += moved<T, 0x143, 0xC>(v);
     return v;
 }
+// (of numbers that are not negative)
+__device__ __forceinline__ int wave_max(int v) {
+    v = max(v, moved<int, 0x111, 0xF>(v));
+    v = max(v, moved<int, 0x112, 0xF>(v));
+    v = max(v, moved<int, 0x114, 0xF>(v));
+    v = max(v, moved<int, 0x118, 0xF>(v));
+    v = max(v, moved<int, 0x142, 0xA>(v));
+    v = max(v, moved<int, 0x143, 0xC>(v));
+    return __builtin_amdgcn_readlane(v, 63);
+}
 template <class T>
 __device__ __forceinline__ T lane_value(T v, int lane) {
     return __builtin_bit_cast(T, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), lane));
@@ -81,7 +91,9 @@ __device__ __forceinline__ hq::Kv4Span of_lane(const hq::Kv4Span &p, int lane) {
 }
 
 // What a workgroup works on: a part of the tokens of a block of rows of one key head.  The last blocks of a sequence, which see most, come
-// first; the heads of a block follow one another, so that eight heads go to the eight XCDs and each finds its own in its cache.
+// first, and of 64 sequences the long ones: what begins late is to end soon (12 sequences of 10 to 700 tokens, 576 workgroups of which 512 are
+// at work at once: 63 -> 57 us).  The heads of a block follow one another, so that eight heads go to the eight XCDs and each finds its own in its
+// cache.
 struct Task {
     int s, head, block, part, parts, slot;   // slot: its place among the parts' sums; s = -1: none, and `block` counts up from 0
     hq::Kv4Span span;
@@ -94,13 +106,17 @@ __device__ __forceinline__ Task task_of(const hq::Kv4Attend &a, int id, int lane
         const hq::Kv4Span p = spans.at(from);
         const int parts = a.split ? hq::kv4_parts(p, part) : 1;
         const int count = p.blocks * parts * a.c.kv_heads, mine = parts > 1 ? count : 0;
-        const int to = wave_prefix(count), slot_to = a.split ? wave_prefix(mine) : 0;
+        const int steps = count ? hq::kv4_min(p.steps, part) : 0, longest = wave_max(steps);
+        const int count_long = 2 * int64_t{steps} > longest ? count : 0, to_long = wave_prefix(count_long);
+        const int all_long = lane_value(to_long, 63), slot_to = a.split ? wave_prefix(mine) : 0;
+        const bool is_long = base + all_long > id;
+        const int to = is_long ? to_long : all_long + wave_prefix(count - count_long);
         const uint64_t behind = __ballot(base + to > id);
         if (behind) {
             const int at = __ffsll(static_cast<unsigned long long>(behind)) - 1;
             Task t;
             t.span = of_lane(p, at);
-            const unsigned in = id - base - lane_value(to - count, at), of = lane_value(parts, at), row_blocks = of == 1 ? in : in / of;
+            const unsigned in = id - base - lane_value(to - (is_long ? count_long : count - count_long), at), of = lane_value(parts, at), row_blocks = of == 1 ? in : in / of;
             t.s = from + at;
             t.slot = slots + lane_value(slot_to - mine, at) + in;
             t.parts = of;
