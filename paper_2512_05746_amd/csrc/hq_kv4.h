@@ -11,9 +11,6 @@ __host__ __device__ __forceinline__ int kv4_pitch(int d) { return (d + 31) & ~31
 __host__ __device__ __forceinline__ int kv4_min(int a, int b) { return a < b ? a : b; }
 __host__ __device__ __forceinline__ int kv4_max(int a, int b) { return a > b ? a : b; }
 
-// (the first page in place of none: what is read there is dropped)
-__host__ __device__ __forceinline__ int64_t kv4_readable(int64_t page) { return page < 0 ? 0 : page; }
-
 struct Kv4 {
     uint8_t *k, *v;             // [pages, kv_heads, page_size, pitch / 2], [pages, kv_heads, page_size / 8, pitch, 4]
     float *k_scale, *v_scale;   // [pages, kv_heads, page_size]

@@ -15,7 +15,15 @@
 // results H q is two halves (2^-22; a rounding of q moves every score of its row, and results were off by twice their own rounding), for
 // 32-bit ones the weights too.  Codes are exact, sums are 32 bits.
 //
-// The reference moves only where s would exceed it by 8, so most turns leave the sums alone.
+// The reference moves only where s would exceed it by 8 (by 2 for 32-bit results), so most turns leave the sums alone.
+//
+// What bounds it.  A few rows over many tokens: the cache's bytes (276 MB for 64 sequences of up to 16384 tokens, 32 query and 8 key heads of 128:
+// 64 us, 4.3 TB/s; a copy reaches 5.1 to 5.4).  Prompts: a turn's instructions (825 GF for 2 sequences of 4096 new tokens over 8192, the same heads:
+// 860 us, 960 TF/s; a large library product in bf16 reaches 1540): 32 products of 7.7 ns beside about 200 vector instructions, which
+// overlap with those of the SIMD's other wave in part only.  One row over few tokens: latencies, 13.5 us: about 1 until a
+// workgroup knows its work, 4 to 5 until its rows are through the transform (with the first k and v under way), 2 a turn, 2 to 3 for the results.
+// Taken back for prompts: the next tile's products beside this one's exponentials (1016 -> 1068 us), k and v asked for two tiles ahead (1110 to
+// 1130), scales one a lane and moved to where they are used (slower by the moves), three waves a SIMD (spills).
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -116,7 +124,8 @@ __device__ __forceinline__ Task task_of(const hq::Kv4Attend &a, int id, int lane
             const int at = __ffsll(static_cast<unsigned long long>(behind)) - 1;
             Task t;
             t.span = of_lane(p, at);
-            const unsigned in = id - base - lane_value(to - (is_long ? count_long : count - count_long), at), of = lane_value(parts, at), row_blocks = of == 1 ? in : in / of;
+            const unsigned in = id - base - lane_value(to - (is_long ? count_long : count - count_long), at), of = lane_value(parts, at);
+            const unsigned row_blocks = of == 1 ? in : in / of;
             t.s = from + at;
             t.slot = slots + lane_value(slot_to - mine, at) + in;
             t.parts = of;
@@ -192,7 +201,8 @@ __device__ __forceinline__ float largest(const float (&v)[8]) {
     asm("v_max_f32 %0, %1, %2" : "=v"(x) : "v"(x), "v"(y));
     return x;
 }
-// Waves a SIMD for which registers are kept: loads of other waves and conversions beside products need them.
+// Waves a SIMD for which registers are kept: loads of other waves and conversions beside products need them.  (One tile of rows: bound by loads,
+// more waves; two tiles: their sums and queries alone are 96 registers at 96 channels.)
 constexpr int waves_of(int ks, int r, int qh, int waves) { return waves == 8 ? 2 : r == 1 && ks <= 4 ? qh == 1 ? 4 : 3 : ks <= 6 ? 2 : 1; }
 // Of a tile's groups of 8 tokens the lane's: one for all, or one of four.
 template <class T, int N>
@@ -222,14 +232,16 @@ __device__ __forceinline__ void order() {
         order<N - 1, PRODUCTS>();
     }
 }
-// Weights times v_scale are kept 2^kRoom times as large as the reference says, next to the end of a half (2^6 2 2^8 = 2^15): below 2^-14 a half
-// has fewer bits, and over long sequences most weights are small.
-constexpr int kRoom = 6;
+// By how much a score may exceed the reference, as a power of two: less where weights are two halves, whose second ones want the room.
+constexpr int lazy_of(int ph) { return ph > 1 ? 2 : 8; }
+// Weights times v_scale are kept 2^room as large as the reference says, next to the end of a half (2^room 2 2^lazy = 2^15): below 2^-14 a half
+// has fewer bits, and over long sequences most weights are small (32-bit results over 3001 tokens: 2.6e-6 off without room, 3.5 to 6e-7 with 2^6).
+constexpr int room_of(int ph) { return 14 - lazy_of(ph); }
 template <bool B> using Flag = std::integral_constant<bool, B>;
 
-// R tiles of 16 rows a wave, WAVES waves a workgroup.  Rows that fill more than one wave's tiles: rows of its own for each wave.  Otherwise all
-// waves have the same rows, and tiles of 32 tokens in turn.  QH, PH: halves for an element of H q, for a weight.  WIDE_PAGES: pages of 32
-// tokens or more, so that a tile's place is one number for the wave.
+// R tiles of 16 rows a wave, WAVES waves a workgroup; a tile of k and v is converted once for R products.  Rows that fill more than one wave's
+// tiles: rows of its own for each wave.  Otherwise all waves have the same rows, and tiles of 32 tokens in turn.  QH, PH: halves for an element of
+// H q, for a weight.  WIDE_PAGES: pages of 32 tokens or more, so that a tile's place is one number for the wave.
 template <int KS, int R, int WAVES, int QH, int PH, bool WIDE_PAGES>
 __global__ __launch_bounds__(64 * WAVES, waves_of(KS, R, QH, WAVES)) void attend_kernel(hq::Kv4Attend a) {
     constexpr int DP = 32 * KS, LP = lanes_of(KS), STAGE = DP + 8, ROW = DP + 4;
@@ -284,10 +296,12 @@ __global__ __launch_bounds__(64 * WAVES, waves_of(KS, R, QH, WAVES)) void attend
     // mean waiting for every k and v that was asked for before it.  Groups of 8 tokens have one place each, tiles of wide pages one.  (Scalar
     // instructions take the wave's turns too: a place is two multiplications of 32 bits, from what one head's page begins with.)
     constexpr int GROUPS = WIDE_PAGES ? 1 : 4;
-    const uint32_t page_slots = static_cast<uint32_t>(a.c.kv_heads) << a.c.page_log2, page_bytes = page_slots * (DP / 2), pages = static_cast<uint32_t>(a.c.pages);
+    const uint32_t page_slots = static_cast<uint32_t>(a.c.kv_heads) << a.c.page_log2, page_bytes = page_slots * (DP / 2);
+    const uint32_t pages = static_cast<uint32_t>(a.c.pages);
     const int64_t head_slot = static_cast<int64_t>(head) << a.c.page_log2;
     const uint8_t *const k_head = a.c.k + head_slot * (DP / 2), *const v_head = a.c.v + head_slot * (DP / 2);
-    const uint8_t *const ks_head = reinterpret_cast<const uint8_t *>(a.c.k_scale + head_slot), *const vs_head = reinterpret_cast<const uint8_t *>(a.c.v_scale + head_slot);
+    const uint8_t *const ks_head = reinterpret_cast<const uint8_t *>(a.c.k_scale + head_slot);
+    const uint8_t *const vs_head = reinterpret_cast<const uint8_t *>(a.c.v_scale + head_slot);
     struct Place {
         uint64_t codes[GROUPS], scales[GROUPS];   // in bytes
         bool none[GROUPS];                        // without a page: the first page is read, and dropped
@@ -339,26 +353,32 @@ __global__ __launch_bounds__(64 * WAVES, waves_of(KS, R, QH, WAVES)) void attend
 #pragma unroll
         for (int e = 0; e < 2; ++e) turn.vs[e] = reinterpret_cast<const float4v *>(vs)[e];
     };
-    // k of a turn is asked for when the products with k of the turn before are done, v likewise; its place a turn before that
-    Entries entries{};
-    if (i < end) {
-        const Place place = place_of(i, entries_of(i));
-        load_k(place);
-        load_v(place);
-        entries = entries_of(i + step < end ? i + step : i);
-    }
-    // ---- the rows: through the transform, to halves, to the lanes of the matrix instruction
+    // ---- the rows are asked for, then the first k and v (by waves without tokens too: loads under way are counted in order, and what the
+    // compiler cannot count it waits for), so that the rows are prepared while these are on their way
     using T = std::conditional_t<(PH > 1), float, std::conditional_t<(QH > 1), _Float16, __bf16>>;
     constexpr int PASSES = LP / 4;   // of a wave through a tile's rows; of all waves fewer
     typename Vec<T, 8>::type raw[R][PASSES];
+    const int begin = i < end ? i : 0;
+    Entries entries = entries_of(begin);
 #pragma unroll
     for (int r = 0; r < R; ++r)
 #pragma unroll
-        for (int pass = 0; pass < PASSES; ++pass) {   // (all rows asked for before the first is looked at)
+        for (int pass = 0; pass < PASSES; ++pass) {
             const int i2 = mine_at + pass * by, row = row0 + 16 * r + i2;
             raw[r][pass] = typename Vec<T, 8>::type{};
-            if (i2 < 16 && row < rows && in * 8 < a.c.d) raw[r][pass] = load_vec<T, 8>(static_cast<const T *>(a.q) + at_of(row, a.q_token, a.q_head) + in * 8);
+            if (i2 < 16 && row < rows && in * 8 < a.c.d)
+                raw[r][pass] = load_vec<T, 8>(static_cast<const T *>(a.q) + at_of(row, a.q_token, a.q_head) + in * 8);
         }
+    __builtin_amdgcn_sched_barrier(0);
+    // k of a turn is asked for when the products with k of the turn before are done, v likewise; its place a turn before that
+    {
+        const Place place = place_of(begin, entries);
+        load_k(place);
+        load_v(place);
+        entries = entries_of(begin + step < end ? begin + step : begin);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    // through the transform, to halves, to the lanes of the matrix instruction
     half8v q[R][QH][KS];
     float factor[R];
     int position[R];
@@ -410,10 +430,11 @@ __global__ __launch_bounds__(64 * WAVES, waves_of(KS, R, QH, WAVES)) void attend
         if (!apart) wave_sync();
     }
 
+    constexpr int LAZY = lazy_of(PH), ROOM = room_of(PH);
     float4v o[R][2 * KS];
     float top[R], sum[R];                  // the reference, this lane's sum of weights
     float most_allowed[R], minus[R];       // what moves the reference, its negative (0 for none)
-    float limit = 0.0f, power = -100.0f;   // the largest v_scale that the reference allows for, its power of two less kRoom
+    float limit = 0.0f, power = -100.0f;   // the largest v_scale that the reference allows for, its power of two less ROOM
 #pragma unroll
     for (int r = 0; r < R; ++r) {
         top[r] = most_allowed[r] = -__builtin_inff();
@@ -487,9 +508,9 @@ __global__ __launch_bounds__(64 * WAVES, waves_of(KS, R, QH, WAVES)) void attend
             v_top = fmaxf(v_top, __shfl_xor(v_top, 32));
             const float before = power;
             if (v_top >= limit && v_top > 0.0f) {
-                const int p = hq::kv4_max(-100, hq::kv4_min(100, __builtin_amdgcn_frexp_expf(v_top) - 1 - kRoom));
+                const int p = hq::kv4_max(-100, hq::kv4_min(100, __builtin_amdgcn_frexp_expf(v_top) - 1 - ROOM));
                 power = fmaxf(power, static_cast<float>(p));
-                limit = power == 100.0f ? __builtin_inff() : __builtin_ldexpf(2.0f, static_cast<int>(power) + kRoom);
+                limit = power == 100.0f ? __builtin_inff() : __builtin_ldexpf(2.0f, static_cast<int>(power) + ROOM);
             }
 #pragma unroll
             for (int r = 0; r < R; ++r) {
@@ -498,7 +519,7 @@ __global__ __launch_bounds__(64 * WAVES, waves_of(KS, R, QH, WAVES)) void attend
                 const float to = fmaxf(top[r] - before, here) + power;
                 const float f = top[r] == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(top[r] - to);
                 top[r] = to;
-                most_allowed[r] = to - power + 8.0f;
+                most_allowed[r] = to - power + LAZY;
                 minus[r] = to == -__builtin_inff() ? 0.0f : -to;
                 sum[r] *= f;
 #pragma unroll
@@ -511,7 +532,10 @@ __global__ __launch_bounds__(64 * WAVES, waves_of(KS, R, QH, WAVES)) void attend
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 const float w = __builtin_amdgcn_exp2f(fmaf(t[r][e >> 2][e & 3], factor[r], minus[r]));
-                const float y = w * scale_v[e];
+                float y = w * scale_v[e];
+                // (the compiler would round the exact product to the first half, by an instruction that does both, and y for the second: next to
+                // a tie they would not belong together)
+                if constexpr (PH > 1) asm("" : "+v"(y));
                 sum[r] += w;
                 p[r][0][e] = static_cast<_Float16>(y);
                 if constexpr (PH > 1) p[r][1][e] = static_cast<_Float16>(y - static_cast<float>(p[r][0][e]));
@@ -697,7 +721,8 @@ void kv4_attend_launch(const Kv4Attend &a, Kv4Shape shape, unsigned blocks, hipS
     else if (shape.tiles == 1) with_halves(std::integral_constant<int, 1>{}, std::integral_constant<int, 4>{});
     else if constexpr (KS <= 4) with_halves(std::integral_constant<int, 2>{}, std::integral_constant<int, 4>{});
     if (!a.split) return;
-    // (2177 tokens of 16 heads whose parts are 2 to 4: a workgroup for a row 45 us)
+    // (many rows have few parts: 2177 tokens of 16 heads, 2 to 4 parts: a workgroup for a row 45 us, for 8 or 16 rows 7; few rows have many parts:
+    // a row's parts are read side by side, 64 tokens of 32 heads 6.5 us)
     constexpr int SLOTS = 256 / lanes_of(KS);
     if (int64_t{a.c.t} * a.heads > 8192) join_kernel<KS, true><<<dim3(a.c.t, (a.heads + SLOTS - 1) / SLOTS), 256, 0, st>>>(a);
     else join_kernel<KS, false><<<dim3(a.c.t, a.heads), 256, 0, st>>>(a);

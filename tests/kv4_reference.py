@@ -96,11 +96,12 @@ class Cache:
         return out
 
 
-def attention(q, cache, table, lengths, begins, scale, window, sinks, block, wide):
+def attention(q, cache, table, lengths, begins, scale, window, sinks, block, wide, least=2.0 ** -25):
     """(out, bound) [t, heads, d] in 64 bits: the definition, and how far a kernel may be from it before its result is rounded.
 
     Roundings counted (u = 2^-11, half a step of a half; two halves 2^-22): of H q, of the weights times the scales of v, where the largest weight is
-    1 and the power of two next to the largest scale is taken out; below 2^-14 such a product is off by 2^-25 of that scale.  fp32: sums of d and of n terms in any order, with 2^-23 a step; the
+    1 and the power of two next to the largest scale is taken out; small products are off by `least` of that scale.  fp32: sums of d and of n
+    terms in any order, with 2^-23 a step; the
     exponential's argument by 2^-23 of itself.  An error e of every score changes a result by at most (exp(2 e) - 1) of sum p |v|."""
     t, heads, d = q.shape
     group, u = heads // cache.heads, 2.0 ** -22 if wide else 2.0 ** -11
@@ -134,7 +135,7 @@ def attention(q, cache, table, lengths, begins, scale, window, sinks, block, wid
                 p /= p.sum()
                 e = abs(scale) * (np.abs(kk) @ np.abs(hq[row, h])) * (u + 2.0 ** -22 + (d + 16) * 2.0 ** -23) + (np.abs(s - top) + 16) * 2.0 ** -22
                 grow = np.expm1(2 * e.max()) + u + (len(s) + 64) * 2.0 ** -23
-                off = grow * (p @ np.abs(vv)) + len(s) * 2.0 ** -25 * most * p.max()
+                off = grow * (p @ np.abs(vv)) + len(s) * least * most * p.max()
                 out[row, h] = walsh(p @ vv, block) / np.sqrt(block)
                 bound[row, h] = size @ off + 2.0 ** -20 * (size @ (p @ np.abs(vv)))
     return out, bound

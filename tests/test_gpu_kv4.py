@@ -170,6 +170,67 @@ def test_peaked_rows():
         call.check_attention(2, dtype, spread=5.0)
 
 
+def test_many_small_weights():
+    """One token has the weight 1 and values of 0, 2000 others the weight 2^-15.3 (416.5 steps of a half below 2^-14, so that a half has it off by 1.2e-3):
+    kept 2^6 times as large they are off by 2^-31 of the largest at most, which with the sums' 2000 x 2^-23 is a third of that."""
+    call = Call([1], [2001], 1, 8, 16, content=False)
+    cache = call.cache
+    cache.k[..., 0], cache.v[...], cache.vs[...] = 2, 2, 1
+    first = call.table[0, 0], 0, 0
+    cache.ks[first], cache.v[first] = 1, 0
+    call.on_gpu = hq.Kv4Cache(*(gpu(x) for x in cache.packed()), 8)
+    q = gpu(np.full((1, 1, 8), np.float32((24 - np.log2(416.5)) * np.log(2) / np.sqrt(8))), torch.float32)
+    want, bound = ref.attention(q.double().cpu().numpy(), cache, call.table, call.lengths, call.begins, 1.0, 0, 0, call.block, True, 2.0 ** -31)
+    assert (bound.max() < 5e-4 * np.abs(want).max())
+    close(hq.hq_kv4_attention(q, call.on_gpu, *call.where(), scale=1.0), want, bound, "f32")
+
+
+@pytest.mark.parametrize("seed", range(3))
+def test_every_weight_by_itself(seed):
+    """256 tokens whose values are a channel of their own each, so that the transformed result shows each weight; keys of one channel, so that scores
+    are one product.  Errors counted, e of a score: the 8 sums and the halves of H q, 2^-22 each of sum |q| 8^-1/2; of the exponential's argument
+    2^-22 (|s| + 16).  A weight: expm1(2 e), its two halves and the scale 2^-21, the sum of n weights n 2^-23 and 64 more for parts; a channel back
+    through the transform 2^-20 of its block's largest.  A weight whose second half does not belong to the first is off by 2^-11 to 2^-10."""
+    n, d, new, heads = 256, 256, 16, 16
+    call = Call([new], [n], 1, d, 32, seed=seed, content=False, had_block=8)
+    cache, where = call.cache, (call.table[0, np.arange(n) // 32], 0, np.arange(n) % 32)
+    cache.k[where + (0,)], cache.v[where + (np.arange(n),)] = 2, 2
+    cache.ks[where], cache.vs[where] = (np.exp(call.rng.normal(-1, 0.5, n)).astype(np.float32) for _ in "kv")
+    call.on_gpu = hq.Kv4Cache(*(gpu(x) for x in cache.packed()), d, 8)
+    q = gpu(call.rng.standard_normal((new, heads, d)) * 2, torch.float32)
+    got = hq.hq_kv4_attention(q, call.on_gpu, *call.where(), scale=1.0).cpu().double().numpy()
+    q, ks, vs = q.cpu().double().numpy()[..., :8], cache.ks[where].astype(np.float64), cache.vs[where].astype(np.float64)
+    s = q.sum(-1)[..., None] / np.sqrt(8) * ks
+    s = np.where(np.arange(n) <= n - new + np.arange(new)[:, None, None], s, -np.inf)
+    top = s.max(-1, keepdims=True)
+    p = np.exp(s - top)
+    want = p / p.sum(-1, keepdims=True) * vs
+    e = np.abs(q).sum(-1)[..., None] / np.sqrt(8) * ks * 10 * 2.0 ** -22 + (np.where(p > 0, top - s, 0) + 16) * 2.0 ** -22
+    grow = np.expm1(2 * e.max(-1, keepdims=True)) + 2.0 ** -21 + (n + 64) * 2.0 ** -23
+    room = want * grow + 2.0 ** -20 * want.reshape(new, heads, -1, 8).max(-1).repeat(8, -1) + 2.0 ** -36 * vs.max()
+    off = np.abs(ref.walsh(got, 8) / np.sqrt(8) - want)
+    worst = np.unravel_index(np.argmax(off - room), off.shape)
+    assert (off <= room).all(), "%s: %g off, %g allowed, of %g; %d" % (worst, off[worst], room[worst], want[worst], (off > room).sum())
+
+
+def test_more_sequences_long_and_short():
+    """Long ones come first, of every 64: of all lengths and orders, divided and not."""
+    rng = np.random.default_rng(5)
+    new = [int(x) for x in rng.integers(1, 40, 70)]
+    lengths = [n + int(x) for n, x in zip(new, np.exp(rng.uniform(0, 7, 70)))]
+    Call(new, lengths, 2, 32, 16, padding=3).check_attention(4, "f16")
+    Call(new[:5], [n + 900 * (i % 2) for i, n in enumerate(lengths[:5])], 1, 32, 16).check_attention(2, "f32")
+
+
+def test_on_another_device_than_the_current_one():
+    if torch.cuda.device_count() < 2:
+        pytest.skip("one device")
+    cache = hq.hq_kv4_cache(2, 16, 1, 32, device="cuda:1")
+    one = torch.ones(1, dtype=torch.int32, device="cuda:1")
+    with pytest.raises(ValueError, match="current device"):
+        hq.hq_kv4_read(cache, one[:, None], one, 1)
+
+
 def test_what_is_not_visible_is_not_looked_at():
     """NaN and infinities in slots behind the sequences' ends, in tokens outside the window, in other pages; entries of the table behind the last page."""
     call = Call([1, 2, 3], [45, 130, 91], 2, 64, 16, seed=9)
