@@ -505,9 +505,11 @@ hq_status hq_qk_norm_rope_backward(const void *dq, const void *dk, const void *q
  * block-diagonal Hadamard matrix of blocks of had_block channels (symmetric and its own inverse), in E2M1 codes (0, 0.5, 1, 1.5, 2, 3, 4, 6;
  * bit 3 the sign) with one fp32 scale for each token and head:
  *
- *   scale = max |H x| / 6, 1 if that is 0, at least 2^-126;   code = E2M1(H x * (1 / scale)), to nearest, ties to even
+ *   scale = max |H x| / 6, 1 if that is 0, at least 2^-126;   code = E2M1(H x / that scale), to nearest, ties to even
  *
- * A head that is not finite has a scale of NaN and codes of 0.
+ * The scale that is kept is worked out in fp32 steps.  A code is the definition's, without roundings of the scale or of H x: decided in 64 bits
+ * where fp32 steps (of the norm, the rotation, the transform) leave it uncertain, a tie wherever the sums of the head are exact in 64 bits.
+ * A head that is not finite, or of which a block's sums of magnitudes are beyond fp32, has a scale of NaN and codes of 0.
  *
  *   k        [pages, kv_heads, page_size, pitch / 2] bytes, pitch = d rounded up to a multiple of 32; channel 2 i in the low bits of byte i
  *   v        [pages, kv_heads, page_size / 8, pitch, 4] bytes: a channel's codes of 8 tokens, token 2 i in the low bits of byte i

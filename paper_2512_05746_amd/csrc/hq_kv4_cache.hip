@@ -1,10 +1,11 @@
 // Keys and values into a paged cache of 4-bit codes, on the way from the projection, and back out of it.
 //
 //     n = x r w,  r = (mean x^2 + eps)^-1/2   (queries and keys, where the call has a norm),   y = R(position) n
-//     queries: y.   keys: z = H y.   values: z = H v.   scale = max |z| / 6,  code = E2M1(z / scale)
+//     queries: y.   keys: z = H y.   values: z = H v.   scale = max |z| / 6,  code = E2M1(6 z / max |z|)
 //
-// H is orthonormal, symmetric, block-diagonal: its blocks spread a large channel over their width, so that one scale serves a head.  All in
-// fp32; roundings: of the query to its type, of the scale, of the code.
+// H is orthonormal, symmetric, block-diagonal: its blocks spread a large channel over their width, so that one scale serves a head.
+// Queries and scales in fp32; roundings: of the query to its type, of the scale, of the code.  A code is the definition's: a head with a number
+// closer to a border between two codes than its fp32 steps can be off is worked out in 64 bits (coded).
 //
 // A workgroup takes the tokens of one group of 8 positions, because a dword of the cache's v holds the codes of a channel for 8 tokens: it
 // is then written by one workgroup, whole where all 8 tokens are new, around what it held where they are not.  A head is owned by LP
@@ -209,33 +210,106 @@ __device__ __forceinline__ void head(const AppendArgs &a, const Raw<T, PAIRS> &x
             if (c0 + i < a.rotary) v[i] = v[i] * t.cos[i] + p[i] * t.sin[i];
     }
 }
-// Its transform in codes.
-template <int LP>
-__device__ __forceinline__ uint32_t coded(float (&v)[8], int in, bool live, int block_log2, float &scale) {
+// The length of a head before weights and norm.
+template <class T, int LP, int PAIRS>
+__device__ __forceinline__ float length_of(const Raw<T, PAIRS> &x, bool live) {
+    float sum = 0.0f;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = live ? v[i] : 0.0f;
-    walsh(v, in, block_log2);
-    const float f = walsh_factor(in, block_log2);
-    uint32_t top = 0;
+    for (int i = 0; i < 8; ++i) sum += static_cast<float>(x.v[i]) * static_cast<float>(x.v[i]);
+    return __builtin_amdgcn_sqrtf(sum_lanes<LP>(live ? sum : 0.0f));
+}
+// Its number in 64 bits, where it is used: what is the same for all heads is not to be converted ahead of them, into registers.
+__device__ __forceinline__ double here(float x) {
+    asm volatile("" : "+v"(x));
+    return x;
+}
+// A head in 64 bits without the norm's factor, which all of its channels share.
+template <class T, int PAIRS>
+__device__ __forceinline__ void head_wide(const AppendArgs &a, const Raw<T, PAIRS> &x, int c0, const Turn &t, const Raw<float, PAIRS> &w,
+                                          double (&v)[8]) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        v[i] *= f;
-        top = max(top, __float_as_uint(v[i]) & 0x7FFFFFFFu);
+    for (int i = 0; i < 8; ++i) v[i] = static_cast<double>(x.v[i]) * here(w.v[i]);
+    if (!a.rotary) return;
+    double p[8];
+    if constexpr (PAIRS == kLanes) {
+        const int half = a.rotary >> 4;   // in blocks
+        if (half == 8) other_lanes_wide<3>(v, p);
+        else if (half == 4) other_lanes_wide<2>(v, p);
+        else if (half == 2) other_lanes_wide<1>(v, p);
+        else other_lanes_wide<0>(v, p);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            if constexpr (PAIRS == kNeighbours) p[i] = v[i ^ 1];
+            else p[i] = static_cast<double>(x.p[i]) * here(w.p[i]);
+        }
     }
-    scale = kv4_scale(max_lanes<LP>(top));
-    return kv4_codes(v, scale == scale ? __fdiv_rn(1.0f, scale) : 0.0f);
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        if (c0 + i < a.rotary) v[i] = v[i] * here(t.cos[i]) + p[i] * here(t.sin[i]);
+}
+// The norm's factor.
+template <class T, int LP, int PAIRS>
+__device__ __forceinline__ double norm_wide(const AppendArgs &a, const Raw<T, PAIRS> &x, bool live) {
+    if (!a.norm) return 1.0;
+    double sum = 0.0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) sum += static_cast<double>(x.v[i]) * static_cast<double>(x.v[i]);
+    sum = reduce_wide<LP>(live ? sum : 0.0, [](double a, double b) { return a + b; });
+    return 1.0 / sqrt(sum / a.c.d + a.eps);
+}
+// A head's transform in codes by fp32 steps (the lanes without channels have zeros), and whether these leave one of its codes uncertain: `near`.
+// With u = 2^-24 and E at least the sum of the head's magnitudes before they are turned, each times |cos| + |sin| of its pair: products and the turn are
+// off by 4 u E at most over a block (none for values), the steps of the transform by 6 u E and u of the result, which with the same error of the
+// largest is 12 (4 + 6) u E / max of a number up to 6, and 12 u; the largest, the scale, its inverse (two), the factor and the product: 6 u of it.
+// Uncertain are codes of which the number less and plus that differ: those of 1 or 2 heads of 128 normal values in 100.  ROUNDINGS: 4 + 6 for keys,
+// 6 for values, with room for terms of second order.
+template <int LP, int ROUNDINGS>
+__device__ __forceinline__ uint32_t coded(float (&v)[8], float size, int in, int block_log2, float &scale, bool &near) {
+    walsh_of<LP>(v, in, block_log2);
+    const float f = walsh_factor(in, block_log2);
+    uint32_t bits = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) bits = max(bits, __float_as_uint(v[i]) & 0x7FFFFFFFu);
+    const float top = __uint_as_float(max_lanes<LP>(bits)) * fabsf(f);
+    scale = kv4_scale(top);
+    const bool none = !(top > 0.0f && top < __builtin_inff());   // (codes of 0)
+    const float by = f * __builtin_amdgcn_rcpf(scale), off = fmaf(size * fabsf(by), 2.02f * ROUNDINGS * 0x1p-24f, 52 * 0x1p-24f);
+    float t[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) t[i] = fmaf(v[i], by, off);
+    const uint32_t w = kv4_codes(t);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) t[i] = fmaf(v[i], by, -off);
+    // (the signs of a 0 may differ; next to the ends of fp32 a step, or a square, can be off by more than u)
+    near = !none && (((w ^ kv4_codes(t)) & 0x77777777u) || !(off < 0.125f) || !(top > 0x1p-50f && top < 0x1p100f));
+    return none ? 0u : w;
+}
+// The codes of such a head from what goes into the transform in 64 bits, times r.
+template <int LP>
+__device__ __forceinline__ uint32_t coded_wide(double (&v)[8], int in, bool live, int block_log2, double r) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = live ? v[i] : 0.0;
+    walsh_wide(v, in, block_log2);
+    // (the least scale is 2^-126: the largest counts as 6 times that, in units of the sums)
+    return kv4_codes_wide<LP>(v, __builtin_ldexp(block_log2 & 1 ? 1.4142135623730951 : 1.0, (block_log2 >> 1) - 126) * 6.0 / r);
+}
+// Whether any of the head's lanes says so.
+template <int LP>
+__device__ __forceinline__ bool any_of_head(uint64_t lanes) {
+    return lanes >> (threadIdx.x & (64 - LP)) & ((uint64_t{1} << LP) - 1);
 }
 
 constexpr int kAtOnce = 4;   // heads of a slot whose loads are under way together
 
-// The heads of a slot's token, from the part's first on, `step` apart: queries go out, keys into the cache.
+// The heads of a slot's token from head `from` on, `step` apart, below `heads`: queries go out, keys into the cache.
 template <class T, int LP, int PAIRS, bool KEYS>
-__device__ __forceinline__ void turned_heads(const AppendArgs &a, int part, int step, int at_once, int first, int row, int64_t place, int in,
-                                             bool live, bool mine, const hq::Kv4Group &g) {
+__device__ __forceinline__ void turned_heads(const AppendArgs &a, int from, int step, int heads, int row, int64_t place, int in, bool live, bool mine,
+                                             const hq::Kv4Group &g) {
     // (positions of a group of 8 are all negative, without a page, or none is)
     const int64_t page = KEYS ? page_of(a.c, g) : 0;
     if (page < 0) return;
-    const int heads = KEYS ? a.c.kv_heads : a.heads, c0 = live ? in * 8 : 0, from = part * at_once + first;
+    const int c0 = live ? in * 8 : 0;
     const int64_t by_head = KEYS ? a.k_head : a.q_head;
     const T *x = static_cast<const T *>(KEYS ? a.k : a.q) + row * (KEYS ? a.k_token : a.q_token) + from * by_head;
     Raw<T, PAIRS> raw[kAtOnce];
@@ -247,17 +321,33 @@ __device__ __forceinline__ void turned_heads(const AppendArgs &a, int part, int 
         }
     };
     load(from);
-    const Raw<float, PAIRS> w = weights_of<T, PAIRS>(a, KEYS ? a.k_weight : a.q_weight, c0);
-    const Turn turn = turn_of<PAIRS>(a, row, place, c0);
+    Raw<float, PAIRS> w = weights_of<T, PAIRS>(a, KEYS ? a.k_weight : a.q_weight, c0);
+    Turn turn = turn_of<PAIRS>(a, row, place, c0);
     T *out = KEYS ? nullptr : static_cast<T *>(a.q_out) + row * a.out_token + from * a.out_head + c0;
     const int64_t at = KEYS ? a.c.slots(page, from) + a.c.slot(static_cast<int>(place)) : 0;
     uint8_t *code_out = a.c.k + at * a.c.row_bytes() + in * 4;
     float *scale_out = a.c.k_scale + at;
+    // Keys: E by lengths, that of x (d^1/2 with a norm) times that of the weights, each times |cos| + |sin|.  Lanes without channels have zeros.
+    float size = 0.0f;
+    uint32_t again = 0;
+    if constexpr (KEYS) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            w.v[i] = live ? w.v[i] : 0.0f;
+            turn.sin[i] = live ? turn.sin[i] : 0.0f;
+            const float y = w.v[i] * (fabsf(turn.cos[i]) + fabsf(turn.sin[i]));
+            size = fmaf(y, y, size);
+        }
+        size = sqrtf(sum_lanes<LP>(size) * (a.norm ? static_cast<float>(a.c.d) : 1.0f));
+        if (a.norm && a.eps < 0x1p-110f) size *= 2.0f;   // (squares that are no normal numbers make the norm's factor up to 1.3 times too large)
+    }
     for (int h = from; h < heads; h += kAtOnce * step) {
 #pragma unroll
         for (int e = 0; e < kAtOnce; ++e) {
             if (h + e * step >= heads) break;
-            float v[8];
+            float v[8], most = size;
+            if constexpr (KEYS)
+                if (!a.norm) most *= length_of<T, LP>(raw[e], live);
             head<T, LP, PAIRS>(a, raw[e], c0, live, turn, w, v);
             if constexpr (!KEYS) {
                 if (__any(turn.pad)) {
@@ -268,7 +358,10 @@ __device__ __forceinline__ void turned_heads(const AppendArgs &a, int part, int 
                 out += step * a.out_head;
             } else {
                 float scale;
-                const uint32_t code = coded<LP>(v, in, live, a.c.block_log2, scale);
+                bool near;
+                const uint32_t code = coded<LP, 10>(v, most, in, a.c.block_log2, scale, near);
+                again = again << 1 | (again & 0x80000000u);
+                if (const uint64_t lanes = __ballot(near)) again |= any_of_head<LP>(lanes);
                 if (mine && !turn.pad) {
                     if (live) *reinterpret_cast<uint32_t *>(code_out) = code;
                     if (in == 0) *scale_out = scale;
@@ -279,33 +372,31 @@ __device__ __forceinline__ void turned_heads(const AppendArgs &a, int part, int 
         }
         load(h + kAtOnce * step);
     }
+    // The uncertain heads, the last one in bit 0, any before the last 31 in bit 31: a loop of its own, from memory again, so that it costs no registers
+    // above.
+    if (KEYS && again)
+        for (int h = from + (heads - 1 - from) / step * step, back = 0; h >= from; h -= step, back = hq::kv4_min(back + 1, 31))
+            if (again >> back & 1) {
+                Raw<T, PAIRS> one;
+                one.load(static_cast<const T *>(a.k) + row * a.k_token + h * a.k_head, c0, a.rotary);
+                const double factor = norm_wide<T, LP>(a, one, live);
+                double v[8];
+                head_wide(a, one, c0, turn, w, v);
+                const uint32_t code = coded_wide<LP>(v, in, live, a.c.block_log2, factor);
+                if (mine && live && !turn.pad)
+                    *reinterpret_cast<uint32_t *>(a.c.k + (a.c.slots(page, h) + a.c.slot(static_cast<int>(place))) * a.c.row_bytes() + in * 4) = code;
+            }
 }
 
-// Workgroups of a group, side by side: q_parts for the queries, k_parts for the keys, as many for the values: the queries are bound by memory, keys
-// and values by arithmetic, and beside each other they overlap.  32768 tokens of 32 + 8 heads of 128 in bf16: 157 us for 0.71 GB, 4.5 TB/s (one
-// workgroup for all three, one after the other: 184 us).  16 tokens: 5.5 us, latencies.
-template <int DT, int LP, int PAIRS>
-__global__ __launch_bounds__(256) void append_kernel(AppendArgs a) {
-    using T = typename Float<DT>::type;
+// The values of a group's tokens, likewise.
+template <class T, int LP>
+__device__ __forceinline__ void stored_heads(const AppendArgs &a, int part, int log2, int at_once, int slot, int first, int row, int64_t place, int in,
+                                             bool live, bool mine, const hq::Kv4Group &g) {
     constexpr int SLOTS = 256 / LP;
-    const int parts_of = a.q_parts + 2 * a.k_parts;
-    const int group = hq::div_magic31(blockIdx.x, parts_of, a.part_magic.m, a.part_magic.s);
-    const hq::Kv4Group g = group_of(a.c, group);
-    if (g.count == 0) return;
-    // slots: tokens, a power of two of them, times heads at once
-    const int log2 = g.count > 4 ? 3 : g.count > 2 ? 2 : g.count - 1, at_once = SLOTS >> log2;
-    const int in = kv4_block(threadIdx.x % LP), slot = threadIdx.x / LP, token = slot & ((1 << log2) - 1), first = slot >> log2;
-    const bool live = in * 8 < a.c.d, mine = token < g.count;
-    const int c0 = live ? in * 8 : 0, row = g.row + (mine ? token : 0);
-    const int64_t place = g.s < a.c.batch ? g.position + (mine ? token : 0) : -1;
-    int part = blockIdx.x - group * parts_of;
-    if (part < a.q_parts) return turned_heads<T, LP, PAIRS, false>(a, part, a.q_parts * at_once, at_once, first, row, place, in, live, mine, g);
-    if (part < a.q_parts + a.k_parts)
-        return turned_heads<T, LP, PAIRS, true>(a, part - a.q_parts, a.k_parts * at_once, at_once, first, row, place, in, live, mine, g);
-    part -= a.q_parts + a.k_parts;
     const int parts = a.k_parts;
     const int64_t page = page_of(a.c, g);
     if (page < 0) return;
+    const int c0 = live ? in * 8 : 0;
     __shared__ uint32_t codes[SLOTS][LP + 1];
     __shared__ uint32_t new_tokens;   // four bits for each token of the group that is stored
     if (threadIdx.x == 0) new_tokens = 0;
@@ -320,11 +411,24 @@ __global__ __launch_bounds__(256) void append_kernel(AppendArgs a) {
     for (int base = part * at_once; base < a.c.kv_heads; base += parts * at_once) {
         const int h = base + first;
         if (h < a.c.kv_heads) {
-            float v[8], scale;
+            float v[8], scale, size = 0.0f;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = next[i];
+            for (int i = 0; i < 8; ++i) {
+                v[i] = live ? next[i] : 0.0f;
+                size += fabsf(v[i]);
+            }
             if (h + parts * at_once < a.c.kv_heads) load8(x + (h + parts * at_once) * a.v_head, next);
-            codes[slot][in] = coded<LP>(v, in, live, a.c.block_log2, scale);
+            bool near;
+            uint32_t code = coded<LP, 6>(v, sum_lanes<LP>(size), in, a.c.block_log2, scale, near);
+            if (const uint64_t lanes = __ballot(near)) {
+                load8(x + h * a.v_head, v);   // (again: no registers for it above)
+                double wide[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) wide[i] = v[i];
+                const uint32_t exact = coded_wide<LP>(wide, in, live, a.c.block_log2, 1.0);
+                if (any_of_head<LP>(lanes)) code = exact;
+            }
+            codes[slot][in] = code;
             if (stored && in == 0) a.c.v_scale[at + (static_cast<int64_t>(h) << a.c.page_log2) + a.c.slot(static_cast<int>(place))] = scale;
         }
         __syncthreads();
@@ -345,6 +449,32 @@ __global__ __launch_bounds__(256) void append_kernel(AppendArgs a) {
         }
         __syncthreads();
     }
+}
+
+// Workgroups of a group, side by side: q_parts for the queries, k_parts for the keys, as many for the values: the queries are bound by memory, keys
+// and values by arithmetic, and beside each other they overlap.  32768 tokens of 32 + 8 heads of 128 in bf16: 157 us for 0.71 GB, 4.5 TB/s (one
+// workgroup for all three, one after the other: 184 us).  16 tokens: 5.5 us, latencies.
+template <int DT, int LP, int PAIRS>
+__global__ __launch_bounds__(256) void append_kernel(AppendArgs a) {
+    using T = typename Float<DT>::type;
+    constexpr int SLOTS = 256 / LP;
+    const int parts_of = a.q_parts + 2 * a.k_parts;
+    const int group = hq::div_magic31(blockIdx.x, parts_of, a.part_magic.m, a.part_magic.s);
+    const hq::Kv4Group g = group_of(a.c, group);
+    if (g.count == 0) return;
+    // slots: tokens, a power of two of them, times heads at once
+    const int log2 = g.count > 4 ? 3 : g.count > 2 ? 2 : g.count - 1, at_once = SLOTS >> log2;
+    const int in = kv4_block(threadIdx.x % LP), slot = threadIdx.x / LP, token = slot & ((1 << log2) - 1), first = slot >> log2;
+    const bool live = in * 8 < a.c.d, mine = token < g.count;
+    const int row = g.row + (mine ? token : 0);
+    const int64_t place = g.s < a.c.batch ? g.position + (mine ? token : 0) : -1;
+    int part = blockIdx.x - group * parts_of;
+    if (part < a.q_parts)
+        return turned_heads<T, LP, PAIRS, false>(a, part * at_once + first, a.q_parts * at_once, a.heads, row, place, in, live, mine, g);
+    part -= a.q_parts;
+    if (part < a.k_parts)
+        return turned_heads<T, LP, PAIRS, true>(a, part * at_once + first, a.k_parts * at_once, a.c.kv_heads, row, place, in, live, mine, g);
+    stored_heads<T, LP>(a, part - a.k_parts, log2, at_once, slot, first, row, place, in, live, mine, g);
 }
 
 // ---- read -------------------------------------------------------------------------------------------------------------

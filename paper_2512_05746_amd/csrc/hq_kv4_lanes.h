@@ -69,6 +69,22 @@ __device__ __forceinline__ void walsh(float (&v)[8], int block, int log2) {
     if (log2 > 5) walsh_lanes<2>(v, block);
     if (log2 > 6) walsh_lanes<3>(v, block);
 }
+// The same for heads of LP lanes; blocks of all their channels (or 128) without a branch between the steps, which would move all values.
+template <int LP>
+__device__ __forceinline__ void walsh_of(float (&v)[8], int block, int log2) {
+    constexpr int FULL = LP == 4 ? 5 : LP == 8 ? 6 : 7;
+    if (log2 == FULL) {
+        walsh_own<1>(v);
+        walsh_own<2>(v);
+        walsh_own<4>(v);
+        walsh_lanes<0>(v, block);
+        walsh_lanes<1>(v, block);
+        if constexpr (FULL > 5) walsh_lanes<2>(v, block);
+        if constexpr (FULL > 6) walsh_lanes<3>(v, block);
+    } else {
+        walsh(v, block, log2);
+    }
+}
 // 2^(-log2 / 2) and the sign that the steps between lanes left the lane with.
 __device__ __forceinline__ float walsh_factor(int block, int log2) {
     const float f = __builtin_ldexpf(log2 & 1 ? 0.70710678118654752f : 1.0f, -(log2 >> 1));
@@ -77,19 +93,86 @@ __device__ __forceinline__ float walsh_factor(int block, int log2) {
 }
 
 // ---- codes ------------------------------------------------------------------------------------------------------------
-// The scale of a head from the bits of its largest magnitude: NaN where that is not finite (the codes are then 0).
-__device__ __forceinline__ float kv4_scale(uint32_t amax_bits) {
-    if (amax_bits >= 0x7F800000u) return __uint_as_float(0x7FC00000u);
-    return amax_bits == 0 ? 1.0f : fmaxf(__fdiv_rn(__uint_as_float(amax_bits), 6.0f), 0x1p-126f);
+// The scale of a head from its largest magnitude: NaN where that is not finite (the codes are then 0).  A sixth to the nearest: the rounded
+// product's remainder is exact, and so is its sixth's part in the second product.
+__device__ __forceinline__ float kv4_scale(float top) {
+    constexpr float SIXTH = 1.0f / 6.0f;
+    const float q = top * SIXTH, scale = fmaxf(fmaf(fmaf(-6.0f, q, top), SIXTH, q), 0x1p-126f);
+    return top == 0.0f ? 1.0f : top < __builtin_inff() ? scale : __builtin_nanf("");
 }
-// E2M1 codes of 8 channels times `inverse` (0 for a head that is not finite), to nearest, ties to even, the first in the low bits
-__device__ __forceinline__ uint32_t kv4_codes(const float (&v)[8], float inverse) {
+// E2M1 codes of 8 numbers, to nearest, ties to even, the first in the low bits.
+__device__ __forceinline__ uint32_t kv4_codes(const float (&t)[8]) {
     uint32_t w = 0;
-    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[0] * inverse, v[1] * inverse, 1.0f, 0);
-    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[2] * inverse, v[3] * inverse, 1.0f, 1);
-    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[4] * inverse, v[5] * inverse, 1.0f, 2);
-    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[6] * inverse, v[7] * inverse, 1.0f, 3);
-    return inverse == 0.0f ? 0u : w;
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, t[0], t[1], 1.0f, 0);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, t[2], t[3], 1.0f, 1);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, t[4], t[5], 1.0f, 2);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, t[6], t[7], 1.0f, 3);
+    return w;
+}
+// Of the lane whose block differs in bit BIT.
+template <int BIT>
+__device__ __forceinline__ double of_lane_wide(double v) {
+    constexpr int CTRL = BIT == 0 ? 0xB1 : BIT == 1 ? 0x4E : BIT == 2 ? 0x141 : 0x140;
+    return __hiloint2double(dpp<CTRL>(__double2hiint(v)), dpp<CTRL>(__double2loint(v)));
+}
+template <int BIT>
+__device__ __forceinline__ void other_lanes_wide(const double (&v)[8], double (&to)[8]) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) to[i] = of_lane_wide<BIT>(v[i]);
+}
+template <int BIT>
+__device__ __forceinline__ void walsh_lanes_wide(double (&v)[8], int block) {
+    const double sign = block >> BIT & 1 ? -1.0 : 1.0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = of_lane_wide<BIT>(v[i]) + sign * v[i];
+}
+// The transform in 64 bits, without its factor.
+__device__ __forceinline__ void walsh_wide(double (&v)[8], int block, int log2) {
+#pragma unroll
+    for (int step = 1; step < 8; step *= 2)
+        if (log2 > __builtin_ctz(step)) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (!(i & step)) {
+                    const double a = v[i], b = v[i + step];
+                    v[i] = a + b;
+                    v[i + step] = a - b;
+                }
+        }
+    if (log2 > 3) walsh_lanes_wide<0>(v, block);
+    if (log2 > 4) walsh_lanes_wide<1>(v, block);
+    if (log2 > 5) walsh_lanes_wide<2>(v, block);
+    if (log2 > 6) walsh_lanes_wide<3>(v, block);
+}
+// Of LP lanes together: op by the steps of reduce_bits.
+template <int LP, class Op>
+__device__ __forceinline__ double reduce_wide(double v, Op op) {
+    v = op(v, of_lane_wide<0>(v));
+    v = op(v, of_lane_wide<1>(v));
+    if constexpr (LP > 4) v = op(v, of_lane_wide<2>(v));
+    if constexpr (LP > 8) v = op(v, of_lane_wide<3>(v));
+    if constexpr (LP > 16) v = op(v, __shfl_xor(v, 16));
+    return v;
+}
+// The codes of 8 of a head's sums, decided in 64 bits: 6 |sum| against each border times the largest of the head, ties to the even code.  Exact
+// wherever the sums are (16-bit values whose sizes are within 2^30 of each other).  least: what the largest counts as at least (the scale has a
+// least, 2^-126).
+template <int LP>
+__device__ __forceinline__ uint32_t kv4_codes_wide(const double (&sum)[8], double least) {
+    double most = least;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) most = fmax(most, fabs(sum[i]));
+    most = reduce_wide<LP>(most, [](double a, double b) { return fmax(a, b); });
+    uint32_t w = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const double x = 6.0 * fabs(sum[i]);
+        uint32_t code = (x > 0.25 * most) + (x >= 0.75 * most) + (x > 1.25 * most) + (x >= 1.75 * most) + (x > 2.5 * most) +
+                        (x >= 3.5 * most) + (x > 5.0 * most);
+        if (sum[i] < 0.0) code |= 8;
+        w |= code << (4 * i);
+    }
+    return w;
 }
 
 typedef _Float16 half2v __attribute__((ext_vector_type(2)));

@@ -1,4 +1,4 @@
-"""The 4-bit key/value cache from its definition, in NumPy: codes and layouts bit for bit (32-bit steps in the documented order), attention in 64 bits."""
+"""The 4-bit key/value cache from its definition, in NumPy: codes and layouts bit for bit, attention in 64 bits."""
 from __future__ import annotations
 
 import numpy as np
@@ -37,20 +37,30 @@ def codes_of(t):
     return (up.sum(-1) + 8 * np.signbit(t)).astype(np.uint8)
 
 
+def exact_codes(sums, least=None):
+    """The codes that the definition gives for heads of sums [.., d] in 64 bits, in units of any size: 6 |sum| / max |sum| against the borders, by
+    products that are exact for sums of up to 47 bits.  least: the smallest that the largest counts as."""
+    a, top = np.abs(sums), np.abs(sums).max(-1, keepdims=True)
+    top = np.where(top == 0, 1, top) if least is None else np.maximum(np.where(top == 0, 1, top), least)
+    up = np.where(np.arange(7) % 2 == 0, 6 * a[..., None] > BORDERS * top[..., None], 6 * a[..., None] >= BORDERS * top[..., None])
+    return (up.sum(-1) + 8 * (sums < 0)).astype(np.uint8)
+
+
 def encode(z):
-    """(codes, scales) of heads z [.., d] fp32, already transformed."""
-    top = np.abs(z).max(-1)
+    """(codes, scales) of heads as transformed() gives them: codes from the sums in 64 bits, scales by 32-bit steps."""
+    sums, steps, f = z
     with np.errstate(all="ignore"):
+        top = np.abs(steps).max(-1)
         scale = np.where(top == 0, np.float32(1), np.maximum(top / np.float32(6), np.float32(2.0 ** -126))).astype(np.float32)
         good = np.isfinite(top)
-        t = z * (np.float32(1) / scale)[..., None]
-    codes = np.where(good[..., None], codes_of(np.where(good[..., None], t, 0)), 0)
+        codes = np.where(good[..., None], exact_codes(np.where(good[..., None], sums, 0), 6 * 2.0 ** -126 / f), 0)
     return codes.astype(np.uint8), np.where(good, scale, np.float32(np.nan))
 
 
 def transformed(x, block):
+    """Of heads x: the sums in 64 bits, the transform by 32-bit steps, the factor between them."""
     with np.errstate(all="ignore"):
-        return walsh(x.astype(np.float32), block) * factor(block)
+        return walsh(x.astype(np.float64), block), walsh(x.astype(np.float32), block) * factor(block), block ** -0.5
 
 
 class Cache:

@@ -1,7 +1,7 @@
 """The 4-bit key/value cache on the GPU: what append stores bit for bit, what read gives, attention against its definition in 64 bits.
 
 The tolerance of attention is derived in kv4_reference.attention.  Codes of values that go in as they are (v; k without norm and rotation) are compared bit
-for bit with the same 32-bit steps in NumPy.  Codes of normalised, rotated keys may differ where the 64-bit value is close to a border:
+for bit with the definition, decided in 64 bits, their scales with the same 32-bit steps in NumPy.  In test_norm_and_rotation codes of normalised, rotated keys may differ where the 64-bit value is close to a border:
 a value of a head is off by (d / 2 + 12) 2^-24 of its pair's length (see test_gpu_qk.py), its transform by the sum of those over a block times
 block^-1/2, with log2(block) + 3 roundings more."""
 import numpy as np
@@ -466,6 +466,112 @@ def test_norm_and_rotation(d, rotary, interleaved, norm, weights, dtype):
     assert differ <= (~sure).sum()
     codes, scale = ref.encode(ref.transformed(v.float().cpu().numpy(), call.block))
     check_codes(call, call.downloaded(), before, "v", codes, scale, np.ones(codes.shape, bool))
+
+
+def stored_codes(call, which, row):
+    """The codes that the cache holds for a row of the call."""
+    after = call.downloaded()
+    s, place = call.places()
+    codes = after.k if which == "k" else after.v
+    return np.stack([codes[call.table[s[r], place[r] // call.page], :, place[r] % call.page] for r in row])
+
+
+# (a, b) of which sums are a + b and a - b: 6 (a - b) / (a + b) is a border, and nothing of it needs more than 6 bits
+TIES = {0.25: (25, 23), 0.75: (9, 7), 1.25: (29, 19), 1.75: (31, 17), 2.5: (17, 7), 3.5: (19, 5), 5.0: (11, 1)}
+
+
+@pytest.mark.parametrize("norm", [False, True])
+@pytest.mark.parametrize("dtype", ["f16", "bf16", "f32"])
+@pytest.mark.parametrize("d,had_block", [(8, 2), (64, None), (128, None), (128, 32), (72, None), (160, None), (256, None)])
+def test_ties_go_to_even(d, had_block, dtype, norm):
+    """Two channels of a block, so that every sum of it is the largest or a border's number of times a sixth of it, exactly; at sizes for which scales have
+    all kinds of roundings, and one step of fp32 to either side.  The norm's factor is the same for all of a head."""
+    call = Call([9, 33, 14], [9, 40, 30], 7, d, 16, seed=d, had_block=had_block)
+    rng, block = call.rng, call.block
+    x = [np.zeros((call.t, h, d), np.float32) for h in (7, 7, 7)]
+    for y in x[1:]:
+        for row in range(call.t):
+            for h, border in enumerate(TIES):
+                pair, at = np.array(TIES[border], np.float32), rng.integers(d // block) * block + rng.choice(block, 2, replace=False)
+                pair *= rng.choice([-1, 1], 2) * 2.0 ** rng.integers(-4, 4)
+                if dtype == "f32" and row % 3 == 1:     # nearly a tie
+                    pair[1] = np.nextafter(pair[1], pair[1] * rng.choice([0, 2]), dtype=np.float32)
+                if dtype == "f32" and row % 3 == 2:     # a tie at any size
+                    pair *= np.float32(rng.integers(1, 1 << 18))
+                y[row, h, at] = pair
+    before = call.downloaded()
+    _, (q, k, v, w, _, _) = append(call, 7, dtype, norm=norm, weights="none", x=x)
+    after, sure = call.downloaded(), np.ones((call.t, 7, d), bool)
+    for which, y in (("v", v), ("k", k)):
+        assert torch.equal(y.float().cpu(), torch.from_numpy(x[2 if which == "v" else 1]))
+        z = ref.transformed(y.float().cpu().numpy(), block)
+        codes, scale = ref.encode(z)
+        ratio = 6 * np.abs(z[0]) / np.abs(z[0]).max(-1, keepdims=True)
+        tied = (np.abs(ratio[..., None] - np.array(list(TIES))) < 1e-12).any(-1)
+        assert tied[::3].any(-1).all() and (codes[tied] % 2 == 0).all()
+        if which == "k" and norm:   # (codes do not depend on the factor; scales are those of normalised heads, off by fp32 steps)
+            n = (y.double() * torch.rsqrt(y.double().square().mean(-1, keepdim=True) + 1e-6)).cpu().numpy()
+            scale = np.abs(ref.walsh(n, block)).max(-1) * block ** -0.5 / 6
+            check_codes(call, after, before, which, codes, scale, sure, (d / 2 + 24) * 2.0 ** -24)
+        else:
+            check_codes(call, after, before, which, codes, scale, sure)
+
+
+@pytest.mark.parametrize("dtype,size", [("f16", 1), ("bf16", 1), ("f32", 1), ("f32", 1e-37), ("f32", 1e-39), ("bf16", 1e-38), ("f32", 1e30)])
+def test_codes_of_many_heads(dtype, size):
+    """Values: every code is that of the definition, next to the least scale too."""
+    call = Call([1500, 1500], [1500, 1501], 8, 128, 64, seed=3, content=False)
+    x = [call.rng.standard_normal((call.t, 8, 128)).astype(np.float32) * np.float32(size) for _ in "qkv"]
+    x[2][:, ::2] *= np.exp(2 * call.rng.standard_normal((call.t, 4, 128))).astype(np.float32)
+    _, (q, k, v, *_) = append(call, 8, dtype, x=x, weights="none", table=1)
+    for which, y in (("k", k), ("v", v)):
+        want, scale = ref.encode(ref.transformed(y.float().cpu().numpy(), call.block))
+        got = stored_codes(call, which, range(call.t))
+        bad = (got != want) & ~((got & 7 == 0) & (want & 7 == 0))
+        assert np.isfinite(scale).all() and not bad.any(), (which, bad.sum(), np.argwhere(bad)[:3])
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16", "f32"])
+@pytest.mark.parametrize("d,rotary,interleaved,norm,weights", [(128, 128, False, True, "same"), (128, 64, False, True, "f32"), (64, 64, True, True, "none"),
+                                                                (80, 72, False, False, "none"), (160, 20, False, True, "f32"), (32, 32, False, True, "same"),
+                                                                (256, 256, False, True, "same"), (192, 32, False, False, "none"), (128, 16, False, False, "none")])
+def test_codes_of_turned_keys(d, rotary, interleaved, norm, weights, dtype):
+    """Keys that are normalised and turned: every code is that of the definition in 64 bits, but next to a border by less than what 64-bit steps are off:
+    2^-53 for each of 3 (log2(block) + 4) and a number up to 6, of sums that are up to a head's length in size, 2^-40 with room."""
+    rows = 600000 // d
+    call = Call([rows, rows], [rows, rows + 5], 2, d, 64, seed=d + rotary, content=False)
+    _, (q, k, v, w, cos, sin) = append(call, 2, dtype, rotary, norm, interleaved, weights=weights)
+    y, _ = turned(k, w[1], cos, sin, call.places()[1], rotary, norm, interleaved)
+    sums = ref.walsh(y, call.block)
+    t = 6 * np.abs(sums) / np.abs(sums).max(-1, keepdims=True)
+    sure = (np.abs(t[..., None] - ref.BORDERS) > 2.0 ** -40).all(-1)
+    assert sure.mean() > 0.999999
+    got, want = stored_codes(call, "k", range(call.t)), ref.exact_codes(sums)
+    bad = (got != want) & ~((got & 7 == 0) & (want & 7 == 0)) & sure
+    assert not bad.any(), (bad.sum(), np.argwhere(bad)[:3])
+
+
+def test_ties_of_many_heads():
+    """40 heads one after the other in a lane: ties in the first ones and the last."""
+    t, heads, d = 17000, 40, 136
+    call = Call([t], [t], heads, d, 256, content=False)
+    gen = torch.Generator(device="cuda").manual_seed(0)
+    k, v = (torch.randn((t, heads, d), generator=gen, device="cuda").to(torch.bfloat16) for _ in "kv")
+    rows = np.sort(call.rng.choice(t, 200, replace=False))
+    for x in (k, v):
+        some = np.zeros((len(rows), heads, d), np.float32)
+        for i in range(len(rows)):
+            for h in range(heads):
+                at = call.rng.integers(d // 8) * 8 + call.rng.choice(8, 2, replace=False)
+                some[i, h, at] = np.array(list(TIES.values())[call.rng.integers(7)], np.float32) * call.rng.choice([-1, 1], 2)
+        x[torch.from_numpy(rows).cuda()] = gpu(some, torch.bfloat16)
+    none = torch.zeros(1, 0, device="cuda")
+    hq.hq_kv4_append(torch.zeros_like(k), k, v, None, None, none, none, call.on_gpu, *call.where(), eps=None)
+    for which, x in (("k", k), ("v", v)):
+        x = x[torch.from_numpy(rows).cuda()].float().cpu().numpy()
+        got, (want, _) = stored_codes(call, which, rows), ref.encode(ref.transformed(x, call.block))
+        bad = (got != want) & ~((got & 7 == 0) & (want & 7 == 0))
+        assert not bad.any(), (which, bad.sum(), np.argwhere(bad)[:3])
 
 
 @pytest.mark.parametrize("page", [8, 32])
