@@ -565,7 +565,8 @@ hq_status hq_kv4_append(const hq_kv4 *cache, const void *q, const void *k, const
  *   scale     finite, magnitude up to 2^100
  *   workspace hq_kv4_attention_workspace(..) bytes, 16-byte aligned; NULL where that is 0
  *
- * Sums and the softmax are fp32.  H q and the weights (1 the largest) times the scales of v are rounded to half, in units of powers of two:
+ * Sums and the softmax are fp32: scores, and |scale| times the largest of |H q|, up to 2^120, scales of keys up to 2^104 (rows beyond can be NaN).
+ * H q and the weights (1 the largest) times the scales of v are rounded to half, in units of powers of two:
  * by 2^-11 of each, products below 2^-14 of the largest scale by 2^-25 of that; HQ_F32: in two halves, by 2^-22.  The order of every
  * sum is fixed by the sizes and what lengths and begins hold: the same inputs give the same bits.
  */

@@ -399,8 +399,10 @@ __global__ __launch_bounds__(64 * WAVES, waves_of(KS, R, QH, WAVES)) void attend
 #pragma unroll
             for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(x[e]) & 0x7FFFFFFFu);
             top = max_lanes<LP>(top);
-            // x = x' 2^power, |x'| < 2^12: halves of full precision down to 2^-26 of the largest
-            const int power = top == 0 || top >= 0x7F800000u ? 0 : __builtin_amdgcn_frexp_expf(__uint_as_float(top)) - 12;
+            // x = x' 2^power, |x'| < 2^12: halves of full precision down to 2^-26 of the largest; smaller for a row so small that its factor would
+            // be below 2^-126 (masked scores are -infinity, and that times 0 is NaN)
+            int power = top == 0 || top >= 0x7F800000u ? 0 : __builtin_amdgcn_frexp_expf(__uint_as_float(top)) - 12;
+            power = max(power, -125 - __builtin_amdgcn_frexp_expf(a.scale));
             float f = __builtin_ldexpf(a.scale, power);
             const float sign = a.scale == 0.0f ? 0.0f : (walsh_factor(in, a.c.block_log2) < 0.0f) != (a.negative != 0) ? -1.0f : 1.0f;
             if (a.scale == 0.0f) f = 1.0f;

@@ -141,6 +141,21 @@ def test_scales():
 
 
 @pytest.mark.parametrize("dtype", ["f16", "bf16", "f32"])
+@pytest.mark.parametrize("d,size,scale,keys", [(128, 1e-40, None, 1), (64, 3e-45, 1.0, 1), (64, 1e-3, 1e-38, 1), (64, 1e-7, 1e-20, 1), (96, 1e-6, 1e-45, 1), (256, 1.0, 3e-39, 1),
+                                               (32, 1e-38, 1e-5, 1e31), (128, 1e-30, 0.1, 1e31), (64, 1e30, 1e-32, 1), (64, 1e30, 1e-20, 1e-10)])
+def test_small_rows_and_scales(d, size, scale, keys, dtype):
+    """Rows whose scores are next to nothing have the mean of what they see; lengths that leave the last tile of 32 with masked places."""
+    if dtype == "f16":
+        size, keys = min(max(size, 1e-7), 1e4), min(keys, 1.0)
+    call = Call([3, 1, 2], [70, 33, 1025], 1, d, 16, seed=d)
+    call.cache.ks *= np.float32(keys)
+    call.on_gpu = hq.Kv4Cache(*(gpu(x) for x in call.cache.packed()), d)
+    got = call.check_attention(2, dtype, scale=scale, spread=size)
+    assert torch.isfinite(got).all()
+    call.check_attention(2, dtype, scale=scale, spread=size, window=9, sinks=2)
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16", "f32"])
 @pytest.mark.parametrize("size", [1e-9, 1e4, 1e25])
 def test_sizes_of_values(size, dtype):
     """Scales of v far from 1, and far from each other; rows of q far from 1."""
