@@ -436,7 +436,10 @@ __global__ __launch_bounds__(64 * WAVES, waves_of(KS, R, QH, WAVES)) void attend
     float4v o[R][2 * KS];
     float top[R], sum[R];                  // the reference, this lane's sum of weights
     float most_allowed[R], minus[R];       // what moves the reference, its negative (0 for none)
-    float limit = 0.0f, power = -100.0f;   // the largest v_scale that the reference allows for, its power of two less ROOM
+    // The largest v_scale that the reference allows for, and its power of two less ROOM: up to 48 of that are in the reference, so that weights and their
+    // sums stay normal numbers down to 2^-78 of the largest and parts can be joined, the rest is taken from v_scale and is in o only.
+    float limit = 0.0f, power = -48.0f;
+    int v_power = -1000, rest = 0;
 #pragma unroll
     for (int r = 0; r < R; ++r) {
         top[r] = most_allowed[r] = -__builtin_inff();
@@ -505,14 +508,19 @@ __global__ __launch_bounds__(64 * WAVES, waves_of(KS, R, QH, WAVES)) void attend
             most[r] = largest(all) * factor[r];
             move |= most[r] > most_allowed[r];
         }
-        if (__any(move)) {
+        if (__ballot(move) | static_cast<uint32_t>(rest)) {
             float v_top = fmaxf(v_most, __shfl_xor(v_most, 16));
             v_top = fmaxf(v_top, __shfl_xor(v_top, 32));
             const float before = power;
+            int by = 0;
             if (v_top >= limit && v_top > 0.0f) {
-                const int p = hq::kv4_max(-100, hq::kv4_min(100, __builtin_amdgcn_frexp_expf(v_top) - 1 - ROOM));
-                power = fmaxf(power, static_cast<float>(p));
-                limit = power == 100.0f ? __builtin_inff() : __builtin_ldexpf(2.0f, static_cast<int>(power) + ROOM);
+                v_power = hq::kv4_max(v_power, __builtin_amdgcn_frexp_expf(v_top) - 1 - ROOM);
+                limit = __builtin_ldexpf(2.0f, v_power + ROOM);   // (infinite for the largest)
+                const int in_reference = hq::kv4_max(-48, hq::kv4_min(48, v_power));
+                power = static_cast<float>(in_reference);
+                by = rest;
+                rest = __builtin_amdgcn_readfirstlane(v_power - in_reference);   // (v's scales are the same for all rows)
+                by -= rest;
             }
 #pragma unroll
             for (int r = 0; r < R; ++r) {
@@ -524,9 +532,12 @@ __global__ __launch_bounds__(64 * WAVES, waves_of(KS, R, QH, WAVES)) void attend
                 most_allowed[r] = to - power + LAZY;
                 minus[r] = to == -__builtin_inff() ? 0.0f : -to;
                 sum[r] *= f;
+                const float of_o = __builtin_ldexpf(f, by);
 #pragma unroll
-                for (int e = 0; e < 2 * KS; ++e) o[r][e] *= f;
+                for (int e = 0; e < 2 * KS; ++e) o[r][e] *= of_o;
             }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) scale_v[e] = __builtin_ldexpf(scale_v[e], -rest);
         }
         half8v p[R][PH];
 #pragma unroll
@@ -557,6 +568,14 @@ __global__ __launch_bounds__(64 * WAVES, waves_of(KS, R, QH, WAVES)) void attend
         load_v(place);
         __builtin_amdgcn_sched_barrier(0);
         entries = entries_of(i + 2 * step < end ? i + 2 * step : next);
+    }
+    if (rest) {
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+#pragma unroll
+            for (int e = 0; e < 2 * KS; ++e)
+#pragma unroll
+                for (int c = 0; c < 4; ++c) o[r][e][c] = __builtin_ldexpf(o[r][e][c], rest);
     }
     // ---- the waves' sums together, and out
 #pragma unroll

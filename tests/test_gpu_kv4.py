@@ -175,6 +175,24 @@ def test_sizes_of_values(size, dtype):
     call.check_attention(2, dtype, q=q)
 
 
+@pytest.mark.parametrize("dtype", ["f16", "bf16", "f32"])
+@pytest.mark.parametrize("size,other", [(1e36, 1), (1e36, 1e-36), (3e37, 1e-70), (1e-34, 1), (1e-34, 1e25), (1e-37, 1), (2e15, 1), (2e15, 1e-30), (1e-13, 1), (1e-13, 1e14)])
+@pytest.mark.parametrize("lengths", [[70, 33, 200], [3000, 2500, 64]])
+def test_ends_of_the_range_of_values(lengths, size, other, dtype):
+    """Scales of v next to the ends of fp32, other pages another size, in one workgroup and in parts that are joined."""
+    if dtype == "f16":      # (results are to be numbers of the type)
+        size, other = (1e3, min(other, 1)) if size > 1 else (size, 1e3 / size if other > 1 else other)
+    call = Call([2, 1, 3], lengths, 1, 64, 64)
+    call.cache.vs *= np.float32(size)
+    with np.errstate(under="ignore"):
+        for b in range(3):
+            call.cache.vs[call.table[b][call.table[b] >= 0][b % 2::2]] *= np.float32(other)
+    call.cache.vs[:] = np.maximum(call.cache.vs, np.float32(2.0 ** -126))
+    call.on_gpu = hq.Kv4Cache(*(gpu(x) for x in call.cache.packed()), 64)
+    call.check_attention(2, dtype)
+    call.check_attention(2, dtype, window=100)
+
+
 def test_peaked_rows():
     """Scores that differ by hundreds, the largest late, early and in the middle."""
     call = Call([1, 1, 1, 2], [300, 290, 64, 128], 1, 64, 16)
