@@ -248,7 +248,7 @@ __global__ __launch_bounds__(64 * WAVES, waves_of(KS, R, QH, WAVES)) void attend
     // per wave: a tile of rows as halves, and later their sums
     constexpr int WAVE_BYTES = 16 * ROW * 4 > 16 * STAGE * 2 * QH ? 16 * ROW * 4 : 16 * STAGE * 2 * QH;
     __shared__ __attribute__((aligned(16))) uint8_t lds[WAVES][WAVE_BYTES];
-    __shared__ float row_factor[WAVES][16], row_top[WAVES][16], row_sum[WAVES][16];
+    __shared__ float row_factor[R][WAVES][16], row_top[WAVES][16], row_sum[WAVES][16];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), m = lane & 15, g = lane >> 4;
     const Task task = task_of(a, blockIdx.x, lane);
     const int in = kv4_block(lane % LP);   // the 8 channels that the lane has where a row is dealt to lanes
@@ -418,7 +418,7 @@ __global__ __launch_bounds__(64 * WAVES, waves_of(KS, R, QH, WAVES)) void attend
                 *reinterpret_cast<half8v *>(stage + (i2 * STAGE + in * 8) * 2) = hi;
                 if constexpr (QH > 1) *reinterpret_cast<half8v *>(stage + (16 * STAGE + i2 * STAGE + in * 8) * 2) = lo;
             }
-            if (in == 0) row_factor[owner][i2] = f;
+            if (in == 0) row_factor[r][owner][i2] = f;
         }
         if (apart) __syncthreads();
         else wave_sync();
@@ -426,7 +426,7 @@ __global__ __launch_bounds__(64 * WAVES, waves_of(KS, R, QH, WAVES)) void attend
         for (int h = 0; h < QH; ++h)
 #pragma unroll
             for (int e = 0; e < KS; ++e) q[r][h][e] = *reinterpret_cast<const half8v *>(stage + (h * 16 * STAGE + m * STAGE + g * (DP / 4) + e * 8) * 2);
-        factor[r] = row_factor[owner][m];
+        factor[r] = row_factor[r][owner][m];
         const int row = row0 + 16 * r + m;
         position[r] = row < rows ? span.length - span.n + a.cut.token_of(row) : -1;
         if (!apart) wave_sync();
@@ -440,6 +440,9 @@ __global__ __launch_bounds__(64 * WAVES, waves_of(KS, R, QH, WAVES)) void attend
     // sums stay normal numbers down to 2^-78 of the largest and parts can be joined, the rest is taken from v_scale and is in o only.
     float limit = 0.0f, power = -48.0f;
     int v_power = -1000, rest = 0;
+    // Scores beyond 2^16 are rounded before the reference is taken from them (in the multiply-add that takes it from the exact product the largest
+    // would be left with what its own rounding was, as a power of two), the reference is the largest, and all of v's power is in rest.
+    int far = 0;
 #pragma unroll
     for (int r = 0; r < R; ++r) {
         top[r] = most_allowed[r] = -__builtin_inff();
@@ -477,8 +480,16 @@ __global__ __launch_bounds__(64 * WAVES, waves_of(KS, R, QH, WAVES)) void attend
 #pragma unroll
         for (int e = 0; e < 8; ++e) scale_v[e] = turn.vs[e >> 2][e & 3];
         const bool whole = first + 31 <= first_position && (first >= seen_from || first + 32 <= a.cut.sinks) && !__any(bad);
-        if (!whole) {
+        if (!whole || far) {
             const int token = first + 8 * g;
+            if (far) {
+#pragma unroll
+                for (int r = 0; r < R; ++r) {
+                    const float f = row_factor[r][apart ? 0 : wave][m];
+                    t[r][0] *= f;
+                    t[r][1] *= f;
+                }
+            }
             // A scale of v that is not finite makes the scores of the rows that see its token NaN instead, so that it does not meet the weight 0
             // of those that do not; behind the sequence's end scales are whatever the page held.
             uint32_t odd = bad ? 0xFFu : 0;
@@ -511,28 +522,40 @@ __global__ __launch_bounds__(64 * WAVES, waves_of(KS, R, QH, WAVES)) void attend
         if (__ballot(move) | static_cast<uint32_t>(rest)) {
             float v_top = fmaxf(v_most, __shfl_xor(v_most, 16));
             v_top = fmaxf(v_top, __shfl_xor(v_top, 32));
-            const float before = power;
-            int by = 0;
             if (v_top >= limit && v_top > 0.0f) {
                 v_power = hq::kv4_max(v_power, __builtin_amdgcn_frexp_expf(v_top) - 1 - ROOM);
                 limit = __builtin_ldexpf(2.0f, v_power + ROOM);   // (infinite for the largest)
-                const int in_reference = hq::kv4_max(-48, hq::kv4_min(48, v_power));
-                power = static_cast<float>(in_reference);
-                by = rest;
-                rest = __builtin_amdgcn_readfirstlane(v_power - in_reference);   // (v's scales are the same for all rows)
-                by -= rest;
             }
+            float to[R];
+            bool large = false;
 #pragma unroll
             for (int r = 0; r < R; ++r) {
                 float here = fmaxf(most[r], __shfl_xor(most[r], 16));
                 here = fmaxf(here, __shfl_xor(here, 32));
-                const float to = fmaxf(top[r] - before, here) + power;
-                const float f = top[r] == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(top[r] - to);
-                top[r] = to;
-                most_allowed[r] = to - power + LAZY;
-                minus[r] = to == -__builtin_inff() ? 0.0f : -to;
+                to[r] = fmaxf(top[r] - power, here);
+                large |= fabsf(to[r]) > 0x1p16f && fabsf(to[r]) < __builtin_inff();
+            }
+            if (!far && __any(large)) {
+                far = 1;
+#pragma unroll
+                for (int r = 0; r < R; ++r) {
+                    t[r][0] *= factor[r];
+                    t[r][1] *= factor[r];
+                    factor[r] = 1.0f;
+                }
+            }
+            const int in_reference = far ? 0 : hq::kv4_max(-48, hq::kv4_min(48, v_power)), before = rest;
+            power = static_cast<float>(in_reference);
+            rest = __builtin_amdgcn_readfirstlane(v_power == -1000 ? 0 : v_power - in_reference);   // (v's scales are the same for all rows)
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                const float ahead = to[r] + power;
+                const float f = top[r] == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(top[r] - ahead);
+                top[r] = ahead;
+                most_allowed[r] = far ? to[r] : to[r] + LAZY;
+                minus[r] = ahead == -__builtin_inff() ? 0.0f : -ahead;
                 sum[r] *= f;
-                const float of_o = __builtin_ldexpf(f, by);
+                const float of_o = __builtin_ldexpf(f, before - rest);
 #pragma unroll
                 for (int e = 0; e < 2 * KS; ++e) o[r][e] *= of_o;
             }

@@ -193,6 +193,46 @@ def test_ends_of_the_range_of_values(lengths, size, other, dtype):
     call.check_attention(2, dtype, window=100)
 
 
+@pytest.mark.parametrize("dtype", ["f16", "bf16", "f32"])
+@pytest.mark.parametrize("scale", [3e3, 3e6, -1e8, 1e10, 1e20, 1e30])
+def test_large_scores(scale, dtype):
+    """Scores so large that a step of fp32 is many powers of two: nearly all of the weight on one token, which is not off by the other ones; one row of
+    each call small, tokens in parts and in one workgroup, sizes of v that need all of the power of two next to scores."""
+    for lengths, size in (([70, 33, 200], 1), ([3000, 2500, 64], 1), ([70, 300, 1400], 1e3 if dtype == "f16" else 1e30)):
+        call = Call([2, 1, 3], lengths, 1, 64, 64, seed=int(np.log10(abs(scale))))
+        call.cache.vs *= np.float32(size)
+        for b, n in enumerate(lengths):          # a key whose score is apart from the others'
+            place = n - 5
+            call.cache.ks[call.table[b, place // 64], 0, place % 64] *= 8
+        call.on_gpu = hq.Kv4Cache(*(gpu(x) for x in call.cache.packed()), 64)
+        q = call.rng.standard_normal((call.t, 2, 64))
+        q[1] *= 1e-7 if dtype == "f16" else 1e-30
+        q = gpu(q, DTYPES[dtype])
+        got = hq.hq_kv4_attention(q, call.on_gpu, *call.where(), scale=scale)
+        assert torch.isfinite(got).all()
+        q = q.cpu().double().numpy()
+        with np.errstate(all="ignore"):
+            want, bound = ref.attention(q, call.cache, call.table, call.lengths, call.begins, scale, 0, 0, call.block, dtype == "f32")
+        if np.isfinite(bound[1]).all():     # (the small row; of large scores the bound knows nothing)
+            close(got[1:2], want[1:2], bound[1:2], dtype)
+        # where the largest score is far from the second: the value of that token
+        apart = 0
+        for row in (0, 2, 3, 4, 5):
+            b = np.searchsorted(call.begins, row, side="right") - 1
+            pos = call.lengths[b] - call.new[b] + row - call.begins[b]
+            k, v = call.cache.rows(call.table[b], pos + 1)
+            hq_row = ref.walsh(q[row], call.block) / 8
+            for h in range(2):
+                s = scale * (k[:, 0] @ hq_row[h])
+                best = np.argsort(s)[-2:]
+                if s[best[1]] - s[best[0]] > 200 + 1e-2 * abs(s[best[1]]):
+                    want = ref.walsh(v[best[1], 0], call.block) / 8
+                    off = np.abs(got[row, h].cpu().double().numpy() - want)
+                    apart += 1
+                    assert (off <= 2 * HALF_STEP["f16" if dtype != "bf16" else dtype] * (np.abs(want) + np.abs(v[best[1], 0]).sum())).all(), (row, h)
+        assert apart
+
+
 def test_peaked_rows():
     """Scores that differ by hundreds, the largest late, early and in the middle."""
     call = Call([1, 1, 1, 2], [300, 290, 64, 128], 1, 64, 16)
