@@ -127,6 +127,43 @@ def test_long_sequences_are_joined(new, lengths, window, sinks, dtype):
     Call(new, lengths, 2, 64, 64, seed=len(new)).check_attention(4, dtype, window=window, sinks=sinks, spread=2.0)
 
 
+@pytest.mark.parametrize("dtype", ["f16", "bf16", "f32"])
+@pytest.mark.parametrize("d,kv_heads", [(80, 2), (96, 1), (128, 2), (160, 1), (200, 2), (256, 1)])
+def test_parts_of_wide_heads(d, kv_heads, dtype):
+    """Parts of few rows and of rows for more than one wave, heads that fill the lanes that own a row and heads that do not."""
+    for new, lengths in (([1], [5000]), ([3, 1], [3333, 2100]), ([40], [3000])):
+        Call(new, lengths, kv_heads, d, 64, seed=d).check_attention(kv_heads * 3, dtype, spread=2.0)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d,kv_heads,heads", [(80, 8, 16), (32, 2, 6), (64, 3, 9), (128, 1, 12), (96, 5, 5), (160, 4, 8), (256, 2, 2)])
+def test_parts_of_many_rows(d, kv_heads, heads, dtype):
+    """Tokens times heads beyond 8192, in parts: heads that are and are not a multiple of those that a workgroup joins.  Some rows of each sequence
+    against the definition."""
+    rng = np.random.default_rng(d)
+    most = 9000 // heads
+    new = [int(n) for n in np.sort(rng.integers(20, most, 5))] + [most, 2]
+    lengths = [n + int(m) for n, m in zip(new, rng.integers(0, 2500, 7))]
+    lengths[2], lengths[6] = new[2] - 3, 1          # (rows that have no place)
+    call = Call(new, lengths, kv_heads, d, 64, seed=d, padding=3)
+    assert call.t * heads > 8192
+    q = gpu(rng.standard_normal((call.t, heads, d)) * 2, DTYPES[dtype])
+    got = hq.hq_kv4_attention(q, call.on_gpu, *call.where())
+    assert not got[-3:].any()
+    s, place = call.places()
+    for b, (n, length) in enumerate(zip(new, lengths)):
+        rows = np.unique(np.concatenate([[0, n - 1], rng.integers(0, n, 2)]))
+        for i in rows:
+            at = int(call.begins[b]) + int(i)
+            seen = length - n + int(i) + 1
+            if seen <= 0:
+                assert not got[at].any()
+                continue
+            want, bound = ref.attention(q[at:at + 1].double().cpu().numpy(), call.cache, call.table[b:b + 1], [seen], [0, 1], d ** -0.5, 0, 0, call.block,
+                                        dtype == "f32")
+            close(got[at:at + 1], want, bound, dtype)
+
+
 def test_more_sequences_than_a_wave_has_lanes():
     rng = np.random.default_rng(3)
     lengths = rng.integers(0, 700, 150)
