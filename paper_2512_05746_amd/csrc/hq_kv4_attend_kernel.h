@@ -17,11 +17,12 @@
 //
 // The reference moves only where s would exceed it by 8 (by 2 for 32-bit results), so most turns leave the sums alone.
 //
-// What bounds it.  A few rows over many tokens: the cache's bytes (276 MB for 64 sequences of up to 16384 tokens, 32 query and 8 key heads of 128:
-// 64 us, 4.3 TB/s; a copy reaches 5.1 to 5.4).  Prompts: a turn's instructions (825 GF for 2 sequences of 4096 new tokens over 8192, the same heads:
-// 860 us, 960 TF/s; a large library product in bf16 reaches 1540): 32 products of 7.7 ns beside about 200 vector instructions, which
-// overlap with those of the SIMD's other wave in part only.  One row over few tokens: latencies, 13.5 us: about 1 until a
-// workgroup knows its work, 4 to 5 until its rows are through the transform (with the first k and v under way), 2 a turn, 2 to 3 for the results.
+// What bounds it (medians of a kernel trace).  A few rows over many tokens: the cache's bytes (276 MB for 64 sequences of up to 16384 tokens, 32 query
+// and 8 key heads of 128: 67 us, 4.1 TB/s; a copy reaches 5.1 to 5.4).  Prompts: a turn's instructions (825 GF for 2 sequences of 4096 new tokens over
+// 8192, the same heads: 930 to 1000 us from card to card, 820 to 890 TF/s, 867 at best; a large library product in bf16 reaches 1540): 32 products of 7.7 ns
+// beside about 200 vector instructions, which overlap with those of the SIMD's other wave in part only (the vector pipe is busy two thirds of the time,
+// the matrix pipe a third).  One row over few tokens: latencies, 13.6 us: about 1 until a workgroup knows its work, 4 to 5 until its rows are through
+// the transform (with the first k and v under way), 2 a turn, of which pages below 32 tokens wait for all of k (below), 2 to 3 for the results.
 // Taken back for prompts: the next tile's products beside this one's exponentials (1016 -> 1068 us), k and v asked for two tiles ahead (1110 to
 // 1130), scales one a lane and moved to where they are used (slower by the moves), three waves a SIMD (spills).
 #pragma once
@@ -202,7 +203,8 @@ __device__ __forceinline__ float largest(const float (&v)[8]) {
     return x;
 }
 // Waves a SIMD for which registers are kept: loads of other waves and conversions beside products need them.  (One tile of rows: bound by loads,
-// more waves; two tiles: their sums and queries alone are 96 registers at 96 channels.)
+// more waves, for which heads of 128 channels keep 9 to 11 registers in scratch memory outside the loop over tokens; two tiles: their sums and queries
+// alone are 96 registers at 96 channels.)
 constexpr int waves_of(int ks, int r, int qh, int waves) { return waves == 8 ? 2 : r == 1 && ks <= 4 ? qh == 1 ? 4 : 3 : ks <= 6 ? 2 : 1; }
 // Of a tile's groups of 8 tokens the lane's: one for all, or one of four.
 template <class T, int N>
@@ -295,6 +297,8 @@ __global__ __launch_bounds__(64 * WAVES, waves_of(KS, R, QH, WAVES)) void attend
     // Where the tokens of a tile are, by scalar loads of the table: vector loads arrive in order, so that waiting for one of these would
     // mean waiting for every k and v that was asked for before it.  Groups of 8 tokens have one place each, tiles of wide pages one.  (Scalar
     // instructions take the wave's turns too: a place is two multiplications of 32 bits, from what one head's page begins with.)
+    // With narrow pages a lane's choice of four places becomes an indexed load from scratch memory (80 bytes a lane; LDS in the kernels of 8 waves from 160
+    // channels on), which arrives in that order as well: there the next k has arrived before v is asked for.
     constexpr int GROUPS = WIDE_PAGES ? 1 : 4;
     const uint32_t page_slots = static_cast<uint32_t>(a.c.kv_heads) << a.c.page_log2, page_bytes = page_slots * (DP / 2);
     const uint32_t pages = static_cast<uint32_t>(a.c.pages);

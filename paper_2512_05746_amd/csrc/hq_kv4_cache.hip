@@ -486,7 +486,7 @@ struct ReadArgs {
 
 // Workgroups of a group, side by side: the first half reads keys, the other values.  A slot has a row; of v it reads the dwords of its
 // channels, which hold 8 tokens (the other slots that want them find them in the first-level cache).  Bound by what it writes: 131072 tokens of 8
-// heads of 128 in bf16 130 to 143 us for 0.68 GB, 4.7 to 5.2 TB/s.
+// heads of 128 in bf16 148 us (median; 127 at best) for 0.68 GB, 4.6 TB/s.
 template <int DT, int LP>
 __global__ __launch_bounds__(256) void read_kernel(ReadArgs a) {
     using T = typename Float<DT>::type;
