@@ -21,9 +21,9 @@ struct Plan {
 // How rows and tokens are dealt to workgroups:
 //   Sequences of up to 16 rows on average, and heads of more than 128 channels (whose second tile of rows would spill): one tile of rows a wave.
 //     Otherwise two: a tile of k and v is converted once for both (12 sequences of 10 to 700 tokens, 16 heads of 80: one 76 us, two 62).
-//   8 waves share the tokens of a row where that leaves no CU without work and the table has room for at most 2048 of them (lengths are known on the
-//     device only, so the table's width stands for them, here and below; it was measured on tables as wide as their sequences): 13.8 us for 777 tokens of 8 key
-//     heads, 4 waves 15.8, 16 waves 17.
+//   8 waves share the tokens of a row where that leaves no CU without work and the table has room for at most 2048 of them (lengths are
+//     known on the device only, so the table's width stands for them, here and below; it was measured on tables as wide as their
+//     sequences): 13.8 us for 777 tokens of 8 key heads, 4 waves 15.8, 16 waves 17.
 //   Tokens are divided where rows alone do not fill the card and are more than 12 turns of the waves (below, the second launch costs more than
 //     it saves), into as many parts as are at work at once, at least 8 turns each.  For two tiles half as many again were slower
 //     (57 -> 68 us), twice as many too.

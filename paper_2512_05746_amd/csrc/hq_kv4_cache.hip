@@ -258,12 +258,12 @@ __device__ __forceinline__ double norm_wide(const AppendArgs &a, const Raw<T, PA
     sum = reduce_wide<LP>(live ? sum : 0.0, [](double a, double b) { return a + b; });
     return 1.0 / sqrt(sum / a.c.d + a.eps);
 }
-// A head's transform in codes by fp32 steps (the lanes without channels have zeros), and whether these leave one of its codes uncertain: `near`.
-// With u = 2^-24 and E at least the sum of the head's magnitudes before they are turned, each times |cos| + |sin| of its pair: products and the turn are
-// off by 4 u E at most over a block (none for values), the steps of the transform by 6 u E and u of the result, which with the same error of the
-// largest is 12 (4 + 6) u E / max of a number up to 6, and 12 u; the largest, the scale, its inverse (two), the factor and the product: 6 u of it.
-// Uncertain are codes of which the number less and plus that differ: those of 1 or 2 heads of 128 normal values in 100.  ROUNDINGS: 4 + 6 for keys,
-// 6 for values, with room for terms of second order.
+// A head's transform in codes by fp32 steps (the lanes without channels have zeros), and whether these leave one of its codes uncertain:
+// `near`.  With u = 2^-24 and E at least the sum of the head's magnitudes before they are turned, each times |cos| + |sin| of its pair:
+// products and the turn are off by 4 u E at most over a block (none for values), the steps of the transform by 6 u E and u of the result,
+// which with the same error of the largest is 12 (4 + 6) u E / max of a number up to 6, and 12 u; the largest, the scale, its inverse (two),
+// the factor and the product: 6 u of it.  Uncertain are codes of which the number less and plus that differ: those of 1 or 2 heads of 128
+// normal values in 100.  ROUNDINGS: 4 + 6 for keys, 6 for values, with room for terms of second order.
 template <int LP, int ROUNDINGS>
 __device__ __forceinline__ uint32_t coded(float (&v)[8], float size, int in, int block_log2, float &scale, bool &near) {
     walsh_of<LP>(v, in, block_log2);
@@ -312,25 +312,43 @@ __device__ __forceinline__ void turned_heads(const AppendArgs &a, int from, int 
     const int c0 = live ? in * 8 : 0;
     const int64_t by_head = KEYS ? a.k_head : a.q_head;
     const T *x = static_cast<const T *>(KEYS ? a.k : a.q) + row * (KEYS ? a.k_token : a.q_token) + from * by_head;
-    Raw<T, PAIRS> raw[kAtOnce];
-    const auto load = [&](int h) {
+    const int64_t x_step = step * by_head;
+    if constexpr (!KEYS) {
+        Raw<T, PAIRS> raw[kAtOnce];
+        const auto load = [&](int h) {
 #pragma unroll
-        for (int e = 0; e < kAtOnce; ++e) {
-            if (h + e * step < heads) raw[e].load(x, c0, a.rotary);
-            x += step * by_head;
+            for (int e = 0; e < kAtOnce; ++e) {
+                if (h + e * step < heads) raw[e].load(x, c0, a.rotary);
+                x += x_step;
+            }
+        };
+        load(from);
+        const Raw<float, PAIRS> w = weights_of<T, PAIRS>(a, a.q_weight, c0);
+        const Turn turn = turn_of<PAIRS>(a, row, place, c0);
+        T *out = static_cast<T *>(a.q_out) + row * a.out_token + from * a.out_head + c0;
+        for (int h = from; h < heads; h += kAtOnce * step) {
+#pragma unroll
+            for (int e = 0; e < kAtOnce; ++e) {
+                if (h + e * step >= heads) break;
+                float v[8];
+                head<T, LP, PAIRS>(a, raw[e], c0, live, turn, w, v);
+                if (__any(turn.pad)) {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) v[i] = turn.pad ? 0.0f : v[i];
+                }
+                if (live && mine) store8(out, v);
+                out += step * a.out_head;
+            }
+            load(h + kAtOnce * step);
         }
-    };
-    load(from);
-    Raw<float, PAIRS> w = weights_of<T, PAIRS>(a, KEYS ? a.k_weight : a.q_weight, c0);
-    Turn turn = turn_of<PAIRS>(a, row, place, c0);
-    T *out = KEYS ? nullptr : static_cast<T *>(a.q_out) + row * a.out_token + from * a.out_head + c0;
-    const int64_t at = KEYS ? a.c.slots(page, from) + a.c.slot(static_cast<int>(place)) : 0;
-    uint8_t *code_out = a.c.k + at * a.c.row_bytes() + in * 4;
-    float *scale_out = a.c.k_scale + at;
-    // Keys: E by lengths, that of x (d^1/2 with a norm) times that of the weights, each times |cos| + |sin|.  Lanes without channels have zeros.
-    float size = 0.0f;
-    uint32_t again = 0;
-    if constexpr (KEYS) {
+    } else {
+        // (one head ahead: four at once, as queries, with the heads in 64 bits beside them cost a wave a SIMD, 182 us for 168 at best)
+        Raw<T, PAIRS> next;
+        if (from < heads) next.load(x, c0, a.rotary);
+        Raw<float, PAIRS> w = weights_of<T, PAIRS>(a, a.k_weight, c0);
+        Turn turn = turn_of<PAIRS>(a, row, place, c0);
+        // E by lengths: that of x (d^1/2 with a norm) times that of the weights, each times |cos| + |sin|.  Lanes without channels have zeros.
+        float size = 0.0f;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             w.v[i] = live ? w.v[i] : 0.0f;
@@ -340,58 +358,49 @@ __device__ __forceinline__ void turned_heads(const AppendArgs &a, int from, int 
         }
         size = sqrtf(sum_lanes<LP>(size) * (a.norm ? static_cast<float>(a.c.d) : 1.0f));
         if (a.norm && a.eps < 0x1p-110f) size *= 2.0f;   // (squares that are no normal numbers make the norm's factor up to 1.3 times too large)
-    }
-    for (int h = from; h < heads; h += kAtOnce * step) {
-#pragma unroll
-        for (int e = 0; e < kAtOnce; ++e) {
-            if (h + e * step >= heads) break;
-            float v[8], most = size;
-            if constexpr (KEYS)
-                if (!a.norm) most *= length_of<T, LP>(raw[e], live);
-            head<T, LP, PAIRS>(a, raw[e], c0, live, turn, w, v);
-            if constexpr (!KEYS) {
-                if (__any(turn.pad)) {
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) v[i] = turn.pad ? 0.0f : v[i];
-                }
-                if (live && mine) store8(out, v);
-                out += step * a.out_head;
-            } else {
-                float scale;
-                bool near;
-                const uint32_t code = coded<LP, 10>(v, most, in, a.c.block_log2, scale, near);
-                again = again << 1 | (again & 0x80000000u);
-                if (const uint64_t lanes = __ballot(near)) again |= any_of_head<LP>(lanes);
-                if (mine && !turn.pad) {
-                    if (live) *reinterpret_cast<uint32_t *>(code_out) = code;
-                    if (in == 0) *scale_out = scale;
-                }
-                code_out += (static_cast<int64_t>(step) << a.c.page_log2) * a.c.row_bytes();
-                scale_out += static_cast<int64_t>(step) << a.c.page_log2;
+        const int64_t at = a.c.slots(page, from) + a.c.slot(static_cast<int>(place)), scale_step = static_cast<int64_t>(step) << a.c.page_log2;
+        uint8_t *code_out = a.c.k + at * a.c.row_bytes() + in * 4;
+        float *scale_out = a.c.k_scale + at;
+        uint32_t again = 0;
+        for (int h = from; h < heads; h += step) {
+            const Raw<T, PAIRS> now = next;
+            x += x_step;
+            if (h + step < heads) next.load(x, c0, a.rotary);
+            float v[8], scale, most = size;
+            if (!a.norm) most *= length_of<T, LP>(now, live);
+            head<T, LP, PAIRS>(a, now, c0, live, turn, w, v);
+            bool near;
+            uint32_t code = coded<LP, 10>(v, most, in, a.c.block_log2, scale, near);
+            again = again << 1 | (again & 0x80000000u);
+            if (const uint64_t lanes = __ballot(near)) again |= any_of_head<LP>(lanes);
+            if (mine && !turn.pad) {
+                if (live) *reinterpret_cast<uint32_t *>(code_out) = code;
+                if (in == 0) *scale_out = scale;
             }
+            code_out += scale_step * a.c.row_bytes();
+            scale_out += scale_step;
         }
-        load(h + kAtOnce * step);
+        // The uncertain heads, the last one in bit 0, any before the last 31 in bit 31: a loop of its own, from memory again, so that it costs
+        // no registers above.
+        if (again)
+            for (int h = from + (heads - 1 - from) / step * step, back = 0; h >= from; h -= step, back = hq::kv4_min(back + 1, 31))
+                if (again >> back & 1) {
+                    Raw<T, PAIRS> one;
+                    one.load(static_cast<const T *>(a.k) + row * a.k_token + h * a.k_head, c0, a.rotary);
+                    const double factor = norm_wide<T, LP>(a, one, live);
+                    double v[8];
+                    head_wide(a, one, c0, turn, w, v);
+                    const uint32_t code = coded_wide<LP>(v, in, live, a.c.block_log2, factor);
+                    uint8_t *const to = a.c.k + (a.c.slots(page, h) + a.c.slot(static_cast<int>(place))) * a.c.row_bytes() + in * 4;
+                    if (mine && live && !turn.pad) *reinterpret_cast<uint32_t *>(to) = code;
+                }
     }
-    // The uncertain heads, the last one in bit 0, any before the last 31 in bit 31: a loop of its own, from memory again, so that it costs no registers
-    // above.
-    if (KEYS && again)
-        for (int h = from + (heads - 1 - from) / step * step, back = 0; h >= from; h -= step, back = hq::kv4_min(back + 1, 31))
-            if (again >> back & 1) {
-                Raw<T, PAIRS> one;
-                one.load(static_cast<const T *>(a.k) + row * a.k_token + h * a.k_head, c0, a.rotary);
-                const double factor = norm_wide<T, LP>(a, one, live);
-                double v[8];
-                head_wide(a, one, c0, turn, w, v);
-                const uint32_t code = coded_wide<LP>(v, in, live, a.c.block_log2, factor);
-                if (mine && live && !turn.pad)
-                    *reinterpret_cast<uint32_t *>(a.c.k + (a.c.slots(page, h) + a.c.slot(static_cast<int>(place))) * a.c.row_bytes() + in * 4) = code;
-            }
 }
 
 // The values of a group's tokens, likewise.
 template <class T, int LP>
-__device__ __forceinline__ void stored_heads(const AppendArgs &a, int part, int log2, int at_once, int slot, int first, int row, int64_t place, int in,
-                                             bool live, bool mine, const hq::Kv4Group &g) {
+__device__ __forceinline__ void stored_heads(const AppendArgs &a, int part, int log2, int at_once, int slot, int first, int row, int64_t place,
+                                             int in, bool live, bool mine, const hq::Kv4Group &g) {
     constexpr int SLOTS = 256 / LP;
     const int parts = a.k_parts;
     const int64_t page = page_of(a.c, g);
@@ -452,8 +461,9 @@ __device__ __forceinline__ void stored_heads(const AppendArgs &a, int part, int 
 }
 
 // Workgroups of a group, side by side: q_parts for the queries, k_parts for the keys, as many for the values: the queries are bound by memory, keys
-// and values by arithmetic, and beside each other they overlap.  32768 tokens of 32 + 8 heads of 128 in bf16: 157 us for 0.71 GB, 4.5 TB/s (one
-// workgroup for all three, one after the other: 184 us).  16 tokens: 5.5 us, latencies.
+// and values by arithmetic, and beside each other they overlap (one workgroup for all three, one after the other, took a fifth more).  Medians: 32768
+// tokens of 32 + 8 heads of 128 in bf16 172 us for 0.71 GB, 4.1 TB/s; 16 tokens 7.2 us, latencies.  Of these the certainty of codes takes 14 us (two
+// conversions of each number, heads in 64 bits) and 1.5.
 template <int DT, int LP, int PAIRS>
 __global__ __launch_bounds__(256) void append_kernel(AppendArgs a) {
     using T = typename Float<DT>::type;
@@ -486,7 +496,7 @@ struct ReadArgs {
 
 // Workgroups of a group, side by side: the first half reads keys, the other values.  A slot has a row; of v it reads the dwords of its
 // channels, which hold 8 tokens (the other slots that want them find them in the first-level cache).  Bound by what it writes: 131072 tokens of 8
-// heads of 128 in bf16 148 us (median; 127 at best) for 0.68 GB, 4.6 TB/s.
+// heads of 128 in bf16 147 us (median; 125 at best) for 0.68 GB, 4.6 TB/s.
 template <int DT, int LP>
 __global__ __launch_bounds__(256) void read_kernel(ReadArgs a) {
     using T = typename Float<DT>::type;
